@@ -445,6 +445,69 @@ mcft_status mcft_stack_routing(const mcft_stack* stack, int layer, int32_t* idx,
 void mcft_stack_destroy(mcft_stack* stack);
 
 /* ---------------------------------------------------------------------------------------------
+ * mx4: microscaled 4-bit floating point (no counterpart in the paper, whose experts are bf16; the paper's
+ * setting, Section 1, is bound by the bytes of the expert blocks that offloaded decoding moves, and a
+ * block in this format has 17/64 of them).
+ *
+ * A block of 32 values along a row is 32 e2m1 codes (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign) and one scale
+ * 2^(floor(log2 max|x|) - 2), clamped to [2^-127, 2^127] and held as its exponent + 127 in a byte. Codes
+ * round to nearest even and saturate at 6; a row's last block may be shorter. A block with a NaN or an
+ * infinity has the scale byte 0xff and reads back as NaN. An mx4 matrix [rows, cols] is opaque: codes in
+ * 8-row groups of 128 columns, then scales, in the order in which the tensor cores read them, padded
+ * with zeros to 8 rows (codes), 128 rows (scales) and 128 columns; mcft_mx4_size bytes, 16-byte aligned.
+ *
+ * mcft_mx4_quantize: x device [rows, cols] of dtype (MCFT_F32 or MCFT_BF16), `ld` elements from row to
+ *   row, any alignment of its type (16-byte rows are read faster); q device, mcft_mx4_size bytes out.
+ * mcft_mx4_dequantize: the values that q stands for, exact in either dtype but for subnormal bf16
+ *   results, which round; y device [rows, cols], `ld` elements from row to row.
+ * rows = 0 is a no-op. Asynchronous. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer, rows < 0,
+ * cols < 1, ld < cols, an unknown dtype. */
+mcft_status mcft_mx4_size(long long rows, long long cols, size_t* bytes);
+mcft_status mcft_mx4_quantize(const void* x, long long rows, long long cols, long long ld, int dtype,
+                              void* q, mcft_stream_t stream);
+mcft_status mcft_mx4_dequantize(const void* q, long long rows, long long cols, int dtype, void* y,
+                                long long ld, mcft_stream_t stream);
+
+/* mcft_mx4_matmul: y = A B^T with A [M, K] and B [N, K] mx4 matrices: products exact, sums in fp32 on the
+ * tensor cores (tcgen05 block-scaled MMAs), rounded once if y is bf16.
+ *   y device [M, N] of dtype, `ldy` elements from row to row (16-byte rows are not required).
+ * M = 0 or N = 0 is a no-op. Asynchronous; no workspace. Errors: MCFT_ERR_INVALID for a NULL or
+ * misaligned pointer, M, N < 0, K < 1, ldy < N, an unknown dtype. */
+mcft_status mcft_mx4_matmul(const void* a, const void* b, int M, int N, int K, int dtype, void* y,
+                            long long ldy, mcft_stream_t stream);
+
+/* mcft_mx4_pack_expert: a packed expert block [W1 | W3 | W2] of the layer dtype to an mx4 expert block: each
+ * row of the three matrices quantised, W1 and W3 interleaved 32 rows by 32, mcft_mx4_expert_size bytes, a
+ * multiple of 512. Both 16-byte aligned device blocks. An mx4 block is one unit of cache traffic like any
+ * expert block: mcft_cache_create takes its size as expert_bytes, mcft_fetch_experts brings it in.
+ * Here and in the next two calls desc may have E up to 256 and K up to 16. Asynchronous. */
+mcft_status mcft_mx4_expert_size(const mcft_layer_desc* desc, size_t* bytes);
+mcft_status mcft_mx4_pack_expert(const mcft_layer_desc* desc, const void* block, void* out,
+                                 mcft_stream_t stream);
+
+/* mcft_moe_forward_mx4: the layer forward (Section 3.1 Eq. topk) on mx4 expert blocks. With Q the rounding
+ * of each row to mx4 and W the values of the blocks,
+ *   y[t] = sum_k gate[t,k] F_{idx[t,k]}(x[t]) + sum_s F^shared_s(x[t]),
+ *   F(x) = W2 Q(silu(W1 Q(x)) * (W3 Q(x))),
+ * sums, SwiGLU and the weighted sum in fp32, y rounded once.
+ *   x, y      device [T, d] of the layer dtype (y may not alias x)
+ *   idx, gate device [T, K]; an idx of -1 is no expert (its gate is not read into the sum), so a token
+ *             may have fewer than K experts, or none; another id outside [0, E) or one whose entry in
+ *             experts is NULL sets the device error word and the call writes nothing to y
+ *   experts   host array [E] of device pointers to mx4 expert blocks, read before the call returns; an
+ *             entry may be NULL if no token selects it
+ *   shared    host array [n_shared] of the same (NULL if n_shared = 0)
+ *   workspace device, mcft_mx4_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's
+ *             kernels finish; enough for any smaller T
+ * Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or
+ * misaligned pointer, bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for E > 256, K > 16. */
+mcft_status mcft_mx4_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
+mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int T, const int32_t* idx,
+                                 const float* gate, const void* const* experts,
+                                 const void* const* shared, void* y, void* workspace, size_t ws_bytes,
+                                 mcft_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
  * mcft_device_error: synchronise `stream`, return and clear the device error word of the current
  * device: MCFT_OK, MCFT_ERR_INVALID (bad id, missing expert pointer) or MCFT_ERR_TIMEOUT. */
 mcft_status mcft_device_error(mcft_stream_t stream);

@@ -18,7 +18,8 @@ Everything is a plain, slow, readable restatement of the paper's definitions in 
 * ``stack``    - the chained decode stack (residual stream, RMSNorm, one masked MoE block per layer)
   and the next-layer prediction that drives expert prefetch; the cache's prefetch event is in
   ``cache``.
+* ``mx4``      - microscaled 4-bit floating point: rounding, products, the layer on rounded experts.
 
 Pins (tests marked ``not gpu``) tie each function to something other than itself; see the tests.
 """
-from . import cache, ffn, mask, routing, stack  # noqa: F401
+from . import cache, ffn, mask, mx4, routing, stack  # noqa: F401

@@ -473,7 +473,8 @@ mcft_status stack_prologue(const mcft_layer_desc* desc, float* x, const void* y,
 enum { kProfRoute, kProfCache, kProfPermute, kProfGather, kProfFfn13, kProfFfn2, kProfGemm13,
        kProfGemm2, kProfCombine, kProfDec13, kProfDec2, kProfFetch, kProfLora, kProfNorm,
        kProfPrefetch, kProfPfFetch, kProfPrologue, kProfDecFused, kProfHostCopy, kProfDecFetch,
-       kProfGemm13Pair, kProfGemm2Pair, kProfCount };
+       kProfGemm13Pair, kProfGemm2Pair, kProfMx4Quant, kProfMx4Dequant, kProfMx4Matmul, kProfMx4Prepare,
+       kProfMx4Up, kProfMx4Down, kProfMx4Combine, kProfRouteScored, kProfRouteScoredGrad, kProfCount };
 void prof_begin(int kid, cudaStream_t s);
 void prof_end(int kid, cudaStream_t s);
 

@@ -1,0 +1,496 @@
+// Products of mx4 matrices on the tensor cores: tcgen05.mma kind::mxf4 with a power-of-two scale for each 32
+// of the contraction, so that
+//   acc[m, n] = sum_blocks 2^(sa[m, b] + sb[n, b] - 254) sum_{k in b} a[m, k] b[n, k]     (fp32)
+// with no value unpacked on the way: codes and scales go from HBM to shared memory as they are stored (the
+// layout of mx4.cuh is the operands' shared-memory image, so plain bulk copies do, without tensor maps), the
+// scales from there to tensor memory by tcgen05.cp.
+//
+// Tokens are on M (128 rows of a tile), weight rows on N, so that in the epilogue a thread owns one token row:
+// 32 outputs of it are a block, quantised without leaving the thread. Three epilogues:
+//   up    the weight rows are 32 gate and 32 up rows in turn: h = silu(gate) * up, to mx4 (Section 3.1's F);
+//   down  fp32 rows of o, to the assignment's place;
+//   out   fp32 or bf16 rows of y (the plain product).
+//
+// Two builds. `wide` tiles of 128 x 256 for prompts: a persistent grid, one CTA an SM; the eight epilogue warps
+// drain the 256 accumulator columns into registers and give them back at once, so that the next tile's MMAs run
+// under the epilogue's arithmetic and stores. `narrow` tiles of up to 128 weight rows for few tokens, where the
+// bytes of the weights bound the time: one item a cluster of 1, 2, 4 or 8 CTAs that split the contraction and
+// add their partial tiles through distributed shared memory, two CTAs an SM; only the 8-row groups that hold
+// tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results).
+//
+// Warp 0 issues the copies, warp 1 the tcgen05.cp and MMAs and owns the tensor memory, warps 2-9 are the
+// epilogue. Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again
+// with a limit) for its copies and MMAs in flight, frees the tensor memory and returns.
+#include <algorithm>
+
+#include "mx4_args.h"
+#include "tc_ptx.cuh"
+
+namespace mcft {
+namespace {
+
+constexpr int kThreads = 320;
+constexpr int kMaxStages = 16;
+constexpr int kWideN = 256, kNarrowN = 128;
+constexpr int kWideRing = 220 * 1024, kNarrowRing = 104 * 1024;
+constexpr int kSfCols = 16;  // tensor memory columns of a chunk's scales: 4 of A, up to 8 of B
+// Instruction descriptor without N and the scale bytes' places: A and B e2m1, scales ue8m0, M = 128.
+constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (1u << 23) | (uint32_t(128 >> 4) << 24);
+
+struct Ctl {
+  uint64_t full[kMaxStages], empty[kMaxStages], tfull, tempty, drain;
+  uint32_t tmem_base;
+  int abort;
+};
+constexpr int kCtlBytes = 512;
+static_assert(sizeof(Ctl) <= kCtlBytes, "control block");
+
+template <bool WIDE>
+constexpr int smem_bytes() {
+  return (WIDE ? kWideRing : kNarrowRing) + 1024 + kCtlBytes;
+}
+static_assert(smem_bytes<true>() <= 227 * 1024 && 2 * (smem_bytes<false>() + 1024) <= 228 * 1024, "shared memory");
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+      "r"(bytes), "r"(bar)
+      : "memory");
+}
+// K-major operand rows of 64 bytes under the 64-byte swizzle: 512 bytes between 8-row groups.
+__device__ __forceinline__ uint64_t sw64_desc(uint32_t saddr) {
+  return uint64_t((saddr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(512 >> 4) << 32) | (uint64_t(1) << 46) |
+         (uint64_t(4) << 61);
+}
+// 32 rows of 16 bytes, no swizzle: 128 bytes between 8-row groups.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
+  return uint64_t((saddr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
+}
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_desc(saddr)) : "memory");
+}
+__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                        uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ float peer_float(uint32_t cluster_addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr));
+  return v;
+}
+// 32 bytes to global memory in one instruction (a whole sector a lane).
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
+__device__ __forceinline__ float swiglu(float g, float u) {
+  return (silu_regular(g) ? silu_branchless(g) : silu(g)) * u;
+}
+
+struct Item {
+  int seg, a_tile, h_tile, rows, n0;  // weights; token tile of A; of the output; its rows; first weight row
+};
+
+// Item -> tile. The device's tile list has a segment's token tiles one after another; a segment's items are its
+// weight tiles with the token tiles innermost, so CTAs that run side by side share weights.
+template <int EPI>
+__device__ __forceinline__ Item item_at(const Mx4GemmArgs& p, int i) {
+  Item t;
+  if (EPI == kMx4Out) {
+    const int m = i % p.m_tiles;
+    t.seg = 0;
+    t.a_tile = t.h_tile = m;
+    t.rows = min(128, p.M - m * 128);
+    t.n0 = i / p.m_tiles * p.tn;
+  } else {
+    const Mx4Tile e = p.tiles[i / p.n_tiles];
+    const int local = i - e.first * p.n_tiles, m = local % e.count;
+    const Mx4Tile f = p.tiles[e.first + m];
+    t.seg = f.seg;
+    t.a_tile = EPI == kMx4Up ? f.a_tile : e.first + m;
+    t.h_tile = e.first + m;
+    t.rows = f.rows;
+    t.n0 = local / e.count * p.tn;
+  }
+  return t;
+}
+
+template <int EPI, bool WIDE>
+__global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const __grid_constant__ Mx4GemmArgs p) {
+  constexpr int kTmemCols = WIDE ? 512 : 256, kSfBase = WIDE ? kWideN : kNarrowN;
+  constexpr int kSets = (kTmemCols - kSfBase) / kSfCols;
+  constexpr int kRing = WIDE ? kWideRing : kNarrowRing;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;  // the same offsets in every CTA of a cluster
+  uint8_t* ring = smem_raw + (base - raw);
+  Ctl* ctl = reinterpret_cast<Ctl*>(ring + kRing);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cs = WIDE ? 1 : p.split;
+  const int rank = WIDE ? 0 : int(cluster_rank());
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    mbar_init(&ctl->tfull, 1);
+    mbar_init(&ctl->tempty, 8);
+    mbar_init(&ctl->drain, 1);
+    ctl->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem_base;
+  volatile int* abort = &ctl->abort;
+  const int total = EPI == kMx4Out ? p.m_tiles * p.n_tiles : (p.hdr->abort ? 0 : p.hdr->tiles * p.n_tiles);
+  const int first = WIDE ? int(blockIdx.x) : int(blockIdx.x) / cs;
+  const int stride = WIDE ? int(gridDim.x) : total;  // narrow: one item
+  // this CTA's share of the contraction, in chunks
+  const int kc0 = int((long long)p.chunks * rank / cs), kc1 = int((long long)p.chunks * (rank + 1) / cs);
+  const uint32_t a_bytes = uint32_t(p.a_groups) * 512u, b_bytes = uint32_t(p.tn) * 64u;
+  const uint32_t sb_bytes = uint32_t(p.tn > 128 ? 2 : 1) * 512u;
+  // a stage: codes of A (all chunks), of B, scales of A, of B
+  const uint32_t off_b = a_bytes * p.depth, off_sa = off_b + b_bytes * p.depth, off_sb = off_sa + 512u * p.depth;
+  const uint32_t stage_bytes = off_sb + sb_bytes * p.depth;
+
+  if (warp == 0) {
+    if (first < total && elect_one()) {
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      for (int i = first; i < total && !*abort; i += stride) {
+        const Item t = item_at<EPI>(p, i);
+        const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
+        const uint8_t* pa = p.a + size_t(t.a_tile) * 8192;
+        const uint8_t* psa = p.a_scales + size_t(t.a_tile) * 512;
+        const uint8_t* pb = w + p.w_codes + size_t(t.n0) * 64;
+        const uint8_t* psb = w + p.w_scales + size_t(t.n0 >> 7) * 512;
+        const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
+        const uint32_t nb = uint32_t(min(p.tn >> 3, p.w_groups - (t.n0 >> 3))) * 512u;
+        const uint32_t nsb = uint32_t(min(p.tn > 128 ? 2 : 1, p.w_blocks - (t.n0 >> 7))) * 512u;
+        for (int kc = kc0; kc < kc1; kc += p.depth) {
+          if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
+          const uint32_t st = base + uint32_t(s) * stage_bytes, bar = smem_u32(&ctl->full[s]);
+          const int nc = min(p.depth, kc1 - kc);
+          mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
+          for (int j = 0; j < nc; ++j) {
+            const size_t c = size_t(kc + j);
+            bulk_load(st + off_b + b_bytes * j, pb + c * p.w_code_stride, nb, bar);
+            bulk_load(st + off_sb + sb_bytes * j, psb + c * p.w_scale_stride, nsb, bar);
+            bulk_load(st + a_bytes * j, pa + c * p.a_code_stride, na, bar);
+            bulk_load(st + off_sa + 512u * j, psa + c * p.a_scale_stride, 512u, bar);
+          }
+          if (issued < p.stages) ++issued;
+          if (++s == p.stages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
+      for (int i = 0; i < issued; ++i) {
+        const int j = s - (issued - i);
+        if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + p.stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
+      }
+    }
+  } else if (warp == 1) {
+    if (first < total && elect_one()) {
+      int s = 0;
+      uint32_t ph = 0, lt = 0, set = 0;
+      for (int i = first; i < total && !*abort; i += stride, ++lt) {
+        const Item t = item_at<EPI>(p, i);
+        const uint32_t idesc = kIdesc | (uint32_t(p.tn >> 3) << 17);
+        const uint32_t sb_shift = uint32_t(t.n0 >> 5) & 3u;  // (tn < 128: which 32-row columns of the block)
+        if (!mbar_wait_cl(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
+        tc_fence_after();
+        bool ok = true;
+        for (int kc = kc0; kc < kc1; kc += p.depth) {
+          if (!mbar_wait_cl(&ctl->full[s], ph, abort, p.err)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t st = base + uint32_t(s) * stage_bytes;
+          const int nc = min(p.depth, kc1 - kc);
+          for (int j = 0; j < nc; ++j) {
+            const uint32_t sfa = tmem + kSfBase + set * kSfCols, sfb = sfa + 4;
+            scales_to_tmem(sfa, st + off_sa + 512u * j);
+            scales_to_tmem(sfb, st + off_sb + sb_bytes * j);
+            if (WIDE) scales_to_tmem(sfb + 4, st + off_sb + sb_bytes * j + 512u);
+            const uint64_t da = sw64_desc(st + a_bytes * j), db = sw64_desc(st + off_b + b_bytes * j);
+            mma_mx4(tmem, da, db, idesc, sfa, sfb + sb_shift, kc + j > kc0 ? 1u : 0u);
+            if ((kc + j) * 2 + 1 < p.ksteps)
+              mma_mx4(tmem, da + 2, db + 2, idesc | (2u << 4) | (2u << 29), sfa, sfb + sb_shift, 1u);
+            set = set + 1 == kSets ? 0 : set + 1;
+          }
+          commit(&ctl->empty[s]);
+          if (++s == p.stages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        if (!ok) break;
+        commit(&ctl->tfull);
+      }
+      commit(&ctl->drain);  // arrives once every MMA issued above has completed
+      mbar_wait_drain_cl(&ctl->drain, 0, p.err);
+    }
+  } else if constexpr (WIDE) {
+    const int q = warp & 3, grp = (warp - 2) >> 2;  // tensor memory lane quarter this warp may read; column half
+    const int row = q * 32 + lane;
+    uint32_t lt = 0;
+    for (int i = first; i < total; i += stride, ++lt) {
+      const Item t = item_at<EPI>(p, i);
+      int ok = 1;
+      if (lane == 0) ok = mbar_wait_cl(&ctl->tfull, lt & 1u, abort, p.err) ? 1 : 0;
+      if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+      tc_fence_after();
+      uint32_t v[128];
+      const uint32_t taddr = tmem + (uint32_t(q * 32) << 16) + uint32_t(grp * 128);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(taddr + c * 32, v + c * 32);
+      tmem_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(&ctl->tempty);
+      const int n = t.n0 + grp * 128;
+      if constexpr (EPI == kMx4Up) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {  // 32 gate and 32 up columns: one block of h
+          const int f = (n >> 1) + b * 32;
+          if (f >= p.n_out || row >= t.rows) break;
+          float h[32];
+          uint32_t m = 0;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            h[j] = swiglu(__uint_as_float(v[b * 64 + j]), __uint_as_float(v[b * 64 + 32 + j]));
+            m = max(m, __float_as_uint(h[j]) & 0x7fffffffu);
+          }
+          const uint32_t sc = mx4_scale(m);
+          const float inv = mx4_inverse(sc);
+          const size_t r = size_t(t.h_tile) * 128 + row;
+          *reinterpret_cast<uint4*>(p.h + size_t(f >> 7) * p.h_code_stride + mx4_code_at(r, (f >> 5) & 3)) =
+              make_uint4(mx4_oct(h, inv), mx4_oct(h + 8, inv), mx4_oct(h + 16, inv), mx4_oct(h + 24, inv));
+          p.h_scales[size_t(f >> 7) * p.h_scale_stride + mx4_scale_at(r) + ((f >> 5) & 3)] = uint8_t(sc);
+        }
+      } else {
+        long long dst = (long long)t.h_tile * 128 + row;
+        if (EPI == kMx4Down) dst = row < t.rows ? p.rowmap[dst] : -1;
+        const int cols = min(128, p.n_out - n);
+        if (dst < 0 || row >= t.rows) {
+        } else if (EPI == kMx4Down || p.out_f32) {
+          float* y = static_cast<float*>(p.out) + dst * p.ldo + n;
+          if (cols == 128 && p.vec) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) store32(y + c * 8, v + c * 8);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c < cols) y[c] = __uint_as_float(v[c]);
+          }
+        } else {
+          uint16_t* y = static_cast<uint16_t*>(p.out) + dst * p.ldo + n;
+          if (cols == 128 && p.vec) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              uint32_t w[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                w[j] = pack2bf(__uint_as_float(v[c * 16 + 2 * j]), __uint_as_float(v[c * 16 + 2 * j + 1]));
+              store32(y + c * 16, w);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c < cols) y[c] = f2bf(__uint_as_float(v[c]));
+          }
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    const int q = warp & 3, grp = (warp - 2) >> 2, row = q * 32 + lane;
+    if (first < total) {
+      const Item t = item_at<EPI>(p, first);
+      int ok = 1;
+      if (lane == 0) ok = mbar_wait_cl(&ctl->tfull, 0, abort, p.err) ? 1 : 0;
+      if (__shfl_sync(0xffffffffu, ok, 0)) {
+        tc_fence_after();
+        // the ring is free: every copy has landed and every MMA has read it
+        const int ldp = p.tn + 4;
+        float* part = reinterpret_cast<float*>(ring) + size_t(row) * ldp;
+        for (int c = grp * 32; c < p.tn; c += 64) {
+          uint32_t v[32];
+          tmem_ld32(tmem + (uint32_t(q * 32) << 16) + uint32_t(c), v);
+          tmem_ld_wait();
+          if (row < t.rows) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<uint4*>(part + c + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          }
+        }
+        tc_fence_before();
+      }
+    }
+  }
+
+  if constexpr (!WIDE) {
+    // every CTA's partial tile is in its shared memory; a wait that ran out anywhere in the cluster stops all
+    cluster_sync();
+    bool run = first < total && warp >= 2;
+    for (int r = 0; run && r < cs; ++r) {
+      int a;
+      asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(a) : "r"(peer_addr(&ctl->abort, r)) : "memory");
+      run = a == 0;
+    }
+    if (run) {
+      const Item t = item_at<EPI>(p, first);
+      const int ldp = p.tn + 4;
+      uint32_t peer[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) peer[r] = peer_addr(ring, r < cs ? r : 0);
+      constexpr int kUnit = EPI == kMx4Up ? 64 : 32;
+      const int units = p.tn / kUnit, mine = (units - rank + cs - 1) / cs;  // units rank, rank + cs, ...
+      for (int i = warp - 2; i < mine * t.rows; i += 8) {
+        const int row = i / mine, unit = rank + (i - row * mine) * cs;
+        const uint32_t at = uint32_t(row * ldp + unit * kUnit + lane) * 4u;
+        float x = 0.f, u = 0.f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r < cs) {
+            x += peer_float(peer[r] + at);
+            if (EPI == kMx4Up) u += peer_float(peer[r] + at + 128u);
+          }
+        if constexpr (EPI == kMx4Up) {
+          const int f = (t.n0 + unit * 64) >> 1;
+          if (f >= p.n_out) continue;
+          const float h = swiglu(x, u);
+          const uint32_t sc = mx4_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(h) & 0x7fffffffu));
+          uint32_t code = mx4_pair(h * mx4_inverse(sc), 0.f) << (4 * (lane & 7));
+          code |= __shfl_xor_sync(0xffffffffu, code, 1);
+          code |= __shfl_xor_sync(0xffffffffu, code, 2);
+          code |= __shfl_xor_sync(0xffffffffu, code, 4);
+          const size_t r = size_t(t.h_tile) * 128 + row;
+          if ((lane & 7) == 0)
+            *reinterpret_cast<uint32_t*>(p.h + size_t(f >> 7) * p.h_code_stride + mx4_code_at(r, (f >> 5) & 3) +
+                                         (lane >> 3) * 4) = code;
+          if (lane == 0) p.h_scales[size_t(f >> 7) * p.h_scale_stride + mx4_scale_at(r) + ((f >> 5) & 3)] = uint8_t(sc);
+        } else {
+          const int n = t.n0 + unit * 32 + lane;
+          long long dst = (long long)t.h_tile * 128 + row;
+          if (EPI == kMx4Down) dst = p.rowmap[dst];
+          if (dst < 0 || n >= p.n_out) continue;
+          if (EPI == kMx4Down || p.out_f32) static_cast<float*>(p.out)[dst * p.ldo + n] = x;
+          else static_cast<uint16_t*>(p.out)[dst * p.ldo + n] = f2bf(x);
+        }
+      }
+    }
+    cluster_sync();  // the peers have read this CTA's partial tile
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ---- host ----
+
+template <int EPI, bool WIDE>
+cudaError_t go(const Mx4GemmArgs& p, int grid, cudaStream_t s) {
+  static SmemOptIn smem;
+  const void* fn = reinterpret_cast<const void*>(mx4_gemm_kernel<EPI, WIDE>);
+  cudaError_t e = smem.allow(fn, smem_bytes<WIDE>());
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(grid));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = size_t(smem_bytes<WIDE>());
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(WIDE ? 1 : p.split);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<EPI, WIDE>, p);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+// max_items(tn): most items of a launch with weight tiles of tn rows; tile_rows: most token rows of a tile.
+cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s) {
+  const int n_rows = epi == kMx4Up ? 2 * p.n_out : p.n_out;
+  auto tiles_of = [&](int tn) { return (n_rows + tn - 1) / tn; };
+  // Wide tiles once they fill the SMs.
+  const bool wide = max_tiles * tiles_of(kWideN) >= num_sms;
+  p.split = 1;
+  int grid;
+  if (wide) {
+    p.tn = kWideN;
+    p.depth = 2;
+    p.a_groups = 16;
+    p.n_tiles = tiles_of(p.tn);
+    grid = int(std::min<long long>(num_sms, max_tiles * p.n_tiles));
+  } else {
+    p.tn = max_tiles * tiles_of(128) >= num_sms ? 128 : 64;
+    p.n_tiles = tiles_of(p.tn);
+    while (p.split < 8 && max_tiles * p.n_tiles * p.split * 2 <= 2 * num_sms && p.chunks >= 8 * p.split) p.split *= 2;
+    p.a_groups = (tile_rows + 7) / 8;
+    p.depth = p.a_groups <= 4 ? 4 : 2;
+    grid = int(max_tiles * p.n_tiles * p.split);
+  }
+  const int stage = p.depth * (p.a_groups * 512 + p.tn * 64 + 512 + (p.tn > 128 ? 1024 : 512));
+  // the MMA reads 128 rows of A wherever the stage's A begins: the last stage's end stays inside the ring
+  const int slack = (16 - p.a_groups) * 512;
+  p.stages = std::min(kMaxStages, ((wide ? kWideRing : kNarrowRing) - slack) / stage);
+  if (p.stages < 2) return cudaErrorInvalidConfiguration;
+  const int kid = epi == kMx4Up ? kProfMx4Up : epi == kMx4Down ? kProfMx4Down : kProfMx4Matmul;
+  prof_begin(kid, s);
+  cudaError_t e;
+  if (epi == kMx4Up) e = wide ? go<kMx4Up, true>(p, grid, s) : go<kMx4Up, false>(p, grid, s);
+  else if (epi == kMx4Down) e = wide ? go<kMx4Down, true>(p, grid, s) : go<kMx4Down, false>(p, grid, s);
+  else e = wide ? go<kMx4Out, true>(p, grid, s) : go<kMx4Out, false>(p, grid, s);
+  prof_end(kid, s);
+  return e;
+}
+
+}  // namespace mcft

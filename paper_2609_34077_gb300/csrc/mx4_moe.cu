@@ -1,0 +1,331 @@
+// The routed layer on mx4 expert blocks, around its two products (mx4_gemm.cu): which token tiles there are,
+// the input quantised into them, and the weighted sum of the experts' outputs (Section 3.1 Eq. topk).
+//
+// Up to 128 tokens (kMx4SharedTileT) a tile of the tensor cores holds the whole batch, so every selected expert
+// reads the same tile, x in its own order, and one launch plans and quantises. More tokens are permuted by
+// expert into tiles of 128 rows: a histogram and placement on one cluster of eight CTAs, then each token is
+// quantised once and written to its K places. The order of an expert's rows is not defined and does not matter:
+// a row's products do not depend on its place in a tile.
+//
+// Rows of o are in the order of the assignments (t, k), then the shared experts' (s, t), so the combine needs no
+// lookup but `src`: the assignment whose row holds expert idx[t, k]'s output for token t (itself; the first of
+// them where a token names an expert twice; -1 where it names none).
+#include <algorithm>
+
+#include "mx4_args.h"
+
+namespace mcft {
+namespace {
+
+constexpr int kPlanThreads = 256, kPermThreads = 1024, kPermCtas = 8;
+
+__device__ __forceinline__ bool has_block(const Mx4MoeArgs& a, int e) { return (a.have[e >> 5] >> (e & 31)) & 1u; }
+
+// 256 columns of one row from column c0 on: each lane eight values -> four bytes of codes, and the word of four
+// scales in lanes 0 and 16.
+template <typename T>
+__device__ __forceinline__ void quantise256(const T* row, int c0, int C, uint32_t& codes, uint32_t& scales) {
+  const int lane = threadIdx.x & 31, c = c0 + lane * 8;
+  float f[8];
+  if (c < C) {  // (C is a multiple of 64)
+    if constexpr (sizeof(T) == 2) {
+      unpack8(ldg16(row + c), f);
+    } else {
+      *reinterpret_cast<uint4*>(f) = ldg16(row + c);
+      *reinterpret_cast<uint4*>(f + 4) = ldg16(row + c + 4);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = 0.f;
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  const uint32_t s = mx4_scale(m);
+  scales = s << (8 * ((lane >> 2) & 3));
+  scales |= __shfl_xor_sync(0xffffffffu, scales, 4);
+  scales |= __shfl_xor_sync(0xffffffffu, scales, 8);
+  codes = mx4_oct(f, mx4_inverse(s));
+}
+
+__device__ __forceinline__ void put256(uint8_t* q, const Mx4Layout& L, size_t r, int c0, uint32_t codes, uint32_t scales) {
+  const int lane = threadIdx.x & 31;
+  const size_t chunk = size_t(c0 + lane * 8) >> 7;
+  if (chunk >= L.chunks) return;
+  *reinterpret_cast<uint32_t*>(q + chunk * L.code_stride() + mx4_code_at(r, (lane >> 2) & 3) + (lane & 3) * 4) = codes;
+  if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(q + L.scales() + chunk * L.scale_stride() + mx4_scale_at(r)) = scales;
+}
+
+// CTA 0 plans; the others quantise eight rows by 1024 columns each.
+template <typename T>
+__global__ void __launch_bounds__(kPlanThreads) mx4_plan_kernel(const __grid_constant__ Mx4MoeArgs a) {
+  pdl_wait();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (blockIdx.x > 0) {
+    const int spans = (a.d + 1023) / 1024, b = int(blockIdx.x) - 1;
+    const int r = b / spans * 8 + warp, c0 = b % spans * 1024;
+    if (r >= a.T) return;
+    const Mx4Layout L(a.x_rows, a.d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t codes, scales;
+      quantise256(static_cast<const T*>(a.x) + size_t(r) * a.d, c0 + 256 * j, a.d, codes, scales);
+      put256(a.xq, L, size_t(r), c0 + 256 * j, codes, scales);
+    }
+    return;
+  }
+  __shared__ int used[kMaxMx4E], tile_of[kMaxMx4E], wsum[kPlanThreads / 32], bad, total;
+  const int n = a.T * a.K;
+  if (tid < kMaxMx4E) used[tid] = 0;
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += kPlanThreads) {
+    const int e = a.idx[i];
+    if (e >= 0 && e < a.E && has_block(a, e)) used[e] = 1;
+    else if (e != -1) bad = 1;
+  }
+  __syncthreads();
+  const int on = tid < a.E ? used[tid] : 0;  // one thread an expert
+  const unsigned ballot = __ballot_sync(0xffffffffu, on != 0);
+  if (lane == 0) wsum[warp] = __popc(ballot);
+  __syncthreads();
+  int before = __popc(ballot & ((1u << lane) - 1u));
+  for (int w = 0; w < warp; ++w) before += wsum[w];
+  if (tid == kPlanThreads - 1) total = before + on;
+  if (tid < a.E) tile_of[tid] = before;
+  if (on) a.tiles[before] = Mx4Tile{tid, 0, before, 1, a.T, {0, 0, 0}};
+  __syncthreads();
+  if (tid < a.S) a.tiles[total + tid] = Mx4Tile{a.E + tid, 0, total + tid, 1, a.T, {0, 0, 0}};
+  if (tid == 0) {
+    if (bad) set_error(a.err, kErrInvalid);
+    a.hdr->abort = bad;
+    a.hdr->tiles = total + a.S;
+  }
+  for (int i = tid; i < (total + a.S) * a.T; i += kPlanThreads) {
+    const int tile = i / a.T, t = i - tile * a.T;
+    a.rowmap[tile * 128 + t] = tile < total ? -1 : n + (tile - total) * a.T + t;
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kPlanThreads) {
+    const int t = i / a.K, e = a.idx[i];
+    int src = -1;
+    if (e >= 0 && e < a.E && used[e]) {
+      src = t * a.K;
+      while (a.idx[src] != e) ++src;  // (ends at i)
+      if (src == i) a.rowmap[tile_of[e] * 128 + t] = i;
+    }
+    a.src[i] = src;
+  }
+}
+
+__device__ __forceinline__ uint32_t cta_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int peer_int(const int* p, uint32_t rank) {
+  int v;
+  asm volatile(
+      "{\n .reg .u32 q;\n mapa.shared::cluster.u32 q, %1, %2;\n ld.shared::cluster.s32 %0, [q];\n}"
+      : "=r"(v)
+      : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank)
+      : "memory");
+  return v;
+}
+
+// One cluster: each CTA counts and places an eighth of the assignments.
+__global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads)
+    mx4_permute_kernel(const __grid_constant__ Mx4MoeArgs a) {
+  __shared__ int cnt[kMaxMx4E + 1], next[kMaxMx4E], tile0[kMaxMx4E], wsum[8], routed;  // cnt[kMaxMx4E]: bad ids
+  pdl_wait();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = int(cta_rank());
+  const long long n = (long long)a.T * a.K;
+  const long long i0 = n * rank / kPermCtas, i1 = n * (rank + 1) / kPermCtas;
+  if (tid <= kMaxMx4E) cnt[tid] = 0;
+  __syncthreads();
+  for (long long i = i0 + tid; i < i1; i += kPermThreads) {
+    const int e = a.idx[i];
+    if (e >= 0 && e < a.E && has_block(a, e)) atomicAdd(&cnt[e], 1);
+    else if (e != -1) cnt[kMaxMx4E] = 1;
+  }
+  cluster_barrier();
+  int before = 0, sum = 0, bad = 0, tiles = 0;
+  if (tid < kMaxMx4E) {
+    for (int r = 0; r < kPermCtas; ++r) {
+      const int c = peer_int(&cnt[tid], r);
+      if (r < rank) before += c;
+      sum += c;
+      bad |= peer_int(&cnt[kMaxMx4E], r);
+    }
+    tiles = (sum + 127) >> 7;
+    int incl = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    tile0[tid] = incl - tiles;
+    if (lane == 31) wsum[warp] = incl;
+  }
+  __syncthreads();
+  if (tid < kMaxMx4E) {
+    int base = tile0[tid];
+    for (int w = 0; w < warp; ++w) base += wsum[w];
+    tile0[tid] = base;
+    next[tid] = base * 128 + before;
+    if (tid == kMaxMx4E - 1) routed = base + tiles;
+    if (rank == 0) {
+      for (int m = 0; m < tiles; ++m)
+        a.tiles[base + m] = Mx4Tile{tid, base + m, base, tiles, min(128, sum - m * 128), {0, 0, 0}};
+      if (tid == 0) {
+        if (bad) set_error(a.err, kErrInvalid);
+        a.hdr->abort = bad;
+      }
+    }
+  }
+  __syncthreads();
+  const int xt = (a.T + 127) >> 7;
+  if (rank == 0) {
+    if (tid == 0) a.hdr->tiles = routed + a.S * xt;
+    for (int i = tid; i < a.S * xt; i += kPermThreads) {
+      const int s = i / xt, m = i - s * xt;
+      a.tiles[routed + i] = Mx4Tile{a.E + s, a.x_tile0 + m, routed + s * xt, xt, min(128, a.T - m * 128), {0, 0, 0}};
+    }
+  }
+  // shared experts' rows; rows that pad a routed expert's last tile are past its count and are not looked at
+  for (long long i = (long long)rank * kPermThreads + tid; i < (long long)a.S * a.T; i += kPermThreads * kPermCtas) {
+    const int s = int(i / a.T), t = int(i - (long long)s * a.T);
+    a.rowmap[((long long)routed + s * xt) * 128 + t] = int(n + i);
+  }
+  for (long long i = i0 + tid; i < i1; i += kPermThreads) {
+    const int e = a.idx[i];
+    int row = -1;
+    if (e >= 0 && e < a.E && has_block(a, e)) {
+      row = atomicAdd(&next[e], 1);
+      a.rowmap[row] = int(i);
+    }
+    a.pos[i] = row;
+    a.src[i] = row >= 0 ? int(i) : -1;
+  }
+  cluster_barrier();  // the peers have read this CTA's counts
+}
+
+// One warp a token: quantised once, written to its K places and (shared experts) to its place in x itself.
+template <typename T>
+__global__ void __launch_bounds__(256) mx4_spread_kernel(const __grid_constant__ Mx4MoeArgs a) {
+  pdl_wait();
+  const int t = int(blockIdx.x) * 8 + int(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (t >= a.T) return;
+  const Mx4Layout L(a.x_rows, a.d);
+  int mine = lane < a.K ? a.pos[(long long)t * a.K + lane] : -1;
+  if (lane == a.K && a.S > 0) mine = a.x_tile0 * 128 + t;
+  const unsigned to = __ballot_sync(0xffffffffu, mine >= 0);
+  const T* row = static_cast<const T*>(a.x) + size_t(t) * a.d;
+  for (int c0 = 0; c0 < a.d; c0 += 256) {
+    uint32_t codes, scales;
+    quantise256(row, c0, a.d, codes, scales);
+    for (unsigned m = to; m; m &= m - 1) {
+      const int r = __shfl_sync(0xffffffffu, mine, __ffs(m) - 1);
+      put256(a.xq, L, size_t(r), c0, codes, scales);
+    }
+  }
+}
+
+// y[t] = sum_k gate[t, k] o[src[t, k]] + sum_s o[shared s, t], in this order; four columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) mx4_combine_kernel(const __grid_constant__ Mx4MoeArgs a) {
+  pdl_wait();
+  if (a.hdr->abort) return;
+  const int t = int(blockIdx.x), c = (int(blockIdx.y) * 256 + int(threadIdx.x)) * 4;
+  if (c >= a.d) return;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](long long row, float g) {
+    const float4 v = *reinterpret_cast<const float4*>(a.o + row * a.d + c);
+    acc.x = fmaf(g, v.x, acc.x);
+    acc.y = fmaf(g, v.y, acc.y);
+    acc.z = fmaf(g, v.z, acc.z);
+    acc.w = fmaf(g, v.w, acc.w);
+  };
+#pragma unroll 4
+  for (int k = 0; k < a.K; ++k) {
+    const int src = a.src[(long long)t * a.K + k];
+    if (src >= 0) add(src, a.gate[(long long)t * a.K + k]);
+  }
+  for (int s = 0; s < a.S; ++s) add((long long)a.T * a.K + (long long)s * a.T + t, 1.f);
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + (long long)t * a.d + c) =
+        make_uint2(pack2bf(acc.x, acc.y), pack2bf(acc.z, acc.w));
+  else
+    *reinterpret_cast<float4*>(static_cast<float*>(a.y) + (long long)t * a.d + c) = acc;
+}
+
+size_t align512(size_t v) { return (v + 511) & ~size_t(511); }
+
+}  // namespace
+
+Mx4MoeLayout::Mx4MoeLayout(int d, int E, int K, int w, int S, int T) {
+  const long long n = (long long)T * K;
+  permuted = T > kMx4SharedTileT;
+  if (permuted) {
+    // at most one part-filled tile for each expert that has rows
+    routed_tiles = std::min<long long>(n / 128 + std::min<long long>(E, n), n);
+    x_tiles = S > 0 ? (T + 127) / 128 : 0;
+    tiles = routed_tiles + (long long)S * x_tiles;
+  } else {
+    routed_tiles = std::min<long long>(E, n);
+    x_tiles = 0;
+    tiles = routed_tiles + S;
+  }
+  const long long x_rows = permuted ? (routed_tiles + x_tiles) * 128 : T;
+  size_t at = 0;
+  auto place = [&](size_t bytes) {
+    const size_t here = at;
+    at = align512(at + bytes);
+    return here;
+  };
+  hdr = place(sizeof(Mx4Header));
+  tile = place(sizeof(Mx4Tile) * size_t(tiles));
+  rowmap = place(sizeof(int) * size_t(tiles) * 128);
+  src = place(sizeof(int) * size_t(n));
+  pos = place(permuted ? sizeof(int) * size_t(n) : 0);
+  x = place(Mx4Layout(x_rows, d).bytes());
+  h = place(Mx4Layout(tiles * 128, w).bytes());
+  o = place(sizeof(float) * (size_t(n) + size_t(S) * T) * d);
+  total = at;
+}
+
+cudaError_t launch_mx4_prepare(const Mx4MoeArgs& a, int dtype, bool permuted, cudaStream_t s) {
+  prof_begin(kProfMx4Prepare, s);
+  cudaError_t e;
+  const bool bf = dtype == MCFT_BF16;
+  if (!permuted) {
+    const unsigned grid = 1u + unsigned((a.T + 7) / 8) * unsigned((a.d + 1023) / 1024);
+    e = bf ? launch_pdl(mx4_plan_kernel<__nv_bfloat16>, dim3(grid), dim3(kPlanThreads), 0, s, a)
+           : launch_pdl(mx4_plan_kernel<float>, dim3(grid), dim3(kPlanThreads), 0, s, a);
+  } else {
+    e = launch_pdl(mx4_permute_kernel, dim3(kPermCtas), dim3(kPermThreads), 0, s, a);
+    const dim3 grid{unsigned((a.T + 7) / 8)};
+    if (e == cudaSuccess)
+      e = bf ? launch_pdl(mx4_spread_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, a)
+             : launch_pdl(mx4_spread_kernel<float>, grid, dim3(256), 0, s, a);
+  }
+  prof_end(kProfMx4Prepare, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+cudaError_t launch_mx4_combine(const Mx4MoeArgs& a, int dtype, cudaStream_t s) {
+  prof_begin(kProfMx4Combine, s);
+  const dim3 grid(unsigned(a.T), unsigned((a.d + 1023) / 1024));
+  const cudaError_t e = dtype == MCFT_BF16 ? launch_pdl(mx4_combine_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, a)
+                                           : launch_pdl(mx4_combine_kernel<float>, grid, dim3(256), 0, s, a);
+  prof_end(kProfMx4Combine, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace mcft

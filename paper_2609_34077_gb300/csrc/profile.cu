@@ -16,7 +16,8 @@ const char* const kNames[kProfCount] = {
     "route",     "cache_step", "permute", "gather",       "ffn13_rowwise", "ffn2_rowwise",
     "gemm13_tc", "gemm2_tc",   "combine", "ffn13_decode", "ffn2_decode", "fetch", "lora_down",
     "rmsnorm",   "prefetch",   "fetch_prefetch", "prologue", "ffn_decode", "host_copy",
-    "ffn_decode_fetch", "gemm13_tc_pair", "gemm2_tc_pair"};
+    "ffn_decode_fetch", "gemm13_tc_pair", "gemm2_tc_pair", "mx4_quantize", "mx4_dequantize", "mx4_matmul",
+    "mx4_prepare", "mx4_up", "mx4_down", "mx4_combine", "route_scored", "route_scored_grad"};
 
 struct Pending {
   int kid;

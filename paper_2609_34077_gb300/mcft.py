@@ -23,7 +23,7 @@ MCFT_CACHE_LRU, MCFT_CACHE_LFU, MCFT_CACHE_FIFO = 0, 1, 2
 POLICY = {"LRU": MCFT_CACHE_LRU, "LFU": MCFT_CACHE_LFU, "FIFO": MCFT_CACHE_FIFO}
 
 # every exported entry point: name -> (restype, argtypes)
-_vp, _i, _sz = C.c_void_p, C.c_int, C.c_size_t
+_vp, _i, _sz, _ll = C.c_void_p, C.c_int, C.c_size_t, C.c_longlong
 SIGNATURES = {
     "mcft_route": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
     "mcft_moe_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
@@ -55,6 +55,14 @@ SIGNATURES = {
     "mcft_cache_export": (_i, [_vp, _vp, C.POINTER(_sz), _vp]),
     "mcft_cache_import": (_i, [_vp, _vp, _sz, _vp]),
     "mcft_cache_destroy": (None, [_vp]),
+    "mcft_mx4_size": (_i, [_ll, _ll, C.POINTER(_sz)]),
+    "mcft_mx4_quantize": (_i, [_vp, _ll, _ll, _ll, _i, _vp, _vp]),
+    "mcft_mx4_dequantize": (_i, [_vp, _ll, _ll, _i, _vp, _ll, _vp]),
+    "mcft_mx4_matmul": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _ll, _vp]),
+    "mcft_mx4_expert_size": (_i, [_vp, C.POINTER(_sz)]),
+    "mcft_mx4_pack_expert": (_i, [_vp, _vp, _vp, _vp]),
+    "mcft_mx4_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
+    "mcft_moe_forward_mx4": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "mcft_device_error": (_i, [_vp]),
     "mcft_test_inject": (_i, [_i, _i, C.c_ulonglong, _i]),
     "mcft_profile_enable": (_i, [_i]),
@@ -534,3 +542,83 @@ def mcft_mask_grad(desc: LayerDesc, idx, gate, dgate, pi, dm=None, dm_tilde=None
     _check(lib().mcft_mask_grad(C.byref(desc), _ptr(idx), _ptr(gate), _ptr(dgate), T, _ptr(pi),
                                 _ptr(dm), _ptr(dm_tilde), 1 if accumulate else 0, _stream(stream)))
     return dm, dm_tilde
+
+
+_MX4_DTYPE = {torch.float32: MCFT_F32, torch.bfloat16: MCFT_BF16}
+
+
+def _rows(t):
+    """Address and row stride of a [rows, cols] tensor whose rows are contiguous."""
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), "a matrix with contiguous rows is wanted"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def mcft_mx4_size(rows: int, cols: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mcft_mx4_size(int(rows), int(cols), C.byref(n)))
+    return n.value
+
+
+def mcft_mx4_quantize(x, q=None, stream=None):
+    """The mx4 matrix (a uint8 tensor of mcft_mx4_size bytes) of x [rows, cols], fp32 or bf16."""
+    rows, cols = x.shape
+    ptr, ld = _rows(x)
+    if q is None:
+        q = torch.empty(mcft_mx4_size(rows, cols), dtype=torch.uint8, device=x.device)
+    _check(lib().mcft_mx4_quantize(ptr, rows, cols, ld, _MX4_DTYPE[x.dtype], _ptr(q), _stream(stream)))
+    return q
+
+
+def mcft_mx4_dequantize(q, rows, cols, dtype=torch.bfloat16, y=None, stream=None):
+    """The values [rows, cols] that the mx4 matrix q stands for, fp32 or bf16."""
+    if y is None:
+        y = torch.empty((rows, cols), dtype=dtype, device=q.device)
+    ptr, ld = _rows(y)
+    _check(lib().mcft_mx4_dequantize(_ptr(q), rows, cols, _MX4_DTYPE[y.dtype], ptr, ld, _stream(stream)))
+    return y
+
+
+def mcft_mx4_matmul(a, b, M, N, K, dtype=torch.bfloat16, y=None, stream=None):
+    """y [M, N] = A B^T of the mx4 matrices a [M, K] and b [N, K], fp32 or bf16."""
+    if y is None:
+        y = torch.empty((M, N), dtype=dtype, device=a.device)
+    ptr, ld = _rows(y)
+    _check(lib().mcft_mx4_matmul(_ptr(a), _ptr(b), M, N, K, _MX4_DTYPE[y.dtype], ptr, ld, _stream(stream)))
+    return y
+
+
+def mcft_mx4_expert_size(desc: LayerDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mcft_mx4_expert_size(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def mcft_mx4_pack_expert(desc: LayerDesc, block, out=None, stream=None):
+    """The mx4 expert block (uint8) of a packed expert block [W1 | W3 | W2] of the layer dtype."""
+    if out is None:
+        out = torch.empty(mcft_mx4_expert_size(desc), dtype=torch.uint8, device=block.device)
+    _check(lib().mcft_mx4_pack_expert(C.byref(desc), _ptr(block), _ptr(out), _stream(stream)))
+    return out
+
+
+def mcft_mx4_workspace_size(desc: LayerDesc, T_max: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mcft_mx4_workspace_size(C.byref(desc), int(T_max), C.byref(n)))
+    return n.value
+
+
+def mcft_moe_forward_mx4(desc: LayerDesc, x, idx, gate, experts, shared=(), y=None, workspace=None,
+                         stream=None):
+    """y [T, d] of the layer on mx4 expert blocks; an idx of -1 is no expert. ``experts`` and
+    ``workspace`` as for mcft_moe_forward."""
+    T = x.shape[0]
+    if y is None:
+        y = torch.empty_like(x)
+    if workspace is None:
+        workspace = torch.empty(mcft_mx4_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
+    ex = _ptr_array(experts, desc.E)
+    sh = _ptr_array(shared, desc.n_shared)
+    _check(lib().mcft_moe_forward_mx4(C.byref(desc), _ptr(x), T, _ptr(idx), _ptr(gate), ex.buffer_info()[0],
+                                      sh.buffer_info()[0], _ptr(y), _ptr(workspace), workspace.numel(),
+                                      _stream(stream)))
+    return y
