@@ -508,6 +508,63 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
                                  mcft_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Scored routing: the routing rules of layers with more experts than mcft_route takes, and of those whose
+ * scores are no softmax (no counterpart in the paper, whose models route by softmax; its Stage 2 fine-tunes
+ * the routers under the mask, Section 3.2, for which the gradient is).
+ *   z = W x;  s = softmax(z) or sigmoid(z);  c = s + b
+ * b is a bias for balance: it moves the choice and not the gates. An entry of -infinity keeps its expert out
+ * of every choice, which makes b a hard mask too. With n_group > 1 the experts are n_group groups of equal
+ * size in order of index; a group's value is the sum of its group_top largest c (-infinity if it has fewer
+ * eligible experts), and only the topk_group best groups' experts are eligible. A = the K largest c among
+ * the eligible; ties, of groups too, go to the lower index.
+ *   gate_i = scale s_i / sum_{j in A} s_j (MCFT_GATE_RENORM; 0 where that sum is 0) or scale s_i.
+ * A token with fewer than K eligible experts has idx -1 and gate 0 in its last places.
+ *   d          multiple of 64
+ *   E          experts, 1..256;  K 1..min(E, 16)
+ *   n_group    1..32, divides E;  topk_group 1..n_group;  group_top 1 or 2, at most E / n_group
+ *   score      mcft_score;  gate mcft_gate_mode;  dtype mcft_dtype of x and w_router
+ *   scale      > 0, finite */
+typedef enum { MCFT_SCORE_SOFTMAX = 0, MCFT_SCORE_SIGMOID = 1 } mcft_score;
+typedef struct {
+  int d, E, K, n_group, topk_group, group_top, score, gate, dtype;
+  float scale;
+} mcft_scored_desc;
+
+/* mcft_route_scored:
+ *   x        device [T, d] layer dtype; w_router device [E, d] layer dtype; both 16-byte aligned
+ *   bias     device [E] fp32, or NULL
+ *   idx      device [T, K] int32 out, by descending c;  gate device [T, K] fp32 out
+ *   logits   device [T, E] fp32 out: z, for mcft_route_scored_grad; or NULL
+ *   load     device [E] int32 out: how many tokens chose each expert, from which a caller moves the bias;
+ *            or NULL
+ * Logits are fp32 sums. A NaN score or bias sets the device error word and keeps its expert out. T = 0 is a
+ * no-op (load is not written). Asynchronous; the same bits whenever the inputs are the same. Errors:
+ * MCFT_ERR_INVALID for a NULL or misaligned pointer, a bad desc, T < 0; MCFT_ERR_UNSUPPORTED for E > 256,
+ * K > 16, n_group > 32, group_top > 2. */
+mcft_status mcft_route_scored(const mcft_scored_desc* desc, const void* x, int T, const void* w_router,
+                              const float* bias, int32_t* idx, float* gate, float* logits, int32_t* load,
+                              mcft_stream_t stream);
+
+/* mcft_route_scored_grad: gradients of a loss that reaches the router through the gates (the choice of
+ * experts is piecewise constant), from dgate = dL/dgate (mcft_gate_grad's, for instance):
+ *   dz = (d gate / d z)^T dgate,  dx = dz W,  dW = dz^T x.
+ *   x, w_router, idx, gate, logits  as given to and written by mcft_route_scored; an idx of -1 contributes
+ *            nothing and its gate and dgate are not read into the sum; another id outside [0, E) sets the
+ *            device error word and counts as -1
+ *   dgate    device [T, K] fp32
+ *   dx       device [T, d] layer dtype out, or NULL
+ *   dw       device [E, d] fp32 out, added to what it holds if accumulate is non-zero; or NULL
+ *   workspace device, mcft_route_scored_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until
+ *            the call's kernels finish; enough for any smaller T
+ * T = 0 writes zeros to dw (unless accumulating). Asynchronous; the same bits whenever the inputs are the
+ * same. Errors as above, and for dx and dw both NULL or a workspace too small. */
+mcft_status mcft_route_scored_grad_workspace_size(const mcft_scored_desc* desc, int T_max, size_t* bytes);
+mcft_status mcft_route_scored_grad(const mcft_scored_desc* desc, const void* x, int T, const void* w_router,
+                                   const int32_t* idx, const float* gate, const float* logits,
+                                   const float* dgate, void* dx, float* dw, int accumulate, void* workspace,
+                                   size_t ws_bytes, mcft_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
  * mcft_device_error: synchronise `stream`, return and clear the device error word of the current
  * device: MCFT_OK, MCFT_ERR_INVALID (bad id, missing expert pointer) or MCFT_ERR_TIMEOUT. */
 mcft_status mcft_device_error(mcft_stream_t stream);

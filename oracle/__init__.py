@@ -19,7 +19,8 @@ Everything is a plain, slow, readable restatement of the paper's definitions in 
   and the next-layer prediction that drives expert prefetch; the cache's prefetch event is in
   ``cache``.
 * ``mx4``      - microscaled 4-bit floating point: rounding, products, the layer on rounded experts.
+* ``scored``   - scored routing (sigmoid or softmax scores, bias, groups) and its gradient.
 
 Pins (tests marked ``not gpu``) tie each function to something other than itself; see the tests.
 """
-from . import cache, ffn, mask, mx4, routing, stack  # noqa: F401
+from . import cache, ffn, mask, mx4, routing, scored, stack  # noqa: F401

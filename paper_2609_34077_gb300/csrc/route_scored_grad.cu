@@ -1,0 +1,178 @@
+// Gradient of the scored routing. With u_i = gate_i (dg_i - [renormalised gates] sum_j gate_j dg_j / scale) on a
+// token's chosen experts and 0 elsewhere,
+//   dz_e = u_e (1 - s_e)         sigmoid scores
+//   dz_e = u_e                   softmax scores, renormalised (the softmax's own sum cancels)
+//   dz_e = u_e - s_e sum_j u_j   softmax scores, plain: every expert
+// (the choice itself is piecewise constant, and the bias does not reach the gates); then dx = dz W, dW = dz^T x.
+#include <algorithm>
+
+#include "route_scored_warp.cuh"
+
+namespace mcft {
+namespace {
+
+// One warp a token.
+__global__ void __launch_bounds__(256) scored_dz_kernel(const __grid_constant__ ScoredGradArgs a, float* dz, unsigned* err) {
+  pdl_wait();
+  __shared__ float rows[8][kMaxScoredE];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E;
+  const int t = int(blockIdx.x) * 8 + warp;
+  if (t >= a.T) return;
+  float* row = rows[warp];
+  const float* z = a.logits + size_t(t) * E;
+  for (int e = lane; e < E; e += 32) row[e] = 0.f;
+  __syncwarp();
+  int e = -1;
+  float g = 0.f, dg = 0.f;
+  if (lane < a.K) {
+    e = a.idx[size_t(t) * a.K + lane];
+    if (e < -1 || e >= E) {
+      set_error(err, kErrInvalid);
+      e = -1;
+    }
+    if (e >= 0) {
+      g = a.gate[size_t(t) * a.K + lane];
+      dg = a.dgate[size_t(t) * a.K + lane];
+    }
+  }
+  float u = g * dg;
+  const float sum_u = warp_sum(u);
+  if (a.gate_mode == MCFT_GATE_RENORM) u = g * (dg - sum_u / a.scale);
+  if (e >= 0) {
+    if (a.score == MCFT_SCORE_SIGMOID) u *= 1.f / (1.f + expf(z[e]));  // 1 - s
+    atomicAdd(row + e, u);  // (one addend an expert, unless the caller names one twice)
+  }
+  __syncwarp();
+  float* out = dz + size_t(t) * E;
+  if (a.score == MCFT_SCORE_SOFTMAX && a.gate_mode == MCFT_GATE_PLAIN) {
+    float m, sum;
+    softmax_stats(z, E, m, sum);
+    for (int i = lane; i < E; i += 32) out[i] = row[i] - expf(z[i] - m) / sum * sum_u;
+  } else {
+    for (int i = lane; i < E; i += 32) out[i] = row[i];
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p) {
+  if constexpr (sizeof(T) == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return make_float4(bf16lo(v.x), bf16hi(v.x), bf16lo(v.y), bf16hi(v.y));
+  } else {
+    return *reinterpret_cast<const float4*>(p);
+  }
+}
+
+// C[m, n] = sum_k A[m, k] B[k, n] in fp32: 64 x 64 tiles, 4 x 4 a thread, 16 of k at a time. A fp32 with strides
+// am, ak; B rows of n (a multiple of 64) contiguous values. blockIdx.z: a range of k, into its own plane.
+struct MultiplyArgs {
+  const float* a;
+  const void* b;
+  void* c;
+  long long am, ak;
+  int M, N, K, k_share, accumulate;
+};
+template <typename TB, typename TC>
+__global__ void __launch_bounds__(256) multiply_kernel(const __grid_constant__ MultiplyArgs p) {
+  __shared__ float as[16][64 + 4], bs[16][64];
+  pdl_wait();
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int m0 = int(blockIdx.y) * 64, n0 = int(blockIdx.x) * 64;
+  const int k0 = int(blockIdx.z) * p.k_share, k1 = min(p.K, k0 + p.k_share);
+  const TB* b = static_cast<const TB*>(p.b);
+  float acc[4][4] = {};
+  for (int kb = k0; kb < k1; kb += 16) {
+    __syncthreads();
+    for (int i = tid; i < 1024; i += 256) {
+      // the index that is contiguous in A goes with the thread
+      const int m = p.am == 1 ? i & 63 : i >> 4, k = p.am == 1 ? i >> 6 : i & 15;
+      as[k][m] = m0 + m < p.M && kb + k < k1 ? p.a[(m0 + m) * p.am + (kb + k) * p.ak] : 0.f;
+    }
+    const int k = tid >> 4, n = (tid & 15) * 4;
+    *reinterpret_cast<float4*>(&bs[k][n]) =
+        kb + k < k1 ? load4(b + (long long)(kb + k) * p.N + n0 + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const float4 x = *reinterpret_cast<const float4*>(&as[q][ty * 4]), y = *reinterpret_cast<const float4*>(&bs[q][tx * 4]);
+      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[i], ys[j], acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = m0 + ty * 4 + i;
+    if (m >= p.M) break;
+    TC* c = static_cast<TC*>(p.c) + ((long long)blockIdx.z * p.M + m) * p.N + n0 + tx * 4;
+    if constexpr (sizeof(TC) == 2)
+      *reinterpret_cast<uint2*>(c) = make_uint2(pack2bf(acc[i][0], acc[i][1]), pack2bf(acc[i][2], acc[i][3]));
+    else
+      *reinterpret_cast<float4*>(c) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  }
+}
+
+// dw (+)= the sum of the planes, in order.
+__global__ void __launch_bounds__(256) add_planes_kernel(const float* planes, float* dw, long long n, int count, int accumulate) {
+  pdl_wait();
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  float4 v = accumulate ? *reinterpret_cast<const float4*>(dw + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < count; ++p) {
+    const float4 q = *reinterpret_cast<const float4*>(planes + p * n + i);
+    v.x += q.x;
+    v.y += q.y;
+    v.z += q.z;
+    v.w += q.w;
+  }
+  *reinterpret_cast<float4*>(dw + i) = v;
+}
+
+size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
+
+// Tokens of one plane of dW.
+int token_share(int T, int d, int E) {
+  const int tiles = (d / 64) * ((E + 63) / 64);
+  const int planes = std::max(1, std::min((304 + tiles - 1) / tiles, (T + 127) / 128));
+  return ((T + planes - 1) / planes + 15) / 16 * 16;
+}
+
+}  // namespace
+
+size_t scored_grad_workspace(int T, int d, int E, int K, int dtype) {
+  (void)K;
+  (void)dtype;
+  const int share = token_share(T, d, E), planes = (T + share - 1) / share;
+  return align256(sizeof(float) * size_t(T) * E) + align256(sizeof(float) * size_t(planes) * E * d);
+}
+
+cudaError_t launch_route_scored_grad(const ScoredGradArgs& a, int dtype, cudaStream_t s) {
+  prof_begin(kProfRouteScoredGrad, s);
+  float* dz = static_cast<float*>(a.workspace);
+  float* planes = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256(sizeof(float) * size_t(a.T) * a.E));
+  const bool bf = dtype == MCFT_BF16;
+  cudaError_t e = launch_pdl(scored_dz_kernel, dim3((a.T + 7) / 8), dim3(256), 0, s, a, dz, device_error_word());
+  if (e == cudaSuccess && a.dx) {
+    const MultiplyArgs p{dz, a.w_router, a.dx, a.E, 1, a.T, a.d, a.E, a.E, 0};
+    const dim3 grid(unsigned(a.d / 64), unsigned((a.T + 63) / 64));
+    e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, __nv_bfloat16>, grid, dim3(256), 0, s, p)
+           : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+  }
+  if (e == cudaSuccess && a.dw) {
+    const int share = token_share(a.T, a.d, a.E), count = (a.T + share - 1) / share;
+    const MultiplyArgs p{dz, a.x, planes, 1, a.E, a.E, a.d, a.T, share, 0};
+    const dim3 grid(unsigned(a.d / 64), unsigned((a.E + 63) / 64), unsigned(count));
+    e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, float>, grid, dim3(256), 0, s, p)
+           : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+    const long long n = (long long)a.E * a.d;
+    if (e == cudaSuccess)
+      e = launch_pdl(add_planes_kernel, dim3(unsigned((n / 4 + 255) / 256)), dim3(256), 0, s,
+                     static_cast<const float*>(planes), a.dw, n, count, a.accumulate);
+  }
+  prof_end(kProfRouteScoredGrad, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace mcft

@@ -55,6 +55,9 @@ SIGNATURES = {
     "mcft_cache_export": (_i, [_vp, _vp, C.POINTER(_sz), _vp]),
     "mcft_cache_import": (_i, [_vp, _vp, _sz, _vp]),
     "mcft_cache_destroy": (None, [_vp]),
+    "mcft_route_scored": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mcft_route_scored_grad_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
+    "mcft_route_scored_grad": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "mcft_mx4_size": (_i, [_ll, _ll, C.POINTER(_sz)]),
     "mcft_mx4_quantize": (_i, [_vp, _ll, _ll, _ll, _i, _vp, _vp]),
     "mcft_mx4_dequantize": (_i, [_vp, _ll, _ll, _i, _vp, _ll, _vp]),
@@ -542,6 +545,54 @@ def mcft_mask_grad(desc: LayerDesc, idx, gate, dgate, pi, dm=None, dm_tilde=None
     _check(lib().mcft_mask_grad(C.byref(desc), _ptr(idx), _ptr(gate), _ptr(dgate), T, _ptr(pi),
                                 _ptr(dm), _ptr(dm_tilde), 1 if accumulate else 0, _stream(stream)))
     return dm, dm_tilde
+
+
+MCFT_SCORE_SOFTMAX, MCFT_SCORE_SIGMOID = 0, 1
+
+
+class ScoredDesc(C.Structure):
+    """mcft_scored_desc"""
+    _fields_ = [("d", C.c_int), ("E", C.c_int), ("K", C.c_int), ("n_group", C.c_int), ("topk_group", C.c_int),
+                ("group_top", C.c_int), ("score", C.c_int), ("gate", C.c_int), ("dtype", C.c_int),
+                ("scale", C.c_float)]
+
+
+def mcft_route_scored(desc: ScoredDesc, x, w_router, bias=None, idx=None, gate=None, logits=None, load=None,
+                      stream=None):
+    """idx [T, K] int32 (-1: no eligible expert) and gate [T, K] fp32 (allocated on x's device if not given);
+    writes logits [T, E] fp32 and load [E] int32 where given."""
+    T = x.shape[0]
+    if idx is None:
+        idx = torch.empty((T, desc.K), dtype=torch.int32, device=x.device)
+    if gate is None:
+        gate = torch.empty((T, desc.K), dtype=torch.float32, device=x.device)
+    _check(lib().mcft_route_scored(C.byref(desc), _ptr(x), T, _ptr(w_router), _ptr(bias), _ptr(idx), _ptr(gate),
+                                   _ptr(logits), _ptr(load), _stream(stream)))
+    return idx, gate
+
+
+def mcft_route_scored_grad_workspace_size(desc: ScoredDesc, T_max: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mcft_route_scored_grad_workspace_size(C.byref(desc), int(T_max), C.byref(n)))
+    return n.value
+
+
+def mcft_route_scored_grad(desc: ScoredDesc, x, w_router, idx, gate, logits, dgate, dx=None, dw=None,
+                           accumulate=False, workspace=None, stream=None):
+    """(dx [T, d] of the layer dtype, dw [E, d] fp32) from dL/dgate and what mcft_route_scored wrote; dw is
+    added to if accumulate."""
+    T = x.shape[0]
+    if dx is None:
+        dx = torch.empty_like(x)
+    if dw is None:
+        assert not accumulate, "accumulate adds to a dw that is given"
+        dw = torch.empty((desc.E, desc.d), dtype=torch.float32, device=x.device)
+    if workspace is None:
+        workspace = torch.empty(mcft_route_scored_grad_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
+    _check(lib().mcft_route_scored_grad(C.byref(desc), _ptr(x), T, _ptr(w_router), _ptr(idx), _ptr(gate), _ptr(logits),
+                                        _ptr(dgate), _ptr(dx), _ptr(dw), 1 if accumulate else 0, _ptr(workspace),
+                                        workspace.numel(), _stream(stream)))
+    return dx, dw
 
 
 _MX4_DTYPE = {torch.float32: MCFT_F32, torch.bfloat16: MCFT_BF16}
