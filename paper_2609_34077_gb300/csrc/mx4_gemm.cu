@@ -293,13 +293,20 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         for (int b = 0; b < 2; ++b) {  // 32 gate and 32 up columns: one block of h
           const int f = (n >> 1) + b * 32;
           if (f >= p.n_out || row >= t.rows) break;
-          float h[32];
+          float h[32], wild = 0.f;
           uint32_t m = 0;
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
-            h[j] = swiglu(__uint_as_float(v[b * 64 + j]), __uint_as_float(v[b * 64 + 32 + j]));
-            m = max(m, __float_as_uint(h[j]) & 0x7fffffffu);
+            const float g = __uint_as_float(v[b * 64 + j]);
+            wild = fmaxf(wild, fabsf(g));
+            h[j] = silu_branchless(g) * __uint_as_float(v[b * 64 + 32 + j]);
           }
+          if (!silu_regular(wild)) {  // rare: this block again, by IEEE division
+#pragma unroll
+            for (int j = 0; j < 32; ++j) h[j] = silu(__uint_as_float(v[b * 64 + j])) * __uint_as_float(v[b * 64 + 32 + j]);
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) m = max(m, __float_as_uint(h[j]) & 0x7fffffffu);
           const uint32_t sc = mx4_scale(m);
           const float inv = mx4_inverse(sc);
           const size_t r = size_t(t.h_tile) * 128 + row;

@@ -21,41 +21,36 @@ constexpr int kPlanThreads = 256, kPermThreads = 1024, kPermCtas = 8;
 
 __device__ __forceinline__ bool has_block(const Mx4MoeArgs& a, int e) { return (a.have[e >> 5] >> (e & 31)) & 1u; }
 
-// 256 columns of one row from column c0 on: each lane eight values -> four bytes of codes, and the word of four
-// scales in lanes 0 and 16.
+// A block of 32 of one row from column c on (zeros past C, a multiple of 64): its codes and scale byte.
 template <typename T>
-__device__ __forceinline__ void quantise256(const T* row, int c0, int C, uint32_t& codes, uint32_t& scales) {
-  const int lane = threadIdx.x & 31, c = c0 + lane * 8;
-  float f[8];
-  if (c < C) {  // (C is a multiple of 64)
-    if constexpr (sizeof(T) == 2) {
-      unpack8(ldg16(row + c), f);
-    } else {
-      *reinterpret_cast<uint4*>(f) = ldg16(row + c);
-      *reinterpret_cast<uint4*>(f + 4) = ldg16(row + c + 4);
-    }
-  } else {
+__device__ __forceinline__ uint4 quantise_block(const T* row, int c, int C, uint32_t& scale) {
+  float f[32];
+  constexpr int N = 16 / int(sizeof(T));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = 0.f;
+  for (int i = 0; i < 32; i += N) {
+    const uint4 v = c < C ? ldg16(row + c + i) : make_uint4(0, 0, 0, 0);
+    if constexpr (sizeof(T) == 2) unpack8(v, f + i);
+    else *reinterpret_cast<uint4*>(f + i) = v;
   }
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  const uint32_t s = mx4_scale(m);
-  scales = s << (8 * ((lane >> 2) & 3));
-  scales |= __shfl_xor_sync(0xffffffffu, scales, 4);
-  scales |= __shfl_xor_sync(0xffffffffu, scales, 8);
-  codes = mx4_oct(f, mx4_inverse(s));
+  for (int i = 0; i < 32; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+  scale = mx4_scale(m);
+  const float inv = mx4_inverse(scale);
+  return make_uint4(mx4_oct(f, inv), mx4_oct(f + 8, inv), mx4_oct(f + 16, inv), mx4_oct(f + 24, inv));
 }
-
-__device__ __forceinline__ void put256(uint8_t* q, const Mx4Layout& L, size_t r, int c0, uint32_t codes, uint32_t scales) {
-  const int lane = threadIdx.x & 31;
-  const size_t chunk = size_t(c0 + lane * 8) >> 7;
+// Four neighbouring lanes' scale bytes as a word.
+__device__ __forceinline__ uint32_t scale_word(uint32_t scale) {
+  uint32_t w = scale << (8 * (threadIdx.x & 3));
+  w |= __shfl_xor_sync(0xffffffffu, w, 1);
+  w |= __shfl_xor_sync(0xffffffffu, w, 2);
+  return w;
+}
+__device__ __forceinline__ void put_block(uint8_t* q, const Mx4Layout& L, size_t r, int c, const uint4& codes, uint32_t word) {
+  const size_t chunk = size_t(c) >> 7;
   if (chunk >= L.chunks) return;
-  *reinterpret_cast<uint32_t*>(q + chunk * L.code_stride() + mx4_code_at(r, (lane >> 2) & 3) + (lane & 3) * 4) = codes;
-  if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(q + L.scales() + chunk * L.scale_stride() + mx4_scale_at(r)) = scales;
+  *reinterpret_cast<uint4*>(q + chunk * L.code_stride() + mx4_code_at(r, (c >> 5) & 3)) = codes;
+  if ((c & 127) == 0) *reinterpret_cast<uint32_t*>(q + L.scales() + chunk * L.scale_stride() + mx4_scale_at(r)) = word;
 }
 
 // CTA 0 plans; the others quantise eight rows by 1024 columns each.
@@ -65,15 +60,11 @@ __global__ void __launch_bounds__(kPlanThreads) mx4_plan_kernel(const __grid_con
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (blockIdx.x > 0) {
     const int spans = (a.d + 1023) / 1024, b = int(blockIdx.x) - 1;
-    const int r = b / spans * 8 + warp, c0 = b % spans * 1024;
+    const int r = b / spans * 8 + warp, c = b % spans * 1024 + lane * 32;
     if (r >= a.T) return;
-    const Mx4Layout L(a.x_rows, a.d);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t codes, scales;
-      quantise256(static_cast<const T*>(a.x) + size_t(r) * a.d, c0 + 256 * j, a.d, codes, scales);
-      put256(a.xq, L, size_t(r), c0 + 256 * j, codes, scales);
-    }
+    uint32_t scale;
+    const uint4 codes = quantise_block(static_cast<const T*>(a.x) + size_t(r) * a.d, c, a.d, scale);
+    put_block(a.xq, Mx4Layout(a.x_rows, a.d), size_t(r), c, codes, scale_word(scale));
     return;
   }
   __shared__ int used[kMaxMx4E], tile_of[kMaxMx4E], wsum[kPlanThreads / 32], bad, total;
@@ -227,12 +218,13 @@ __global__ void __launch_bounds__(256) mx4_spread_kernel(const __grid_constant__
   if (lane == a.K && a.S > 0) mine = a.x_tile0 * 128 + t;
   const unsigned to = __ballot_sync(0xffffffffu, mine >= 0);
   const T* row = static_cast<const T*>(a.x) + size_t(t) * a.d;
-  for (int c0 = 0; c0 < a.d; c0 += 256) {
-    uint32_t codes, scales;
-    quantise256(row, c0, a.d, codes, scales);
+  for (int c = lane * 32; c < (a.d + 1023) / 1024 * 1024; c += 1024) {
+    uint32_t scale;
+    const uint4 codes = quantise_block(row, c, a.d, scale);
+    const uint32_t word = scale_word(scale);
     for (unsigned m = to; m; m &= m - 1) {
       const int r = __shfl_sync(0xffffffffu, mine, __ffs(m) - 1);
-      put256(a.xq, L, size_t(r), c0, codes, scales);
+      put_block(a.xq, L, size_t(r), c, codes, word);
     }
   }
 }

@@ -1,14 +1,16 @@
-// mx4 quantisation and its inverse (format and layout: mx4.cuh). Four neighbouring lanes hold a block of 32:
-// the largest magnitude is a maximum over their bit patterns (two shuffles), each lane rounds its eight values
-// to four bytes, and the four scale bytes of a row's 128 columns leave as one word. Bound by HBM: each value is
-// read once (16 bytes a lane, four loads in flight), 17/32 byte a value written.
+// mx4 quantisation and its inverse (format and layout: mx4.cuh). A warp takes an 8-row group by 128 columns, whose
+// codes are 512 contiguous bytes: a lane holds one block of 32 (row lane / 4), so that nothing but the four scale
+// bytes of a row crosses lanes, and reads or writes its values in whole 32-byte sectors. Bound by HBM: each value is
+// moved once, 17/32 byte of it as codes and scales. (One value's eighth of a block a lane, with the largest magnitude
+// found by shuffles and 4-byte stores: 91 us for 28672 x 4096 bf16, and 75 us back; see the launcher for the figures
+// now.)
 #include "mx4_args.h"
 
 namespace mcft {
 namespace {
 
-constexpr int kSteps = 4;               // of 256 columns, one 8-row group a CTA
-constexpr int kSpan = 256 * kSteps;
+constexpr int kChunks = 2;  // of a warp
+constexpr int kWarps = 8;   // a CTA: one group of rows, kWarps * kChunks chunks
 
 template <typename T>
 __device__ __forceinline__ float load1(const T* p) {
@@ -16,30 +18,51 @@ __device__ __forceinline__ float load1(const T* p) {
   else return *p;
 }
 
-// Eight values from column c on, zeros past C.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, long long c, long long C, float* f) {
-  if (VEC && c + 8 <= C) {
-    if constexpr (sizeof(T) == 2) {
-      unpack8(ld_stream16(row + c), f);
+__device__ __forceinline__ void load32(const void* p, uint32_t* r) {
+  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
+// A block: sizeof(T) * 32 bytes as words (zeros past C). ALIGN: bytes to which rows are aligned (32, 16, or 0: only
+// to their type).
+template <typename T, int ALIGN>
+__device__ __forceinline__ void load_block(const T* row, long long c, long long C, uint32_t* w) {
+  constexpr int kWords = int(sizeof(T)) * 8;
+  if (ALIGN && c + 32 <= C) {
+    if constexpr (ALIGN == 32) {
+#pragma unroll
+      for (int i = 0; i < kWords; i += 8) load32(reinterpret_cast<const uint32_t*>(row + c) + i, w + i);
     } else {
-      *reinterpret_cast<uint4*>(f) = ld_stream16(row + c);
-      *reinterpret_cast<uint4*>(f + 4) = ld_stream16(row + c + 4);
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4)
+        *reinterpret_cast<uint4*>(w + i) = ldg16(reinterpret_cast<const uint32_t*>(row + c) + i);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = c + i < C ? load1(row + c + i) : 0.f;
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        w[i] = c + i < C ? __float_as_uint(row[c + i]) : 0u;
+      } else {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + c + 2 * i;
+        w[i] = (c + 2 * i < C ? uint32_t(p[0]) : 0u) | (c + 2 * i + 1 < C ? uint32_t(p[1]) << 16 : 0u);
+      }
+    }
   }
 }
 
-// One warp a row; blockIdx.x an 8-row group (the groups past the last one of codes, up to a multiple of 128
-// rows, only write zero scales).
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) mx4_quantize_kernel(const __grid_constant__ Mx4QuantArgs a) {
+template <typename T, int ALIGN>
+__global__ void __launch_bounds__(32 * kWarps) mx4_quantize_kernel(const __grid_constant__ Mx4QuantArgs a) {
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Mx4Layout L(a.R, a.C);
-  const long long r = (long long)blockIdx.x * 8 + warp;
+  // (the groups past the last one of codes, up to a multiple of 128 rows, only write zero scales)
+  const long long r = (long long)blockIdx.x * 8 + (lane >> 2);
   const bool in = r < a.R;
   long long src = r;
   if (a.interleave) {  // [W1 ; W3] rows as 32 of one, 32 of the other
@@ -48,78 +71,104 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const __grid_constant
   }
   const T* row = static_cast<const T*>(a.x) + src * a.ld;
   uint8_t* out = static_cast<uint8_t*>(a.q);
-  const long long c0 = (long long)blockIdx.y * kSpan + lane * 8;
-  float f[kSteps][8];
+  const size_t k0 = (size_t(blockIdx.y) * kWarps + warp) * kChunks;
+  constexpr int kWords = int(sizeof(T)) * 8;
+  uint32_t w[kChunks][kWords];
 #pragma unroll
-  for (int j = 0; j < kSteps; ++j)
-    if (in) load8<T, VEC>(row, c0 + j * 256, a.C, f[j]);
-    else
+  for (int j = 0; j < kChunks; ++j)
+    if (in && k0 + j < L.chunks) {
+      load_block<T, ALIGN>(row, (long long)(k0 + j) * 128 + (lane & 3) * 32, a.C, w[j]);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[j][i] = 0.f;
-#pragma unroll
-  for (int j = 0; j < kSteps; ++j) {
-    const size_t chunk = size_t(c0 + j * 256) >> 7;
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[j][i]) & 0x7fffffffu);
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    const uint32_t s = mx4_scale(m);
-    uint32_t word = s << (8 * ((lane >> 2) & 3));
-    word |= __shfl_xor_sync(0xffffffffu, word, 4);
-    word |= __shfl_xor_sync(0xffffffffu, word, 8);
-    if (chunk < L.chunks) {
-      if (size_t(blockIdx.x) < L.groups)
-        *reinterpret_cast<uint32_t*>(out + chunk * L.code_stride() + mx4_code_at(size_t(r), (lane >> 2) & 3) +
-                                     (lane & 3) * 4) = mx4_oct(f[j], mx4_inverse(s));
-      if ((lane & 15) == 0)
-        *reinterpret_cast<uint32_t*>(out + L.scales() + chunk * L.scale_stride() + mx4_scale_at(size_t(r))) = word;
+      for (int i = 0; i < kWords; ++i) w[j][i] = 0;
     }
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    if (k0 + j >= L.chunks) break;
+    uint32_t m = 0;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) m = max(m, w[j][i] & 0x7fffffffu);
+    } else {  // two halves at a time: the order of magnitudes is that of their bits
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) m = __vmaxu2(m, w[j][i] & 0x7fff7fffu);
+      m = max(m & 0xffffu, m >> 16) << 16;
+    }
+    const uint32_t s = mx4_scale(m);
+    const float inv = mx4_inverse(s);
+    uint32_t code[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(w[j][8 * i + k]);
+        else v[k] = k & 1 ? bf16hi(w[j][4 * i + k / 2]) : bf16lo(w[j][4 * i + k / 2]);
+      }
+      code[i] = mx4_oct(v, inv);
+    }
+    if (size_t(blockIdx.x) < L.groups)
+      *reinterpret_cast<uint4*>(out + (k0 + j) * L.code_stride() + mx4_code_at(size_t(r), lane & 3)) =
+          make_uint4(code[0], code[1], code[2], code[3]);
+    uint32_t word = s << (8 * (lane & 3));
+    word |= __shfl_xor_sync(0xffffffffu, word, 1);
+    word |= __shfl_xor_sync(0xffffffffu, word, 2);
+    if ((lane & 3) == 0)
+      *reinterpret_cast<uint32_t*>(out + L.scales() + (k0 + j) * L.scale_stride() + mx4_scale_at(size_t(r))) = word;
   }
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const __grid_constant__ Mx4QuantArgs a) {
+template <typename T, int ALIGN>
+__global__ void __launch_bounds__(32 * kWarps) mx4_dequantize_kernel(const __grid_constant__ Mx4QuantArgs a) {
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Mx4Layout L(a.R, a.C);
-  const long long r = (long long)blockIdx.x * 8 + warp;
+  const long long r = (long long)blockIdx.x * 8 + (lane >> 2);
   if (r >= a.R) return;
   const uint8_t* q = static_cast<const uint8_t*>(a.q);
   T* row = static_cast<T*>(const_cast<void*>(a.x)) + r * a.ld;
-  const long long c0 = (long long)blockIdx.y * kSpan + lane * 8;
-  uint32_t code[kSteps], scale[kSteps];
+  const size_t k0 = (size_t(blockIdx.y) * kWarps + warp) * kChunks;
+  uint4 code[kChunks];
+  uint32_t scale[kChunks];
 #pragma unroll
-  for (int j = 0; j < kSteps; ++j) {
-    const size_t chunk = size_t(c0 + j * 256) >> 7;
-    if (c0 + j * 256 < a.C) {
-      code[j] = __ldg(reinterpret_cast<const uint32_t*>(q + chunk * L.code_stride() +
-                                                        mx4_code_at(size_t(r), (lane >> 2) & 3) + (lane & 3) * 4));
-      scale[j] = __ldg(q + L.scales() + chunk * L.scale_stride() + mx4_scale_at(size_t(r)) + ((lane >> 2) & 3));
+  for (int j = 0; j < kChunks; ++j)
+    if (k0 + j < L.chunks) {
+      code[j] = ld_stream16(q + (k0 + j) * L.code_stride() + mx4_code_at(size_t(r), lane & 3));
+      scale[j] = __ldg(q + L.scales() + (k0 + j) * L.scale_stride() + mx4_scale_at(size_t(r)) + (lane & 3));
     }
-  }
 #pragma unroll
-  for (int j = 0; j < kSteps; ++j) {
-    const long long c = c0 + j * 256;
+  for (int j = 0; j < kChunks; ++j) {
+    const long long c = (long long)(k0 + j) * 128 + (lane & 3) * 32;
     if (c >= a.C) break;
     const float u = mx4_unit(scale[j]);
-    float v[8];
+    const uint32_t word[4] = {code[j].x, code[j].y, code[j].z, code[j].w};
+    if (ALIGN && c + 32 <= a.C) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = mx4_code_value(code[j] >> (4 * i)) * u;
-    if (VEC && c + 8 <= a.C) {
-      if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(row + c) =
-            make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
-      } else {
-        *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      for (int i = 0; i < 32; i += 32 / int(sizeof(T))) {  // 32 bytes
+        constexpr int kValues = 32 / int(sizeof(T));
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          constexpr int kPer = kValues / 8;
+          const int at = i + k * kPer;
+          const float lo = mx4_code_value(word[at >> 3] >> (4 * (at & 7))) * u;
+          if constexpr (sizeof(T) == 4) w[k] = __float_as_uint(lo);
+          else w[k] = pack2bf(lo, mx4_code_value(word[at >> 3] >> (4 * (at & 7) + 4)) * u);
+        }
+        if constexpr (ALIGN == 32) {
+          store32(row + c + i, w);
+        } else {
+          *reinterpret_cast<uint4*>(row + c + i) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(row + c + i + kValues / 2) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 32; ++i)
         if (c + i < a.C) {
-          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(row + c + i) = f2bf(v[i]);
-          else row[c + i] = v[i];
+          const float v = mx4_code_value(word[i >> 3] >> (4 * (i & 7))) * u;
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(row + c + i) = f2bf(v);
+          else row[c + i] = v;
         }
     }
   }
@@ -127,13 +176,14 @@ __global__ void __launch_bounds__(256) mx4_dequantize_kernel(const __grid_consta
 
 template <typename T>
 cudaError_t launch(const Mx4QuantArgs& a, bool back, cudaStream_t s) {
-  const bool vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (size_t(a.ld) * sizeof(T)) % 16 == 0;
+  const size_t at = reinterpret_cast<uintptr_t>(a.x) | size_t(a.ld) * sizeof(T);
   const Mx4Layout L(a.R, a.C);
-  const size_t groups = back ? L.groups : L.blocks * 16, spans = size_t(a.C + kSpan - 1) / kSpan;
+  const size_t groups = back ? L.groups : L.blocks * 16, spans = (L.chunks + kWarps * kChunks - 1) / (kWarps * kChunks);
   const dim3 grid{unsigned(groups), unsigned(spans)};
-  auto* k = back ? (vec ? mx4_dequantize_kernel<T, true> : mx4_dequantize_kernel<T, false>)
-                 : (vec ? mx4_quantize_kernel<T, true> : mx4_quantize_kernel<T, false>);
-  return launch_pdl(k, grid, dim3(256), 0, s, a);
+  auto* k = at % 32 == 0   ? (back ? mx4_dequantize_kernel<T, 32> : mx4_quantize_kernel<T, 32>)
+            : at % 16 == 0 ? (back ? mx4_dequantize_kernel<T, 16> : mx4_quantize_kernel<T, 16>)
+                           : (back ? mx4_dequantize_kernel<T, 0> : mx4_quantize_kernel<T, 0>);
+  return launch_pdl(k, grid, dim3(32 * kWarps), 0, s, a);
 }
 
 }  // namespace

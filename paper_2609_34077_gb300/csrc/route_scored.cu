@@ -5,6 +5,7 @@
 // in the leader's shared memory, where one warp ranks a token.
 // Otherwise: CTAs of 16 tokens by all experts, fp32 multiply-adds from shared memory tiles, ranked in place.
 #include "route_scored_warp.cuh"
+#include "scored_tc.h"
 
 namespace mcft {
 namespace {
@@ -39,12 +40,12 @@ struct Vec {
   }
 };
 
-template <typename T>
+template <typename T, int PL>
 __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
     route_scored_few_kernel(const __grid_constant__ ScoredArgs a) {
   extern __shared__ float xs[];  // [tokens][d]
-  __shared__ float zs[kFewTokens][kMaxScoredE], cs[kFewTokens][kMaxScoredE];
-  __shared__ int count[kMaxScoredE];
+  __shared__ float zs[kFewTokens][32 * PL], buf[kFewTokens][64 * PL];
+  __shared__ int count[32 * PL];
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = int(cta_rank());
@@ -57,7 +58,7 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
 #pragma unroll
     for (int j = 0; j < N; ++j) xs[i + j] = v.f[j];
   }
-  if (tid < kMaxScoredE) count[tid] = 0;
+  if (tid < 32 * PL) count[tid] = 0;
   __syncthreads();
   for (int e = rank + kFewCtas * warp; e < a.E; e += kFewCtas * (kFewThreads / 32)) {
     const T* w = static_cast<const T*>(a.w_router) + size_t(e) * a.d;
@@ -82,7 +83,12 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
   cluster_barrier();
   if (rank != 0) return;
   const bool alone = int(gridDim.x) == kFewCtas;  // this cluster has all tokens: no counters to add to
-  if (warp < nt) rank_scored_warp(a, zs[warp], cs[warp], t0 + warp, a.load ? (alone ? count : a.load) : nullptr);
+  if (warp < nt) {
+    float z[PL];
+#pragma unroll
+    for (int j = 0; j < PL; ++j) z[j] = lane + 32 * j < a.E ? zs[warp][lane + 32 * j] : 0.f;
+    rank_scored_warp<PL>(a, z, buf[warp], t0 + warp, a.load ? (alone ? count : a.load) : nullptr);
+  }
   if (alone && a.load) {
     __syncthreads();
     if (tid < a.E) a.load[tid] = count[tid];
@@ -95,7 +101,7 @@ constexpr int kTileT = 16, kTileK = 32;
 template <typename T>
 __global__ void __launch_bounds__(256) route_scored_tile_kernel(const __grid_constant__ ScoredArgs a) {
   __shared__ float xs[kTileK][kTileT + 2];
-  __shared__ float ws[kTileK * (kMaxScoredE + 1)];  // [k][expert]; then the logits and the choice values
+  __shared__ __align__(16) float ws[kTileK * (kMaxScoredE + 1)];  // [k][expert]; then the ranking's buffers
   __shared__ int count[kMaxScoredE];
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -104,7 +110,8 @@ __global__ void __launch_bounds__(256) route_scored_tile_kernel(const __grid_con
   const T* w = static_cast<const T*>(a.w_router);
   constexpr int N = Vec<T>::n, kRow = kMaxScoredE + 1;
   count[tid] = 0;
-  float acc[2][kScoredPerLane] = {};
+  constexpr int PL = kMaxScoredE / 32;
+  float acc[2][PL] = {};
   for (int k0 = 0; k0 < a.d; k0 += kTileK) {
     __syncthreads();
     for (int i = tid; i < kTileT * (kTileK / N); i += 256) {
@@ -126,7 +133,7 @@ __global__ void __launch_bounds__(256) route_scored_tile_kernel(const __grid_con
     for (int k = 0; k < kTileK; ++k) {
       const float x0 = xs[k][warp * 2], x1 = xs[k][warp * 2 + 1];
 #pragma unroll
-      for (int j = 0; j < kScoredPerLane; ++j)
+      for (int j = 0; j < PL; ++j)
         if (lane + 32 * j < a.E) {
           const float v = ws[k * kRow + lane + 32 * j];
           acc[0][j] = fmaf(x0, v, acc[0][j]);
@@ -135,25 +142,16 @@ __global__ void __launch_bounds__(256) route_scored_tile_kernel(const __grid_con
     }
   }
   __syncthreads();
-  float* z = ws + warp * 3 * kMaxScoredE;  // two rows of logits and one of choice values a warp
+  float* buf = ws + warp * 64 * PL;
 #pragma unroll
-  for (int j = 0; j < kScoredPerLane; ++j)
-    if (lane + 32 * j < a.E) {
-      z[lane + 32 * j] = acc[0][j];
-      z[kMaxScoredE + lane + 32 * j] = acc[1][j];
-    }
-  __syncwarp();
-  for (int i = 0; i < 2; ++i) {
-    if (warp * 2 + i < nt)
-      rank_scored_warp(a, z + i * kMaxScoredE, z + 2 * kMaxScoredE, t0 + warp * 2 + i, a.load ? count : nullptr);
-    __syncwarp();
-  }
+  for (int i = 0; i < 2; ++i)
+    if (warp * 2 + i < nt) rank_scored_warp<PL>(a, acc[i], buf, t0 + warp * 2 + i, a.load ? count : nullptr);
   if (a.load) {
     __syncthreads();
     if (tid < a.E && count[tid]) atomicAdd(a.load + tid, count[tid]);
   }
 }
-static_assert(8 * 3 * kMaxScoredE <= kTileK * (kMaxScoredE + 1), "logits fit the weight tile");
+static_assert(8 * 2 * kMaxScoredE <= kTileK * (kMaxScoredE + 1), "the ranking's buffers fit the weight tile");
 
 // The counters that several CTAs add to, zeroed in a launch before them.
 __global__ void __launch_bounds__(kMaxScoredE) zero_load_kernel(int32_t* load, int E) {
@@ -163,6 +161,15 @@ __global__ void __launch_bounds__(kMaxScoredE) zero_load_kernel(int32_t* load, i
 
 constexpr int kFewSmem = 160 * 1024;
 
+template <typename T, int PL>
+cudaError_t launch_few(const ScoredArgs& a, size_t bytes, cudaStream_t s) {
+  static SmemOptIn smem;
+  const cudaError_t e = smem.allow(reinterpret_cast<const void*>(route_scored_few_kernel<T, PL>), kFewSmem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(route_scored_few_kernel<T, PL>, dim3((a.T + kFewTokens - 1) / kFewTokens * kFewCtas),
+                    dim3(kFewThreads), bytes, s, a);
+}
+
 template <typename T>
 cudaError_t launch(const ScoredArgs& a, cudaStream_t s) {
   const size_t bytes = sizeof(float) * size_t(a.d) * (a.T < kFewTokens ? a.T : kFewTokens);
@@ -171,12 +178,9 @@ cudaError_t launch(const ScoredArgs& a, cudaStream_t s) {
     const cudaError_t e = launch_pdl(zero_load_kernel, dim3(1), dim3(kMaxScoredE), 0, s, a.load, a.E);
     if (e != cudaSuccess) return e;
   }
+  if (sizeof(T) == 2 && a.T > kScoredTcMinT) return launch_scored_forward_tc(a, s);
   if (!few) return launch_pdl(route_scored_tile_kernel<T>, dim3((a.T + kTileT - 1) / kTileT), dim3(256), 0, s, a);
-  static SmemOptIn smem;
-  const cudaError_t e = smem.allow(reinterpret_cast<const void*>(route_scored_few_kernel<T>), kFewSmem);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(route_scored_few_kernel<T>, dim3((a.T + kFewTokens - 1) / kFewTokens * kFewCtas), dim3(kFewThreads),
-                    bytes, s, a);
+  return a.E <= 64 ? launch_few<T, 2>(a, bytes, s) : launch_few<T, 8>(a, bytes, s);
 }
 
 }  // namespace

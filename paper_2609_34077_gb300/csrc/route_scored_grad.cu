@@ -7,12 +7,14 @@
 #include <algorithm>
 
 #include "route_scored_warp.cuh"
+#include "scored_tc.h"
 
 namespace mcft {
 namespace {
 
-// One warp a token.
-__global__ void __launch_bounds__(256) scored_dz_kernel(const __grid_constant__ ScoredGradArgs a, float* dz, unsigned* err) {
+// One warp a token. dz as fp32 [T, E], or (PARTS) as the bf16 parts that the tensor cores take.
+template <bool PARTS>
+__global__ void __launch_bounds__(256) scored_dz_kernel(const __grid_constant__ ScoredGradArgs a, void* dz, unsigned* err) {
   pdl_wait();
   __shared__ float rows[8][kMaxScoredE];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E;
@@ -43,13 +45,26 @@ __global__ void __launch_bounds__(256) scored_dz_kernel(const __grid_constant__ 
     atomicAdd(row + e, u);  // (one addend an expert, unless the caller names one twice)
   }
   __syncwarp();
-  float* out = dz + size_t(t) * E;
-  if (a.score == MCFT_SCORE_SOFTMAX && a.gate_mode == MCFT_GATE_PLAIN) {
-    float m, sum;
-    softmax_stats(z, E, m, sum);
-    for (int i = lane; i < E; i += 32) out[i] = row[i] - expf(z[i] - m) / sum * sum_u;
+  const bool dense = a.score == MCFT_SCORE_SOFTMAX && a.gate_mode == MCFT_GATE_PLAIN;
+  float m = 0.f, sum = 1.f;
+  if (dense) softmax_stats(z, E, m, sum);
+  auto value = [&](int i) { return i >= E ? 0.f : dense ? row[i] - expf(z[i] - m) / sum * sum_u : row[i]; };
+  if constexpr (PARTS) {
+    const int ep = (E + 127) / 128 * 128;
+    uint32_t* out = static_cast<uint32_t*>(dz) + size_t(t) * kScoredParts * (ep / 2);
+    for (int i = lane; i < ep / 2; i += 32) {
+      float v[2] = {value(2 * i), value(2 * i + 1)};
+#pragma unroll
+      for (int q = 0; q < kScoredParts; ++q) {
+        const uint32_t w = pack2bf(v[0], v[1]);
+        out[q * (ep / 2) + i] = w;
+        v[0] -= bf16lo(w);
+        v[1] -= bf16hi(w);
+      }
+    }
   } else {
-    for (int i = lane; i < E; i += 32) out[i] = row[i];
+    float* out = static_cast<float*>(dz) + size_t(t) * E;
+    for (int i = lane; i < E; i += 32) out[i] = value(i);
   }
 }
 
@@ -70,7 +85,7 @@ struct MultiplyArgs {
   const void* b;
   void* c;
   long long am, ak;
-  int M, N, K, k_share, accumulate;
+  int M, N, K, k_share;
 };
 template <typename TB, typename TC>
 __global__ void __launch_bounds__(256) multiply_kernel(const __grid_constant__ MultiplyArgs p) {
@@ -132,44 +147,61 @@ __global__ void __launch_bounds__(256) add_planes_kernel(const float* planes, fl
 
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Tokens of one plane of dW.
-int token_share(int T, int d, int E) {
+// Most planes of dW, by fp32 multiply-adds.
+int most_planes(int T, int d, int E) {
   const int tiles = (d / 64) * ((E + 63) / 64);
-  const int planes = std::max(1, std::min((304 + tiles - 1) / tiles, (T + 127) / 128));
-  return ((T + planes - 1) / planes + 15) / 16 * 16;
+  return std::max(1, std::min((304 + tiles - 1) / tiles, (T + 127) / 128));
+}
+
+bool on_tensor_cores(int T, int dtype) { return dtype == MCFT_BF16 && T > kScoredTcMinT; }
+
+size_t dz_bytes(int T, int E, int dtype) {
+  return align256(on_tensor_cores(T, dtype) ? size_t(T) * kScoredParts * scored_ep(E) * 2 : sizeof(float) * size_t(T) * E);
 }
 
 }  // namespace
 
+// (never less than for a smaller T)
 size_t scored_grad_workspace(int T, int d, int E, int K, int dtype) {
   (void)K;
-  (void)dtype;
-  const int share = token_share(T, d, E), planes = (T + share - 1) / share;
-  return align256(sizeof(float) * size_t(T) * E) + align256(sizeof(float) * size_t(planes) * E * d);
+  const int planes = on_tensor_cores(T, dtype) ? scored_dw_planes(T, d) : most_planes(T, d, E);
+  return dz_bytes(T, E, dtype) + align256(sizeof(float) * size_t(planes) * E * d);
 }
 
 cudaError_t launch_route_scored_grad(const ScoredGradArgs& a, int dtype, cudaStream_t s) {
   prof_begin(kProfRouteScoredGrad, s);
-  float* dz = static_cast<float*>(a.workspace);
-  float* planes = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256(sizeof(float) * size_t(a.T) * a.E));
-  const bool bf = dtype == MCFT_BF16;
-  cudaError_t e = launch_pdl(scored_dz_kernel, dim3((a.T + 7) / 8), dim3(256), 0, s, a, dz, device_error_word());
+  void* dz = a.workspace;
+  float* planes = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + dz_bytes(a.T, a.E, dtype));
+  const bool bf = dtype == MCFT_BF16, tc = on_tensor_cores(a.T, dtype);
+  cudaError_t e = launch_pdl(tc ? scored_dz_kernel<true> : scored_dz_kernel<false>, dim3((a.T + 7) / 8), dim3(256), 0, s, a,
+                             dz, device_error_word());
   if (e == cudaSuccess && a.dx) {
-    const MultiplyArgs p{dz, a.w_router, a.dx, a.E, 1, a.T, a.d, a.E, a.E, 0};
-    const dim3 grid(unsigned(a.d / 64), unsigned((a.T + 63) / 64));
-    e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, __nv_bfloat16>, grid, dim3(256), 0, s, p)
-           : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+    if (tc) {
+      e = launch_scored_dx_tc(a, dz, s);
+    } else {
+      const MultiplyArgs p{static_cast<const float*>(dz), a.w_router, a.dx, a.E, 1, a.T, a.d, a.E, a.E};
+      const dim3 grid(unsigned(a.d / 64), unsigned((a.T + 63) / 64));
+      e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, __nv_bfloat16>, grid, dim3(256), 0, s, p)
+             : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+    }
   }
   if (e == cudaSuccess && a.dw) {
-    const int share = token_share(a.T, a.d, a.E), count = (a.T + share - 1) / share;
-    const MultiplyArgs p{dz, a.x, planes, 1, a.E, a.E, a.d, a.T, share, 0};
-    const dim3 grid(unsigned(a.d / 64), unsigned((a.E + 63) / 64), unsigned(count));
-    e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, float>, grid, dim3(256), 0, s, p)
-           : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+    int share;
+    if (tc) {
+      share = scored_dw_share(a.T, a.d);
+      e = launch_scored_dw_tc(a, dz, planes, s);
+    } else {
+      const int most = most_planes(a.T, a.d, a.E);
+      share = ((a.T + most - 1) / most + 15) / 16 * 16;
+      const MultiplyArgs p{static_cast<const float*>(dz), a.x, planes, 1, a.E, a.E, a.d, a.T, share};
+      const dim3 grid(unsigned(a.d / 64), unsigned((a.E + 63) / 64), unsigned((a.T + share - 1) / share));
+      e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, float>, grid, dim3(256), 0, s, p)
+             : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+    }
     const long long n = (long long)a.E * a.d;
     if (e == cudaSuccess)
       e = launch_pdl(add_planes_kernel, dim3(unsigned((n / 4 + 255) / 256)), dim3(256), 0, s,
-                     static_cast<const float*>(planes), a.dw, n, count, a.accumulate);
+                     static_cast<const float*>(planes), a.dw, n, (a.T + share - 1) / share, a.accumulate);
   }
   prof_end(kProfRouteScoredGrad, s);
   return e != cudaSuccess ? e : cudaGetLastError();

@@ -1,19 +1,18 @@
 // Scored Top-K of one token from its router logits, by one warp: scores s = sigmoid(z) or softmax(z), choice
 // values c = s + bias, the best groups of experts, the K best of their experts by c (ties to the lower index, of
 // groups too), gates from s. Not part of the C ABI.
+//
+// A warp's instructions bound it (one token's are a chain of shuffles and reductions; other warps fill the gaps), so
+// the choice first narrows the field: the K-th largest of the 32 lanes' own maxima is a bound below which nothing can
+// be chosen, and what reaches it (K to about 2 K experts) is packed one to a lane, where a round of the choice is a
+// warp maximum and a ballot. 8192 tokens of 256 experts in 8 groups, forward: 70 us with all eight experts of every
+// lane looked at in each of the K rounds, on ten warps a CTA; see scored_tc.cu for the figure now.
 #pragma once
 
 #include "route_scored.h"
 #include "route_warp.cuh"
 
 namespace mcft {
-
-constexpr int kScoredPerLane = kMaxScoredE / 32;
-
-// Score of a logit; m and inv_sum: the softmax's largest logit and sum.
-__device__ __forceinline__ float scored_value(int score, float z, float m, float sum) {
-  return score == MCFT_SCORE_SIGMOID ? 1.f / (1.f + expf(-z)) : expf(z - m) / sum;
-}
 
 // Largest logit and sum of exponentials of one row (lanes hold experts lane, lane + 32, ...).
 __device__ __forceinline__ void softmax_stats(const float* z, int E, float& m, float& sum) {
@@ -27,85 +26,161 @@ __device__ __forceinline__ void softmax_stats(const float* z, int E, float& m, f
   sum = warp_sum(sum);
 }
 
-// zs: the token's E logits, cs: room for E floats (both shared memory, this warp's alone); t: its row.
-// load: shared or global counters of the experts' choices, or NULL.
-__device__ inline void rank_scored_warp(const ScoredArgs& a, const float* zs, float* cs, int t, int32_t* load) {
+// z[j]: logit of expert lane + 32 j (PL = ceil(E / 32) of them). buf: 2 * 32 * PL floats of shared memory, this warp's
+// alone. load: shared or global counters of the experts' choices, or NULL.
+template <int PL>
+__device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL], float* buf, int t, int32_t* load) {
   constexpr int kNone = -2147483647 - 1;  // below every key: not there, or taken
+  constexpr unsigned kAll = 0xffffffffu;
   const int lane = threadIdx.x & 31, E = a.E;
-  float m = 0.f, sum = 1.f;
-  if (a.score == MCFT_SCORE_SOFTMAX) softmax_stats(zs, E, m, sum);
-  float c[kScoredPerLane];
+  float* ss = buf;             // scores, by expert
+  float* cs = buf + 32 * PL;   // choice values by expert; then the narrowed field
+  float s[PL], c[PL];
+  if (a.score == MCFT_SCORE_SOFTMAX) {
+    float m = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < kScoredPerLane; ++j) {
+    for (int j = 0; j < PL; ++j) m = lane + 32 * j < E ? fmaxf(m, z[j]) : m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
+#pragma unroll
+    for (int j = 0; j < PL; ++j) {
+      s[j] = lane + 32 * j < E ? expf(z[j] - m) : 0.f;
+      sum += s[j];
+    }
+    const float inv = 1.f / warp_sum(sum);
+#pragma unroll
+    for (int j = 0; j < PL; ++j) s[j] *= inv;
+  } else {
+#pragma unroll
+    for (int j = 0; j < PL; ++j) s[j] = __frcp_rn(1.f + expf(-z[j]));
+  }
+  bool nan = false;
+#pragma unroll
+  for (int j = 0; j < PL; ++j) {
     const int e = lane + 32 * j;
     c[j] = -INFINITY;
     if (e < E) {
-      if (a.logits) a.logits[size_t(t) * E + e] = zs[e];
-      float v = scored_value(a.score, zs[e], m, sum);
+      if (a.logits) a.logits[size_t(t) * E + e] = z[j];
+      float v = s[j];
       if (a.bias) v += __ldg(a.bias + e);
-      if (v != v) {
-        set_error(a.err, kErrInvalid);
-        v = -INFINITY;
-      }
-      c[j] = v;
+      nan |= v != v;
+      c[j] = v != v ? -INFINITY : v;
+      ss[e] = s[j];
     }
   }
-  unsigned groups = 0xffffffffu;
-  const int gsz = E / a.n_group;
+  if (nan) set_error(a.err, kErrInvalid);
+  int key[PL];
+#pragma unroll
+  for (int j = 0; j < PL; ++j) key[j] = c[j] > -INFINITY ? ordered_int(c[j]) : kNone;
   if (a.n_group > 1) {
-    for (int j = 0; j < kScoredPerLane; ++j)
+    const int gsz = E / a.n_group;
+#pragma unroll
+    for (int j = 0; j < PL; ++j)
       if (lane + 32 * j < E) cs[lane + 32 * j] = c[j];
     __syncwarp();
-    int key = kNone;
-    if (lane < a.n_group) {
-      float best = -INFINITY, second = -INFINITY;
-      for (int i = 0, j = lane % gsz; i < gsz; ++i, j = j + 1 == gsz ? 0 : j + 1) {  // (lanes start apart: other banks)
-        const float v = cs[lane * gsz + j];
+    // the lanes share the groups: 2^shift lanes each, whose two best values meet by shuffles
+    const int shift = 31 - __clz(32 / a.n_group), per = 1 << shift;
+    const int g = lane >> shift, sub = lane & (per - 1), n = (gsz + per - 1) >> shift;
+    float best = -INFINITY, second = -INFINITY;
+    if (g < a.n_group) {
+      for (int i = 0, k = g % n; i < n; ++i, k = k + 1 == n ? 0 : k + 1) {  // (groups start apart: other banks)
+        const int at = sub + (k << shift);
+        const float v = at < gsz ? cs[g * gsz + at] : -INFINITY;
         second = fmaxf(second, fminf(best, v));
         best = fmaxf(best, v);
       }
-      key = ordered_int(a.group_top == 2 ? best + second : best);
     }
-    groups = 0;
+    for (int o = 1; o < per; o <<= 1) {
+      const float b = __shfl_xor_sync(kAll, best, o), b2 = __shfl_xor_sync(kAll, second, o);
+      second = fmaxf(fmaxf(second, b2), fminf(best, b));
+      best = fmaxf(best, b);
+    }
+    int gkey = sub == 0 && g < a.n_group ? ordered_int(a.group_top == 2 ? best + second : best) : kNone;
+    unsigned groups = 0;
     for (int k = 0; k < a.topk_group; ++k) {
-      const int best = __reduce_max_sync(0xffffffffu, key);
-      const int g = __ffs(__ballot_sync(0xffffffffu, key == best)) - 1;
-      groups |= 1u << g;
-      if (lane == g) key = kNone;
+      const int top = __reduce_max_sync(kAll, gkey);
+      const int l = __ffs(__ballot_sync(kAll, gkey == top)) - 1;
+      groups |= 1u << (l >> shift);
+      if (lane == l) gkey = kNone;
+    }
+#pragma unroll
+    for (int j = 0; j < PL; ++j) {
+      const int e = lane + 32 * j;
+      if (e < E && !((groups >> (e / gsz)) & 1u)) key[j] = kNone;
     }
   }
-  int key[kScoredPerLane];
+  __syncwarp();
+  // narrow the field
+  int most = key[0];
 #pragma unroll
-  for (int j = 0; j < kScoredPerLane; ++j) {
-    const int e = lane + 32 * j;
-    const bool in = a.n_group == 1 || ((groups >> (e < E ? e / gsz : 0)) & 1u);
-    key[j] = in && c[j] > -INFINITY ? ordered_int(c[j]) : kNone;
-  }
-  int sel = -1;
+  for (int j = 1; j < PL; ++j) most = max(most, key[j]);
+  int floor_key = kNone;
   for (int k = 0; k < a.K; ++k) {
-    int mine = kNone, at = 0;
-#pragma unroll
-    for (int j = kScoredPerLane - 1; j >= 0; --j)
-      if (key[j] >= mine) {
-        mine = key[j];
-        at = lane + 32 * j;
-      }
-    const int best = __reduce_max_sync(0xffffffffu, mine);
-    if (best == kNone) break;  // no eligible expert is left
-    const int e = int(__reduce_min_sync(0xffffffffu, unsigned(mine == best ? at : 0x7fffffff)));
-#pragma unroll
-    for (int j = 0; j < kScoredPerLane; ++j)
-      if (e == lane + 32 * j) key[j] = kNone;
-    if (lane == k) sel = e;
+    floor_key = __reduce_max_sync(kAll, most);
+    if (floor_key == kNone) break;
+    const int l = __ffs(__ballot_sync(kAll, most == floor_key)) - 1;
+    if (lane == l) most = kNone;
   }
-  const float s = sel >= 0 ? scored_value(a.score, zs[sel], m, sum) : 0.f;
+  int count = 0;
+  int2* field = reinterpret_cast<int2*>(cs);  // (32 entries fit where PL >= 2)
+  int sel = -1;
+  bool packed = PL > 1;
+  if constexpr (PL > 1) {
+    int base[PL];
+#pragma unroll
+    for (int j = 0; j < PL; ++j) {
+      const bool in = key[j] >= floor_key && key[j] != kNone;
+      const unsigned b = __ballot_sync(kAll, in);
+      base[j] = in ? count + __popc(b & ((1u << lane) - 1u)) : 32;
+      count += __popc(b);
+    }
+    packed = count <= 32;  // (more only where many experts tie)
+    if (packed) {
+#pragma unroll
+      for (int j = 0; j < PL; ++j)
+        if (base[j] < 32) field[base[j]] = make_int2(key[j], lane + 32 * j);
+      __syncwarp();
+    }
+  }
+  if (packed || PL == 1) {
+    // one expert a lane, in the order of their index
+    int2 mine = make_int2(key[0], lane);
+    if (PL > 1) mine = lane < count ? field[lane] : make_int2(kNone, 0);
+    for (int k = 0; k < a.K; ++k) {
+      const int best = __reduce_max_sync(kAll, mine.x);
+      if (best == kNone) break;  // no eligible expert is left
+      const int l = __ffs(__ballot_sync(kAll, mine.x == best)) - 1;
+      const int e = __shfl_sync(kAll, mine.y, l);
+      if (lane == l) mine.x = kNone;
+      if (lane == k) sel = e;
+    }
+  } else {
+    for (int k = 0; k < a.K; ++k) {
+      int top = kNone, at = 0;
+#pragma unroll
+      for (int j = PL - 1; j >= 0; --j)
+        if (key[j] >= top) {
+          top = key[j];
+          at = lane + 32 * j;
+        }
+      const int best = __reduce_max_sync(kAll, top);
+      if (best == kNone) break;
+      const int e = int(__reduce_min_sync(kAll, unsigned(top == best ? at : 0x7fffffff)));
+#pragma unroll
+      for (int j = 0; j < PL; ++j)
+        if (e == lane + 32 * j) key[j] = kNone;
+      if (lane == k) sel = e;
+    }
+  }
+  const float score = sel >= 0 ? ss[sel] : 0.f;
   float total = 1.f;
-  if (a.gate_mode == MCFT_GATE_RENORM) total = warp_sum(s);
+  if (a.gate_mode == MCFT_GATE_RENORM) total = warp_sum(score);
   if (lane < a.K) {
     a.idx[size_t(t) * a.K + lane] = sel;
-    a.gate[size_t(t) * a.K + lane] = total > 0.f ? s / total * a.scale : 0.f;
+    a.gate[size_t(t) * a.K + lane] = total > 0.f ? score / total * a.scale : 0.f;
     if (load && sel >= 0) atomicAdd(load + sel, 1);
   }
+  __syncwarp();  // (buf may be used again)
 }
 
 }  // namespace mcft
