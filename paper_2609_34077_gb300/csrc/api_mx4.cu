@@ -63,7 +63,7 @@ struct ExpertBlock {
 mcft_status check_tokens(const mcft_layer_desc* d, int T) {
   if (T < 0) return fail(MCFT_ERR_INVALID, "T = %d < 0", T);
   if (T == 0) return MCFT_OK;
-  const Mx4MoeLayout L(d->d, d->E, d->K, d->w, d->n_shared, T);
+  const Mx4MoeLayout L(d, T);
   const long long widest = d->d > 2LL * d->w ? d->d : 2LL * d->w;
   if (L.tiles > INT_MAX / 256 || L.tiles * ((widest + 63) / 64) > INT_MAX / 8 ||
       (long long)T * (d->K + d->n_shared) > INT_MAX / 2)
@@ -174,7 +174,7 @@ mcft_status mcft_mx4_workspace_size(const mcft_layer_desc* desc, int T_max, size
   if (!bytes) return fail(MCFT_ERR_INVALID, "bytes is NULL");
   st = check_tokens(desc, T_max);
   if (st != MCFT_OK) return st;
-  *bytes = T_max == 0 ? 0 : Mx4MoeLayout(desc->d, desc->E, desc->K, desc->w, desc->n_shared, T_max).total;
+  *bytes = T_max == 0 ? 0 : Mx4MoeLayout(desc, T_max).total;
   return MCFT_OK;
 }
 
@@ -191,7 +191,7 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
     return fail(MCFT_ERR_INVALID, "NULL pointer argument");
   if (!aligned(x, 16) || !aligned(y, 16)) return fail(MCFT_ERR_INVALID, "x and y must be 16-byte aligned");
   if (!aligned(workspace, 256)) return fail(MCFT_ERR_INVALID, "workspace must be 256-byte aligned");
-  const Mx4MoeLayout L(d, E, K, w, S, T);
+  const Mx4MoeLayout L(desc, T);
   if (ws_bytes < L.total) return fail(MCFT_ERR_INVALID, "workspace of %zu bytes, %zu needed", ws_bytes, L.total);
 
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -227,7 +227,8 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   m.xq = ws + L.x;
   m.x_tile0 = int(L.routed_tiles);
   m.x_rows = x_rows;
-  m.o = reinterpret_cast<const float*>(ws + L.o);
+  m.o = ws + L.o;
+  m.o_unit = L.half_o ? reinterpret_cast<const float*>(ws + L.o_unit) : nullptr;
   m.y = y;
   m.err = device_error_word();
   cudaError_t e = launch_mx4_prepare(m, desc->dtype, L.permuted, stream);
@@ -265,6 +266,7 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   operand(p.h, lh, B.down, B.up.bytes(), w);
   p.n_out = d;
   p.out = ws + L.o;
+  p.out_scale = L.half_o ? reinterpret_cast<float*>(ws + L.o_unit) : nullptr;
   p.ldo = d;
   p.vec = 1;
   e = launch_mx4_gemm(p, kMx4Down, L.tiles, tile_rows, num_sms(), stream);

@@ -51,6 +51,7 @@ struct Mx4GemmArgs {
   void* out;                    // down, out
   long long ldo;
   int out_f32, vec;             // vec: 32-byte stores fit
+  float* out_scale;             // down: units of an fp16 o, [rows of o][ceil(n_out / 128)]; NULL: o is fp32
   uint8_t *h, *h_scales;        // up
   size_t h_code_stride, h_scale_stride;
   unsigned* err;
@@ -58,14 +59,18 @@ struct Mx4GemmArgs {
   int tn, n_tiles, split, depth, stages, a_groups;
   const void* w[kMaxMx4Seg];
 };
+// Whether a product of up to max_tiles token tiles with n_rows weight rows takes the wide tiles: once they fill the
+// SMs.
+bool mx4_wide(long long max_tiles, int n_rows);
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s);
 
 // Workspace of one layer forward.
 struct Mx4MoeLayout {
   bool permuted;
   long long routed_tiles, x_tiles, tiles;  // most tiles of the routed experts; tiles of x itself; all tiles
-  size_t hdr, tile, rowmap, src, pos, x, h, o, total;
-  Mx4MoeLayout(int d, int E, int K, int w, int S, int T);
+  bool half_o;     // o as fp16 under a unit for each row's 128 columns (bf16 layers, wide tiles), else fp32
+  size_t hdr, tile, rowmap, src, pos, x, h, o, o_unit, total;
+  Mx4MoeLayout(const mcft_layer_desc* desc, int T);
 };
 
 struct Mx4MoeArgs {
@@ -80,7 +85,8 @@ struct Mx4MoeArgs {
   uint8_t* xq;
   int x_tile0;     // first tile of x itself, in the permuted form
   long long x_rows;  // rows of xq
-  const float* o;
+  const void* o;         // fp32, or (with o_unit) fp16
+  const float* o_unit;
   void* y;
   unsigned* err;
 };

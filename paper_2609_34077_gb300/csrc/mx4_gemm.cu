@@ -8,7 +8,7 @@
 // Tokens are on M (128 rows of a tile), weight rows on N, so that in the epilogue a thread owns one token row:
 // 32 outputs of it are a block, quantised without leaving the thread. Three epilogues:
 //   up    the weight rows are 32 gate and 32 up rows in turn: h = silu(gate) * up, to mx4 (Section 3.1's F);
-//   down  fp32 rows of o, to the assignment's place;
+//   down  rows of o, to the assignment's place: fp32, or 16 bits (below);
 //   out   fp32 or bf16 rows of y (the plain product).
 //
 // Two builds. `wide` tiles of 128 x 256 for prompts: a persistent grid, one CTA an SM; the eight epilogue warps
@@ -18,9 +18,15 @@
 // add their partial tiles through distributed shared memory, two CTAs an SM; only the 8-row groups that hold
 // tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results).
 //
+// For bf16 layers wide tiles write o as fp16 under a power-of-two unit for each row's 128 columns (the largest of them in [2^14, 2^15)
+// units): its 11 bits cost y an error of 2^-12, an eighth of its own rounding to bf16, and o is moved twice (here and
+// by the combine), which in fp32 took most of both kernels' time.
+//
 // Warp 0 issues the copies, warp 1 the tcgen05.cp and MMAs and owns the tensor memory, warps 2-9 are the
 // epilogue. Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again
 // with a limit) for its copies and MMAs in flight, frees the tensor memory and returns.
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "mx4_args.h"
@@ -293,17 +299,17 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         for (int b = 0; b < 2; ++b) {  // 32 gate and 32 up columns: one block of h
           const int f = (n >> 1) + b * 32;
           if (f >= p.n_out || row >= t.rows) break;
-          float h[32], wild = 0.f;
+          float wild = 0.f;
           uint32_t m = 0;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float g = __uint_as_float(v[b * 64 + j]);
-            wild = fmaxf(wild, fabsf(g));
-            h[j] = silu_branchless(g) * __uint_as_float(v[b * 64 + 32 + j]);
-          }
-          if (!silu_regular(wild)) {  // rare: this block again, by IEEE division
+          for (int j = 0; j < 32; ++j) wild = fmaxf(wild, fabsf(__uint_as_float(v[b * 64 + j])));
+          float* h = reinterpret_cast<float*>(v + b * 64);  // in the gates' place
+          if (silu_regular(wild)) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) h[j] = silu(__uint_as_float(v[b * 64 + j])) * __uint_as_float(v[b * 64 + 32 + j]);
+            for (int j = 0; j < 32; ++j) h[j] = silu_branchless(h[j]) * __uint_as_float(v[b * 64 + 32 + j]);
+          } else {  // (rare)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) h[j] = silu(h[j]) * __uint_as_float(v[b * 64 + 32 + j]);
           }
 #pragma unroll
           for (int j = 0; j < 32; ++j) m = max(m, __float_as_uint(h[j]) & 0x7fffffffu);
@@ -318,7 +324,28 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         long long dst = (long long)t.h_tile * 128 + row;
         if (EPI == kMx4Down) dst = row < t.rows ? p.rowmap[dst] : -1;
         const int cols = min(128, p.n_out - n);
-        if (dst < 0 || row >= t.rows) {
+        if (dst < 0 || row >= t.rows || cols <= 0) {
+        } else if (EPI == kMx4Down && p.out_scale) {
+          uint32_t m = 0;  // largest finite magnitude (past n_out: leftovers of other rows; the store leaves them out)
+#pragma unroll
+          for (int c = 0; c < 128; ++c) {
+            const uint32_t b = v[c] & 0x7fffffffu;
+            m = max(m, c < cols && b < 0x7f800000u ? b : 0u);
+          }
+          const int e = max(int(m >> 23), 15);  // (values below 2^-112 in units of 2^-126)
+          const float unit = __uint_as_float(uint32_t(e - 14) << 23), inv = __uint_as_float(uint32_t(268 - e) << 23);
+          __half* y = static_cast<__half*>(p.out) + dst * p.ldo + n;
+          p.out_scale[dst * ((p.n_out + 127) >> 7) + (n >> 7)] = unit;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {  // (n_out is a multiple of 64)
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const __half2 h = __floats2half2_rn(__uint_as_float(v[c * 16 + 2 * j]) * inv, __uint_as_float(v[c * 16 + 2 * j + 1]) * inv);
+              w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            if (c * 16 < cols) store32(y + c * 16, w);
+          }
         } else if (EPI == kMx4Down || p.out_f32) {
           float* y = static_cast<float*>(p.out) + dst * p.ldo + n;
           if (cols == 128 && p.vec) {
@@ -378,13 +405,9 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   if constexpr (!WIDE) {
     // every CTA's partial tile is in its shared memory; a wait that ran out anywhere in the cluster stops all
     cluster_sync();
-    bool run = first < total && warp >= 2;
-    for (int r = 0; run && r < cs; ++r) {
-      int a;
-      asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(a) : "r"(peer_addr(&ctl->abort, r)) : "memory");
-      run = a == 0;
-    }
-    if (run) {
+    int stopped = 0;
+    if (lane < cs) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(stopped) : "r"(peer_addr(&ctl->abort, lane)) : "memory");
+    if (first < total && warp >= 2 && !__any_sync(0xffffffffu, stopped)) {
       const Item t = item_at<EPI>(p, first);
       const int ldp = p.tn + 4;
       uint32_t peer[8];
@@ -395,13 +418,17 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
       for (int i = warp - 2; i < mine * t.rows; i += 8) {
         const int row = i / mine, unit = rank + (i - row * mine) * cs;
         const uint32_t at = uint32_t(row * ldp + unit * kUnit + lane) * 4u;
-        float x = 0.f, u = 0.f;
+        float x = 0.f, u = 0.f, v[2][8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (r < cs) {
-            x += peer_float(peer[r] + at);
-            if (EPI == kMx4Up) u += peer_float(peer[r] + at + 128u);
-          }
+        for (int r = 0; r < 8; ++r) {  // (all loads in flight before the first sum)
+          v[0][r] = r < cs ? peer_float(peer[r] + at) : 0.f;
+          v[1][r] = EPI == kMx4Up && r < cs ? peer_float(peer[r] + at + 128u) : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          x += v[0][r];
+          u += v[1][r];
+        }
         if constexpr (EPI == kMx4Up) {
           const int f = (t.n0 + unit * 64) >> 1;
           if (f >= p.n_out) continue;
@@ -463,12 +490,13 @@ cudaError_t go(const Mx4GemmArgs& p, int grid, cudaStream_t s) {
 
 }  // namespace
 
-// max_items(tn): most items of a launch with weight tiles of tn rows; tile_rows: most token rows of a tile.
+bool mx4_wide(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN) >= num_sms(); }
+
+// tile_rows: most token rows of a tile.
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s) {
   const int n_rows = epi == kMx4Up ? 2 * p.n_out : p.n_out;
   auto tiles_of = [&](int tn) { return (n_rows + tn - 1) / tn; };
-  // Wide tiles once they fill the SMs.
-  const bool wide = max_tiles * tiles_of(kWideN) >= num_sms;
+  const bool wide = mx4_wide(max_tiles, n_rows);
   p.split = 1;
   int grid;
   if (wide) {

@@ -10,6 +10,8 @@
 // Rows of o are in the order of the assignments (t, k), then the shared experts' (s, t), so the combine needs no
 // lookup but `src`: the assignment whose row holds expert idx[t, k]'s output for token t (itself; the first of
 // them where a token names an expert twice; -1 where it names none).
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "mx4_args.h"
@@ -229,39 +231,78 @@ __global__ void __launch_bounds__(256) mx4_spread_kernel(const __grid_constant__
   }
 }
 
-// y[t] = sum_k gate[t, k] o[src[t, k]] + sum_s o[shared s, t], in this order; four columns a thread.
-template <typename T>
-__global__ void __launch_bounds__(256) mx4_combine_kernel(const __grid_constant__ Mx4MoeArgs a) {
+// y[t] = sum_k gate[t, k] o[src[t, k]] + sum_s o[shared s, t], in this order; eight columns a thread. HALF: o is fp16
+// in units.
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(128) mx4_combine_kernel(const __grid_constant__ Mx4MoeArgs a) {
   pdl_wait();
   if (a.hdr->abort) return;
-  const int t = int(blockIdx.x), c = (int(blockIdx.y) * 256 + int(threadIdx.x)) * 4;
+  const int t = int(blockIdx.x), c = (int(blockIdx.y) * 128 + int(threadIdx.x)) * 8;
   if (c >= a.d) return;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](long long row, float g) {
-    const float4 v = *reinterpret_cast<const float4*>(a.o + row * a.d + c);
-    acc.x = fmaf(g, v.x, acc.x);
-    acc.y = fmaf(g, v.y, acc.y);
-    acc.z = fmaf(g, v.z, acc.z);
-    acc.w = fmaf(g, v.w, acc.w);
-  };
-#pragma unroll 4
-  for (int k = 0; k < a.K; ++k) {
-    const int src = a.src[(long long)t * a.K + k];
-    if (src >= 0) add(src, a.gate[(long long)t * a.K + k]);
+  const int units = (a.d + 127) >> 7, n = a.K + a.S;
+  const float* o32 = static_cast<const float*>(a.o);
+  const __half* o16 = static_cast<const __half*>(a.o);
+  float acc[8] = {};
+  constexpr int kAtOnce = 4;  // rows in flight
+  for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+    float g[kAtOnce];
+    uint4 v[kAtOnce][HALF ? 1 : 2];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = k0 + i;
+      long long row = -1;
+      g[i] = 1.f;
+      if (k < a.K) {
+        row = a.src[(long long)t * a.K + k];
+        if (row >= 0) g[i] = a.gate[(long long)t * a.K + k];
+      } else if (k < n) {
+        row = (long long)a.T * a.K + (long long)(k - a.K) * a.T + t;
+      }
+      if (row < 0) {
+        g[i] = 0.f;
+#pragma unroll
+        for (int q = 0; q < (HALF ? 1 : 2); ++q) v[i][q] = make_uint4(0, 0, 0, 0);
+      } else if constexpr (HALF) {
+        v[i][0] = ld_stream16(o16 + row * a.d + c);
+        g[i] *= __ldg(a.o_unit + row * units + (c >> 7));
+      } else {
+        v[i][0] = ld_stream16(o32 + row * a.d + c);
+        v[i][1] = ld_stream16(o32 + row * a.d + c + 4);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if constexpr (HALF) {
+        const uint32_t w[4] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+          acc[2 * j] = fmaf(g[i], f.x, acc[2 * j]);
+          acc[2 * j + 1] = fmaf(g[i], f.y, acc[2 * j + 1]);
+        }
+      } else {
+        const uint32_t w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(g[i], __uint_as_float(w[j]), acc[j]);
+      }
+    }
   }
-  for (int s = 0; s < a.S; ++s) add((long long)a.T * a.K + (long long)s * a.T + t, 1.f);
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + (long long)t * a.d + c) =
-        make_uint2(pack2bf(acc.x, acc.y), pack2bf(acc.z, acc.w));
-  else
-    *reinterpret_cast<float4*>(static_cast<float*>(a.y) + (long long)t * a.d + c) = acc;
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + (long long)t * a.d + c) =
+        make_uint4(pack2bf(acc[0], acc[1]), pack2bf(acc[2], acc[3]), pack2bf(acc[4], acc[5]), pack2bf(acc[6], acc[7]));
+  } else {
+    float* y = static_cast<float*>(a.y) + (long long)t * a.d + c;
+    *reinterpret_cast<float4*>(y) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    *reinterpret_cast<float4*>(y + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+  }
 }
 
 size_t align512(size_t v) { return (v + 511) & ~size_t(511); }
 
 }  // namespace
 
-Mx4MoeLayout::Mx4MoeLayout(int d, int E, int K, int w, int S, int T) {
+Mx4MoeLayout::Mx4MoeLayout(const mcft_layer_desc* desc, int T) {
+  const int d = desc->d, E = desc->E, K = desc->K, w = desc->w, S = desc->n_shared, dtype = desc->dtype;
   const long long n = (long long)T * K;
   permuted = T > kMx4SharedTileT;
   if (permuted) {
@@ -288,7 +329,10 @@ Mx4MoeLayout::Mx4MoeLayout(int d, int E, int K, int w, int S, int T) {
   pos = place(permuted ? sizeof(int) * size_t(n) : 0);
   x = place(Mx4Layout(x_rows, d).bytes());
   h = place(Mx4Layout(tiles * 128, w).bytes());
-  o = place(sizeof(float) * (size_t(n) + size_t(S) * T) * d);
+  const size_t o_rows = size_t(n) + size_t(S) * T;
+  half_o = dtype == MCFT_BF16 && mx4_wide(tiles, d);
+  o = place(sizeof(float) * o_rows * d);  // (also where fp16 takes half of it: fewer tokens may need fp32)
+  o_unit = place(half_o ? sizeof(float) * o_rows * ((d + 127) / 128) : 0);
   total = at;
 }
 
@@ -314,8 +358,9 @@ cudaError_t launch_mx4_prepare(const Mx4MoeArgs& a, int dtype, bool permuted, cu
 cudaError_t launch_mx4_combine(const Mx4MoeArgs& a, int dtype, cudaStream_t s) {
   prof_begin(kProfMx4Combine, s);
   const dim3 grid(unsigned(a.T), unsigned((a.d + 1023) / 1024));
-  const cudaError_t e = dtype == MCFT_BF16 ? launch_pdl(mx4_combine_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, a)
-                                           : launch_pdl(mx4_combine_kernel<float>, grid, dim3(256), 0, s, a);
+  auto* k = dtype == MCFT_BF16 ? (a.o_unit ? mx4_combine_kernel<__nv_bfloat16, true> : mx4_combine_kernel<__nv_bfloat16, false>)
+                               : (a.o_unit ? mx4_combine_kernel<float, true> : mx4_combine_kernel<float, false>);
+  const cudaError_t e = launch_pdl(k, grid, dim3(128), 0, s, a);
   prof_end(kProfMx4Combine, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -84,10 +84,11 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
   if (rank != 0) return;
   const bool alone = int(gridDim.x) == kFewCtas;  // this cluster has all tokens: no counters to add to
   if (warp < nt) {
-    float z[PL];
+    float z[PL], bias[PL];
+    load_bias(a, bias);
 #pragma unroll
     for (int j = 0; j < PL; ++j) z[j] = lane + 32 * j < a.E ? zs[warp][lane + 32 * j] : 0.f;
-    rank_scored_warp<PL>(a, z, buf[warp], t0 + warp, a.load ? (alone ? count : a.load) : nullptr);
+    rank_scored_warp<PL>(a, z, bias, buf[warp], t0 + warp, a.load ? (alone ? count : a.load) : nullptr);
   }
   if (alone && a.load) {
     __syncthreads();
@@ -143,9 +144,11 @@ __global__ void __launch_bounds__(256) route_scored_tile_kernel(const __grid_con
   }
   __syncthreads();
   float* buf = ws + warp * 64 * PL;
+  float bias[PL];
+  load_bias(a, bias);
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    if (warp * 2 + i < nt) rank_scored_warp<PL>(a, acc[i], buf, t0 + warp * 2 + i, a.load ? count : nullptr);
+    if (warp * 2 + i < nt) rank_scored_warp<PL>(a, acc[i], bias, buf, t0 + warp * 2 + i, a.load ? count : nullptr);
   if (a.load) {
     __syncthreads();
     if (tid < a.E && count[tid]) atomicAdd(a.load + tid, count[tid]);

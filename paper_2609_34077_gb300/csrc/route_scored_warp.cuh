@@ -26,10 +26,21 @@ __device__ __forceinline__ void softmax_stats(const float* z, int E, float& m, f
   sum = warp_sum(sum);
 }
 
-// z[j]: logit of expert lane + 32 j (PL = ceil(E / 32) of them). buf: 2 * 32 * PL floats of shared memory, this warp's
-// alone. load: shared or global counters of the experts' choices, or NULL.
+// The biases of a lane's experts (the same for every token).
 template <int PL>
-__device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL], float* buf, int t, int32_t* load) {
+__device__ __forceinline__ void load_bias(const ScoredArgs& a, float (&b)[PL]) {
+#pragma unroll
+  for (int j = 0; j < PL; ++j) {
+    const int e = int(threadIdx.x & 31) + 32 * j;
+    b[j] = a.bias && e < a.E ? __ldg(a.bias + e) : 0.f;
+  }
+}
+
+// z[j], bias[j]: logit and bias of expert lane + 32 j (PL of them, E <= 32 PL). buf: 2 * 32 * PL floats of shared
+// memory, this warp's alone. load: shared or global counters of the experts' choices, or NULL.
+template <int PL>
+__device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL], const float (&bias)[PL], float* buf, int t,
+                                        int32_t* load) {
   constexpr int kNone = -2147483647 - 1;  // below every key: not there, or taken
   constexpr unsigned kAll = 0xffffffffu;
   const int lane = threadIdx.x & 31, E = a.E;
@@ -61,8 +72,7 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     c[j] = -INFINITY;
     if (e < E) {
       if (a.logits) a.logits[size_t(t) * E + e] = z[j];
-      float v = s[j];
-      if (a.bias) v += __ldg(a.bias + e);
+      const float v = s[j] + bias[j];
       nan |= v != v;
       c[j] = v != v ? -INFINITY : v;
       ss[e] = s[j];
@@ -83,6 +93,7 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     const int g = lane >> shift, sub = lane & (per - 1), n = (gsz + per - 1) >> shift;
     float best = -INFINITY, second = -INFINITY;
     if (g < a.n_group) {
+#pragma unroll 4
       for (int i = 0, k = g % n; i < n; ++i, k = k + 1 == n ? 0 : k + 1) {  // (groups start apart: other banks)
         const int at = sub + (k << shift);
         const float v = at < gsz ? cs[g * gsz + at] : -INFINITY;
@@ -103,10 +114,11 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
       groups |= 1u << (l >> shift);
       if (lane == l) gkey = kNone;
     }
+    const float inv = 1.f / float(gsz);
 #pragma unroll
-    for (int j = 0; j < PL; ++j) {
+    for (int j = 0; j < PL; ++j) {  // e / gsz: (e + 1/2) / gsz is 1/512 or more from the next whole number
       const int e = lane + 32 * j;
-      if (e < E && !((groups >> (e / gsz)) & 1u)) key[j] = kNone;
+      if (e < E && !((groups >> int((float(e) + 0.5f) * inv)) & 1u)) key[j] = kNone;
     }
   }
   __syncwarp();

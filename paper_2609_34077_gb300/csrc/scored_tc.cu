@@ -211,13 +211,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
       tc_fence_before();
     }
   }
+  float bias[PL];
+  load_bias(p.a, bias);
   cluster_sync();  // every CTA's partial logits are in its shared memory; a wait that ran out anywhere stops all
-  bool run = true;
-  for (int r = 0; run && r < cs; ++r) {
-    int a;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(a) : "r"(peer_addr(&ctl->abort, r)) : "memory");
-    run = a == 0;
-  }
+  int stopped = 0;
+  if (lane < cs) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(stopped) : "r"(peer_addr(&ctl->abort, lane)) : "memory");
+  const bool run = !__any_sync(0xffffffffu, stopped);
   if (run) {
     uint32_t peer[8];
 #pragma unroll
@@ -229,13 +228,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
 #pragma unroll
       for (int j = 0; j < PL; ++j) z[j] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 8; ++r)
+      for (int r = 0; r < 8; r += 2)  // the loads of two peers in flight at once
         if (r < cs) {
+          float v[2][PL];
 #pragma unroll
-          for (int j = 0; j < PL; ++j)
-            if (lane + 32 * j < p.a.E) z[j] += peer_float(peer[r] + uint32_t(row * (p.n + 4) + lane + 32 * j) * 4u);
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < PL; ++j)
+              v[h][j] = r + h < cs && lane + 32 * j < p.a.E
+                            ? peer_float(peer[r + h] + uint32_t(row * (p.n + 4) + lane + 32 * j) * 4u)
+                            : 0.f;
+#pragma unroll
+          for (int j = 0; j < PL; ++j) z[j] = z[j] + v[0][j] + v[1][j];
         }
-      rank_scored_warp<PL>(p.a, z, rows + warp * 64 * PL, t0 + row, p.a.load ? ctl->count : nullptr);
+      rank_scored_warp<PL>(p.a, z, bias, rows + warp * 64 * PL, t0 + row, p.a.load ? ctl->count : nullptr);
     }
   }
   cluster_sync();  // the peers have read this CTA's logits; its counts are complete
