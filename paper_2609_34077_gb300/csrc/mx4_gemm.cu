@@ -39,6 +39,8 @@ constexpr int kThreads = 320;
 constexpr int kMaxStages = 16;
 constexpr int kWideN = 256, kNarrowN = 128;
 constexpr int kWideRing = 220 * 1024, kNarrowRing = 104 * 1024;
+constexpr int kWideDepth = 2;                                                       // chunks of a stage
+constexpr int kWideStages = kWideRing / (kWideDepth * (8192 + kWideN * 64 + 512 + 1024));
 constexpr int kSfCols = 16;  // tensor memory columns of a chunk's scales: 4 of A, up to 8 of B
 // Instruction descriptor without N and the scale bytes' places: A and B e2m1, scales ue8m0, M = 128.
 constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (1u << 23) | (uint32_t(128 >> 4) << 24);
@@ -63,24 +65,22 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
       "r"(bytes), "r"(bar)
       : "memory");
 }
-// K-major operand rows of 64 bytes under the 64-byte swizzle: 512 bytes between 8-row groups.
-__device__ __forceinline__ uint64_t sw64_desc(uint32_t saddr) {
-  return uint64_t((saddr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(512 >> 4) << 32) | (uint64_t(1) << 46) |
-         (uint64_t(4) << 61);
+// Shared-memory descriptors by their low word (the address / 16 and a constant), which alone changes in the issuing
+// loop. Operands: K-major rows of 64 bytes under the 64-byte swizzle, 512 bytes between 8-row groups. Scales: 32 rows
+// of 16 bytes, no swizzle, 128 bytes between 8-row groups.
+constexpr uint32_t kOperandHi = (512u >> 4) | (1u << 14) | (4u << 29), kScaleHi = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t lo) {
+  asm volatile("{\n .reg .b64 d;\n mov.b64 d, {%1, %2};\n tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n}" ::"r"(taddr),
+               "r"(lo), "r"(kScaleHi)
+               : "memory");
 }
-// 32 rows of 16 bytes, no swizzle: 128 bytes between 8-row groups.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
-  return uint64_t((saddr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
-}
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_desc(saddr)) : "memory");
-}
-__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+__device__ __forceinline__ void mma_mx4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
                                         uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)
+      "{\n .reg .pred p;\n .reg .b64 x, y;\n mov.b64 x, {%1, %7};\n mov.b64 y, {%2, %7};\n setp.ne.b32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, %3, [%4], [%5], p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(kOperandHi)
       : "memory");
 }
 __device__ __forceinline__ void commit(uint64_t* bar) {
@@ -148,7 +148,8 @@ __device__ __forceinline__ Item item_at(const Mx4GemmArgs& p, int i) {
 template <int EPI, bool WIDE>
 __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const __grid_constant__ Mx4GemmArgs p) {
   constexpr int kTmemCols = WIDE ? 512 : 256, kSfBase = WIDE ? kWideN : kNarrowN;
-  constexpr int kSets = (kTmemCols - kSfBase) / kSfCols;
+  constexpr uint32_t kSets = (kTmemCols - kSfBase) / kSfCols;
+  static_assert((kSets & (kSets - 1)) == 0, "a power of two");
   constexpr int kRing = WIDE ? kWideRing : kNarrowRing;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   const int rank = WIDE ? 0 : int(cluster_rank());
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < p.stages; ++s) {
+    for (int s = 0; s < (WIDE ? kWideStages : p.stages); ++s) {
       mbar_init(&ctl->full[s], 1);
       mbar_init(&ctl->empty[s], 1);
     }
@@ -188,11 +189,12 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   const int stride = WIDE ? int(gridDim.x) : total;  // narrow: one item
   // this CTA's share of the contraction, in chunks
   const int kc0 = int((long long)p.chunks * rank / cs), kc1 = int((long long)p.chunks * (rank + 1) / cs);
-  const uint32_t a_bytes = uint32_t(p.a_groups) * 512u, b_bytes = uint32_t(p.tn) * 64u;
-  const uint32_t sb_bytes = uint32_t(p.tn > 128 ? 2 : 1) * 512u;
+  const uint32_t a_bytes = WIDE ? 8192u : uint32_t(p.a_groups) * 512u, tn = WIDE ? kWideN : uint32_t(p.tn);
+  const uint32_t b_bytes = tn * 64u, sb_bytes = WIDE ? 1024u : 512u, depth = WIDE ? kWideDepth : uint32_t(p.depth);
   // a stage: codes of A (all chunks), of B, scales of A, of B
-  const uint32_t off_b = a_bytes * p.depth, off_sa = off_b + b_bytes * p.depth, off_sb = off_sa + 512u * p.depth;
-  const uint32_t stage_bytes = off_sb + sb_bytes * p.depth;
+  const uint32_t off_b = a_bytes * depth, off_sa = off_b + b_bytes * depth, off_sb = off_sa + 512u * depth;
+  const uint32_t stage_bytes = off_sb + sb_bytes * depth;
+  const int stages = WIDE ? kWideStages : p.stages;
 
   if (warp == 0) {
     if (first < total && elect_one()) {
@@ -201,27 +203,31 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
       for (int i = first; i < total && !*abort; i += stride) {
         const Item t = item_at<EPI>(p, i);
         const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
-        const uint8_t* pa = p.a + size_t(t.a_tile) * 8192;
-        const uint8_t* psa = p.a_scales + size_t(t.a_tile) * 512;
-        const uint8_t* pb = w + p.w_codes + size_t(t.n0) * 64;
-        const uint8_t* psb = w + p.w_scales + size_t(t.n0 >> 7) * 512;
+        const uint8_t* pa = p.a + size_t(t.a_tile) * 8192 + kc0 * p.a_code_stride;
+        const uint8_t* psa = p.a_scales + size_t(t.a_tile) * 512 + kc0 * p.a_scale_stride;
+        const uint8_t* pb = w + p.w_codes + size_t(t.n0) * 64 + kc0 * p.w_code_stride;
+        const uint8_t* psb = w + p.w_scales + size_t(t.n0 >> 7) * 512 + kc0 * p.w_scale_stride;
         const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
-        const uint32_t nb = uint32_t(min(p.tn >> 3, p.w_groups - (t.n0 >> 3))) * 512u;
-        const uint32_t nsb = uint32_t(min(p.tn > 128 ? 2 : 1, p.w_blocks - (t.n0 >> 7))) * 512u;
-        for (int kc = kc0; kc < kc1; kc += p.depth) {
+        const uint32_t nb = uint32_t(min(int(tn >> 3), p.w_groups - (t.n0 >> 3))) * 512u;
+        const uint32_t nsb = uint32_t(min(WIDE ? 2 : 1, p.w_blocks - (t.n0 >> 7))) * 512u;
+        for (int kc = kc0; kc < kc1; kc += depth) {
           if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
           const uint32_t st = base + uint32_t(s) * stage_bytes, bar = smem_u32(&ctl->full[s]);
-          const int nc = min(p.depth, kc1 - kc);
+          const int nc = min(int(depth), kc1 - kc);
           mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
+#pragma unroll 2
           for (int j = 0; j < nc; ++j) {
-            const size_t c = size_t(kc + j);
-            bulk_load(st + off_b + b_bytes * j, pb + c * p.w_code_stride, nb, bar);
-            bulk_load(st + off_sb + sb_bytes * j, psb + c * p.w_scale_stride, nsb, bar);
-            bulk_load(st + a_bytes * j, pa + c * p.a_code_stride, na, bar);
-            bulk_load(st + off_sa + 512u * j, psa + c * p.a_scale_stride, 512u, bar);
+            bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
+            bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
+            bulk_load(st + a_bytes * j, pa, na, bar);
+            bulk_load(st + off_sa + 512u * j, psa, 512u, bar);
+            pa += p.a_code_stride;
+            psa += p.a_scale_stride;
+            pb += p.w_code_stride;
+            psb += p.w_scale_stride;
           }
-          if (issued < p.stages) ++issued;
-          if (++s == p.stages) {
+          if (issued < stages) ++issued;
+          if (++s == stages) {
             s = 0;
             ph ^= 1u;
           }
@@ -230,41 +236,43 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
       // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
       for (int i = 0; i < issued; ++i) {
         const int j = s - (issued - i);
-        if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + p.stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
+        if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
       }
     }
   } else if (warp == 1) {
     if (first < total && elect_one()) {
       int s = 0;
       uint32_t ph = 0, lt = 0, set = 0;
+      const uint32_t lo0 = desc_lo(base), idesc = kIdesc | (tn >> 3 << 17), idesc2 = idesc | (2u << 4) | (2u << 29);
       for (int i = first; i < total && !*abort; i += stride, ++lt) {
-        const Item t = item_at<EPI>(p, i);
-        const uint32_t idesc = kIdesc | (uint32_t(p.tn >> 3) << 17);
-        const uint32_t sb_shift = uint32_t(t.n0 >> 5) & 3u;  // (tn < 128: which 32-row columns of the block)
+        // narrow tiles: which 32-row columns of the 128-row block of scales
+        const uint32_t sb_shift = WIDE ? 0u : uint32_t(item_at<EPI>(p, i).n0 >> 5) & 3u;
         if (!mbar_wait_cl(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
         tc_fence_after();
         bool ok = true;
-        for (int kc = kc0; kc < kc1; kc += p.depth) {
+        uint32_t acc = 0;
+        for (int kc = kc0; kc < kc1; kc += depth) {
           if (!mbar_wait_cl(&ctl->full[s], ph, abort, p.err)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t st = base + uint32_t(s) * stage_bytes;
-          const int nc = min(p.depth, kc1 - kc);
-          for (int j = 0; j < nc; ++j) {
+          const uint32_t st = lo0 + (uint32_t(s) * stage_bytes >> 4);
+          const int nc = min(int(depth), kc1 - kc);
+#pragma unroll 2
+          for (uint32_t j = 0; j < uint32_t(nc); ++j) {
             const uint32_t sfa = tmem + kSfBase + set * kSfCols, sfb = sfa + 4;
-            scales_to_tmem(sfa, st + off_sa + 512u * j);
-            scales_to_tmem(sfb, st + off_sb + sb_bytes * j);
-            if (WIDE) scales_to_tmem(sfb + 4, st + off_sb + sb_bytes * j + 512u);
-            const uint64_t da = sw64_desc(st + a_bytes * j), db = sw64_desc(st + off_b + b_bytes * j);
-            mma_mx4(tmem, da, db, idesc, sfa, sfb + sb_shift, kc + j > kc0 ? 1u : 0u);
-            if ((kc + j) * 2 + 1 < p.ksteps)
-              mma_mx4(tmem, da + 2, db + 2, idesc | (2u << 4) | (2u << 29), sfa, sfb + sb_shift, 1u);
-            set = set + 1 == kSets ? 0 : set + 1;
+            scales_to_tmem(sfa, st + (off_sa >> 4) + 32u * j);
+            scales_to_tmem(sfb, st + (off_sb >> 4) + (sb_bytes >> 4) * j);
+            if (WIDE) scales_to_tmem(sfb + 4, st + (off_sb >> 4) + (sb_bytes >> 4) * j + 32u);
+            const uint32_t da = st + (a_bytes >> 4) * j, db = st + (off_b >> 4) + (b_bytes >> 4) * j;
+            mma_mx4(tmem, da, db, idesc, sfa, sfb + sb_shift, acc);
+            acc = 1;
+            if ((kc + int(j)) * 2 + 1 < p.ksteps) mma_mx4(tmem, da + 2, db + 2, idesc2, sfa, sfb + sb_shift, 1u);
+            set = (set + 1) & (kSets - 1);
           }
           commit(&ctl->empty[s]);
-          if (++s == p.stages) {
+          if (++s == stages) {
             s = 0;
             ph ^= 1u;
           }
@@ -501,7 +509,7 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
   int grid;
   if (wide) {
     p.tn = kWideN;
-    p.depth = 2;
+    p.depth = kWideDepth;
     p.a_groups = 16;
     p.n_tiles = tiles_of(p.tn);
     grid = int(std::min<long long>(num_sms, max_tiles * p.n_tiles));
@@ -516,7 +524,7 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
   const int stage = p.depth * (p.a_groups * 512 + p.tn * 64 + 512 + (p.tn > 128 ? 1024 : 512));
   // the MMA reads 128 rows of A wherever the stage's A begins: the last stage's end stays inside the ring
   const int slack = (16 - p.a_groups) * 512;
-  p.stages = std::min(kMaxStages, ((wide ? kWideRing : kNarrowRing) - slack) / stage);
+  p.stages = wide ? kWideStages : std::min(kMaxStages, (kNarrowRing - slack) / stage);
   if (p.stages < 2) return cudaErrorInvalidConfiguration;
   const int kid = epi == kMx4Up ? kProfMx4Up : epi == kMx4Down ? kProfMx4Down : kProfMx4Matmul;
   prof_begin(kid, s);
