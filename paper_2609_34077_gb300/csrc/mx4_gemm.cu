@@ -117,6 +117,17 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   return (silu_regular(g) ? silu_branchless(g) : silu(g)) * u;
 }
 
+// As mbar_wait_cl, for barriers that only this CTA arrives on.
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort, unsigned* err) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0 || mbar_wait_cl(bar, parity, abort, err);
+}
+
 struct Item {
   int seg, a_tile, h_tile, rows, n0;  // weights; token tile of A; of the output; its rows; first weight row
 };
@@ -149,7 +160,7 @@ template <int EPI, bool WIDE>
 __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const __grid_constant__ Mx4GemmArgs p) {
   constexpr int kTmemCols = WIDE ? 512 : 256, kSfBase = WIDE ? kWideN : kNarrowN;
   constexpr uint32_t kSets = (kTmemCols - kSfBase) / kSfCols;
-  static_assert((kSets & (kSets - 1)) == 0, "a power of two");
+  static_assert((kSets & (kSets - 1)) == 0 && (!WIDE || kWideStages * kWideDepth <= kSets), "sets of scales");
   constexpr int kRing = WIDE ? kWideRing : kNarrowRing;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -182,7 +193,8 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;
+  // (all columns of an SM begin at column 0; a constant keeps the issuing loop's operands out of the registers)
+  const uint32_t tmem = WIDE ? 0u : ctl->tmem_base;
   volatile int* abort = &ctl->abort;
   const int total = EPI == kMx4Out ? p.m_tiles * p.n_tiles : (p.hdr->abort ? 0 : p.hdr->tiles * p.n_tiles);
   const int first = WIDE ? int(blockIdx.x) : int(blockIdx.x) / cs;
@@ -242,34 +254,37 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   } else if (warp == 1) {
     if (first < total && elect_one()) {
       int s = 0;
-      uint32_t ph = 0, lt = 0, set = 0;
+      uint32_t ph = 0, lt = 0;
       const uint32_t lo0 = desc_lo(base), idesc = kIdesc | (tn >> 3 << 17), idesc2 = idesc | (2u << 4) | (2u << 29);
       for (int i = first; i < total && !*abort; i += stride, ++lt) {
         // narrow tiles: which 32-row columns of the 128-row block of scales
         const uint32_t sb_shift = WIDE ? 0u : uint32_t(item_at<EPI>(p, i).n0 >> 5) & 3u;
-        if (!mbar_wait_cl(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
+        if (!wait(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
         tc_fence_after();
         bool ok = true;
-        uint32_t acc = 0;
         for (int kc = kc0; kc < kc1; kc += depth) {
-          if (!mbar_wait_cl(&ctl->full[s], ph, abort, p.err)) {
+          if (!wait(&ctl->full[s], ph, abort, p.err)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t st = lo0 + (uint32_t(s) * stage_bytes >> 4);
-          const int nc = min(int(depth), kc1 - kc);
-#pragma unroll 2
-          for (uint32_t j = 0; j < uint32_t(nc); ++j) {
-            const uint32_t sfa = tmem + kSfBase + set * kSfCols, sfb = sfa + 4;
+          const uint32_t st = lo0 + uint32_t(s) * (stage_bytes >> 4);
+          const uint32_t sf0 = tmem + kSfBase + uint32_t(s) * (WIDE ? kWideDepth * kSfCols : 0u);
+          auto step = [&](uint32_t j, uint32_t acc) {  // 128 columns
+            const uint32_t sfa = sf0 + (WIDE ? j : j & (kSets - 1)) * kSfCols, sfb = sfa + 4;
             scales_to_tmem(sfa, st + (off_sa >> 4) + 32u * j);
             scales_to_tmem(sfb, st + (off_sb >> 4) + (sb_bytes >> 4) * j);
             if (WIDE) scales_to_tmem(sfb + 4, st + (off_sb >> 4) + (sb_bytes >> 4) * j + 32u);
             const uint32_t da = st + (a_bytes >> 4) * j, db = st + (off_b >> 4) + (b_bytes >> 4) * j;
             mma_mx4(tmem, da, db, idesc, sfa, sfb + sb_shift, acc);
-            acc = 1;
             if ((kc + int(j)) * 2 + 1 < p.ksteps) mma_mx4(tmem, da + 2, db + 2, idesc2, sfa, sfb + sb_shift, 1u);
-            set = (set + 1) & (kSets - 1);
+          };
+          const int nc = min(int(depth), kc1 - kc);
+          step(0, kc > kc0 ? 1u : 0u);
+          if constexpr (WIDE) {
+            if (nc == kWideDepth) step(1, 1u);
+          } else {
+            for (int j = 1; j < nc; ++j) step(uint32_t(j), 1u);
           }
           commit(&ctl->empty[s]);
           if (++s == stages) {
