@@ -45,12 +45,20 @@ constexpr int kSfCols = 16;  // tensor memory columns of a chunk's scales: 4 of 
 // Instruction descriptor without N and the scale bytes' places: A and B e2m1, scales ue8m0, M = 128.
 constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (1u << 23) | (uint32_t(128 >> 4) << 24);
 
+struct Item {
+  int seg, a_tile, h_tile, rows, n0;  // weights; token tile of A; of the output; its rows; first weight row
+};
+// The copying warp finds the items and leaves them here for the epilogue. It is at most the ring's stages (and an item)
+// ahead of the MMAs, and those one item ahead of the epilogue.
+constexpr int kSlots = 16;
+
 struct Ctl {
   uint64_t full[kMaxStages], empty[kMaxStages], tfull, tempty, drain;
   uint32_t tmem_base;
   int abort;
+  Item item[kSlots];
 };
-constexpr int kCtlBytes = 512;
+constexpr int kCtlBytes = 1024;
 static_assert(sizeof(Ctl) <= kCtlBytes, "control block");
 
 template <bool WIDE>
@@ -127,10 +135,6 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
       : "memory");
   return ok != 0 || mbar_wait_cl(bar, parity, abort, err);
 }
-
-struct Item {
-  int seg, a_tile, h_tile, rows, n0;  // weights; token tile of A; of the output; its rows; first weight row
-};
 
 // Item -> tile. The device's tile list has a segment's token tiles one after another; a segment's items are its
 // weight tiles with the token tiles innermost, so CTAs that run side by side share weights.
@@ -212,8 +216,11 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
     if (first < total && elect_one()) {
       int s = 0, issued = 0;
       uint32_t ph = 0;
-      for (int i = first; i < total && !*abort; i += stride) {
-        const Item t = item_at<EPI>(p, i);
+      Item next = item_at<EPI>(p, first);
+      for (int i = first, n = 0; i < total && !*abort; i += stride, ++n) {
+        const Item t = next;
+        ctl->item[n % kSlots] = t;  // (before the arrivals on the item's `full` barriers)
+        if (i + stride < total) next = item_at<EPI>(p, i + stride);  // its loads return under this item's copies
         const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
         const uint8_t* pa = p.a + size_t(t.a_tile) * 8192 + kc0 * p.a_code_stride;
         const uint8_t* psa = p.a_scales + size_t(t.a_tile) * 512 + kc0 * p.a_scale_stride;
@@ -303,11 +310,11 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
     const int row = q * 32 + lane;
     uint32_t lt = 0;
     for (int i = first; i < total; i += stride, ++lt) {
-      const Item t = item_at<EPI>(p, i);
       int ok = 1;
       if (lane == 0) ok = mbar_wait_cl(&ctl->tfull, lt & 1u, abort, p.err) ? 1 : 0;
       if (!__shfl_sync(0xffffffffu, ok, 0)) break;
       tc_fence_after();
+      const Item t = ctl->item[lt % kSlots];
       uint32_t v[128];
       const uint32_t taddr = tmem + (uint32_t(q * 32) << 16) + uint32_t(grp * 128);
 #pragma unroll
@@ -402,11 +409,11 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   } else {
     const int q = warp & 3, grp = (warp - 2) >> 2, row = q * 32 + lane;
     if (first < total) {
-      const Item t = item_at<EPI>(p, first);
       int ok = 1;
       if (lane == 0) ok = mbar_wait_cl(&ctl->tfull, 0, abort, p.err) ? 1 : 0;
       if (__shfl_sync(0xffffffffu, ok, 0)) {
         tc_fence_after();
+        const Item t = ctl->item[0];
         // the ring is free: every copy has landed and every MMA has read it
         const int ldp = p.tn + 4;
         float* part = reinterpret_cast<float*>(ring) + size_t(row) * ldp;
@@ -431,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
     int stopped = 0;
     if (lane < cs) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(stopped) : "r"(peer_addr(&ctl->abort, lane)) : "memory");
     if (first < total && warp >= 2 && !__any_sync(0xffffffffu, stopped)) {
-      const Item t = item_at<EPI>(p, first);
+      const Item t = ctl->item[0];
       const int ldp = p.tn + 4;
       uint32_t peer[8];
 #pragma unroll
