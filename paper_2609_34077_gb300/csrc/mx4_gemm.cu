@@ -193,10 +193,14 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // The narrow down product starts under the up product (which lets it, once the plan is complete): its copying warp
+  // reads the plan and brings weights, and waits before the first hidden activations.
+  constexpr bool kAhead = EPI == kMx4Down && !WIDE;
+  if (!kAhead || warp != 0) pdl_wait();
+  if (!WIDE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // (all columns of an SM begin at column 0; a constant keeps the issuing loop's operands out of the registers)
   const uint32_t tmem = WIDE ? 0u : ctl->tmem_base;
   volatile int* abort = &ctl->abort;
@@ -229,21 +233,39 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
         const uint32_t nb = uint32_t(min(int(tn >> 3), p.w_groups - (t.n0 >> 3))) * 512u;
         const uint32_t nsb = uint32_t(min(WIDE ? 2 : 1, p.w_blocks - (t.n0 >> 7))) * 512u;
+        int ahead = kc0;  // chunks up to here have their weights under way
+        if constexpr (kAhead) {
+          for (int q = 0; q < stages && ahead < kc1; ++q) {
+            const uint32_t st = base + uint32_t(q) * stage_bytes, bar = smem_u32(&ctl->full[q]);
+            const int nc = min(int(depth), kc1 - ahead);
+            mbar_expect_tx(&ctl->full[q], uint32_t(nc) * (na + nb + 512u + nsb));
+            for (int j = 0; j < nc; ++j, ++ahead) {
+              bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
+              bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
+              pb += p.w_code_stride;
+              psb += p.w_scale_stride;
+            }
+          }
+          pdl_wait();
+        }
         for (int kc = kc0; kc < kc1; kc += depth) {
           if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
           const uint32_t st = base + uint32_t(s) * stage_bytes, bar = smem_u32(&ctl->full[s]);
           const int nc = min(int(depth), kc1 - kc);
-          mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
+          const bool weights = !kAhead || kc >= ahead;
+          if (weights) mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
 #pragma unroll 2
           for (int j = 0; j < nc; ++j) {
-            bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
-            bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
+            if (weights) {
+              bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
+              bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
+              pb += p.w_code_stride;
+              psb += p.w_scale_stride;
+            }
             bulk_load(st + a_bytes * j, pa, na, bar);
             bulk_load(st + off_sa + 512u * j, psa, 512u, bar);
             pa += p.a_code_stride;
             psa += p.a_scale_stride;
-            pb += p.w_code_stride;
-            psb += p.w_scale_stride;
           }
           if (issued < stages) ++issued;
           if (++s == stages) {
@@ -253,6 +275,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         }
       }
       // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
+      // (a break above leaves no stage whose weights came without its activations: a first round's stages are empty)
       for (int i = 0; i < issued; ++i) {
         const int j = s - (issued - i);
         if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;

@@ -59,6 +59,7 @@ __device__ __forceinline__ void put_block(uint8_t* q, const Mx4Layout& L, size_t
 template <typename T>
 __global__ void __launch_bounds__(kPlanThreads) mx4_plan_kernel(const __grid_constant__ Mx4MoeArgs a) {
   pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the up product sets itself up meanwhile)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (blockIdx.x > 0) {
     const int spans = (a.d + 1023) / 1024, b = int(blockIdx.x) - 1;
