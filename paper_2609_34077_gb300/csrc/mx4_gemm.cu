@@ -150,7 +150,7 @@ __device__ __forceinline__ Item item_at(const Mx4GemmArgs& p, int i) {
   } else {
     const Mx4Tile e = p.tiles[i / p.n_tiles];
     const int local = i - e.first * p.n_tiles, m = local % e.count;
-    const Mx4Tile f = p.tiles[e.first + m];
+    const Mx4Tile f = e.count == 1 ? e : p.tiles[e.first + m];
     t.seg = f.seg;
     t.a_tile = EPI == kMx4Up ? f.a_tile : e.first + m;
     t.h_tile = e.first + m;
@@ -196,10 +196,10 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  // The narrow down product starts under the up product (which lets it, once the plan is complete): its copying warp
-  // reads the plan and brings weights, and waits before the first hidden activations.
+  // The narrow down product starts under the up product (which lets it, once the plan is complete): the warps that copy
+  // weights read the plan and begin before the up product has ended; the others wait for it.
   constexpr bool kAhead = EPI == kMx4Down && !WIDE;
-  if (!kAhead || warp != 0) pdl_wait();
+  if (!kAhead || (warp != 0 && warp != 2)) pdl_wait();
   if (!WIDE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // (all columns of an SM begin at column 0; a constant keeps the issuing loop's operands out of the registers)
   const uint32_t tmem = WIDE ? 0u : ctl->tmem_base;
@@ -216,8 +216,68 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   const uint32_t stage_bytes = off_sb + sb_bytes * depth;
   const int stages = WIDE ? kWideStages : p.stages;
 
+  // Narrow: a bulk copy takes its thread 45 to 70 cycles to issue, and a chunk's four bring 5 KB only, so four warps (0 and
+  // the epilogue's first three, which have nothing to do yet) issue one kind each: codes and scales of the weights, then
+  // of the tokens. Warp 0 alone announces a stage's bytes.
+  const int kind = warp == 0 ? 0 : warp - 1;  // (warps 0, 2, 3, 4)
+  if (!WIDE && warp != 1 && kind < 4 && first < total && elect_one()) {
+    const Item t = item_at<EPI>(p, first);
+    if (kind == 0) ctl->item[0] = t;  // (before the arrivals on the `full` barriers)
+    const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
+    const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
+    const uint32_t nb = uint32_t(min(int(tn >> 3), p.w_groups - (t.n0 >> 3))) * 512u;
+    const uint8_t* src;
+    size_t pitch;
+    uint32_t bytes = 512u, at, step = 512u;
+    if (kind == 0) {
+      src = w + p.w_codes + size_t(t.n0) * 64;
+      pitch = p.w_code_stride;
+      bytes = nb;
+      at = off_b;
+      step = b_bytes;
+    } else if (kind == 1) {
+      src = w + p.w_scales + size_t(t.n0 >> 7) * 512;
+      pitch = p.w_scale_stride;
+      at = off_sb;
+    } else if (kind == 2) {
+      src = p.a + size_t(t.a_tile) * 8192;
+      pitch = p.a_code_stride;
+      bytes = na;
+      at = 0;
+      step = a_bytes;
+    } else {
+      src = p.a_scales + size_t(t.a_tile) * 512;
+      pitch = p.a_scale_stride;
+      at = off_sa;
+    }
+    src += size_t(kc0) * pitch;
+    int s = 0, issued = 0;
+    uint32_t ph = 0;
+    for (int kc = kc0; kc < kc1; kc += depth) {
+      if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
+      const uint32_t st = base + uint32_t(s) * stage_bytes + at, bar = smem_u32(&ctl->full[s]);
+      const int nc = min(int(depth), kc1 - kc);
+      if (kind == 0) mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 1024u));
+      for (int j = 0; j < nc; ++j, src += pitch) bulk_load(st + step * uint32_t(j), src, bytes, bar);
+      if (issued < stages) ++issued;
+      if (++s == stages) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+    if (kind == 0) {
+      // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
+      for (int i = 0; i < issued; ++i) {
+        const int j = s - (issued - i);
+        if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
+      }
+    }
+  }
+  __syncwarp();
+  if (kAhead && (warp == 0 || warp == 2)) pdl_wait();
+
   if (warp == 0) {
-    if (first < total && elect_one()) {
+    if (WIDE && first < total && elect_one()) {
       int s = 0, issued = 0;
       uint32_t ph = 0;
       Item next = item_at<EPI>(p, first);
@@ -232,40 +292,22 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         const uint8_t* psb = w + p.w_scales + size_t(t.n0 >> 7) * 512 + kc0 * p.w_scale_stride;
         const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
         const uint32_t nb = uint32_t(min(int(tn >> 3), p.w_groups - (t.n0 >> 3))) * 512u;
-        const uint32_t nsb = uint32_t(min(WIDE ? 2 : 1, p.w_blocks - (t.n0 >> 7))) * 512u;
-        int ahead = kc0;  // chunks up to here have their weights under way
-        if constexpr (kAhead) {
-          for (int q = 0; q < stages && ahead < kc1; ++q) {
-            const uint32_t st = base + uint32_t(q) * stage_bytes, bar = smem_u32(&ctl->full[q]);
-            const int nc = min(int(depth), kc1 - ahead);
-            mbar_expect_tx(&ctl->full[q], uint32_t(nc) * (na + nb + 512u + nsb));
-            for (int j = 0; j < nc; ++j, ++ahead) {
-              bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
-              bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
-              pb += p.w_code_stride;
-              psb += p.w_scale_stride;
-            }
-          }
-          pdl_wait();
-        }
+        const uint32_t nsb = uint32_t(min(2, p.w_blocks - (t.n0 >> 7))) * 512u;
         for (int kc = kc0; kc < kc1; kc += depth) {
           if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
           const uint32_t st = base + uint32_t(s) * stage_bytes, bar = smem_u32(&ctl->full[s]);
           const int nc = min(int(depth), kc1 - kc);
-          const bool weights = !kAhead || kc >= ahead;
-          if (weights) mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
+          mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
 #pragma unroll 2
           for (int j = 0; j < nc; ++j) {
-            if (weights) {
-              bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
-              bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
-              pb += p.w_code_stride;
-              psb += p.w_scale_stride;
-            }
+            bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
+            bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
             bulk_load(st + a_bytes * j, pa, na, bar);
             bulk_load(st + off_sa + 512u * j, psa, 512u, bar);
             pa += p.a_code_stride;
             psa += p.a_scale_stride;
+            pb += p.w_code_stride;
+            psb += p.w_scale_stride;
           }
           if (issued < stages) ++issued;
           if (++s == stages) {
@@ -275,7 +317,6 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         }
       }
       // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
-      // (a break above leaves no stage whose weights came without its activations: a first round's stages are empty)
       for (int i = 0; i < issued; ++i) {
         const int j = s - (issued - i);
         if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
@@ -457,7 +498,8 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
 
   if constexpr (!WIDE) {
     // every CTA's partial tile is in its shared memory; a wait that ran out anywhere in the cluster stops all
-    cluster_sync();
+    if (cs > 1) cluster_sync();
+    else if (warp >= 2) asm volatile("bar.sync 1, 256;" ::: "memory");
     int stopped = 0;
     if (lane < cs) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(stopped) : "r"(peer_addr(&ctl->abort, lane)) : "memory");
     if (first < total && warp >= 2 && !__any_sync(0xffffffffu, stopped)) {
@@ -506,7 +548,8 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         }
       }
     }
-    cluster_sync();  // the peers have read this CTA's partial tile
+    if (cs > 1) cluster_sync();  // the peers have read this CTA's partial tile
+    else __syncthreads();
   } else {
     __syncthreads();
   }
