@@ -224,6 +224,8 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   m.rowmap = reinterpret_cast<int*>(ws + L.rowmap);
   m.src = reinterpret_cast<int*>(ws + L.src);
   m.pos = reinterpret_cast<int*>(ws + L.pos);
+  m.done = reinterpret_cast<int*>(ws + L.done);
+  m.n_done = d / 64;
   m.xq = ws + L.x;
   m.x_tile0 = int(L.routed_tiles);
   m.x_rows = x_rows;
@@ -269,8 +271,19 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   p.out_scale = L.half_o ? reinterpret_cast<float*>(ws + L.o_unit) : nullptr;
   p.ldo = d;
   p.vec = 1;
+  if (L.fused_combine) {
+    p.y = y;
+    p.gate = gate;
+    p.src = m.src;
+    p.done = m.done;
+    p.T = T;
+    p.K = K;
+    p.S = S;
+    p.y_bf16 = desc->dtype == MCFT_BF16;
+  }
   e = launch_mx4_gemm(p, kMx4Down, L.tiles, tile_rows, num_sms(), stream);
   if (e != cudaSuccess) return cuda_fail(e, "mx4 down product launch");
+  if (L.fused_combine) return MCFT_OK;
   e = launch_mx4_combine(m, desc->dtype, stream);
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "combine kernel launch");
 }

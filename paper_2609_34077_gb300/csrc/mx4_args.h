@@ -55,10 +55,20 @@ struct Mx4GemmArgs {
   uint8_t *h, *h_scales;        // up
   size_t h_code_stride, h_scale_stride;
   unsigned* err;
+  // down, narrow, few tokens: the last CTA to finish a column range adds up the outputs there (y not NULL)
+  void* y;
+  const float* gate;
+  const int* src;
+  int* done;  // [column ranges], zeroed by the plan
+  int T, K, S, y_bf16;
   // set by the launcher
   int tn, n_tiles, split, depth, stages, a_groups;
   const void* w[kMaxMx4Seg];
 };
+// Up to this many tokens the down product adds up the outputs itself: a launch less, and the last CTA's share of the
+// sums (T rows of 64 or 128 columns) stays short.
+constexpr int kMx4FusedCombineT = 16;
+
 // Whether a product of up to max_tiles token tiles with n_rows weight rows takes the wide tiles: once they fill the
 // SMs.
 bool mx4_wide(long long max_tiles, int n_rows);
@@ -69,7 +79,8 @@ struct Mx4MoeLayout {
   bool permuted;
   long long routed_tiles, x_tiles, tiles;  // most tiles of the routed experts; tiles of x itself; all tiles
   bool half_o;     // o as fp16 under a unit for each row's 128 columns (bf16 layers, wide tiles), else fp32
-  size_t hdr, tile, rowmap, src, pos, x, h, o, o_unit, total;
+  bool fused_combine;
+  size_t hdr, tile, rowmap, src, pos, done, x, h, o, o_unit, total;
   Mx4MoeLayout(const mcft_layer_desc* desc, int T);
 };
 
@@ -81,7 +92,8 @@ struct Mx4MoeArgs {
   uint32_t have[(kMaxMx4E + 31) / 32];  // experts with a block
   Mx4Header* hdr;
   Mx4Tile* tiles;
-  int *rowmap, *src, *pos;
+  int *rowmap, *src, *pos, *done;
+  int n_done;
   uint8_t* xq;
   int x_tile0;     // first tile of x itself, in the permuted form
   long long x_rows;  // rows of xq

@@ -55,7 +55,7 @@ constexpr int kSlots = 16;
 struct Ctl {
   uint64_t full[kMaxStages], empty[kMaxStages], tfull, tempty, drain;
   uint32_t tmem_base;
-  int abort;
+  int abort, last;
   Item item[kSlots];
 };
 constexpr int kCtlBytes = 1024;
@@ -158,6 +158,33 @@ __device__ __forceinline__ Item item_at(const Mx4GemmArgs& p, int i) {
     t.n0 = local / e.count * p.tn;
   }
   return t;
+}
+
+// y = sum_k gate o + the shared experts' o, columns [n0, n1) of every token, by 256 threads, in the order of k.
+__device__ __forceinline__ void combine_columns(const Mx4GemmArgs& p, int n0, int n1, int thread) {
+  const int quads = (n1 - n0) >> 2;
+  for (int i = thread; i < p.T * quads; i += 256) {
+    const int t = i / quads, c = n0 + (i - t * quads) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](long long row, float g) {
+      const uint4 v = ldcg16(static_cast<const float*>(p.out) + row * p.ldo + c);
+      acc.x = fmaf(g, __uint_as_float(v.x), acc.x);
+      acc.y = fmaf(g, __uint_as_float(v.y), acc.y);
+      acc.z = fmaf(g, __uint_as_float(v.z), acc.z);
+      acc.w = fmaf(g, __uint_as_float(v.w), acc.w);
+    };
+#pragma unroll 4
+    for (int k = 0; k < p.K; ++k) {
+      const int src = p.src[t * p.K + k];
+      if (src >= 0) add(src, p.gate[t * p.K + k]);
+    }
+    for (int s = 0; s < p.S; ++s) add((long long)p.T * p.K + s * p.T + t, 1.f);
+    if (p.y_bf16)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.y) + (long long)t * p.n_out + c) =
+          make_uint2(pack2bf(acc.x, acc.y), pack2bf(acc.z, acc.w));
+    else
+      *reinterpret_cast<float4*>(static_cast<float*>(p.y) + (long long)t * p.n_out + c) = acc;
+  }
 }
 
 template <int EPI, bool WIDE>
@@ -502,7 +529,8 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
     else if (warp >= 2) asm volatile("bar.sync 1, 256;" ::: "memory");
     int stopped = 0;
     if (lane < cs) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(stopped) : "r"(peer_addr(&ctl->abort, lane)) : "memory");
-    if (first < total && warp >= 2 && !__any_sync(0xffffffffu, stopped)) {
+    const bool run = first < total && warp >= 2 && !__any_sync(0xffffffffu, stopped);
+    if (run) {
       const Item t = ctl->item[0];
       const int ldp = p.tn + 4;
       uint32_t peer[8];
@@ -545,6 +573,23 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
           if (dst < 0 || n >= p.n_out) continue;
           if (EPI == kMx4Down || p.out_f32) static_cast<float*>(p.out)[dst * p.ldo + n] = x;
           else static_cast<uint16_t*>(p.out)[dst * p.ldo + n] = f2bf(x);
+        }
+      }
+    }
+    if (EPI == kMx4Down && p.y) {
+      if (total == 0 && !p.hdr->abort) {  // no expert at all: zeros
+        if (warp >= 2 && int(blockIdx.x) < p.n_tiles)
+          combine_columns(p, int(blockIdx.x) * p.tn, min(p.n_out, (int(blockIdx.x) + 1) * p.tn), int(threadIdx.x) - 64);
+      } else if (run) {
+        // this CTA's rows of o are visible to the device before it counts itself as done
+        __threadfence();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (threadIdx.x == 64)
+          ctl->last = atomicAdd(p.done + ctl->item[0].n0 / p.tn, 1) == p.hdr->tiles * cs - 1 ? 1 : 0;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (ctl->last) {
+          __threadfence();
+          combine_columns(p, ctl->item[0].n0, min(p.n_out, ctl->item[0].n0 + p.tn), int(threadIdx.x) - 64);
         }
       }
     }

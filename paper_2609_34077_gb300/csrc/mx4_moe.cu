@@ -74,6 +74,7 @@ __global__ void __launch_bounds__(kPlanThreads) mx4_plan_kernel(const __grid_con
   const int n = a.T * a.K;
   if (tid < kMaxMx4E) used[tid] = 0;
   if (tid == 0) bad = 0;
+  for (int i = tid; i < a.n_done; i += kPlanThreads) a.done[i] = 0;
   __syncthreads();
   for (int i = tid; i < n; i += kPlanThreads) {
     const int e = a.idx[i];
@@ -328,9 +329,11 @@ Mx4MoeLayout::Mx4MoeLayout(const mcft_layer_desc* desc, int T) {
   rowmap = place(sizeof(int) * size_t(tiles) * 128);
   src = place(sizeof(int) * size_t(n));
   pos = place(permuted ? sizeof(int) * size_t(n) : 0);
+  done = place(sizeof(int) * size_t(d / 64));
   x = place(Mx4Layout(x_rows, d).bytes());
   h = place(Mx4Layout(tiles * 128, w).bytes());
   const size_t o_rows = size_t(n) + size_t(S) * T;
+  fused_combine = T <= kMx4FusedCombineT && !mx4_wide(tiles, d);
   half_o = dtype == MCFT_BF16 && mx4_wide(tiles, d);
   o = place(sizeof(float) * o_rows * d);  // (also where fp16 takes half of it: fewer tokens may need fp32)
   o_unit = place(half_o ? sizeof(float) * o_rows * ((d + 127) / 128) : 0);
