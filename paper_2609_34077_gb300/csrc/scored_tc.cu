@@ -4,10 +4,13 @@
 //   dx       dx = dz W;
 //   dw       dW = dz^T x.
 // dz is an fp32 value and is multiplied as the sum of bf16 parts, each the rounding of what the ones before leave,
-// side by side in [T, kScoredParts, Ep]. Two parts keep 16 bits, ample for dx, which is rounded to 8; with two, dW's error
-// against 64 bits was more than 1.5 times that of fp32 multiply-adds, with three it is theirs.
+// side by side in [T, kScoredParts, Ep]. Two parts keep 16 bits, ample for dx, which is rounded to 8. dW takes three, the
+// two small ones in a pass over the tokens before the large one's: the tensor cores cut an accumulator's last bits at
+// every step, which costs little while it holds the small parts' sum (a third of the steps at full size).
 //
-// Forward: a tile is 128 tokens by all experts (one accumulator, N = E). There are few tiles, so a cluster of up to 8
+// Forward: a tile is 128 tokens by all experts (N = E), in two accumulators, or four of up to 128 experts, that take the
+// contraction's blocks in turn: the tensor cores cut an accumulator's last bits at every step, always towards zero, and
+// with one accumulator the logits of 4096-wide tokens came out 1.2e-6 short, which the gradient of large sigmoids shows. There are few tiles, so a cluster of up to 8
 // CTAs splits a tile's contraction, each CTA puts its partial logits into its shared memory, and each ranks its share
 // of the tokens from the sum of its peers' rows, in the order of the peers.
 // dx and dw read W, x and (dw) dz along their contiguous index, which is not the contraction's: their shared-memory
@@ -152,9 +155,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cs = p.split, rank = int(cluster_rank());
   if (threadIdx.x < kMaxScoredE) ctl->count[threadIdx.x] = 0;
-  setup(ctl, warp, p.stages, 256);
+  setup(ctl, warp, p.stages, 512);
   const uint32_t tmem = ctl->tmem_base;
   volatile int* abort = &ctl->abort;
+  // 512 columns of accumulators, which the 64-column blocks take in turn
+  const int accs = p.n <= 128 ? 4 : 2, acc_cols = 512 / accs;
   const int t0 = int(blockIdx.x) / cs * 128, nkb = p.a.d / kBox;
   const int k0 = nkb * rank / cs, k1 = nkb * (rank + 1) / cs;
   const uint32_t stage = uint32_t(kATile + p.n * 128);
@@ -185,7 +190,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
         const uint32_t st = base + uint32_t(r.s) * stage;
         const uint64_t da = sw128_desc(st), db = sw128_desc(st + kATile);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma(tmem, da + uint64_t(2 * k), db + uint64_t(2 * k), idesc, (kb > k0 || k > 0) ? 1u : 0u);
+        for (int k = 0; k < 4; ++k)
+          mma(tmem + uint32_t(((kb - k0) & (accs - 1)) * acc_cols), da + uint64_t(2 * k), db + uint64_t(2 * k), idesc,
+              (kb - k0 >= accs || k > 0) ? 1u : 0u);
         commit(&ctl->empty[r.s]);
         r.next(p.stages);
       }
@@ -202,11 +209,16 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
       // the ring is free: every copy has landed and every MMA has read it
       float* part = reinterpret_cast<float*>(ring) + row * (p.n + 4);
       for (int c = grp * 16; c < p.n; c += 32) {
-        uint32_t v[16];
-        tmem_ld16(tmem + (uint32_t(q * 32) << 16) + uint32_t(c), v);
-        tmem_ld_wait();
+        float sum[16] = {};
+        for (int a = 0; a < min(accs, k1 - k0); ++a) {
+          uint32_t v[16];
+          tmem_ld16(tmem + (uint32_t(q * 32) << 16) + uint32_t(a * acc_cols + c), v);
+          tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(part + c + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(part + c + 4 * j) = make_float4(sum[4 * j], sum[4 * j + 1], sum[4 * j + 2], sum[4 * j + 3]);
       }
       tc_fence_before();
     }
@@ -248,7 +260,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
   if (p.a.load)
     for (int e = threadIdx.x; e < p.a.E; e += kFwdThreads)
       if (ctl->count[e]) atomicAdd(p.a.load + e, ctl->count[e]);
-  release(warp, tmem, 256);
+  release(warp, tmem, 512);
 }
 
 // ---- dx = dz W ----
@@ -381,18 +393,22 @@ __global__ void __launch_bounds__(kThreads, 1) scored_dw_kernel(const __grid_con
   const int n0 = int(blockIdx.x) * 256, ta = int(blockIdx.y) * p.share, tb = min(p.T, ta + p.share);
   constexpr uint32_t kBoxBytes = kDwK * 128;
   const int boxes = p.ep / kBox, mt = p.ep / 128;
-  const uint32_t part = uint32_t(boxes) * kBoxBytes, off_x = kScoredParts * part, stage = off_x + 4 * kBoxBytes;
+  // a stage: 4 boxes of x, then up to two parts of dz
+  const uint32_t part = uint32_t(boxes) * kBoxBytes, off_dz = 4 * kBoxBytes, stage = off_dz + 2 * part;
+  const int steps = (tb - ta + kDwK - 1) / kDwK;
 
   if (warp == 0) {
     if (elect_one()) {
       Ring r;
-      for (int t = ta; t < tb; t += kDwK) {
+      for (int i = 0; i < 2 * steps; ++i) {
+        const int t = ta + (i < steps ? i : i - steps) * kDwK, q0 = i < steps ? 1 : 0, q1 = i < steps ? kScoredParts : 1;
         if (!mbar_wait_cl(&ctl->empty[r.s], r.ph ^ 1u, abort, p.err)) break;
         const uint32_t st = base + uint32_t(r.s) * stage, bar = smem_u32(&ctl->full[r.s]);
-        mbar_expect_tx(&ctl->full[r.s], stage);
-        for (int c = 0; c < kScoredParts * boxes; ++c) tma_load(st + c * kBoxBytes, &p.dz, c * kBox, t, bar);
+        mbar_expect_tx(&ctl->full[r.s], off_dz + uint32_t(q1 - q0) * part);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tma_load(st + off_x + c * kBoxBytes, &p.x, n0 + c * kBox, t, bar);
+        for (int c = 0; c < 4; ++c) tma_load(st + c * kBoxBytes, &p.x, n0 + c * kBox, t, bar);
+        for (int c = 0; c < (q1 - q0) * boxes; ++c)
+          tma_load(st + off_dz + c * kBoxBytes, &p.dz, (q0 * boxes + c) * kBox, t, bar);
         if (r.issued < p.stages) ++r.issued;
         r.next(p.stages);
       }
@@ -403,20 +419,19 @@ __global__ void __launch_bounds__(kThreads, 1) scored_dw_kernel(const __grid_con
       Ring r;
       bool ok = true;
       constexpr uint32_t idesc = kIdesc | kAMn | kBMn | (uint32_t(256 >> 3) << 17);
-      for (int t = ta; t < tb; t += kDwK) {
+      for (int i = 0; i < 2 * steps; ++i) {
+        const int parts = i < steps ? kScoredParts - 1 : 1;
         ok = mbar_wait_cl(&ctl->full[r.s], r.ph, abort, p.err);
         if (!ok) break;
         tc_fence_after();
         const uint32_t st = base + uint32_t(r.s) * stage;
-        const uint64_t db = mn_desc(st + off_x, kDwK);
+        const uint64_t db = mn_desc(st, kDwK);
         for (int m = 0; m < mt; ++m)
-#pragma unroll
-          for (int q = 0; q < kScoredParts; ++q) {
-            const uint64_t da = mn_desc(st + q * part + uint32_t(m) * 2 * kBoxBytes, kDwK);
+          for (int q = 0; q < parts; ++q) {
+            const uint64_t da = mn_desc(st + off_dz + uint32_t(q) * part + uint32_t(m) * 2 * kBoxBytes, kDwK);
 #pragma unroll
             for (int k = 0; k < kDwK / 16; ++k)
-              mma(tmem + uint32_t(m) * 256, da + uint64_t(128 * k), db + uint64_t(128 * k), idesc,
-                  (t > ta || q > 0 || k > 0) ? 1u : 0u);
+              mma(tmem + uint32_t(m) * 256, da + uint64_t(128 * k), db + uint64_t(128 * k), idesc, (i | q | k) ? 1u : 0u);
           }
         commit(&ctl->empty[r.s]);
         r.next(p.stages);
@@ -562,7 +577,7 @@ cudaError_t launch_scored_dw_tc(const ScoredGradArgs& a, const void* parts, floa
   p.d = a.d;
   p.E = a.E;
   p.share = scored_dw_share(a.T, a.d);
-  p.stages = std::min(kMaxStages, kDwRing / (kDwK * 128 * (kScoredParts * p.ep / kBox + 4)));
+  p.stages = std::min(kMaxStages, kDwRing / (kDwK * 128 * (2 * p.ep / kBox + 4)));
   static SmemOptIn smem;
   const cudaError_t e = smem.allow(reinterpret_cast<const void*>(scored_dw_kernel), kDwSmem);
   if (e != cudaSuccess) return e;
