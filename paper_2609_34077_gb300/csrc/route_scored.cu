@@ -44,7 +44,7 @@ template <typename T, int PL>
 __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
     route_scored_few_kernel(const __grid_constant__ ScoredArgs a) {
   extern __shared__ float xs[];  // [tokens][d]
-  __shared__ float zs[kFewTokens][32 * PL], buf[kFewTokens][64 * PL];
+  __shared__ __align__(16) float zs[kFewTokens][32 * PL], buf[kFewTokens][64 * PL];
   __shared__ int count[32 * PL];
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -87,7 +87,7 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
     float z[PL], bias[PL];
     load_bias(a, bias);
 #pragma unroll
-    for (int j = 0; j < PL; ++j) z[j] = lane + 32 * j < a.E ? zs[warp][lane + 32 * j] : 0.f;
+    for (int j = 0; j < PL; ++j) z[j] = expert_of<PL>(j) < a.E ? zs[warp][expert_of<PL>(j)] : 0.f;
     rank_scored_warp<PL>(a, z, bias, buf[warp], t0 + warp, a.load ? (alone ? count : a.load) : nullptr);
   }
   if (alone && a.load) {
@@ -96,7 +96,7 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
   }
 }
 
-// 16 tokens by up to 256 experts; 256 threads of 2 tokens x 8 experts (experts tx + 32 j).
+// 16 tokens by up to 256 experts; 256 threads of 2 tokens x 8 experts.
 constexpr int kTileT = 16, kTileK = 32;
 
 template <typename T>
@@ -135,8 +135,8 @@ __global__ void __launch_bounds__(256) route_scored_tile_kernel(const __grid_con
       const float x0 = xs[k][warp * 2], x1 = xs[k][warp * 2 + 1];
 #pragma unroll
       for (int j = 0; j < PL; ++j)
-        if (lane + 32 * j < a.E) {
-          const float v = ws[k * kRow + lane + 32 * j];
+        if (expert_of<PL>(j) < a.E) {
+          const float v = ws[k * kRow + expert_of<PL>(j)];
           acc[0][j] = fmaf(x0, v, acc[0][j]);
           acc[1][j] = fmaf(x1, v, acc[1][j]);
         }

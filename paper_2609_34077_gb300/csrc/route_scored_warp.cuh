@@ -26,36 +26,44 @@ __device__ __forceinline__ void softmax_stats(const float* z, int E, float& m, f
   sum = warp_sum(sum);
 }
 
+// A lane's PL experts: runs of VW = min(PL, 4) consecutive ones, 32 VW apart, so that a run is one vector access.
+template <int PL>
+__device__ __forceinline__ int expert_of(int j) {
+  constexpr int VW = PL < 4 ? PL : 4;
+  return (j / VW) * 32 * VW + int(threadIdx.x & 31) * VW + j % VW;
+}
+
 // The biases of a lane's experts (the same for every token).
 template <int PL>
 __device__ __forceinline__ void load_bias(const ScoredArgs& a, float (&b)[PL]) {
 #pragma unroll
   for (int j = 0; j < PL; ++j) {
-    const int e = int(threadIdx.x & 31) + 32 * j;
+    const int e = expert_of<PL>(j);
     b[j] = a.bias && e < a.E ? __ldg(a.bias + e) : 0.f;
   }
 }
 
-// z[j], bias[j]: logit and bias of expert lane + 32 j (PL of them, E <= 32 PL). buf: 2 * 32 * PL floats of shared
-// memory, this warp's alone. load: shared or global counters of the experts' choices, or NULL.
+// z[j], bias[j]: logit and bias of expert expert_of<PL>(j) (E <= 32 PL). buf: 2 * 32 * PL floats of shared memory, this
+// warp's alone, 16-byte aligned. load: shared or global counters of the experts' choices, or NULL.
 template <int PL>
 __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL], const float (&bias)[PL], float* buf, int t,
                                         int32_t* load) {
   constexpr int kNone = -2147483647 - 1;  // below every key: not there, or taken
   constexpr unsigned kAll = 0xffffffffu;
+  constexpr int VW = PL < 4 ? PL : 4;
   const int lane = threadIdx.x & 31, E = a.E;
-  float* ss = buf;             // scores, by expert
-  float* cs = buf + 32 * PL;   // choice values by expert; then the narrowed field
+  float* ss = buf;            // scores, by expert
+  float* cs = buf + 32 * PL;  // choice values by expert; then the narrowed field
   float s[PL], c[PL];
   if (a.score == MCFT_SCORE_SOFTMAX) {
     float m = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < PL; ++j) m = lane + 32 * j < E ? fmaxf(m, z[j]) : m;
+    for (int j = 0; j < PL; ++j) m = expert_of<PL>(j) < E ? fmaxf(m, z[j]) : m;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
 #pragma unroll
     for (int j = 0; j < PL; ++j) {
-      s[j] = lane + 32 * j < E ? expf(z[j] - m) : 0.f;
+      s[j] = expert_of<PL>(j) < E ? expf(z[j] - m) : 0.f;
       sum += s[j];
     }
     const float inv = 1.f / warp_sum(sum);
@@ -66,16 +74,27 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     for (int j = 0; j < PL; ++j) s[j] = __frcp_rn(1.f + expf(-z[j]));
   }
   bool nan = false;
+  const bool whole = E % VW == 0;  // (runs end with the experts, and rows of logits are aligned to them)
 #pragma unroll
-  for (int j = 0; j < PL; ++j) {
-    const int e = lane + 32 * j;
-    c[j] = -INFINITY;
-    if (e < E) {
-      if (a.logits) a.logits[size_t(t) * E + e] = z[j];
-      const float v = s[j] + bias[j];
-      nan |= v != v;
-      c[j] = v != v ? -INFINITY : v;
-      ss[e] = s[j];
+  for (int h = 0; h < PL; h += VW) {
+    const int e0 = expert_of<PL>(h);
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+      const float v = s[h + i] + bias[h + i];
+      const bool in = e0 + i < E;
+      nan |= in && v != v;
+      c[h + i] = !in || v != v ? -INFINITY : v;
+      ss[e0 + i] = s[h + i];
+    }
+    if (a.logits) {
+      float* row = a.logits + size_t(t) * E + e0;
+      if (VW == 4 && whole) {
+        if (e0 < E) *reinterpret_cast<float4*>(row) = make_float4(z[h], z[h + VW / 4], z[h + VW / 2], z[h + VW - 1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+          if (e0 + i < E) row[i] = z[h + i];
+      }
     }
   }
   if (nan) set_error(a.err, kErrInvalid);
@@ -85,8 +104,7 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
   if (a.n_group > 1) {
     const int gsz = E / a.n_group;
 #pragma unroll
-    for (int j = 0; j < PL; ++j)
-      if (lane + 32 * j < E) cs[lane + 32 * j] = c[j];
+    for (int j = 0; j < PL; ++j) cs[expert_of<PL>(j)] = c[j];
     __syncwarp();
     // the lanes share the groups: 2^shift lanes each, whose two best values meet by shuffles
     const int shift = 31 - __clz(32 / a.n_group), per = 1 << shift;
@@ -117,7 +135,7 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     const float inv = 1.f / float(gsz);
 #pragma unroll
     for (int j = 0; j < PL; ++j) {  // e / gsz: (e + 1/2) / gsz is 1/512 or more from the next whole number
-      const int e = lane + 32 * j;
+      const int e = expert_of<PL>(j);
       if (e < E && !((groups >> int((float(e) + 0.5f) * inv)) & 1u)) key[j] = kNone;
     }
   }
@@ -133,31 +151,33 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     const int l = __ffs(__ballot_sync(kAll, most == floor_key)) - 1;
     if (lane == l) most = kNone;
   }
-  int count = 0;
-  int2* field = reinterpret_cast<int2*>(cs);  // (32 entries fit where PL >= 2)
-  int sel = -1;
-  bool packed = PL > 1;
-  if constexpr (PL > 1) {
-    int base[PL];
+  // what reaches the floor, one to a lane in the order of the index (lanes' runs, then the next 32 lanes' runs)
+  int2* field = reinterpret_cast<int2*>(cs);
+  int at[PL], count = 0;
 #pragma unroll
-    for (int j = 0; j < PL; ++j) {
-      const bool in = key[j] >= floor_key && key[j] != kNone;
-      const unsigned b = __ballot_sync(kAll, in);
-      base[j] = in ? count + __popc(b & ((1u << lane) - 1u)) : 32;
-      count += __popc(b);
-    }
-    packed = count <= 32;  // (more only where many experts tie)
-    if (packed) {
+  for (int h = 0; h < PL; h += VW) {
+    int before = 0, total = 0;
 #pragma unroll
-      for (int j = 0; j < PL; ++j)
-        if (base[j] < 32) field[base[j]] = make_int2(key[j], lane + 32 * j);
-      __syncwarp();
+    for (int i = 0; i < VW; ++i) {
+      const unsigned b = __ballot_sync(kAll, key[h + i] >= floor_key && key[h + i] != kNone);
+      before += __popc(b & ((1u << lane) - 1u));
+      total += __popc(b);
     }
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+      const bool in = key[h + i] >= floor_key && key[h + i] != kNone;
+      at[h + i] = in ? count + before : 32;
+      before += in;
+    }
+    count += total;
   }
-  if (packed || PL == 1) {
-    // one expert a lane, in the order of their index
-    int2 mine = make_int2(key[0], lane);
-    if (PL > 1) mine = lane < count ? field[lane] : make_int2(kNone, 0);
+  int sel = -1;
+  if (count <= 32) {  // (more only where many experts tie)
+#pragma unroll
+    for (int j = 0; j < PL; ++j)
+      if (at[j] < 32) field[at[j]] = make_int2(key[j], expert_of<PL>(j));
+    __syncwarp();
+    int2 mine = lane < count ? field[lane] : make_int2(kNone, 0);
     for (int k = 0; k < a.K; ++k) {
       const int best = __reduce_max_sync(kAll, mine.x);
       if (best == kNone) break;  // no eligible expert is left
@@ -168,19 +188,19 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     }
   } else {
     for (int k = 0; k < a.K; ++k) {
-      int top = kNone, at = 0;
+      int top = kNone, first = 0;
 #pragma unroll
       for (int j = PL - 1; j >= 0; --j)
         if (key[j] >= top) {
           top = key[j];
-          at = lane + 32 * j;
+          first = expert_of<PL>(j);
         }
       const int best = __reduce_max_sync(kAll, top);
       if (best == kNone) break;
-      const int e = int(__reduce_min_sync(kAll, unsigned(top == best ? at : 0x7fffffff)));
+      const int e = int(__reduce_min_sync(kAll, unsigned(top == best ? first : 0x7fffffff)));
 #pragma unroll
       for (int j = 0; j < PL; ++j)
-        if (e == lane + 32 * j) key[j] = kNone;
+        if (e == expert_of<PL>(j)) key[j] = kNone;
       if (lane == k) sel = e;
     }
   }

@@ -76,10 +76,15 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* v) {
                "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-__device__ __forceinline__ float peer_float(uint32_t cluster_addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr));
-  return v;
+template <int N>
+__device__ __forceinline__ void peer_vector(uint32_t cluster_addr, uint32_t* v) {
+  static_assert(N == 2 || N == 4, "vector");
+  if constexpr (N == 4)
+    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                 : "r"(cluster_addr));
+  else
+    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(cluster_addr));
 }
 
 struct Ring {
@@ -140,18 +145,19 @@ struct ForwardArgs {
   ScoredArgs a;
   int n, split, stages;  // experts rounded up to 16; CTAs of a cluster
 };
-constexpr int kFwdRing = 3 * (kATile + 256 * 128);
-constexpr int kFwdRows = (kFwdThreads / 32) * 2 * kMaxScoredE * 4;  // the ranking's buffers
-constexpr int kFwdSmem = 1024 + kFwdRing + kFwdRows + kCtlBytes;
-static_assert(kFwdSmem <= 227 * 1024 && 128 * (kMaxScoredE + 4) * 4 <= kFwdRing, "shared memory");
+constexpr int kFwdPart = 128 * (kMaxScoredE + 4) * 4;               // partial logits, and after them
+constexpr int kFwdRows = (kFwdThreads / 32) * 2 * kMaxScoredE * 4;  // the ranking's buffers: both in the ring's place
+constexpr int kFwdRing = kFwdPart + kFwdRows;
+constexpr int kFwdSmem = 1024 + kFwdRing + kCtlBytes;
+static_assert(kFwdSmem <= 227 * 1024 && kFwdRing >= 4 * (kATile + 256 * 128), "shared memory");
 
 template <int PL>
 __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __grid_constant__ ForwardArgs p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* ring = smem_raw + (base - raw);
-  float* rows = reinterpret_cast<float*>(ring + kFwdRing);
-  Ctl* ctl = reinterpret_cast<Ctl*>(ring + kFwdRing + kFwdRows);
+  float* rows = reinterpret_cast<float*>(ring + kFwdPart);
+  Ctl* ctl = reinterpret_cast<Ctl*>(ring + kFwdRing);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cs = p.split, rank = int(cluster_rank());
   if (threadIdx.x < kMaxScoredE) ctl->count[threadIdx.x] = 0;
@@ -239,20 +245,28 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
       float z[PL];
 #pragma unroll
       for (int j = 0; j < PL; ++j) z[j] = 0.f;
+      constexpr int VW = PL < 4 ? PL : 4;
+      uint32_t v[4][PL];
 #pragma unroll
-      for (int r = 0; r < 8; r += 2)  // the loads of two peers in flight at once
-        if (r < cs) {
-          float v[2][PL];
+      for (int r0 = 0; r0 < 8; r0 += 4) {  // (four peers' rows in flight at once)
+        if (r0 >= cs) break;
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int j = 0; j < PL; ++j)
-              v[h][j] = r + h < cs && lane + 32 * j < p.a.E
-                            ? peer_float(peer[r + h] + uint32_t(row * (p.n + 4) + lane + 32 * j) * 4u)
-                            : 0.f;
+          for (int h = 0; h < PL; h += VW) {
+            const int e = expert_of<PL>(h);
+            if (r0 + r < cs && e < p.n) {
+              peer_vector<VW>(peer[r0 + r] + uint32_t(row * (p.n + 4) + e) * 4u, &v[r][h]);
+            } else {
 #pragma unroll
-          for (int j = 0; j < PL; ++j) z[j] = z[j] + v[0][j] + v[1][j];
-        }
+              for (int i = 0; i < VW; ++i) v[r][h + i] = 0;
+            }
+          }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < PL; ++j) z[j] += __uint_as_float(v[r][j]);
+      }
       rank_scored_warp<PL>(p.a, z, bias, rows + warp * 64 * PL, t0 + row, p.a.load ? ctl->count : nullptr);
     }
   }
