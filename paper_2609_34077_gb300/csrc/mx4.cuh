@@ -66,11 +66,19 @@ __device__ __forceinline__ uint32_t mx4_oct(const float* v, float inv) {
   return mx4_pair(v[0] * inv, v[1] * inv) | (mx4_pair(v[2] * inv, v[3] * inv) << 8) |
          (mx4_pair(v[4] * inv, v[5] * inv) << 16) | (mx4_pair(v[6] * inv, v[7] * inv) << 24);
 }
-// The value of a code (low 4 bits), before its scale.
-__device__ __forceinline__ float mx4_code_value(uint32_t c) {
-  const uint32_t m = c & 7u;  // values of m >= 2 are floats of exponent (m >> 1) - 1 and one mantissa bit
-  const uint32_t bits = m >= 2 ? ((126u + (m >> 1)) << 23) | ((m & 1u) << 22) : m ? 0x3f000000u : 0u;
-  return __uint_as_float(bits | ((c & 8u) << 28));
-}
+// The value of a code (low 4 bits) under a scale: its three bits read as a float's last exponent bits and first
+// mantissa bit are the value times 2^-126 (the code of 0.5 included: a subnormal), so one product does for the scales
+// up to 2 (byte 128), whose factor fits a float; larger ones take two.
+struct Mx4Decode {
+  float first, second;
+  __device__ __forceinline__ explicit Mx4Decode(uint32_t scale) {
+    first = __uint_as_float((scale <= 128 ? scale + 126u : 253u) << 23);
+    second = scale <= 128 ? 1.f : mx4_unit(scale);
+  }
+  __device__ __forceinline__ float operator()(uint32_t code, bool large) const {
+    const float v = __uint_as_float(((code & 8u) << 28) | ((code & 7u) << 22)) * first;
+    return large ? v * second : v;
+  }
+};
 
 }  // namespace mcft

@@ -140,7 +140,8 @@ __global__ void __launch_bounds__(32 * kWarps) mx4_dequantize_kernel(const __gri
   for (int j = 0; j < kChunks; ++j) {
     const long long c = (long long)(k0 + j) * 128 + (lane & 3) * 32;
     if (c >= a.C) break;
-    const float u = mx4_unit(scale[j]);
+    const Mx4Decode value(scale[j]);
+    const bool large = scale[j] > 128;
     const uint32_t word[4] = {code[j].x, code[j].y, code[j].z, code[j].w};
     if (ALIGN && c + 32 <= a.C) {
 #pragma unroll
@@ -151,9 +152,9 @@ __global__ void __launch_bounds__(32 * kWarps) mx4_dequantize_kernel(const __gri
         for (int k = 0; k < 8; ++k) {
           constexpr int kPer = kValues / 8;
           const int at = i + k * kPer;
-          const float lo = mx4_code_value(word[at >> 3] >> (4 * (at & 7))) * u;
+          const float lo = value(word[at >> 3] >> (4 * (at & 7)), large);
           if constexpr (sizeof(T) == 4) w[k] = __float_as_uint(lo);
-          else w[k] = pack2bf(lo, mx4_code_value(word[at >> 3] >> (4 * (at & 7) + 4)) * u);
+          else w[k] = pack2bf(lo, value(word[at >> 3] >> (4 * (at & 7) + 4), large));
         }
         if constexpr (ALIGN == 32) {
           store32(row + c + i, w);
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(32 * kWarps) mx4_dequantize_kernel(const __gri
 #pragma unroll
       for (int i = 0; i < 32; ++i)
         if (c + i < a.C) {
-          const float v = mx4_code_value(word[i >> 3] >> (4 * (i & 7))) * u;
+          const float v = value(word[i >> 3] >> (4 * (i & 7)), large);
           if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(row + c + i) = f2bf(v);
           else row[c + i] = v;
         }
