@@ -78,8 +78,9 @@ __device__ __forceinline__ float4 load4(const T* p) {
   }
 }
 
-// C[m, n] = sum_k A[m, k] B[k, n] in fp32: 64 x 64 tiles, 4 x 4 a thread, 16 of k at a time. A fp32 with strides
-// am, ak; B rows of n (a multiple of 64) contiguous values. blockIdx.z: a range of k, into its own plane.
+// C[m, n] = sum_k A[m, k] B[k, n] in fp32: tiles of 16 MT x 64, MT x 4 a thread (rows of 64 apart by 4), 16 of k at a
+// time, the next 16 on their way to registers meanwhile. A fp32 with strides am, ak, one of them 1; B rows of N (a
+// multiple of 64) contiguous values. blockIdx.z: a range of k, into its own plane.
 struct MultiplyArgs {
   const float* a;
   const void* b;
@@ -87,46 +88,75 @@ struct MultiplyArgs {
   long long am, ak;
   int M, N, K, k_share;
 };
-template <typename TB, typename TC>
+template <typename TB, typename TC, int MT>
 __global__ void __launch_bounds__(256) multiply_kernel(const __grid_constant__ MultiplyArgs p) {
-  __shared__ float as[16][64 + 4], bs[16][64];
+  constexpr int BM = 16 * MT;
+  __shared__ __align__(16) float as[2][16][BM + 4], bs[2][16][64];
   pdl_wait();
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int m0 = int(blockIdx.y) * 64, n0 = int(blockIdx.x) * 64;
+  const int m0 = int(blockIdx.x) * BM, n0 = int(blockIdx.y) * 64;
   const int k0 = int(blockIdx.z) * p.k_share, k1 = min(p.K, k0 + p.k_share);
   const TB* b = static_cast<const TB*>(p.b);
-  float acc[4][4] = {};
-  for (int kb = k0; kb < k1; kb += 16) {
-    __syncthreads();
-    for (int i = tid; i < 1024; i += 256) {
+  float acc[MT][4] = {};
+  float ra[MT];
+  float4 rb;
+  auto fetch = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
       // the index that is contiguous in A goes with the thread
-      const int m = p.am == 1 ? i & 63 : i >> 4, k = p.am == 1 ? i >> 6 : i & 15;
-      as[k][m] = m0 + m < p.M && kb + k < k1 ? p.a[(m0 + m) * p.am + (kb + k) * p.ak] : 0.f;
+      const int q = tid + 256 * i, m = p.am == 1 ? q % BM : q >> 4, k = p.am == 1 ? q / BM : q & 15;
+      ra[i] = m0 + m < p.M && kb + k < k1 ? p.a[(m0 + m) * p.am + (kb + k) * p.ak] : 0.f;
     }
-    const int k = tid >> 4, n = (tid & 15) * 4;
-    *reinterpret_cast<float4*>(&bs[k][n]) =
-        kb + k < k1 ? load4(b + (long long)(kb + k) * p.N + n0 + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const int k = tid >> 4;
+    rb = kb + k < k1 ? load4(b + (long long)(kb + k) * p.N + n0 + (tid & 15) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  fetch(k0);
+  int buf = 0;
+  for (int kb = k0; kb < k1; kb += 16, buf ^= 1) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int q = tid + 256 * i, m = p.am == 1 ? q % BM : q >> 4, k = p.am == 1 ? q / BM : q & 15;
+      as[buf][k][m] = ra[i];
+    }
+    *reinterpret_cast<float4*>(&bs[buf][tid >> 4][(tid & 15) * 4]) = rb;
     __syncthreads();
+    if (kb + 16 < k1) fetch(kb + 16);
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-      const float4 x = *reinterpret_cast<const float4*>(&as[q][ty * 4]), y = *reinterpret_cast<const float4*>(&bs[q][tx * 4]);
-      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+      const float4 y = *reinterpret_cast<const float4*>(&bs[buf][q][tx * 4]);
+      const float ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int h = 0; h < MT; h += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(&as[buf][q][h * 16 + ty * 4]);
+        const float xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[i], ys[j], acc[i][j]);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[h + i][j] = fmaf(xs[i], ys[j], acc[h + i][j]);
+      }
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + ty * 4 + i;
-    if (m >= p.M) break;
+  for (int i = 0; i < MT; ++i) {
+    const int m = m0 + (i >> 2) * 64 + ty * 4 + (i & 3);
+    if (m >= p.M) continue;
     TC* c = static_cast<TC*>(p.c) + ((long long)blockIdx.z * p.M + m) * p.N + n0 + tx * 4;
     if constexpr (sizeof(TC) == 2)
       *reinterpret_cast<uint2*>(c) = make_uint2(pack2bf(acc[i][0], acc[i][1]), pack2bf(acc[i][2], acc[i][3]));
     else
       *reinterpret_cast<float4*>(c) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
   }
+}
+
+// 128 rows a tile where such tiles fill the SMs.
+template <typename TB, typename TC>
+cudaError_t launch_multiply(const MultiplyArgs& p, int planes, cudaStream_t s) {
+  const long long wide = (p.M + 127LL) / 128 * (p.N / 64) * planes;
+  if (wide >= num_sms())
+    return launch_pdl(multiply_kernel<TB, TC, 8>, dim3(unsigned((p.M + 127) / 128), unsigned(p.N / 64), unsigned(planes)),
+                      dim3(256), 0, s, p);
+  return launch_pdl(multiply_kernel<TB, TC, 4>, dim3(unsigned((p.M + 63) / 64), unsigned(p.N / 64), unsigned(planes)),
+                    dim3(256), 0, s, p);
 }
 
 // dw (+)= the sum of the planes, in order.
@@ -180,9 +210,7 @@ cudaError_t launch_route_scored_grad(const ScoredGradArgs& a, int dtype, cudaStr
       e = launch_scored_dx_tc(a, dz, s);
     } else {
       const MultiplyArgs p{static_cast<const float*>(dz), a.w_router, a.dx, a.E, 1, a.T, a.d, a.E, a.E};
-      const dim3 grid(unsigned(a.d / 64), unsigned((a.T + 63) / 64));
-      e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, __nv_bfloat16>, grid, dim3(256), 0, s, p)
-             : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+      e = bf ? launch_multiply<__nv_bfloat16, __nv_bfloat16>(p, 1, s) : launch_multiply<float, float>(p, 1, s);
     }
   }
   if (e == cudaSuccess && a.dw) {
@@ -194,9 +222,8 @@ cudaError_t launch_route_scored_grad(const ScoredGradArgs& a, int dtype, cudaStr
       const int most = most_planes(a.T, a.d, a.E);
       share = ((a.T + most - 1) / most + 15) / 16 * 16;
       const MultiplyArgs p{static_cast<const float*>(dz), a.x, planes, 1, a.E, a.E, a.d, a.T, share};
-      const dim3 grid(unsigned(a.d / 64), unsigned((a.E + 63) / 64), unsigned((a.T + share - 1) / share));
-      e = bf ? launch_pdl(multiply_kernel<__nv_bfloat16, float>, grid, dim3(256), 0, s, p)
-             : launch_pdl(multiply_kernel<float, float>, grid, dim3(256), 0, s, p);
+      const int planes = (a.T + share - 1) / share;
+      e = bf ? launch_multiply<__nv_bfloat16, float>(p, planes, s) : launch_multiply<float, float>(p, planes, s);
     }
     const long long n = (long long)a.E * a.d;
     if (e == cudaSuccess)

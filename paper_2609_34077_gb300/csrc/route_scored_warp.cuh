@@ -43,6 +43,52 @@ __device__ __forceinline__ void load_bias(const ScoredArgs& a, float (&b)[PL]) {
   }
 }
 
+template <int N>
+__device__ __forceinline__ void peer_vector(uint32_t cluster_addr, uint32_t* v) {
+  static_assert(N == 2 || N == 4, "vector");
+  if constexpr (N == 4)
+    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                 : "r"(cluster_addr));
+  else
+    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(cluster_addr));
+}
+
+// Where the CTAs of a cluster have this CTA's shared variable at p.
+__device__ __forceinline__ void peer_addresses(const void* p, int cs, uint32_t (&peer)[8]) {
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(peer[r])
+                 : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(r < cs ? r : 0));
+}
+// Adds the rows of n partial logits at byte `offset` of the first cs peers, in their order; four in flight at once.
+template <int PL>
+__device__ __forceinline__ void add_peer_logits(const uint32_t (&peer)[8], uint32_t offset, int cs, int n, float (&z)[PL]) {
+  constexpr int VW = PL < 4 ? PL : 4;
+#pragma unroll
+  for (int r0 = 0; r0 < 8; r0 += 4) {
+    if (r0 >= cs) break;
+    uint32_t v[4][PL];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int h = 0; h < PL; h += VW) {
+        const int e = expert_of<PL>(h);
+        if (r0 + r < cs && e < n) {
+          peer_vector<VW>(peer[r0 + r] + offset + uint32_t(e) * 4u, &v[r][h]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < VW; ++i) v[r][h + i] = 0;
+        }
+      }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < PL; ++j) z[j] += __uint_as_float(v[r][j]);
+  }
+}
+
 // z[j], bias[j]: logit and bias of expert expert_of<PL>(j) (E <= 32 PL). buf: 2 * 32 * PL floats of shared memory, this
 // warp's alone, 16-byte aligned. load: shared or global counters of the experts' choices, or NULL.
 template <int PL>

@@ -76,17 +76,6 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* v) {
                "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-template <int N>
-__device__ __forceinline__ void peer_vector(uint32_t cluster_addr, uint32_t* v) {
-  static_assert(N == 2 || N == 4, "vector");
-  if constexpr (N == 4)
-    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                 : "r"(cluster_addr));
-  else
-    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(cluster_addr));
-}
-
 struct Ring {
   int s = 0, issued = 0;
   uint32_t ph = 0;
@@ -237,36 +226,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
   const bool run = !__any_sync(0xffffffffu, stopped);
   if (run) {
     uint32_t peer[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) peer[r] = peer_addr(ring, r < cs ? r : 0);
+    peer_addresses(ring, cs, peer);
     const int mine = 128 / cs;  // tokens rank * mine + ...
     for (int i = warp; i < mine && t0 + rank * mine + i < p.a.T; i += kFwdThreads / 32) {
       const int row = rank * mine + i;
       float z[PL];
 #pragma unroll
       for (int j = 0; j < PL; ++j) z[j] = 0.f;
-      constexpr int VW = PL < 4 ? PL : 4;
-      uint32_t v[4][PL];
-#pragma unroll
-      for (int r0 = 0; r0 < 8; r0 += 4) {  // (four peers' rows in flight at once)
-        if (r0 >= cs) break;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int h = 0; h < PL; h += VW) {
-            const int e = expert_of<PL>(h);
-            if (r0 + r < cs && e < p.n) {
-              peer_vector<VW>(peer[r0 + r] + uint32_t(row * (p.n + 4) + e) * 4u, &v[r][h]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < VW; ++i) v[r][h + i] = 0;
-            }
-          }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int j = 0; j < PL; ++j) z[j] += __uint_as_float(v[r][j]);
-      }
+      add_peer_logits<PL>(peer, uint32_t(row * (p.n + 4)) * 4u, cs, p.n, z);
       rank_scored_warp<PL>(p.a, z, bias, rows + warp * 64 * PL, t0 + row, p.a.load ? ctl->count : nullptr);
     }
   }
