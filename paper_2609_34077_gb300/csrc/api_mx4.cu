@@ -1,29 +1,13 @@
 // C ABI of the mx4 operators (include/mcft.h): argument checks, the expert block's and the workspace's layout,
 // launches.
 #include <limits.h>
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
+#include "api_check.h"
 #include "mx4_args.h"
 
 namespace mcft {
 namespace {
-
-mcft_status fail(mcft_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-mcft_status fail(mcft_status st, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  return set_error_message(st, buf);
-}
-mcft_status cuda_fail(cudaError_t e, const char* where) {
-  return fail(e == cudaErrorMemoryAllocation ? MCFT_ERR_OOM : MCFT_ERR_CUDA, "%s: %s", where, cudaGetErrorString(e));
-}
-
-bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 mcft_status check_matrix(const void* q, long long rows, long long cols, int dtype, const void* x, long long ld) {
   if (rows < 0 || cols < 1) return fail(MCFT_ERR_INVALID, "bad rows = %lld or cols = %lld", rows, cols);

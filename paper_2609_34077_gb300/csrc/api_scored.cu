@@ -1,28 +1,12 @@
 // C ABI of the scored routing and its gradient (include/mcft.h): argument checks and launches.
 #include <limits.h>
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
 
+#include "api_check.h"
 #include "route_scored.h"
 
 namespace mcft {
 namespace {
-
-mcft_status fail(mcft_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-mcft_status fail(mcft_status st, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  return set_error_message(st, buf);
-}
-mcft_status cuda_fail(cudaError_t e, const char* where) {
-  return fail(e == cudaErrorMemoryAllocation ? MCFT_ERR_OOM : MCFT_ERR_CUDA, "%s: %s", where, cudaGetErrorString(e));
-}
-
-bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 mcft_status check(const mcft_scored_desc* d, int T) {
   if (!d) return fail(MCFT_ERR_INVALID, "desc is NULL");

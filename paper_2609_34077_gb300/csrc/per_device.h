@@ -47,11 +47,20 @@ struct SmemOptIn {
 };
 
 // Clusters of a kernel that fit the device at once (0: none, or the query failed), found once per device.
+// size: CTAs of a cluster, where the launch sets it (one object for each size).
 struct ResidentClusters {
   PerDeviceInt clusters;
-  int get(const void* kernel, int grid, int block, size_t smem) {
+  int get(const void* kernel, int grid, int block, size_t smem, int size = 0) {
     return clusters.get([&] {
       cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute attr[1];
+      if (size > 0) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = unsigned(size);
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+      }
       cfg.gridDim = dim3(unsigned(grid));
       cfg.blockDim = dim3(unsigned(block));
       cfg.dynamicSmemBytes = smem;

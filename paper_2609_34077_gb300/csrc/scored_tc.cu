@@ -486,20 +486,12 @@ cudaError_t launch_forward(ForwardArgs& p, cudaStream_t s) {
   cfg.attrs = attr;
   // The contraction in as many shares as leave all clusters resident at once (clusters of 8 fit 15 times, not 19: the
   // GPU's processor groups are not multiples of 8), each of two 64-column blocks or more.
-  static PerDeviceInt resident[4];
+  static ResidentClusters resident[4];
   int log = 3;
   for (; log > 0; --log) {
     const int size = 1 << log;
     if (p.a.d / kBox < 2 * size || tiles * size > num_sms()) continue;
-    const int most = resident[log].get([&] {
-      attr[0].val.clusterDim.x = unsigned(size);
-      cfg.gridDim = dim3(unsigned(num_sms() / size * size));
-      cfg.numAttrs = 1;
-      int n = 0;
-      if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) (void)cudaGetLastError();
-      return n;
-    });
-    if (tiles <= most) break;
+    if (tiles <= resident[log].get(fn, num_sms() / size * size, kFwdThreads, kFwdSmem, size)) break;
   }
   p.split = 1 << log;
   attr[0].val.clusterDim.x = unsigned(p.split);
