@@ -30,6 +30,7 @@
 #include <algorithm>
 
 #include "mx4_args.h"
+#include "row_store.cuh"
 #include "tc_ptx.cuh"
 
 namespace mcft {
@@ -114,13 +115,6 @@ __device__ __forceinline__ float peer_float(uint32_t cluster_addr) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr));
   return v;
 }
-// 32 bytes to global memory in one instruction (a whole sector a lane).
-__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
-
 __device__ __forceinline__ float swiglu(float g, float u) {
   return (silu_regular(g) ? silu_branchless(g) : silu(g)) * u;
 }
@@ -442,56 +436,52 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
           p.h_scales[size_t(f >> 7) * p.h_scale_stride + mx4_scale_at(r) + ((f >> 5) & 3)] = uint8_t(sc);
         }
       } else {
-        long long dst = (long long)t.h_tile * 128 + row;
-        if (EPI == kMx4Down) dst = row < t.rows ? p.rowmap[dst] : -1;
+        long long dst = -1;
+        if (row < t.rows) {
+          dst = (long long)t.h_tile * 128 + row;
+          if (EPI == kMx4Down) dst = p.rowmap[dst];
+        }
         const int cols = min(128, p.n_out - n);
-        if (dst < 0 || row >= t.rows || cols <= 0) {
-        } else if (EPI == kMx4Down && p.out_scale) {
-          uint32_t m = 0;  // largest finite magnitude (past n_out: leftovers of other rows; the store leaves them out)
-#pragma unroll
-          for (int c = 0; c < 128; ++c) {
-            const uint32_t b = v[c] & 0x7fffffffu;
-            m = max(m, c < cols && b < 0x7f800000u ? b : 0u);
-          }
-          const int e = max(int(m >> 23), 15);  // (values below 2^-112 in units of 2^-126)
-          const float unit = __uint_as_float(uint32_t(e - 14) << 23), inv = __uint_as_float(uint32_t(268 - e) << 23);
-          __half* y = static_cast<__half*>(p.out) + dst * p.ldo + n;
-          p.out_scale[dst * ((p.n_out + 127) >> 7) + (n >> 7)] = unit;
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {  // (n_out is a multiple of 64)
-            uint32_t w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const __half2 h = __floats2half2_rn(__uint_as_float(v[c * 16 + 2 * j]) * inv, __uint_as_float(v[c * 16 + 2 * j + 1]) * inv);
-              w[j] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            if (c * 16 < cols) store32(y + c * 16, w);
-          }
-        } else if (EPI == kMx4Down || p.out_f32) {
+        const bool f32 = EPI == kMx4Down ? !p.out_scale : p.out_f32;
+        if (cols <= 0) {
+        } else if (f32) {
           float* y = static_cast<float*>(p.out) + dst * p.ldo + n;
           if (cols == 128 && p.vec) {
 #pragma unroll
-            for (int c = 0; c < 16; ++c) store32(y + c * 8, v + c * 8);
-          } else {
+            for (int c = 0; c < 128; c += 16) store_rows64(dst < 0 ? nullptr : y + c, v + c);
+          } else if (dst >= 0) {
 #pragma unroll
             for (int c = 0; c < 128; ++c)
               if (c < cols) y[c] = __uint_as_float(v[c]);
           }
         } else {
-          uint16_t* y = static_cast<uint16_t*>(p.out) + dst * p.ldo + n;
-          if (cols == 128 && p.vec) {
+          if (EPI == kMx4Down) {
+            uint32_t m = 0;  // largest finite magnitude (past n_out: leftovers of other rows; the store leaves them out)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              uint32_t w[8];
+            for (int c = 0; c < 128; ++c) {
+              const uint32_t b = v[c] & 0x7fffffffu;
+              m = max(m, c < cols && b < 0x7f800000u ? b : 0u);
+            }
+            const int e = max(int(m >> 23), 15);  // (values below 2^-112 in units of 2^-126)
+            const float inv = __uint_as_float(uint32_t(268 - e) << 23);
+            if (dst >= 0) p.out_scale[dst * ((p.n_out + 127) >> 7) + (n >> 7)] = __uint_as_float(uint32_t(e - 14) << 23);
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                w[j] = pack2bf(__uint_as_float(v[c * 16 + 2 * j]), __uint_as_float(v[c * 16 + 2 * j + 1]));
-              store32(y + c * 16, w);
+            for (int c = 0; c < 64; ++c) {
+              const __half2 h = __floats2half2_rn(__uint_as_float(v[2 * c]) * inv, __uint_as_float(v[2 * c + 1]) * inv);
+              v[c] = *reinterpret_cast<const uint32_t*>(&h);
             }
           } else {
 #pragma unroll
+            for (int c = 0; c < 64; ++c) v[c] = pack2bf(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+          }
+          uint16_t* y = static_cast<uint16_t*>(p.out) + dst * p.ldo + n;
+          if (cols == 128 && p.vec) {
+#pragma unroll
+            for (int c = 0; c < 64; c += 16) store_rows64(dst < 0 ? nullptr : y + 2 * c, v + c);
+          } else if (dst >= 0) {
+#pragma unroll
             for (int c = 0; c < 128; ++c)
-              if (c < cols) y[c] = f2bf(__uint_as_float(v[c]));
+              if (c < cols) y[c] = uint16_t(v[c >> 1] >> (16 * (c & 1)));
           }
         }
       }

@@ -18,6 +18,7 @@
 #include <algorithm>
 
 #include "route_scored_warp.cuh"
+#include "row_store.cuh"
 #include "scored_tc.h"
 #include "tc_ptx.cuh"
 
@@ -70,11 +71,6 @@ __device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t rows) {
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   tmem_ld16(taddr, r);
   tmem_ld16(taddr + 16, r + 16);
-}
-__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
 }
 struct Ring {
   int s = 0, issued = 0;
@@ -335,11 +331,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_dx_kernel(const __grid_con
         tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 16; ++j) w[j] = pack2bf(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-        if (row < p.T && n + c * 32 < p.d) {  // (d is a multiple of 64)
-          uint16_t* y = static_cast<uint16_t*>(p.dx) + size_t(row) * p.d + n + c * 32;
-          store32(y, w);
-          store32(y + 16, w + 8);
-        }
+        if (n + c * 32 < p.d)  // (d is a multiple of 64)
+          store_rows64(row < p.T ? static_cast<uint16_t*>(p.dx) + size_t(row) * p.d + n + c * 32 : nullptr, w);
       }
       tc_fence_before();
       __syncwarp();
@@ -436,10 +429,10 @@ __global__ void __launch_bounds__(kThreads, 1) scored_dw_kernel(const __grid_con
           tmem_ld32(taddr + c * 32, v);
           tmem_ld_wait();
           const int n = n0 + grp * 128 + c * 32;
-          if (e < p.E && n < p.d) {
+          if (n < p.d) {
             float* y = p.planes + (size_t(blockIdx.y) * p.E + e) * p.d + n;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) store32(y + 8 * j, v + 8 * j);
+            store_rows64(e < p.E ? y : nullptr, v);
+            store_rows64(e < p.E ? y + 16 : nullptr, v + 16);
           }
         }
       }
