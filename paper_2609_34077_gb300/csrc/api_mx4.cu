@@ -118,10 +118,12 @@ mcft_status mcft_mx4_matmul(const void* a, const void* b, int M, int N, int K, i
   p.ksteps = (K + 63) / 64;
   p.M = M;
   p.m_tiles = int(m_tiles);
+  p.pairs = m_tiles > 1;
   p.out = y;
   p.ldo = ldy;
   p.out_f32 = dtype == MCFT_F32;
-  p.vec = aligned(y, 32) && (size_t(ldy) * (p.out_f32 ? 4 : 2)) % 32 == 0;
+  const size_t elem = p.out_f32 ? 4 : 2;
+  p.vec = aligned(y, 32) && (size_t(ldy) * elem) % 32 == 0 && (size_t(N) * elem) % 64 == 0;
   p.err = device_error_word();
   const cudaError_t e = launch_mx4_gemm(p, kMx4Out, m_tiles, M < 128 ? M : 128, num_sms(), stream);
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "mx4 product launch");
@@ -223,6 +225,10 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   const Mx4Layout lx(x_rows, d), lh(L.tiles * 128, w);
   const ExpertBlock B(desc);
   const int tile_rows = T < 128 ? T : 128;
+  // pairs of token tiles waste half a pair for each expert with an odd number of them: from four tiles an expert on average
+  // (d = 2048, w = 1408, E = 64, K = 6: 4096 tokens, three tiles, 196 us by single tiles and 202 by pairs; 16384 tokens 654
+  // and 644; d = 4096, w = 14336, E = 8, K = 2: 4096 tokens 530 and 487)
+  p.pairs = L.permuted && (long long)T * K >= 512LL * E;
   p.hdr = m.hdr;
   p.tiles = m.tiles;
   p.rowmap = m.rowmap;
@@ -254,7 +260,6 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   p.out = ws + L.o;
   p.out_scale = L.half_o ? reinterpret_cast<float*>(ws + L.o_unit) : nullptr;
   p.ldo = d;
-  p.vec = 1;
   if (L.fused_combine) {
     p.y = y;
     p.gate = gate;

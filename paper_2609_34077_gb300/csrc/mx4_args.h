@@ -27,14 +27,17 @@ struct Mx4Tile {
   int seg;
   int a_tile;        // tile of the quantised input that holds its rows
   int first, count;  // the segment's tiles
-  int rows, pad[3];
+  int rows;
+  int pair0;      // the segment's first pair of tiles (its last may be half a pair)
+  int pair_tile;  // entry j: the first tile of pair j
+  int pad;
 };
 struct Mx4Header {
   int abort;  // set when a kernel of the call found bad data; later kernels skip their work
-  int tiles;
+  int tiles, pairs;
 };
 
-enum { kMx4Up, kMx4Down, kMx4Out };
+enum { kMx4Up, kMx4Down, kMx4Out, kMx4OutAny };  // (the last: `out` of any width and stride, in wide tiles)
 
 struct Mx4GemmArgs {
   const uint8_t *a, *a_scales;  // token rows, as an mx4 matrix
@@ -48,9 +51,10 @@ struct Mx4GemmArgs {
   const Mx4Tile* tiles;
   const int* rowmap;            // down: row of o for each row of each tile, -1: none
   int M, m_tiles;               // out
+  int pairs;                    // wide tiles may go by CTA pairs: the segments have tiles enough
   void* out;                    // down, out
   long long ldo;
-  int out_f32, vec;             // vec: 32-byte stores fit
+  int out_f32, vec;             // vec: rows of y are whole 64-byte pieces on 32-byte boundaries
   float* out_scale;             // down: units of an fp16 o, [rows of o][ceil(n_out / 128)]; NULL: o is fp32
   uint8_t *h, *h_scales;        // up
   size_t h_code_stride, h_scale_stride;
@@ -69,16 +73,16 @@ struct Mx4GemmArgs {
 // sums (T rows of 64 or 128 columns) stays short.
 constexpr int kMx4FusedCombineT = 16;
 
-// Whether a product of up to max_tiles token tiles with n_rows weight rows takes the wide tiles: once they fill the
-// SMs.
-bool mx4_wide(long long max_tiles, int n_rows);
+// Most items of a product by wide tiles; whether it takes them. tile_rows: most token rows of a tile.
+long long mx4_wide_items(long long max_tiles, int n_rows);
+bool mx4_wide(long long max_tiles, int n_rows, int tile_rows);
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s);
 
 // Workspace of one layer forward.
 struct Mx4MoeLayout {
   bool permuted;
   long long routed_tiles, x_tiles, tiles;  // most tiles of the routed experts; tiles of x itself; all tiles
-  bool half_o;     // o as fp16 under a unit for each row's 128 columns (bf16 layers, wide tiles), else fp32
+  bool half_o;     // o as fp16 under a unit for each row's 128 columns (bf16 layers whose wide tiles fill the SMs), else fp32
   bool fused_combine;
   size_t hdr, tile, rowmap, src, pos, done, x, h, o, o_unit, total;
   Mx4MoeLayout(const mcft_layer_desc* desc, int T);

@@ -19,7 +19,7 @@
 // tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results).
 //
 // For bf16 layers wide tiles write o as fp16 under a power-of-two unit for each row's 128 columns (the largest of them in [2^14, 2^15)
-// units): its 11 bits cost y an error of 2^-12, an eighth of its own rounding to bf16, and o is moved twice (here and
+// units): its 11 bits cost y an error of 2^-11, an eighth of its own rounding to bf16, and o is moved twice (here and
 // by the combine), which in fp32 took most of both kernels' time.
 //
 // Warp 0 issues the copies, warp 1 the tcgen05.cp and MMAs and owns the tensor memory, warps 2-9 are the
@@ -28,6 +28,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mx4_args.h"
 #include "row_store.cuh"
@@ -36,15 +37,17 @@
 namespace mcft {
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int threads(int build) { return build == 2 ? 352 : 320; }
 constexpr int kMaxStages = 16;
 constexpr int kWideN = 256, kNarrowN = 128;
 constexpr int kWideRing = 220 * 1024, kNarrowRing = 104 * 1024;
 constexpr int kWideDepth = 2;                                                       // chunks of a stage
-constexpr int kWideStages = kWideRing / (kWideDepth * (8192 + kWideN * 64 + 512 + 1024));
+enum { kNarrow, kWide, kPair };  // the builds
+constexpr int wide_stages(bool pair) { return kWideRing / (kWideDepth * (8192 + kWideN * (pair ? 32 : 64) + 512 + 1024)); }
 constexpr int kSfCols = 16;  // tensor memory columns of a chunk's scales: 4 of A, up to 8 of B
 // Instruction descriptor without N and the scale bytes' places: A and B e2m1, scales ue8m0, M = 128.
 constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (1u << 23) | (uint32_t(128 >> 4) << 24);
+constexpr uint32_t kIdescPair = (1u << 7) | (1u << 10) | (1u << 23) | (uint32_t(256 >> 4) << 24);
 
 struct Item {
   int seg, a_tile, h_tile, rows, n0;  // weights; token tile of A; of the output; its rows; first weight row
@@ -62,11 +65,8 @@ struct Ctl {
 constexpr int kCtlBytes = 1024;
 static_assert(sizeof(Ctl) <= kCtlBytes, "control block");
 
-template <bool WIDE>
-constexpr int smem_bytes() {
-  return (WIDE ? kWideRing : kNarrowRing) + 1024 + kCtlBytes;
-}
-static_assert(smem_bytes<true>() <= 227 * 1024 && 2 * (smem_bytes<false>() + 1024) <= 228 * 1024, "shared memory");
+constexpr int smem_bytes(int build) { return (build ? kWideRing : kNarrowRing) + 1024 + kCtlBytes; }
+static_assert(smem_bytes(kWide) <= 227 * 1024 && 2 * (smem_bytes(kNarrow) + 1024) <= 228 * 1024, "shared memory");
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile(
@@ -79,25 +79,49 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 // of 16 bytes, no swizzle, 128 bytes between 8-row groups.
 constexpr uint32_t kOperandHi = (512u >> 4) | (1u << 14) | (4u << 29), kScaleHi = (128u >> 4) | (1u << 14);
 __device__ __forceinline__ uint32_t desc_lo(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+// (PAIR: in both CTAs, each from its own shared memory)
+template <bool PAIR>
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t lo) {
-  asm volatile("{\n .reg .b64 d;\n mov.b64 d, {%1, %2};\n tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n}" ::"r"(taddr),
-               "r"(lo), "r"(kScaleHi)
-               : "memory");
+  if constexpr (PAIR)
+    asm volatile("{\n .reg .b64 d;\n mov.b64 d, {%1, %2};\n tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n}" ::"r"(taddr),
+                 "r"(lo), "r"(kScaleHi)
+                 : "memory");
+  else
+    asm volatile("{\n .reg .b64 d;\n mov.b64 d, {%1, %2};\n tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n}" ::"r"(taddr),
+                 "r"(lo), "r"(kScaleHi)
+                 : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void mma_mx4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
                                         uint32_t acc) {
-  asm volatile(
-      "{\n .reg .pred p;\n .reg .b64 x, y;\n mov.b64 x, {%1, %7};\n mov.b64 y, {%2, %7};\n setp.ne.b32 p, %6, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, %3, [%4], [%5], p;\n}" ::"r"(d),
-      "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(kOperandHi)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b64 x, y;\n mov.b64 x, {%1, %7};\n mov.b64 y, {%2, %7};\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, %3, [%4], [%5], p;\n}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(kOperandHi)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b64 x, y;\n mov.b64 x, {%1, %7};\n mov.b64 y, {%2, %7};\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, %3, [%4], [%5], p;\n}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(kOperandHi)
+        : "memory");
 }
+// Arrives on the barrier (PAIR: of both CTAs) once the MMAs and scale copies issued so far have completed.
+template <bool PAIR>
 __device__ __forceinline__ void commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-               : "memory");
+  if constexpr (PAIR) tc_commit_pair_both(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+                 : "memory");
 }
 __device__ __forceinline__ void arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// Relaxed: what it tells of (bulk copies that have landed, tensor memory that has been read) is complete and is not this
+// thread's writes. With release it first waits for the SM's stores on their way to memory, 1250 cycles on average.
+__device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
@@ -119,8 +143,10 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   return (silu_regular(g) ? silu_branchless(g) : silu(g)) * u;
 }
 
-// As mbar_wait_cl, for barriers that only this CTA arrives on.
+// As mbar_wait_cl, but (unless PAIR) for barriers that only this CTA arrives on.
+template <bool PAIR>
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort, unsigned* err) {
+  if constexpr (PAIR) return mbar_wait_cl(bar, parity, abort, err);
   uint32_t ok;
   asm volatile(
       "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
@@ -131,16 +157,26 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
 }
 
 // Item -> tile. The device's tile list has a segment's token tiles one after another; a segment's items are its
-// weight tiles with the token tiles innermost, so CTAs that run side by side share weights.
-template <int EPI>
-__device__ __forceinline__ Item item_at(const Mx4GemmArgs& p, int i) {
+// weight tiles with the token tiles (PAIR: pairs of them, of which this CTA takes the one of its rank) innermost, so
+// CTAs that run side by side share weights.
+template <int EPI, bool PAIR>
+__device__ __forceinline__ Item item_at(const Mx4GemmArgs& p, int i, int rank) {
   Item t;
-  if (EPI == kMx4Out) {
-    const int m = i % p.m_tiles;
+  if (EPI >= kMx4Out) {
+    const int m_items = PAIR ? (p.m_tiles + 1) >> 1 : p.m_tiles, m = i % m_items * (PAIR ? 2 : 1) + (PAIR ? rank : 0);
     t.seg = 0;
-    t.a_tile = t.h_tile = m;
-    t.rows = min(128, p.M - m * 128);
-    t.n0 = i / p.m_tiles * p.tn;
+    t.a_tile = t.h_tile = min(m, p.m_tiles - 1);
+    t.rows = max(0, min(128, p.M - m * 128));
+    t.n0 = i / m_items * p.tn;
+  } else if (PAIR) {
+    const Mx4Tile e = p.tiles[p.tiles[i / p.n_tiles].pair_tile];
+    const int local = i - e.pair0 * p.n_tiles, count = (e.count + 1) >> 1, m = local % count * 2 + rank;
+    t.h_tile = e.first + min(m, e.count - 1);
+    const Mx4Tile f = p.tiles[t.h_tile];
+    t.seg = f.seg;
+    t.a_tile = EPI == kMx4Up ? f.a_tile : t.h_tile;
+    t.rows = m < e.count ? f.rows : 0;
+    t.n0 = local / count * p.tn;
   } else {
     const Mx4Tile e = p.tiles[i / p.n_tiles];
     const int local = i - e.first * p.n_tiles, m = local % e.count;
@@ -181,8 +217,10 @@ __device__ __forceinline__ void combine_columns(const Mx4GemmArgs& p, int n0, in
   }
 }
 
-template <int EPI, bool WIDE>
-__global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const __grid_constant__ Mx4GemmArgs p) {
+template <int EPI, int BUILD>
+__global__ void __launch_bounds__(threads(BUILD), BUILD ? 1 : 2) mx4_gemm_kernel(const __grid_constant__ Mx4GemmArgs p) {
+  constexpr bool WIDE = BUILD != kNarrow, PAIR = BUILD == kPair;
+  constexpr int kWideStages = wide_stages(PAIR);
   constexpr int kTmemCols = WIDE ? 512 : 256, kSfBase = WIDE ? kWideN : kNarrowN;
   constexpr uint32_t kSets = (kTmemCols - kSfBase) / kSfCols;
   static_assert((kSets & (kSets - 1)) == 0 && (!WIDE || kWideStages * kWideDepth <= kSets), "sets of scales");
@@ -193,29 +231,38 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   uint8_t* ring = smem_raw + (base - raw);
   Ctl* ctl = reinterpret_cast<Ctl*>(ring + kRing);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int cs = WIDE ? 1 : p.split;
-  const int rank = WIDE ? 0 : int(cluster_rank());
+  const int cs = WIDE ? 1 : p.split;  // CTAs that share an item's contraction
+  // (of the block's index, so that the compiler knows that a warp has one value)
+  const int rank = BUILD == kWide ? 0 : PAIR ? int(blockIdx.x & 1u) : int(cluster_rank());
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < (WIDE ? kWideStages : p.stages); ++s) {
-      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->full[s], PAIR && rank == 0 ? 2 : 1);  // (the leader's also by the peer's copies)
       mbar_init(&ctl->empty[s], 1);
     }
     mbar_init(&ctl->tfull, 1);
-    mbar_init(&ctl->tempty, 8);
+    mbar_init(&ctl->tempty, PAIR ? 16 : 8);
     mbar_init(&ctl->drain, 1);
     ctl->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
-                 "r"(kTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                   "r"(kTmemCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                   "r"(kTmemCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
-  __syncthreads();
+  if (PAIR) cluster_sync();
+  else __syncthreads();
   tc_fence_after();
   // The narrow down product starts under the up product (which lets it, once the plan is complete): the warps that copy
   // weights read the plan and begin before the up product has ended; the others wait for it.
@@ -225,13 +272,16 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   // (all columns of an SM begin at column 0; a constant keeps the issuing loop's operands out of the registers)
   const uint32_t tmem = WIDE ? 0u : ctl->tmem_base;
   volatile int* abort = &ctl->abort;
-  const int total = EPI == kMx4Out ? p.m_tiles * p.n_tiles : (p.hdr->abort ? 0 : p.hdr->tiles * p.n_tiles);
-  const int first = WIDE ? int(blockIdx.x) : int(blockIdx.x) / cs;
-  const int stride = WIDE ? int(gridDim.x) : total;  // narrow: one item
+  const int total = EPI >= kMx4Out  ? (PAIR ? (p.m_tiles + 1) >> 1 : p.m_tiles) * p.n_tiles
+                    : p.hdr->abort ? 0
+                                   : (PAIR ? p.hdr->pairs : p.hdr->tiles) * p.n_tiles;
+  const int first = PAIR ? int(blockIdx.x) >> 1 : WIDE ? int(blockIdx.x) : int(blockIdx.x) / cs;
+  const int stride = PAIR ? int(gridDim.x) >> 1 : WIDE ? int(gridDim.x) : total;  // narrow: one item
   // this CTA's share of the contraction, in chunks
-  const int kc0 = int((long long)p.chunks * rank / cs), kc1 = int((long long)p.chunks * (rank + 1) / cs);
+  const int kc0 = WIDE ? 0 : int((long long)p.chunks * rank / cs);
+  const int kc1 = WIDE ? p.chunks : int((long long)p.chunks * (rank + 1) / cs);
   const uint32_t a_bytes = WIDE ? 8192u : uint32_t(p.a_groups) * 512u, tn = WIDE ? kWideN : uint32_t(p.tn);
-  const uint32_t b_bytes = tn * 64u, sb_bytes = WIDE ? 1024u : 512u, depth = WIDE ? kWideDepth : uint32_t(p.depth);
+  const uint32_t b_bytes = tn * (PAIR ? 32u : 64u), sb_bytes = WIDE ? 1024u : 512u, depth = WIDE ? kWideDepth : uint32_t(p.depth);
   // a stage: codes of A (all chunks), of B, scales of A, of B
   const uint32_t off_b = a_bytes * depth, off_sa = off_b + b_bytes * depth, off_sb = off_sa + 512u * depth;
   const uint32_t stage_bytes = off_sb + sb_bytes * depth;
@@ -242,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   // of the tokens. Warp 0 alone announces a stage's bytes.
   const int kind = warp == 0 ? 0 : warp - 1;  // (warps 0, 2, 3, 4)
   if (!WIDE && warp != 1 && kind < 4 && first < total && elect_one()) {
-    const Item t = item_at<EPI>(p, first);
+    const Item t = item_at<EPI, PAIR>(p, first, rank);
     if (kind == 0) ctl->item[0] = t;  // (before the arrivals on the `full` barriers)
     const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
     const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
@@ -297,65 +347,96 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
   __syncwarp();
   if (kAhead && (warp == 0 || warp == 2)) pdl_wait();
 
-  if (warp == 0) {
-    if (WIDE && first < total && elect_one()) {
-      int s = 0, issued = 0;
-      uint32_t ph = 0;
-      Item next = item_at<EPI>(p, first);
-      for (int i = first, n = 0; i < total && !*abort; i += stride, ++n) {
-        const Item t = next;
-        ctl->item[n % kSlots] = t;  // (before the arrivals on the item's `full` barriers)
-        if (i + stride < total) next = item_at<EPI>(p, i + stride);  // its loads return under this item's copies
-        const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
-        const uint8_t* pa = p.a + size_t(t.a_tile) * 8192 + kc0 * p.a_code_stride;
-        const uint8_t* psa = p.a_scales + size_t(t.a_tile) * 512 + kc0 * p.a_scale_stride;
-        const uint8_t* pb = w + p.w_codes + size_t(t.n0) * 64 + kc0 * p.w_code_stride;
-        const uint8_t* psb = w + p.w_scales + size_t(t.n0 >> 7) * 512 + kc0 * p.w_scale_stride;
-        const uint32_t na = uint32_t((t.rows + 7) >> 3) * 512u;
-        const uint32_t nb = uint32_t(min(int(tn >> 3), p.w_groups - (t.n0 >> 3))) * 512u;
-        const uint32_t nsb = uint32_t(min(2, p.w_blocks - (t.n0 >> 7))) * 512u;
-        for (int kc = kc0; kc < kc1; kc += depth) {
-          if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
-          const uint32_t st = base + uint32_t(s) * stage_bytes, bar = smem_u32(&ctl->full[s]);
-          const int nc = min(int(depth), kc1 - kc);
-          mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
+  // Wide: codes and scales of the weights (B) and of the tokens (A), by one thread or (PAIR) one each. B's thread announces
+  // a stage's bytes.
+  auto copy_items = [&](auto which) {
+    constexpr bool A = decltype(which)::value & 1, B = decltype(which)::value & 2;
+    int s = 0, issued = 0;
+    uint32_t ph = 0;
+    Item next = item_at<EPI, PAIR>(p, first, rank);
+    for (int i = first, n = 0; i < total && !*abort; i += stride, ++n) {
+      const Item t = next;
+      if (B) ctl->item[n % kSlots] = t;  // (before the arrivals on the item's `full` barriers)
+      if (i + stride < total) next = item_at<EPI, PAIR>(p, i + stride, rank);  // its loads return under this item's copies
+      const uint8_t* w = static_cast<const uint8_t*>(p.w[t.seg]);
+      // (PAIR: a half without rows brings in a group all the same, which nothing looks at)
+      const int nb0 = PAIR && rank == 1 && (t.n0 >> 3) + 16 < p.w_groups ? t.n0 + 128 : t.n0;
+      const uint8_t* pa = p.a + size_t(t.a_tile) * 8192;
+      const uint8_t* psa = p.a_scales + size_t(t.a_tile) * 512;
+      const uint8_t* pb = w + p.w_codes + size_t(nb0) * 64;
+      const uint8_t* psb = w + p.w_scales + size_t(t.n0 >> 7) * 512;
+      const uint32_t na = uint32_t(max(1, (t.rows + 7) >> 3)) * 512u;
+      const uint32_t nb = uint32_t(min(int(b_bytes >> 9), p.w_groups - (nb0 >> 3))) * 512u;
+      const uint32_t nsb = uint32_t(min(2, p.w_blocks - (t.n0 >> 7))) * 512u;
+      for (int kc = 0; kc < kc1; kc += depth) {
+        if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, p.err)) break;
+        const uint32_t st = base + uint32_t(s) * stage_bytes, bar = smem_u32(&ctl->full[s]);
+        const int nc = min(int(depth), kc1 - kc);
+        if (B) mbar_expect_tx(&ctl->full[s], uint32_t(nc) * (na + nb + 512u + nsb));
 #pragma unroll 2
-          for (int j = 0; j < nc; ++j) {
+        for (int j = 0; j < nc; ++j) {
+          if (B) {
             bulk_load(st + off_b + b_bytes * j, pb, nb, bar);
             bulk_load(st + off_sb + sb_bytes * j, psb, nsb, bar);
+            pb += p.w_code_stride;
+            psb += p.w_scale_stride;
+          }
+          if (A) {
             bulk_load(st + a_bytes * j, pa, na, bar);
             bulk_load(st + off_sa + 512u * j, psa, 512u, bar);
             pa += p.a_code_stride;
             psa += p.a_scale_stride;
-            pb += p.w_code_stride;
-            psb += p.w_scale_stride;
-          }
-          if (issued < stages) ++issued;
-          if (++s == stages) {
-            s = 0;
-            ph ^= 1u;
           }
         }
-      }
-      // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
-      for (int i = 0; i < issued; ++i) {
-        const int j = s - (issued - i);
-        if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
+        if (issued < stages) ++issued;
+        if (++s == stages) {
+          s = 0;
+          ph ^= 1u;
+        }
       }
     }
+    // the copies still in flight, oldest first; after the first wait that runs out the rest are skipped
+    for (int i = 0; i < issued; ++i) {
+      const int j = s - (issued - i);
+      if (!mbar_wait_drain_cl(&ctl->full[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, p.err)) break;
+    }
+  };
+  if (warp == 0) {
+    if (WIDE && first < total && elect_one()) copy_items(std::integral_constant<int, PAIR ? 2 : 3>());
+  } else if (PAIR && warp == 10) {
+    if (first < total && elect_one()) copy_items(std::integral_constant<int, 1>());
   } else if (warp == 1) {
-    if (first < total && elect_one()) {
+    if (PAIR && rank == 1) {
+      // the leader's MMAs read this CTA's stages too
+      if (first < total && elect_one()) {
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int i = first; i < total && ok; i += stride) {
+          for (int kc = kc0; kc < kc1; kc += depth) {
+            ok = mbar_wait_cl(&ctl->full[s], ph, abort, p.err);
+            if (!ok) break;
+            arrive_relaxed(peer_addr(&ctl->full[s], 0));
+            if (++s == stages) {
+              s = 0;
+              ph ^= 1u;
+            }
+          }
+        }
+        mbar_wait_drain_cl(&ctl->drain, 0, p.err);  // nothing of the leader's is still to arrive here
+      }
+    } else if (first < total && elect_one()) {
       int s = 0;
       uint32_t ph = 0, lt = 0;
-      const uint32_t lo0 = desc_lo(base), idesc = kIdesc | (tn >> 3 << 17), idesc2 = idesc | (2u << 4) | (2u << 29);
+      const uint32_t lo0 = desc_lo(base), idesc = (PAIR ? kIdescPair : kIdesc) | (tn >> 3 << 17), idesc2 = idesc | (2u << 4) | (2u << 29);
       for (int i = first; i < total && !*abort; i += stride, ++lt) {
         // narrow tiles: which 32-row columns of the 128-row block of scales
-        const uint32_t sb_shift = WIDE ? 0u : uint32_t(item_at<EPI>(p, i).n0 >> 5) & 3u;
-        if (!wait(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
+        const uint32_t sb_shift = WIDE ? 0u : uint32_t(item_at<EPI, PAIR>(p, i, rank).n0 >> 5) & 3u;
+        if (!wait<PAIR>(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
         tc_fence_after();
         bool ok = true;
         for (int kc = kc0; kc < kc1; kc += depth) {
-          if (!wait(&ctl->full[s], ph, abort, p.err)) {
+          if (!wait<PAIR>(&ctl->full[s], ph, abort, p.err)) {
             ok = false;
             break;
           }
@@ -364,12 +445,12 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
           const uint32_t sf0 = tmem + kSfBase + uint32_t(s) * (WIDE ? kWideDepth * kSfCols : 0u);
           auto step = [&](uint32_t j, uint32_t acc) {  // 128 columns
             const uint32_t sfa = sf0 + (WIDE ? j : j & (kSets - 1)) * kSfCols, sfb = sfa + 4;
-            scales_to_tmem(sfa, st + (off_sa >> 4) + 32u * j);
-            scales_to_tmem(sfb, st + (off_sb >> 4) + (sb_bytes >> 4) * j);
-            if (WIDE) scales_to_tmem(sfb + 4, st + (off_sb >> 4) + (sb_bytes >> 4) * j + 32u);
+            scales_to_tmem<PAIR>(sfa, st + (off_sa >> 4) + 32u * j);
+            scales_to_tmem<PAIR>(sfb, st + (off_sb >> 4) + (sb_bytes >> 4) * j);
+            if (WIDE) scales_to_tmem<PAIR>(sfb + 4, st + (off_sb >> 4) + (sb_bytes >> 4) * j + 32u);
             const uint32_t da = st + (a_bytes >> 4) * j, db = st + (off_b >> 4) + (b_bytes >> 4) * j;
-            mma_mx4(tmem, da, db, idesc, sfa, sfb + sb_shift, acc);
-            if ((kc + int(j)) * 2 + 1 < p.ksteps) mma_mx4(tmem, da + 2, db + 2, idesc2, sfa, sfb + sb_shift, 1u);
+            mma_mx4<PAIR>(tmem, da, db, idesc, sfa, sfb + sb_shift, acc);
+            if ((kc + int(j)) * 2 + 1 < p.ksteps) mma_mx4<PAIR>(tmem, da + 2, db + 2, idesc2, sfa, sfb + sb_shift, 1u);
           };
           const int nc = min(int(depth), kc1 - kc);
           step(0, kc > kc0 ? 1u : 0u);
@@ -378,16 +459,16 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
           } else {
             for (int j = 1; j < nc; ++j) step(uint32_t(j), 1u);
           }
-          commit(&ctl->empty[s]);
+          commit<PAIR>(&ctl->empty[s]);
           if (++s == stages) {
             s = 0;
             ph ^= 1u;
           }
         }
         if (!ok) break;
-        commit(&ctl->tfull);
+        commit<PAIR>(&ctl->tfull);
       }
-      commit(&ctl->drain);  // arrives once every MMA issued above has completed
+      commit<PAIR>(&ctl->drain);  // arrives once every MMA issued above has completed
       mbar_wait_drain_cl(&ctl->drain, 0, p.err);
     }
   } else if constexpr (WIDE) {
@@ -407,7 +488,10 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
       tmem_ld_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) arrive(&ctl->tempty);
+      if (lane == 0) {
+        if (PAIR) arrive_relaxed(peer_addr(&ctl->tempty, 0));
+        else arrive(&ctl->tempty);
+      }
       const int n = t.n0 + grp * 128;
       if constexpr (EPI == kMx4Up) {
 #pragma unroll
@@ -446,13 +530,21 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
         if (cols <= 0) {
         } else if (f32) {
           float* y = static_cast<float*>(p.out) + dst * p.ldo + n;
-          if (cols == 128 && p.vec) {
+          if constexpr (EPI != kMx4OutAny) {
 #pragma unroll
-            for (int c = 0; c < 128; c += 16) store_rows64(dst < 0 ? nullptr : y + c, v + c);
-          } else if (dst >= 0) {
+            for (int c = 0; c < 128; c += 16)
+              if (c < cols) store_rows64(dst < 0 ? nullptr : y + c, v + c);
+          } else {
+            // any N and stride: a row at a time, a column a lane
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (c < cols) y[c] = __uint_as_float(v[c]);
+            for (int c = 0; c < 128; c += 32) {
+              transpose32(v + c);
+              float* x = static_cast<float*>(p.out) + ((long long)t.h_tile * 128 + q * 32) * p.ldo + n + c + lane;
+              const int rows = c + lane < cols ? t.rows - q * 32 : 0;
+#pragma unroll
+              for (int r = 0; r < 32; ++r, x += p.ldo)
+                if (r < rows) *x = __uint_as_float(v[c + r]);
+            }
           }
         } else {
           if (EPI == kMx4Down) {
@@ -475,13 +567,22 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
             for (int c = 0; c < 64; ++c) v[c] = pack2bf(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
           }
           uint16_t* y = static_cast<uint16_t*>(p.out) + dst * p.ldo + n;
-          if (cols == 128 && p.vec) {
+          if constexpr (EPI != kMx4OutAny) {
 #pragma unroll
-            for (int c = 0; c < 64; c += 16) store_rows64(dst < 0 ? nullptr : y + 2 * c, v + c);
-          } else if (dst >= 0) {
+            for (int c = 0; c < 64; c += 16)
+              if (2 * c < cols) store_rows64(dst < 0 ? nullptr : y + 2 * c, v + c);
+          } else {
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (c < cols) y[c] = uint16_t(v[c >> 1] >> (16 * (c & 1)));
+            for (int c = 0; c < 64; c += 32) {
+              transpose32(v + c);
+              uint16_t* x = static_cast<uint16_t*>(p.out) + ((long long)t.h_tile * 128 + q * 32) * p.ldo + n + 2 * (c + lane);
+              const int left = cols - 2 * (c + lane), rows = t.rows - q * 32;
+#pragma unroll
+              for (int r = 0; r < 32; ++r, x += p.ldo) {
+                if (r < rows && left > 0) x[0] = uint16_t(v[c + r]);
+                if (r < rows && left > 1) x[1] = uint16_t(v[c + r] >> 16);
+              }
+            }
           }
         }
       }
@@ -586,48 +687,63 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 1 : 2) mx4_gemm_kernel(const 
     if (cs > 1) cluster_sync();  // the peers have read this CTA's partial tile
     else __syncthreads();
   } else {
-    __syncthreads();
+    if (PAIR) cluster_sync();  // (the leader's MMAs have read and written this CTA's memory)
+    else __syncthreads();
   }
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    if constexpr (PAIR)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    else
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
 }
 
 // ---- host ----
 
-template <int EPI, bool WIDE>
+template <int EPI, int BUILD>
 cudaError_t go(const Mx4GemmArgs& p, int grid, cudaStream_t s) {
   static SmemOptIn smem;
-  const void* fn = reinterpret_cast<const void*>(mx4_gemm_kernel<EPI, WIDE>);
-  cudaError_t e = smem.allow(fn, smem_bytes<WIDE>());
+  const void* fn = reinterpret_cast<const void*>(mx4_gemm_kernel<EPI, BUILD>);
+  cudaError_t e = smem.allow(fn, smem_bytes(BUILD));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(grid));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = size_t(smem_bytes<WIDE>());
+  cfg.blockDim = dim3(unsigned(threads(BUILD)));
+  cfg.dynamicSmemBytes = size_t(smem_bytes(BUILD));
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = unsigned(WIDE ? 1 : p.split);
+  attr[1].val.clusterDim.x = unsigned(BUILD == kPair ? 2 : BUILD == kWide ? 1 : p.split);
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<EPI, WIDE>, p);
+  e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<EPI, BUILD>, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-bool mx4_wide(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN) >= num_sms(); }
+long long mx4_wide_items(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN); }
+
+// Few tokens: wide tiles once they fill the SMs, since the narrow ones spread the weights' bytes over all SMs. Full tiles:
+// from a quarter of that, since a narrow tile of 128 tokens brings them in for each 64 or 128 weight rows (narrow against
+// wide, bf16 out: 384 x 4096 x 4096 18.3 and 9.8 us, 1024 x 4096 x 1408 25.1 and 7.7, 256 x 14336 x 4096 28.9 and 10.3;
+// below a quarter 256 x 4096 x 14336 18.5 and 21.6).
+bool mx4_wide(long long max_tiles, int n_rows, int tile_rows) {
+  return mx4_wide_items(max_tiles, n_rows) * (tile_rows == 128 ? 4 : 1) >= num_sms();
+}
 
 // tile_rows: most token rows of a tile.
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s) {
   const int n_rows = epi == kMx4Up ? 2 * p.n_out : p.n_out;
   auto tiles_of = [&](int tn) { return (n_rows + tn - 1) / tn; };
-  const bool wide = mx4_wide(max_tiles, n_rows);
+  const bool wide = mx4_wide(max_tiles, n_rows, tile_rows);
+  // CTA pairs pay where items follow one another on every SM and are long: 4096 x 14336 x 4096 82.4 us by single CTAs and
+  // 73.5 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
+  const bool pair = wide && p.pairs && mx4_wide_items(max_tiles, n_rows) > num_sms && p.chunks >= 16;
   p.split = 1;
   int grid;
   if (wide) {
@@ -635,7 +751,8 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
     p.depth = kWideDepth;
     p.a_groups = 16;
     p.n_tiles = tiles_of(p.tn);
-    grid = int(std::min<long long>(num_sms, max_tiles * p.n_tiles));
+    grid = pair ? 2 * int(std::min<long long>(num_sms / 2, max_tiles * p.n_tiles))
+                : int(std::min<long long>(num_sms, max_tiles * p.n_tiles));
   } else {
     p.tn = max_tiles * tiles_of(128) >= num_sms ? 128 : 64;
     p.n_tiles = tiles_of(p.tn);
@@ -647,14 +764,22 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
   const int stage = p.depth * (p.a_groups * 512 + p.tn * 64 + 512 + (p.tn > 128 ? 1024 : 512));
   // the MMA reads 128 rows of A wherever the stage's A begins: the last stage's end stays inside the ring
   const int slack = (16 - p.a_groups) * 512;
-  p.stages = wide ? kWideStages : std::min(kMaxStages, (kNarrowRing - slack) / stage);
+  p.stages = wide ? wide_stages(pair) : std::min(kMaxStages, (kNarrowRing - slack) / stage);
   if (p.stages < 2) return cudaErrorInvalidConfiguration;
   const int kid = epi == kMx4Up ? kProfMx4Up : epi == kMx4Down ? kProfMx4Down : kProfMx4Matmul;
   prof_begin(kid, s);
   cudaError_t e;
-  if (epi == kMx4Up) e = wide ? go<kMx4Up, true>(p, grid, s) : go<kMx4Up, false>(p, grid, s);
-  else if (epi == kMx4Down) e = wide ? go<kMx4Down, true>(p, grid, s) : go<kMx4Down, false>(p, grid, s);
-  else e = wide ? go<kMx4Out, true>(p, grid, s) : go<kMx4Out, false>(p, grid, s);
+  auto run = [&](auto build) {
+    constexpr int B = decltype(build)::value;
+    if (epi == kMx4Up) return go<kMx4Up, B>(p, grid, s);
+    if (epi == kMx4Down) return go<kMx4Down, B>(p, grid, s);
+    if constexpr (B != kNarrow)
+      if (!p.vec) return go<kMx4OutAny, B>(p, grid, s);
+    return go<kMx4Out, B>(p, grid, s);
+  };
+  e = pair   ? run(std::integral_constant<int, kPair>())
+      : wide ? run(std::integral_constant<int, kWide>())
+             : run(std::integral_constant<int, kNarrow>());
   prof_end(kid, s);
   return e;
 }

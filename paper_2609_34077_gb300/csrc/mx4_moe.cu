@@ -90,9 +90,9 @@ __global__ void __launch_bounds__(kPlanThreads) mx4_plan_kernel(const __grid_con
   for (int w = 0; w < warp; ++w) before += wsum[w];
   if (tid == kPlanThreads - 1) total = before + on;
   if (tid < a.E) tile_of[tid] = before;
-  if (on) a.tiles[before] = Mx4Tile{tid, 0, before, 1, a.T, {0, 0, 0}};
+  if (on) a.tiles[before] = Mx4Tile{tid, 0, before, 1, a.T, 0, 0, 0};
   __syncthreads();
-  if (tid < a.S) a.tiles[total + tid] = Mx4Tile{a.E + tid, 0, total + tid, 1, a.T, {0, 0, 0}};
+  if (tid < a.S) a.tiles[total + tid] = Mx4Tile{a.E + tid, 0, total + tid, 1, a.T, 0, 0, 0};
   if (tid == 0) {
     if (bad) set_error(a.err, kErrInvalid);
     a.hdr->abort = bad;
@@ -136,7 +136,7 @@ __device__ __forceinline__ int peer_int(const int* p, uint32_t rank) {
 // One cluster: each CTA counts and places an eighth of the assignments.
 __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads)
     mx4_permute_kernel(const __grid_constant__ Mx4MoeArgs a) {
-  __shared__ int cnt[kMaxMx4E + 1], next[kMaxMx4E], tile0[kMaxMx4E], wsum[8], routed;  // cnt[kMaxMx4E]: bad ids
+  __shared__ int cnt[kMaxMx4E + 1], next[kMaxMx4E], tile0[kMaxMx4E], wsum[8], wpairs[8], routed, routed_pairs;  // cnt[kMaxMx4E]: bad ids
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = int(cta_rank());
@@ -150,7 +150,7 @@ __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads
     else if (e != -1) cnt[kMaxMx4E] = 1;
   }
   cluster_barrier();
-  int before = 0, sum = 0, bad = 0, tiles = 0;
+  int before = 0, sum = 0, bad = 0, tiles = 0, pair0 = 0;
   if (tid < kMaxMx4E) {
     for (int r = 0; r < kPermCtas; ++r) {
       const int c = peer_int(&cnt[tid], r);
@@ -159,25 +159,47 @@ __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads
       bad |= peer_int(&cnt[kMaxMx4E], r);
     }
     tiles = (sum + 127) >> 7;
-    int incl = tiles;
+    const int pairs = (tiles + 1) >> 1;
+    int incl = tiles, incl2 = pairs;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
+      const int v = __shfl_up_sync(0xffffffffu, incl, o), v2 = __shfl_up_sync(0xffffffffu, incl2, o);
+      if (lane >= o) {
+        incl += v;
+        incl2 += v2;
+      }
     }
     tile0[tid] = incl - tiles;
-    if (lane == 31) wsum[warp] = incl;
+    pair0 = incl2 - pairs;
+    if (lane == 31) {
+      wsum[warp] = incl;
+      wpairs[warp] = incl2;
+    }
   }
   __syncthreads();
   if (tid < kMaxMx4E) {
     int base = tile0[tid];
-    for (int w = 0; w < warp; ++w) base += wsum[w];
+    for (int w = 0; w < warp; ++w) {
+      base += wsum[w];
+      pair0 += wpairs[w];
+    }
     tile0[tid] = base;
     next[tid] = base * 128 + before;
-    if (tid == kMaxMx4E - 1) routed = base + tiles;
+    if (tid == kMaxMx4E - 1) {
+      routed = base + tiles;
+      routed_pairs = pair0 + ((tiles + 1) >> 1);
+    }
     if (rank == 0) {
-      for (int m = 0; m < tiles; ++m)
-        a.tiles[base + m] = Mx4Tile{tid, base + m, base, tiles, min(128, sum - m * 128), {0, 0, 0}};
+      for (int m = 0; m < tiles; ++m) {
+        Mx4Tile& t = a.tiles[base + m];  // (pair_tile is another thread's)
+        t.seg = tid;
+        t.a_tile = base + m;
+        t.first = base;
+        t.count = tiles;
+        t.rows = min(128, sum - m * 128);
+        t.pair0 = pair0;
+        if ((m & 1) == 0) a.tiles[pair0 + (m >> 1)].pair_tile = base + m;
+      }
       if (tid == 0) {
         if (bad) set_error(a.err, kErrInvalid);
         a.hdr->abort = bad;
@@ -187,10 +209,21 @@ __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads
   __syncthreads();
   const int xt = (a.T + 127) >> 7;
   if (rank == 0) {
-    if (tid == 0) a.hdr->tiles = routed + a.S * xt;
+    const int xp = (xt + 1) >> 1;
+    if (tid == 0) {
+      a.hdr->tiles = routed + a.S * xt;
+      a.hdr->pairs = routed_pairs + a.S * xp;
+    }
     for (int i = tid; i < a.S * xt; i += kPermThreads) {
       const int s = i / xt, m = i - s * xt;
-      a.tiles[routed + i] = Mx4Tile{a.E + s, a.x_tile0 + m, routed + s * xt, xt, min(128, a.T - m * 128), {0, 0, 0}};
+      Mx4Tile& t = a.tiles[routed + i];
+      t.seg = a.E + s;
+      t.a_tile = a.x_tile0 + m;
+      t.first = routed + s * xt;
+      t.count = xt;
+      t.rows = min(128, a.T - m * 128);
+      t.pair0 = routed_pairs + s * xp;
+      if ((m & 1) == 0) a.tiles[t.pair0 + (m >> 1)].pair_tile = routed + i;
     }
   }
   // shared experts' rows; rows that pad a routed expert's last tile are past its count and are not looked at
@@ -333,8 +366,8 @@ Mx4MoeLayout::Mx4MoeLayout(const mcft_layer_desc* desc, int T) {
   x = place(Mx4Layout(x_rows, d).bytes());
   h = place(Mx4Layout(tiles * 128, w).bytes());
   const size_t o_rows = size_t(n) + size_t(S) * T;
-  fused_combine = T <= kMx4FusedCombineT && !mx4_wide(tiles, d);
-  half_o = dtype == MCFT_BF16 && mx4_wide(tiles, d);
+  fused_combine = T <= kMx4FusedCombineT && !mx4_wide(tiles, d, T);
+  half_o = dtype == MCFT_BF16 && mx4_wide_items(tiles, d) >= num_sms();  // (a smaller o stays in L2 anyway)
   o = place(sizeof(float) * o_rows * d);  // (also where fp16 takes half of it: fewer tokens may need fp32)
   o_unit = place(half_o ? sizeof(float) * o_rows * ((d + 127) / 128) : 0);
   total = at;

@@ -33,4 +33,21 @@ __device__ __forceinline__ void store_rows64(void* row, uint32_t* u) {
   }
 }
 
+// u[i] of lane j <-> u[j] of lane i: the rows that 32 lanes own, turned so that lane j holds word j of each row, by halves
+// of 16, 8, 4, 2 and 1.
+__device__ __forceinline__ void transpose32(uint32_t* u) {
+  const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll
+  for (int h = 16; h > 0; h >>= 1) {
+    const bool up = lane & uint32_t(h);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (i & h) continue;
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? u[i] : u[i | h], h);
+      if (up) u[i] = got;
+      else u[i | h] = got;
+    }
+  }
+}
+
 }  // namespace mcft
