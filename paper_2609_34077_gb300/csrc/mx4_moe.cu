@@ -138,6 +138,7 @@ __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads
     mx4_permute_kernel(const __grid_constant__ Mx4MoeArgs a) {
   __shared__ int cnt[kMaxMx4E + 1], next[kMaxMx4E], tile0[kMaxMx4E], wsum[8], wpairs[8], routed, routed_pairs;  // cnt[kMaxMx4E]: bad ids
   pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (x is complete: mx4_spread_kernel quantises it meanwhile)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = int(cta_rank());
   const long long n = (long long)a.T * a.K;
@@ -244,25 +245,23 @@ __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads
   cluster_barrier();  // the peers have read this CTA's counts
 }
 
-// One warp a token: quantised once, written to its K places and (shared experts) to its place in x itself.
+// One warp a token's 1024 columns: quantised once, while the placement is still going on, then written to the token's K
+// places and (shared experts) to its place in x itself.
 template <typename T>
 __global__ void __launch_bounds__(256) mx4_spread_kernel(const __grid_constant__ Mx4MoeArgs a) {
-  pdl_wait();
   const int t = int(blockIdx.x) * 8 + int(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int c = int(blockIdx.y) * 1024 + lane * 32;
+  uint32_t scale;
+  const uint4 codes = quantise_block(static_cast<const T*>(a.x) + size_t(min(t, a.T - 1)) * a.d, c, a.d, scale);
+  const uint32_t word = scale_word(scale);
+  pdl_wait();
   if (t >= a.T) return;
   const Mx4Layout L(a.x_rows, a.d);
   int mine = lane < a.K ? a.pos[(long long)t * a.K + lane] : -1;
   if (lane == a.K && a.S > 0) mine = a.x_tile0 * 128 + t;
-  const unsigned to = __ballot_sync(0xffffffffu, mine >= 0);
-  const T* row = static_cast<const T*>(a.x) + size_t(t) * a.d;
-  for (int c = lane * 32; c < (a.d + 1023) / 1024 * 1024; c += 1024) {
-    uint32_t scale;
-    const uint4 codes = quantise_block(row, c, a.d, scale);
-    const uint32_t word = scale_word(scale);
-    for (unsigned m = to; m; m &= m - 1) {
-      const int r = __shfl_sync(0xffffffffu, mine, __ffs(m) - 1);
-      put_block(a.xq, L, size_t(r), c, codes, word);
-    }
+  for (unsigned m = __ballot_sync(0xffffffffu, mine >= 0); m; m &= m - 1) {
+    const int r = __shfl_sync(0xffffffffu, mine, __ffs(m) - 1);
+    put_block(a.xq, L, size_t(r), c, codes, word);
   }
 }
 
@@ -272,37 +271,49 @@ template <typename T, bool HALF>
 __global__ void __launch_bounds__(128) mx4_combine_kernel(const __grid_constant__ Mx4MoeArgs a) {
   pdl_wait();
   if (a.hdr->abort) return;
+  const int lane = threadIdx.x & 31;
   const int t = int(blockIdx.x), c = (int(blockIdx.y) * 128 + int(threadIdx.x)) * 8;
-  if (c >= a.d) return;
   const int units = (a.d + 127) >> 7, n = a.K + a.S;
   const float* o32 = static_cast<const float*>(a.o);
   const __half* o16 = static_cast<const __half*>(a.o);
+  static_assert(kMaxMx4K + kMaxShared <= 32, "a lane each");
+  // lane k: the k-th row and its factor (HALF: times the units of the warp's first and last 128 columns)
+  long long row = -1;
+  float g = 0.f, g_last = 0.f;
+  if (lane < a.K) {
+    row = a.src[(long long)t * a.K + lane];
+    if (row >= 0) g = a.gate[(long long)t * a.K + lane];
+  } else if (lane < n) {
+    row = (long long)a.T * a.K + (long long)(lane - a.K) * a.T + t;
+    g = 1.f;
+  }
+  if (HALF && row >= 0) {
+    const int u = (c - lane * 8) >> 7;
+    const float* unit = a.o_unit + row * units;
+    g_last = u + 1 < units ? g * __ldg(unit + u + 1) : 0.f;
+    g = u < units ? g * __ldg(unit + u) : 0.f;
+  }
   float acc[8] = {};
   constexpr int kAtOnce = 4;  // rows in flight
   for (int k0 = 0; k0 < n; k0 += kAtOnce) {
-    float g[kAtOnce];
+    float f[kAtOnce];
     uint4 v[kAtOnce][HALF ? 1 : 2];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const int k = k0 + i;
-      long long row = -1;
-      g[i] = 1.f;
-      if (k < a.K) {
-        row = a.src[(long long)t * a.K + k];
-        if (row >= 0) g[i] = a.gate[(long long)t * a.K + k];
-      } else if (k < n) {
-        row = (long long)a.T * a.K + (long long)(k - a.K) * a.T + t;
+      const long long r = __shfl_sync(0xffffffffu, row, k0 + i);  // (past n: -1)
+      f[i] = __shfl_sync(0xffffffffu, g, k0 + i);
+      if constexpr (HALF) {
+        const float last = __shfl_sync(0xffffffffu, g_last, k0 + i);
+        if (lane >= 16) f[i] = last;
       }
-      if (row < 0) {
-        g[i] = 0.f;
+      if (r < 0 || c >= a.d) {
 #pragma unroll
         for (int q = 0; q < (HALF ? 1 : 2); ++q) v[i][q] = make_uint4(0, 0, 0, 0);
       } else if constexpr (HALF) {
-        v[i][0] = ld_stream16(o16 + row * a.d + c);
-        g[i] *= __ldg(a.o_unit + row * units + (c >> 7));
+        v[i][0] = ld_stream16(o16 + r * a.d + c);
       } else {
-        v[i][0] = ld_stream16(o32 + row * a.d + c);
-        v[i][1] = ld_stream16(o32 + row * a.d + c + 4);
+        v[i][0] = ld_stream16(o32 + r * a.d + c);
+        v[i][1] = ld_stream16(o32 + r * a.d + c + 4);
       }
     }
 #pragma unroll
@@ -311,17 +322,18 @@ __global__ void __launch_bounds__(128) mx4_combine_kernel(const __grid_constant_
         const uint32_t w[4] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-          acc[2 * j] = fmaf(g[i], f.x, acc[2 * j]);
-          acc[2 * j + 1] = fmaf(g[i], f.y, acc[2 * j + 1]);
+          const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+          acc[2 * j] = fmaf(f[i], h.x, acc[2 * j]);
+          acc[2 * j + 1] = fmaf(f[i], h.y, acc[2 * j + 1]);
         }
       } else {
         const uint32_t w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = fmaf(g[i], __uint_as_float(w[j]), acc[j]);
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(f[i], __uint_as_float(w[j]), acc[j]);
       }
     }
   }
+  if (c >= a.d) return;
   if constexpr (sizeof(T) == 2) {
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + (long long)t * a.d + c) =
         make_uint4(pack2bf(acc[0], acc[1]), pack2bf(acc[2], acc[3]), pack2bf(acc[4], acc[5]), pack2bf(acc[6], acc[7]));
@@ -383,7 +395,7 @@ cudaError_t launch_mx4_prepare(const Mx4MoeArgs& a, int dtype, bool permuted, cu
            : launch_pdl(mx4_plan_kernel<float>, dim3(grid), dim3(kPlanThreads), 0, s, a);
   } else {
     e = launch_pdl(mx4_permute_kernel, dim3(kPermCtas), dim3(kPermThreads), 0, s, a);
-    const dim3 grid{unsigned((a.T + 7) / 8)};
+    const dim3 grid(unsigned((a.T + 7) / 8), unsigned((a.d + 1023) / 1024));
     if (e == cudaSuccess)
       e = bf ? launch_pdl(mx4_spread_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, a)
              : launch_pdl(mx4_spread_kernel<float>, grid, dim3(256), 0, s, a);
