@@ -11,19 +11,24 @@
 //   down  rows of o, to the assignment's place: fp32, or 16 bits (below);
 //   out   fp32 or bf16 rows of y (the plain product).
 //
-// Two builds. `wide` tiles of 128 x 256 for prompts: a persistent grid, one CTA an SM; the eight epilogue warps
+// Three builds. `wide` tiles of 128 x 256 for prompts: a persistent grid, one CTA an SM; the eight epilogue warps
 // drain the 256 accumulator columns into registers and give them back at once, so that the next tile's MMAs run
-// under the epilogue's arithmetic and stores. `narrow` tiles of up to 128 weight rows for few tokens, where the
-// bytes of the weights bound the time: one item a cluster of 1, 2, 4 or 8 CTAs that split the contraction and
-// add their partial tiles through distributed shared memory, two CTAs an SM; only the 8-row groups that hold
-// tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results).
+// under the epilogue's arithmetic and stores (one accumulator: two of 256 columns and the scales do not fit into tensor
+// memory, and two of 192 were slower). An SM takes about 70 bytes a cycle in from L2, so a tile's copies take longer than
+// its MMAs (128 cycles for 128 x 256 x 64): 4096 x 14336 x 4096 75 us with the copies alone, 82 in all, 50 at the MMAs' rate.
+// `pair`: the same under tcgen05's CTA pairs, M = 256: each CTA brings in its 128 token rows and half of the weight rows,
+// two thirds of the bytes, and copies and MMAs are level: 73.7 us (6.5 PFLOP/s). `narrow` tiles of up to 128 weight rows
+// for few tokens, where the bytes of the weights bound the time: one item a cluster of 1, 2, 4 or 8 CTAs that split the
+// contraction and add their partial tiles through distributed shared memory, two CTAs an SM; only the 8-row groups that
+// hold tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results). 1 x 4096 x 14336:
+// 8.0 us a replayed graph's node, 4.6 at HBM's rate; the layer of 16 tokens on 8 experts of 4096 x 14336 109 us, its floor.
 //
 // For bf16 layers wide tiles write o as fp16 under a power-of-two unit for each row's 128 columns (the largest of them in [2^14, 2^15)
 // units): its 11 bits cost y an error of 2^-11, an eighth of its own rounding to bf16, and o is moved twice (here and
 // by the combine), which in fp32 took most of both kernels' time.
 //
-// Warp 0 issues the copies, warp 1 the tcgen05.cp and MMAs and owns the tensor memory, warps 2-9 are the
-// epilogue. Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again
+// Warp 0 issues the copies (pair: warp 10 those of the tokens), warp 1 the tcgen05.cp and MMAs and owns the tensor memory
+// (pair: the second CTA's tells the first of its copies), warps 2-9 are the epilogue. Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again
 // with a limit) for its copies and MMAs in flight, frees the tensor memory and returns.
 #include <cuda_fp16.h>
 

@@ -7,6 +7,10 @@
 // quantised once and written to its K places. The order of an expert's rows is not defined and does not matter:
 // a row's products do not depend on its place in a tile.
 //
+// All four kernels are short: 16 tokens' plan 4 us (launch and a chain of barriers), 4096 tokens of d = 2048 on 64 experts
+// permutation 9.7 us (one cluster: latency), spread 11.4 us alone and mostly behind the permutation (17 MB in, 31 out),
+// combine 30.4 us (134 MB of fp16 outputs in, 17 out: 5 TB/s, HBM and L2).
+//
 // Rows of o are in the order of the assignments (t, k), then the shared experts' (s, t), so the combine needs no
 // lookup but `src`: the assignment whose row holds expert idx[t, k]'s output for token t (itself; the first of
 // them where a token names an expert twice; -1 where it names none).
@@ -294,7 +298,7 @@ __global__ void __launch_bounds__(128) mx4_combine_kernel(const __grid_constant_
     g = u < units ? g * __ldg(unit + u) : 0.f;
   }
   float acc[8] = {};
-  constexpr int kAtOnce = 4;  // rows in flight
+  constexpr int kAtOnce = 4;  // rows in flight (2 and 8: 34.5 and 41 us where 4 take 30.4)
   for (int k0 = 0; k0 < n; k0 += kAtOnce) {
     float f[kAtOnce];
     uint4 v[kAtOnce][HALF ? 1 : 2];

@@ -2,7 +2,9 @@
 //
 // Few tokens (kFewT) and small weights: latency bounds it. A cluster of eight CTAs takes kFewTokens tokens: its 64 warps share the
 // experts, each streaming its rows of W once against all of the tokens (held in shared memory), and the logits meet
-// in the leader's shared memory, where one warp ranks a token.
+// in the leader's shared memory, where one warp ranks a token. One token of d = 2048, E = 64: 5.1 us a replayed graph's
+// node, of which the 256 kB of W are 0.04 at HBM's rate; the rest is the launch, one round of loads, two cluster barriers
+// and the choice's chain of shuffles.
 // Otherwise: fp32 layers (and rows too wide for the first) take tiles of 32 tokens by all experts, fp32 multiply-adds
 // from shared memory, ranked in place; bf16 layers the tensor cores (scored_tc.cu).
 #include "route_scored_warp.cuh"
@@ -97,6 +99,7 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
 // 32 tokens by up to 256 experts; 256 threads of 4 tokens x 8 experts (of 2 tokens, shared memory reads took twice the
 // time of the multiply-adds: 2048 tokens of d = 4096, E = 256 in fp32 227 us). A cluster of up to 8 CTAs shares the
 // contraction; each then ranks its share of the tokens from the sums of all CTAs' partial logits, in the CTAs' order.
+// Bound by its fp32 multiply-adds and the shared-memory loads that feed them.
 constexpr int kTileT = 32, kTileK = 32, kPerWarp = kTileT / 8;
 template <int PL>
 constexpr int kTileSmem = 4 * (kTileK * (kTileT + 4) + kTileK * (32 * PL + 1) + 8 * 64 * PL);

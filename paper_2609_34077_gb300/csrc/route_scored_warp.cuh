@@ -6,7 +6,7 @@
 // the choice first narrows the field: the K-th largest of the 32 lanes' own maxima is a bound below which nothing can
 // be chosen, and what reaches it (K to about 2 K experts) is packed one to a lane, where a round of the choice is a
 // warp maximum and a ballot. 8192 tokens of 256 experts in 8 groups, forward: 70 us with all eight experts of every
-// lane looked at in each of the K rounds, on ten warps a CTA; see scored_tc.cu for the figure now.
+// lane looked at in each of the K rounds, on ten warps a CTA; 34 us as it is now, on 32 warps.
 #pragma once
 
 #include "route_scored.h"

@@ -582,6 +582,8 @@ def mcft_route_scored_grad(desc: ScoredDesc, x, w_router, idx, gate, logits, dga
     """(dx [T, d] of the layer dtype, dw [E, d] fp32) from dL/dgate and what mcft_route_scored wrote; dw is
     added to if accumulate."""
     T = x.shape[0]
+    assert idx.dtype == torch.int32 and idx.shape == gate.shape == dgate.shape == (T, desc.K) and logits.shape == (T, desc.E), \
+        "idx, gate and dgate are [T, K], logits [T, E]"
     if dx is None:
         dx = torch.empty_like(x)
     if dw is None:
