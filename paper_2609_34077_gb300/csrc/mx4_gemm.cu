@@ -17,7 +17,7 @@
 // memory, and two of 192 were slower). An SM takes about 70 bytes a cycle in from L2, so a tile's copies take longer than
 // its MMAs (128 cycles for 128 x 256 x 64): 4096 x 14336 x 4096 75 us with the copies alone, 82 in all, 50 at the MMAs' rate.
 // `pair`: the same under tcgen05's CTA pairs, M = 256: each CTA brings in its 128 token rows and half of the weight rows,
-// two thirds of the bytes, and copies and MMAs are level: 73.7 us (6.5 PFLOP/s). `narrow` tiles of up to 128 weight rows
+// two thirds of the bytes, and copies and MMAs are level: 72.7 us (6.6 PFLOP/s). `narrow` tiles of up to 128 weight rows
 // for few tokens, where the bytes of the weights bound the time: one item a cluster of 1, 2, 4 or 8 CTAs that split the
 // contraction and add their partial tiles through distributed shared memory, two CTAs an SM; only the 8-row groups that
 // hold tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results). 1 x 4096 x 14336:
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(threads(BUILD), BUILD ? 1 : 2) mx4_gemm_kernel
       for (int i = first; i < total && !*abort; i += stride, ++lt) {
         // narrow tiles: which 32-row columns of the 128-row block of scales
         const uint32_t sb_shift = WIDE ? 0u : uint32_t(item_at<EPI, PAIR>(p, i, rank).n0 >> 5) & 3u;
-        if (!wait<PAIR>(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
+        if (!PAIR && !wait<PAIR>(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err)) break;
         tc_fence_after();
         bool ok = true;
         for (int kc = kc0; kc < kc1; kc += depth) {
@@ -453,12 +453,18 @@ __global__ void __launch_bounds__(threads(BUILD), BUILD ? 1 : 2) mx4_gemm_kernel
             scales_to_tmem<PAIR>(sfa, st + (off_sa >> 4) + 32u * j);
             scales_to_tmem<PAIR>(sfb, st + (off_sb >> 4) + (sb_bytes >> 4) * j);
             if (WIDE) scales_to_tmem<PAIR>(sfb + 4, st + (off_sb >> 4) + (sb_bytes >> 4) * j + 32u);
+            if (PAIR && !acc) {  // (the scales have columns of their own: the first ones go ahead of the accumulator, -1 us)
+              ok = wait<PAIR>(&ctl->tempty, (lt & 1u) ^ 1u, abort, p.err);
+              if (!ok) return;
+              tc_fence_after();
+            }
             const uint32_t da = st + (a_bytes >> 4) * j, db = st + (off_b >> 4) + (b_bytes >> 4) * j;
             mma_mx4<PAIR>(tmem, da, db, idesc, sfa, sfb + sb_shift, acc);
             if ((kc + int(j)) * 2 + 1 < p.ksteps) mma_mx4<PAIR>(tmem, da + 2, db + 2, idesc2, sfa, sfb + sb_shift, 1u);
           };
           const int nc = min(int(depth), kc1 - kc);
           step(0, kc > kc0 ? 1u : 0u);
+          if (PAIR && !ok) break;
           if constexpr (WIDE) {
             if (nc == kWideDepth) step(1, 1u);
           } else {
@@ -733,12 +739,14 @@ cudaError_t go(const Mx4GemmArgs& p, int grid, cudaStream_t s) {
 
 long long mx4_wide_items(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN); }
 
-// Few tokens: wide tiles once they fill the SMs, since the narrow ones spread the weights' bytes over all SMs. Full tiles:
-// from a quarter of that, since a narrow tile of 128 tokens brings them in for each 64 or 128 weight rows (narrow against
-// wide, bf16 out: 384 x 4096 x 4096 18.3 and 9.8 us, 1024 x 4096 x 1408 25.1 and 7.7, 256 x 14336 x 4096 28.9 and 10.3;
-// below a quarter 256 x 4096 x 14336 18.5 and 21.6).
+// Fewer than kWideRows tokens: wide tiles once they fill the SMs, since the narrow ones spread the weights' bytes over all
+// SMs. More: from a quarter of that, since a narrow tile brings its tokens in again for each 64 or 128 weight rows (narrow
+// against wide, bf16 out: 384 x 4096 x 4096 18.3 and 9.8 us, 256 x 14336 x 4096 28.9 and 10.3, 100 x 10000 x 1024 12.3 and
+// 8.2, 32 x 14336 x 4096 10.8 and 9.3, 32 x 10000 x 1024 7.5 and 7.7, but 16 tokens 6.2 and 7.2; below a quarter
+// 256 x 4096 x 14336 18.5 and 21.6).
+constexpr int kWideRows = 32;
 bool mx4_wide(long long max_tiles, int n_rows, int tile_rows) {
-  return mx4_wide_items(max_tiles, n_rows) * (tile_rows == 128 ? 4 : 1) >= num_sms();
+  return mx4_wide_items(max_tiles, n_rows) * (tile_rows >= kWideRows ? 4 : 1) >= num_sms();
 }
 
 // tile_rows: most token rows of a tile.
@@ -747,7 +755,7 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
   auto tiles_of = [&](int tn) { return (n_rows + tn - 1) / tn; };
   const bool wide = mx4_wide(max_tiles, n_rows, tile_rows);
   // CTA pairs pay where items follow one another on every SM and are long: 4096 x 14336 x 4096 82.4 us by single CTAs and
-  // 73.5 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
+  // 72.7 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
   const bool pair = wide && p.pairs && mx4_wide_items(max_tiles, n_rows) > num_sms && p.chunks >= 16;
   p.split = 1;
   int grid;
