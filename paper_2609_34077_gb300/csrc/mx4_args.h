@@ -73,9 +73,10 @@ struct Mx4GemmArgs {
 // sums (T rows of 64 or 128 columns) stays short.
 constexpr int kMx4FusedCombineT = 16;
 
-// Most items of a product by wide tiles; whether it takes them. tile_rows: most token rows of a tile.
+// Most items of a product by wide tiles; whether it takes them. tile_rows: most token rows of a tile; chunks: of the
+// contraction.
 long long mx4_wide_items(long long max_tiles, int n_rows);
-bool mx4_wide(long long max_tiles, int n_rows, int tile_rows);
+bool mx4_wide(long long max_tiles, int n_rows, int tile_rows, int chunks);
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s);
 
 // Workspace of one layer forward.

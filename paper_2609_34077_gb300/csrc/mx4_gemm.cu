@@ -740,20 +740,24 @@ cudaError_t go(const Mx4GemmArgs& p, int grid, cudaStream_t s) {
 long long mx4_wide_items(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN); }
 
 // Fewer than kWideRows tokens: wide tiles once they fill the SMs, since the narrow ones spread the weights' bytes over all
-// SMs. More: from a quarter of that, since a narrow tile brings its tokens in again for each 64 or 128 weight rows (narrow
-// against wide, bf16 out: 384 x 4096 x 4096 18.3 and 9.8 us, 256 x 14336 x 4096 28.9 and 10.3, 100 x 10000 x 1024 12.3 and
-// 8.2, 32 x 14336 x 4096 10.8 and 9.3, 32 x 10000 x 1024 7.5 and 7.7, but 16 tokens 6.2 and 7.2; below a quarter
-// 256 x 4096 x 14336 18.5 and 21.6).
+// SMs. More: from a quarter of that, since a narrow tile brings its tokens in again for each 64 or 128 weight rows and joins
+// them through shared memory; full tiles from an eighth, but for long contractions, which want to be split; and always for
+// short ones, where a narrow tile's fixed 10 us are most of its time. Narrow against wide, us, bf16 out: 256 x 14336 x 4096
+// 28.9 and 10.3, 100 x 10000 x 1024 12.3 and 8.2, 32 x 14336 x 4096 10.8 and 9.3, 32 x 10000 x 1024 7.5 and 7.7, but 16 tokens
+// 6.2 and 7.2; 256 x 4096 x 6144 13.9 and 11.8, but 256 x 4096 x 14336 18.5 and 21.6; 500 x 512 x 512 10.8 and 6.2, 129 x 256 x
+// 2944 9.8 and 8.2, 128 x 1000 x 4096 11.3 and 11.8.
 constexpr int kWideRows = 32;
-bool mx4_wide(long long max_tiles, int n_rows, int tile_rows) {
-  return mx4_wide_items(max_tiles, n_rows) * (tile_rows >= kWideRows ? 4 : 1) >= num_sms();
+bool mx4_wide(long long max_tiles, int n_rows, int tile_rows, int chunks) {
+  if (tile_rows == 128 && chunks <= 32) return true;
+  const int share = tile_rows < kWideRows ? 1 : tile_rows < 128 || chunks > 64 ? 4 : 8;
+  return mx4_wide_items(max_tiles, n_rows) * share >= num_sms();
 }
 
 // tile_rows: most token rows of a tile.
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s) {
   const int n_rows = epi == kMx4Up ? 2 * p.n_out : p.n_out;
   auto tiles_of = [&](int tn) { return (n_rows + tn - 1) / tn; };
-  const bool wide = mx4_wide(max_tiles, n_rows, tile_rows);
+  const bool wide = mx4_wide(max_tiles, n_rows, tile_rows, p.chunks);
   // CTA pairs pay where items follow one another on every SM and are long: 4096 x 14336 x 4096 82.4 us by single CTAs and
   // 72.7 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
   const bool pair = wide && p.pairs && mx4_wide_items(max_tiles, n_rows) > num_sms && p.chunks >= 16;

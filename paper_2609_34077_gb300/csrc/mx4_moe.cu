@@ -382,7 +382,7 @@ Mx4MoeLayout::Mx4MoeLayout(const mcft_layer_desc* desc, int T) {
   x = place(Mx4Layout(x_rows, d).bytes());
   h = place(Mx4Layout(tiles * 128, w).bytes());
   const size_t o_rows = size_t(n) + size_t(S) * T;
-  fused_combine = T <= kMx4FusedCombineT && !mx4_wide(tiles, d, T);
+  fused_combine = T <= kMx4FusedCombineT && !mx4_wide(tiles, d, T, int((w + 127) / 128));
   half_o = dtype == MCFT_BF16 && mx4_wide_items(tiles, d) >= num_sms();  // (a smaller o stays in L2 anyway)
   o = place(sizeof(float) * o_rows * d);  // (also where fp16 takes half of it: fewer tokens may need fp32)
   o_unit = place(half_o ? sizeof(float) * o_rows * ((d + 127) / 128) : 0);
