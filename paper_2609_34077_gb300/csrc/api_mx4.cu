@@ -215,8 +215,7 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   m.xq = ws + L.x;
   m.x_tile0 = int(L.routed_tiles);
   m.x_rows = x_rows;
-  m.o = ws + L.o;
-  m.o_unit = L.half_o ? reinterpret_cast<const float*>(ws + L.o_unit) : nullptr;
+  m.o = reinterpret_cast<const float*>(ws + L.o);
   m.y = y;
   m.err = device_error_word();
   cudaError_t e = launch_mx4_prepare(m, desc->dtype, L.permuted, stream);
@@ -258,7 +257,6 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   operand(p.h, lh, B.down, B.up.bytes(), w);
   p.n_out = d;
   p.out = ws + L.o;
-  p.out_scale = L.half_o ? reinterpret_cast<float*>(ws + L.o_unit) : nullptr;
   p.ldo = d;
   if (L.fused_combine) {
     p.y = y;

@@ -54,8 +54,7 @@ struct Mx4GemmArgs {
   int pairs;                    // wide tiles may go by CTA pairs: the segments have tiles enough
   void* out;                    // down, out
   long long ldo;
-  int out_f32, vec;             // vec: rows of y are whole 64-byte pieces on 32-byte boundaries
-  float* out_scale;             // down: units of an fp16 o, [rows of o][ceil(n_out / 128)]; NULL: o is fp32
+  int out_f32, vec;             // out; vec: rows of y are whole 64-byte pieces on 32-byte boundaries
   uint8_t *h, *h_scales;        // up
   size_t h_code_stride, h_scale_stride;
   unsigned* err;
@@ -73,9 +72,7 @@ struct Mx4GemmArgs {
 // sums (T rows of 64 or 128 columns) stays short.
 constexpr int kMx4FusedCombineT = 16;
 
-// Most items of a product by wide tiles; whether it takes them. tile_rows: most token rows of a tile; chunks: of the
-// contraction.
-long long mx4_wide_items(long long max_tiles, int n_rows);
+// Whether a product goes by wide tiles. tile_rows: most token rows of a tile; chunks: of the contraction.
 bool mx4_wide(long long max_tiles, int n_rows, int tile_rows, int chunks);
 cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int tile_rows, int num_sms, cudaStream_t s);
 
@@ -83,9 +80,8 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
 struct Mx4MoeLayout {
   bool permuted;
   long long routed_tiles, x_tiles, tiles;  // most tiles of the routed experts; tiles of x itself; all tiles
-  bool half_o;     // o as fp16 under a unit for each row's 128 columns (bf16 layers whose wide tiles fill the SMs), else fp32
   bool fused_combine;
-  size_t hdr, tile, rowmap, src, pos, done, x, h, o, o_unit, total;
+  size_t hdr, tile, rowmap, src, pos, done, x, h, o, total;
   Mx4MoeLayout(const mcft_layer_desc* desc, int T);
 };
 
@@ -102,8 +98,7 @@ struct Mx4MoeArgs {
   uint8_t* xq;
   int x_tile0;     // first tile of x itself, in the permuted form
   long long x_rows;  // rows of xq
-  const void* o;         // fp32, or (with o_unit) fp16
-  const float* o_unit;
+  const float* o;
   void* y;
   unsigned* err;
 };

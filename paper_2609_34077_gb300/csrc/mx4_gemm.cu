@@ -8,7 +8,7 @@
 // Tokens are on M (128 rows of a tile), weight rows on N, so that in the epilogue a thread owns one token row:
 // 32 outputs of it are a block, quantised without leaving the thread. Three epilogues:
 //   up    the weight rows are 32 gate and 32 up rows in turn: h = silu(gate) * up, to mx4 (Section 3.1's F);
-//   down  rows of o, to the assignment's place: fp32, or 16 bits (below);
+//   down  fp32 rows of o, to the assignment's place;
 //   out   fp32 or bf16 rows of y (the plain product).
 //
 // Three builds. `wide` tiles of 128 x 256 for prompts: a persistent grid, one CTA an SM; the eight epilogue warps
@@ -23,15 +23,9 @@
 // hold tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results). 1 x 4096 x 14336:
 // 8.0 us a replayed graph's node, 4.6 at HBM's rate; the layer of 16 tokens on 8 experts of 4096 x 14336 109 us, its floor.
 //
-// For bf16 layers wide tiles write o as fp16 under a power-of-two unit for each row's 128 columns (the largest of them in [2^14, 2^15)
-// units): its 11 bits cost y an error of 2^-11, an eighth of its own rounding to bf16, and o is moved twice (here and
-// by the combine), which in fp32 took most of both kernels' time.
-//
 // Warp 0 issues the copies (pair: warp 10 those of the tokens), warp 1 the tcgen05.cp and MMAs and owns the tensor memory
 // (pair: the second CTA's tells the first of its copies), warps 2-9 are the epilogue. Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again
 // with a limit) for its copies and MMAs in flight, frees the tensor memory and returns.
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <type_traits>
 
@@ -537,9 +531,8 @@ __global__ void __launch_bounds__(threads(BUILD), BUILD ? 1 : 2) mx4_gemm_kernel
           if (EPI == kMx4Down) dst = p.rowmap[dst];
         }
         const int cols = min(128, p.n_out - n);
-        const bool f32 = EPI == kMx4Down ? !p.out_scale : p.out_f32;
         if (cols <= 0) {
-        } else if (f32) {
+        } else if (EPI == kMx4Down || p.out_f32) {
           float* y = static_cast<float*>(p.out) + dst * p.ldo + n;
           if constexpr (EPI != kMx4OutAny) {
 #pragma unroll
@@ -558,25 +551,8 @@ __global__ void __launch_bounds__(threads(BUILD), BUILD ? 1 : 2) mx4_gemm_kernel
             }
           }
         } else {
-          if (EPI == kMx4Down) {
-            uint32_t m = 0;  // largest finite magnitude (past n_out: leftovers of other rows; the store leaves them out)
 #pragma unroll
-            for (int c = 0; c < 128; ++c) {
-              const uint32_t b = v[c] & 0x7fffffffu;
-              m = max(m, c < cols && b < 0x7f800000u ? b : 0u);
-            }
-            const int e = max(int(m >> 23), 15);  // (values below 2^-112 in units of 2^-126)
-            const float inv = __uint_as_float(uint32_t(268 - e) << 23);
-            if (dst >= 0) p.out_scale[dst * ((p.n_out + 127) >> 7) + (n >> 7)] = __uint_as_float(uint32_t(e - 14) << 23);
-#pragma unroll
-            for (int c = 0; c < 64; ++c) {
-              const __half2 h = __floats2half2_rn(__uint_as_float(v[2 * c]) * inv, __uint_as_float(v[2 * c + 1]) * inv);
-              v[c] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-          } else {
-#pragma unroll
-            for (int c = 0; c < 64; ++c) v[c] = pack2bf(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
-          }
+          for (int c = 0; c < 64; ++c) v[c] = pack2bf(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
           uint16_t* y = static_cast<uint16_t*>(p.out) + dst * p.ldo + n;
           if constexpr (EPI != kMx4OutAny) {
 #pragma unroll
@@ -737,7 +713,8 @@ cudaError_t go(const Mx4GemmArgs& p, int grid, cudaStream_t s) {
 
 }  // namespace
 
-long long mx4_wide_items(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN); }
+// Most items of a product by wide tiles.
+static long long wide_items(long long max_tiles, int n_rows) { return max_tiles * ((n_rows + kWideN - 1) / kWideN); }
 
 // Fewer than kWideRows tokens: wide tiles once they fill the SMs, since the narrow ones spread the weights' bytes over all
 // SMs. More: from a quarter of that, since a narrow tile brings its tokens in again for each 64 or 128 weight rows and joins
@@ -750,7 +727,7 @@ constexpr int kWideRows = 32;
 bool mx4_wide(long long max_tiles, int n_rows, int tile_rows, int chunks) {
   if (tile_rows == 128 && chunks <= 32) return true;
   const int share = tile_rows < kWideRows ? 1 : tile_rows < 128 || chunks > 64 ? 4 : 8;
-  return mx4_wide_items(max_tiles, n_rows) * share >= num_sms();
+  return wide_items(max_tiles, n_rows) * share >= num_sms();
 }
 
 // tile_rows: most token rows of a tile.
@@ -760,7 +737,7 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
   const bool wide = mx4_wide(max_tiles, n_rows, tile_rows, p.chunks);
   // CTA pairs pay where items follow one another on every SM and are long: 4096 x 14336 x 4096 82.4 us by single CTAs and
   // 72.7 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
-  const bool pair = wide && p.pairs && mx4_wide_items(max_tiles, n_rows) > num_sms && p.chunks >= 16;
+  const bool pair = wide && p.pairs && wide_items(max_tiles, n_rows) > num_sms && p.chunks >= 16;
   p.split = 1;
   int grid;
   if (wide) {

@@ -9,13 +9,11 @@
 //
 // All four kernels are short: 16 tokens' plan 4 us (launch and a chain of barriers), 4096 tokens of d = 2048 on 64 experts
 // permutation 9.7 us (one cluster: latency), spread 11.4 us alone and mostly behind the permutation (17 MB in, 31 out),
-// combine 30.4 us (134 MB of fp16 outputs in, 17 out: 5 TB/s, HBM and L2).
+// combine 43 us (268 MB of fp32 outputs in, 17 out: 6.6 TB/s, HBM and L2).
 //
 // Rows of o are in the order of the assignments (t, k), then the shared experts' (s, t), so the combine needs no
 // lookup but `src`: the assignment whose row holds expert idx[t, k]'s output for token t (itself; the first of
 // them where a token names an expert twice; -1 where it names none).
-#include <cuda_fp16.h>
-
 #include <algorithm>
 
 #include "mx4_args.h"
@@ -269,21 +267,19 @@ __global__ void __launch_bounds__(256) mx4_spread_kernel(const __grid_constant__
   }
 }
 
-// y[t] = sum_k gate[t, k] o[src[t, k]] + sum_s o[shared s, t], in this order; eight columns a thread. HALF: o is fp16
-// in units.
-template <typename T, bool HALF>
+// y[t] = sum_k gate[t, k] o[src[t, k]] + sum_s o[shared s, t], in this order; eight columns a thread. o is fp32: terms that
+// nearly cancel leave their difference, and y is rounded once.
+template <typename T>
 __global__ void __launch_bounds__(128) mx4_combine_kernel(const __grid_constant__ Mx4MoeArgs a) {
   pdl_wait();
   if (a.hdr->abort) return;
   const int lane = threadIdx.x & 31;
   const int t = int(blockIdx.x), c = (int(blockIdx.y) * 128 + int(threadIdx.x)) * 8;
-  const int units = (a.d + 127) >> 7, n = a.K + a.S;
-  const float* o32 = static_cast<const float*>(a.o);
-  const __half* o16 = static_cast<const __half*>(a.o);
+  const int n = a.K + a.S;
   static_assert(kMaxMx4K + kMaxShared <= 32, "a lane each");
-  // lane k: the k-th row and its factor (HALF: times the units of the warp's first and last 128 columns)
+  // lane k: the k-th row and its factor
   long long row = -1;
-  float g = 0.f, g_last = 0.f;
+  float g = 0.f;
   if (lane < a.K) {
     row = a.src[(long long)t * a.K + lane];
     if (row >= 0) g = a.gate[(long long)t * a.K + lane];
@@ -291,50 +287,27 @@ __global__ void __launch_bounds__(128) mx4_combine_kernel(const __grid_constant_
     row = (long long)a.T * a.K + (long long)(lane - a.K) * a.T + t;
     g = 1.f;
   }
-  if (HALF && row >= 0) {
-    const int u = (c - lane * 8) >> 7;
-    const float* unit = a.o_unit + row * units;
-    g_last = u + 1 < units ? g * __ldg(unit + u + 1) : 0.f;
-    g = u < units ? g * __ldg(unit + u) : 0.f;
-  }
   float acc[8] = {};
-  constexpr int kAtOnce = 4;  // rows in flight (2 and 8: 34.5 and 41 us where 4 take 30.4)
+  constexpr int kAtOnce = 4;  // rows in flight (with 2 and 8 the same 43 us)
   for (int k0 = 0; k0 < n; k0 += kAtOnce) {
     float f[kAtOnce];
-    uint4 v[kAtOnce][HALF ? 1 : 2];
+    uint4 v[kAtOnce][2];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const long long r = __shfl_sync(0xffffffffu, row, k0 + i);  // (past n: -1)
       f[i] = __shfl_sync(0xffffffffu, g, k0 + i);
-      if constexpr (HALF) {
-        const float last = __shfl_sync(0xffffffffu, g_last, k0 + i);
-        if (lane >= 16) f[i] = last;
-      }
       if (r < 0 || c >= a.d) {
-#pragma unroll
-        for (int q = 0; q < (HALF ? 1 : 2); ++q) v[i][q] = make_uint4(0, 0, 0, 0);
-      } else if constexpr (HALF) {
-        v[i][0] = ld_stream16(o16 + r * a.d + c);
+        v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
       } else {
-        v[i][0] = ld_stream16(o32 + r * a.d + c);
-        v[i][1] = ld_stream16(o32 + r * a.d + c + 4);
+        v[i][0] = ld_stream16(a.o + r * a.d + c);
+        v[i][1] = ld_stream16(a.o + r * a.d + c + 4);
       }
     }
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      if constexpr (HALF) {
-        const uint32_t w[4] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w};
+      const uint32_t w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-          acc[2 * j] = fmaf(f[i], h.x, acc[2 * j]);
-          acc[2 * j + 1] = fmaf(f[i], h.y, acc[2 * j + 1]);
-        }
-      } else {
-        const uint32_t w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = fmaf(f[i], __uint_as_float(w[j]), acc[j]);
-      }
+      for (int j = 0; j < 8; ++j) acc[j] = fmaf(f[i], __uint_as_float(w[j]), acc[j]);
     }
   }
   if (c >= a.d) return;
@@ -353,7 +326,7 @@ size_t align512(size_t v) { return (v + 511) & ~size_t(511); }
 }  // namespace
 
 Mx4MoeLayout::Mx4MoeLayout(const mcft_layer_desc* desc, int T) {
-  const int d = desc->d, E = desc->E, K = desc->K, w = desc->w, S = desc->n_shared, dtype = desc->dtype;
+  const int d = desc->d, E = desc->E, K = desc->K, w = desc->w, S = desc->n_shared;
   const long long n = (long long)T * K;
   permuted = T > kMx4SharedTileT;
   if (permuted) {
@@ -383,9 +356,7 @@ Mx4MoeLayout::Mx4MoeLayout(const mcft_layer_desc* desc, int T) {
   h = place(Mx4Layout(tiles * 128, w).bytes());
   const size_t o_rows = size_t(n) + size_t(S) * T;
   fused_combine = T <= kMx4FusedCombineT && !mx4_wide(tiles, d, T, int((w + 127) / 128));
-  half_o = dtype == MCFT_BF16 && mx4_wide_items(tiles, d) >= num_sms();  // (a smaller o stays in L2 anyway)
-  o = place(sizeof(float) * o_rows * d);  // (also where fp16 takes half of it: fewer tokens may need fp32)
-  o_unit = place(half_o ? sizeof(float) * o_rows * ((d + 127) / 128) : 0);
+  o = place(sizeof(float) * o_rows * d);
   total = at;
 }
 
@@ -411,8 +382,7 @@ cudaError_t launch_mx4_prepare(const Mx4MoeArgs& a, int dtype, bool permuted, cu
 cudaError_t launch_mx4_combine(const Mx4MoeArgs& a, int dtype, cudaStream_t s) {
   prof_begin(kProfMx4Combine, s);
   const dim3 grid(unsigned(a.T), unsigned((a.d + 1023) / 1024));
-  auto* k = dtype == MCFT_BF16 ? (a.o_unit ? mx4_combine_kernel<__nv_bfloat16, true> : mx4_combine_kernel<__nv_bfloat16, false>)
-                               : (a.o_unit ? mx4_combine_kernel<float, true> : mx4_combine_kernel<float, false>);
+  auto* k = dtype == MCFT_BF16 ? mx4_combine_kernel<__nv_bfloat16> : mx4_combine_kernel<float>;
   const cudaError_t e = launch_pdl(k, grid, dim3(128), 0, s, a);
   prof_end(kProfMx4Combine, s);
   return e != cudaSuccess ? e : cudaGetLastError();
