@@ -2,7 +2,7 @@
 //
 // Few tokens (kFewT) and small weights: latency bounds it. A cluster of eight CTAs takes kFewTokens tokens: its 64 warps share the
 // experts, each streaming its rows of W once against all of the tokens (held in shared memory), and the logits meet
-// in the leader's shared memory, where one warp ranks a token. One token of d = 2048, E = 64: 5.1 us a replayed graph's
+// in the leader's shared memory, where one warp ranks a token. One token of d = 2048, E = 64: 5.2 us a replayed graph's
 // node, of which the 256 kB of W are 0.04 at HBM's rate; the rest is the launch, one round of loads, two cluster barriers
 // and the choice's chain of shuffles.
 // Otherwise: fp32 layers (and rows too wide for the first) take tiles of 32 tokens by all experts, fp32 multiply-adds
@@ -20,8 +20,11 @@ __device__ __forceinline__ uint32_t cta_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
 __device__ __forceinline__ void store_leader(float* p, float v) {
   asm volatile(
@@ -49,6 +52,7 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
   extern __shared__ uint4 xs[];  // [tokens][d] of T
   __shared__ __align__(16) float zs[kFewTokens][32 * PL], buf[kFewTokens][64 * PL];
   __shared__ int count[32 * PL];
+  cluster_arrive();  // waited for ahead of the first store to the leader: its shared memory is there once it has begun
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = int(cta_rank());
@@ -59,6 +63,7 @@ __global__ void __cluster_dims__(kFewCtas, 1, 1) __launch_bounds__(kFewThreads)
   for (int i = tid; i < nt * words; i += kFewThreads) xs[i] = __ldg(x + i);
   if (tid < 32 * PL) count[tid] = 0;
   __syncthreads();
+  cluster_wait();
   for (int e = rank + kFewCtas * warp; e < a.E; e += kFewCtas * (kFewThreads / 32)) {
     const T* w = static_cast<const T*>(a.w_router) + size_t(e) * a.d;
     float acc[kFewTokens] = {};
@@ -219,7 +224,7 @@ cudaError_t launch_tiles(const ScoredArgs& a, cudaStream_t s) {
 }
 
 // bf16 calls on the tensor cores: many tokens, or weights that one cluster is slow to read (replayed graphs, us: 5 tokens
-// of d = 2048, E = 64 7.1 by clusters, 7.9 on the tensor cores; 64 tokens 7.5 and 8.5; d = 4096, E = 256: one token
+// of d = 2048, E = 64 7.1 by clusters, 7.9 on the tensor cores; 64 tokens 7.9 and 8.5; d = 4096, E = 256: one token
 // 16.7 and 11.3, 64 tokens 25.9 and 13.4).
 bool scored_forward_on_tc(const ScoredArgs& a) { return a.T > kScoredTcMinT || (long long)a.E * a.d >= 1 << 18; }
 
