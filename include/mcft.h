@@ -534,7 +534,7 @@ typedef struct {
  *   x        device [T, d] layer dtype; w_router device [E, d] layer dtype; both 16-byte aligned
  *   bias     device [E] fp32, or NULL
  *   idx      device [T, K] int32 out, by descending c;  gate device [T, K] fp32 out
- *   logits   device [T, E] fp32 out: z, for mcft_route_scored_grad; or NULL
+ *   logits   device [T, E] fp32 out: z, for mcft_route_scored_grad; or NULL (any fp32 alignment)
  *   load     device [E] int32 out: how many tokens chose each expert, from which a caller moves the bias;
  *            or NULL
  * Logits are fp32 sums. A NaN score or bias sets the device error word and keeps its expert out. T = 0 is a

@@ -120,7 +120,8 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
     for (int j = 0; j < PL; ++j) s[j] = __frcp_rn(1.f + expf(-z[j]));
   }
   bool nan = false;
-  const bool whole = E % VW == 0;  // (runs end with the experts, and rows of logits are aligned to them)
+  // runs end with the experts, and rows of logits are aligned to them (16 bytes, wherever the caller's logits begin)
+  const bool whole = E % VW == 0 && (reinterpret_cast<uintptr_t>(a.logits) & 15u) == 0;
 #pragma unroll
   for (int h = 0; h < PL; h += VW) {
     const int e0 = expert_of<PL>(h);
