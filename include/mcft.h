@@ -552,8 +552,8 @@ mcft_status mcft_route_scored(const mcft_scored_desc* desc, const void* x, int T
  *            nothing and its gate and dgate are not read into the sum; another id outside [0, E) sets the
  *            device error word and counts as -1
  *   dgate    device [T, K] fp32
- *   dx       device [T, d] layer dtype out, or NULL
- *   dw       device [E, d] fp32 out, added to what it holds if accumulate is non-zero; or NULL
+ *   dx       device [T, d] layer dtype out, 16-byte aligned, or NULL
+ *   dw       device [E, d] fp32 out, 16-byte aligned, added to what it holds if accumulate is non-zero; or NULL
  *   workspace device, mcft_route_scored_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until
  *            the call's kernels finish; enough for any smaller T
  * T = 0 writes zeros to dw (unless accumulating). Asynchronous; the same bits whenever the inputs are the

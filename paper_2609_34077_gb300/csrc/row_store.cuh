@@ -12,12 +12,21 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* v) {
                : "memory");
 }
 
-// 64 bytes u of each lane's own row to global memory, at `row` (NULL: none), by a whole warp. Two neighbouring lanes
+// The same in two instructions; 16-byte aligned.
+__device__ __forceinline__ void store32_by16(void* p, const uint32_t* v) {
+  uint4* q = reinterpret_cast<uint4*>(p);
+  q[0] = make_uint4(v[0], v[1], v[2], v[3]);
+  q[1] = make_uint4(v[4], v[5], v[6], v[7]);
+}
+
+// 64 bytes u of each lane's own row to global memory, at `row` (NULL: none; ALIGN: bytes to which it is aligned, 32 or 16), by a whole warp. Two neighbouring lanes
 // first exchange halves, so that an instruction writes 64 contiguous bytes of 16 rows, not 32 of 32: each line that a
 // store touches takes the way through L1 that the copies into shared memory take too (mx4 product of 4096 x 14336 x
 // 4096: 16, 32, 64 and 128 bytes a row 109, 83.2, 82.2 and 83.8 us, the exchange of four lanes costing more than it
 // gives).
+template <int ALIGN = 32>
 __device__ __forceinline__ void store_rows64(void* row, uint32_t* u) {
+  static_assert(ALIGN == 32 || ALIGN == 16, "alignment of the rows");
   const uint32_t lane = threadIdx.x & 31u;
   const bool odd = lane & 1u;
 #pragma unroll
@@ -29,7 +38,9 @@ __device__ __forceinline__ void store_rows64(void* row, uint32_t* u) {
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     const unsigned long long at = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), (lane & ~1u) + r);
-    if (at) store32(reinterpret_cast<char*>(at) + odd * 32, u + 8 * r);
+    char* to = reinterpret_cast<char*>(at) + odd * 32;
+    if (at && ALIGN == 32) store32(to, u + 8 * r);
+    if (at && ALIGN == 16) store32_by16(to, u + 8 * r);
   }
 }
 

@@ -47,3 +47,35 @@ def test_logits_anywhere(T, d, E, K, dtype, offset):
     a, b = (M.mcft_route_scored_grad(D, x, w, idx, gate, z, dg) for z in (want, logits))
     M.mcft_device_error()
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# up to 64 tokens and fp32 by multiply-adds, else the tensor cores; 16-byte offsets of which one is on 32 bytes
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,d,E,K", [(3, 256, 64, 4), (64, 128, 256, 8), (65, 64, 16, 2), (300, 320, 100, 3), (1100, 2048, 256, 8)])
+@pytest.mark.parametrize("at", [16, 32, 48])
+def test_gradients_on_16_bytes(T, d, E, K, dtype, at):
+    x, w = inputs(T, d, E, dtype)
+    D = desc_of(d, E, K, dtype, "sigmoid")
+    logits = torch.empty(T, E, device="cuda")
+    idx, gate = M.mcft_route_scored(D, x, w, logits=logits)
+    dg = torch.randn(T, K, generator=torch.Generator().manual_seed(1)).cuda()
+    want = M.mcft_route_scored_grad(D, x, w, idx, gate, logits, dg)
+    dx, xbuf = inside(at // x.element_size(), dtype, T, d)
+    dw, wbuf = inside(at // 4, torch.float32, E, d)
+    assert dx.data_ptr() % 32 == at % 32 == dw.data_ptr() % 32
+    M.mcft_route_scored_grad(D, x, w, idx, gate, logits, dg, dx=dx, dw=dw)
+    M.mcft_device_error()
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
+    assert untouched(xbuf, at // x.element_size(), T * d) and untouched(wbuf, at // 4, E * d)
+
+
+def test_a_dx_off_16_bytes_is_refused():
+    x, w = inputs(70, 64, 16, torch.bfloat16)
+    D = desc_of(64, 16, 2, torch.bfloat16)
+    logits = torch.empty(70, 16, device="cuda")
+    idx, gate = M.mcft_route_scored(D, x, w, logits=logits)
+    for offset in (1, 4, 7):
+        with pytest.raises(M.MCFTError) as e:
+            M.mcft_route_scored_grad(D, x, w, idx, gate, logits, gate, dx=inside(offset, torch.bfloat16, 70, 64)[0])
+        assert e.value.status == M.MCFT_ERR_INVALID
+    M.mcft_device_error()
