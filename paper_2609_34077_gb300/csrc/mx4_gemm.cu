@@ -117,10 +117,19 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
 __device__ __forceinline__ void arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-// Relaxed: what it tells of (bulk copies that have landed, tensor memory that has been read) is complete and is not this
-// thread's writes. With release it first waits for the SM's stores on their way to memory, 1250 cycles on average.
+// Of tensor memory that this warp has read, once tcgen05.fence::before_thread_sync has ordered those reads before it: a relaxed
+// arrival does, there are no writes of this thread to be seen.
 __device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Of bulk copies that have landed in this CTA's shared memory, as this thread has seen by an acquiring wait: released to the other
+// CTA by a fence that is restricted to shared memory. (A release of everything first waits for the SM's stores on their
+// way to global memory: 1250 cycles on average.)
+__device__ __forceinline__ void announce(uint32_t cluster_addr) {
+  asm volatile(
+      "fence.release.sync_restrict::shared::cta.cluster;\n\tmbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+          cluster_addr)
+      : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
@@ -415,7 +424,7 @@ __global__ void __launch_bounds__(threads(BUILD), BUILD ? 1 : 2) mx4_gemm_kernel
           for (int kc = kc0; kc < kc1; kc += depth) {
             ok = mbar_wait_cl(&ctl->full[s], ph, abort, p.err);
             if (!ok) break;
-            arrive_relaxed(peer_addr(&ctl->full[s], 0));
+            announce(peer_addr(&ctl->full[s], 0));
             if (++s == stages) {
               s = 0;
               ph ^= 1u;
