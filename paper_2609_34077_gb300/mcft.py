@@ -550,6 +550,21 @@ def mcft_mask_grad(desc: LayerDesc, idx, gate, dgate, pi, dm=None, dm_tilde=None
 MCFT_SCORE_SOFTMAX, MCFT_SCORE_SIGMOID = 0, 1
 
 
+def _wants(ok, what):
+    """The calls below take sizes that the library cannot compare with the memory behind an address: a tensor of another
+    size or type is refused here, as the library refuses other arguments."""
+    if not ok:
+        raise MCFTError(MCFT_ERR_INVALID, what)
+
+
+def _is(t, dtype, *shape):
+    return t.dtype == dtype and t.shape == shape
+
+
+def _nbytes(t):
+    return t.numel() * t.element_size()
+
+
 class ScoredDesc(C.Structure):
     """mcft_scored_desc"""
     _fields_ = [("d", C.c_int), ("E", C.c_int), ("K", C.c_int), ("n_group", C.c_int), ("topk_group", C.c_int),
@@ -557,15 +572,29 @@ class ScoredDesc(C.Structure):
                 ("scale", C.c_float)]
 
 
+def _wants_router(desc, x, w_router):
+    dtype = torch_dtype(desc)
+    _wants(_is(x, dtype, x.shape[0], desc.d), "x is [T, d] of the layer dtype")
+    _wants(w_router.dtype == dtype and w_router.numel() >= desc.E * desc.d, "w_router is [E, d] of the layer dtype")
+
+
 def mcft_route_scored(desc: ScoredDesc, x, w_router, bias=None, idx=None, gate=None, logits=None, load=None,
                       stream=None):
     """idx [T, K] int32 (-1: no eligible expert) and gate [T, K] fp32 (allocated on x's device if not given);
     writes logits [T, E] fp32 and load [E] int32 where given."""
     T = x.shape[0]
+    _wants_router(desc, x, w_router)
+    _wants(bias is None or _is(bias, torch.float32, desc.E), "bias is fp32 [E]")
     if idx is None:
         idx = torch.empty((T, desc.K), dtype=torch.int32, device=x.device)
+    else:
+        _wants(_is(idx, torch.int32, T, desc.K), "idx is int32 [T, K]")
     if gate is None:
         gate = torch.empty((T, desc.K), dtype=torch.float32, device=x.device)
+    else:
+        _wants(_is(gate, torch.float32, T, desc.K), "gate is fp32 [T, K]")
+    _wants(logits is None or _is(logits, torch.float32, T, desc.E), "logits is fp32 [T, E]")
+    _wants(load is None or _is(load, torch.int32, desc.E), "load is int32 [E]")
     _check(lib().mcft_route_scored(C.byref(desc), _ptr(x), T, _ptr(w_router), _ptr(bias), _ptr(idx), _ptr(gate),
                                    _ptr(logits), _ptr(load), _stream(stream)))
     return idx, gate
@@ -582,13 +611,18 @@ def mcft_route_scored_grad(desc: ScoredDesc, x, w_router, idx, gate, logits, dga
     """(dx [T, d] of the layer dtype, dw [E, d] fp32) from dL/dgate and what mcft_route_scored wrote; dw is
     added to if accumulate."""
     T = x.shape[0]
-    assert idx.dtype == torch.int32 and idx.shape == gate.shape == dgate.shape == (T, desc.K) and logits.shape == (T, desc.E), \
-        "idx, gate and dgate are [T, K], logits [T, E]"
+    _wants_router(desc, x, w_router)
+    _wants(_is(idx, torch.int32, T, desc.K) and _is(gate, torch.float32, T, desc.K) and _is(dgate, torch.float32, T, desc.K)
+           and _is(logits, torch.float32, T, desc.E), "idx is int32 [T, K], gate and dgate fp32 [T, K], logits fp32 [T, E]")
     if dx is None:
         dx = torch.empty_like(x)
+    else:
+        _wants(_is(dx, x.dtype, T, desc.d), "dx is [T, d] of the layer dtype")
     if dw is None:
-        assert not accumulate, "accumulate adds to a dw that is given"
+        _wants(not accumulate, "accumulate adds to a dw that is given")
         dw = torch.empty((desc.E, desc.d), dtype=torch.float32, device=x.device)
+    else:
+        _wants(_is(dw, torch.float32, desc.E, desc.d), "dw is fp32 [E, d]")
     if workspace is None:
         workspace = torch.empty(mcft_route_scored_grad_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
     _check(lib().mcft_route_scored_grad(C.byref(desc), _ptr(x), T, _ptr(w_router), _ptr(idx), _ptr(gate), _ptr(logits),
@@ -612,20 +646,29 @@ def mcft_mx4_size(rows: int, cols: int) -> int:
     return n.value
 
 
+def _wants_mx4(q, rows, cols, what):
+    _wants(rows <= 0 or cols <= 0 or _nbytes(q) >= -(-cols // 128) * 512 * (-(-rows // 8) - (-rows // 128)), what)
+
+
 def mcft_mx4_quantize(x, q=None, stream=None):
     """The mx4 matrix (a uint8 tensor of mcft_mx4_size bytes) of x [rows, cols], fp32 or bf16."""
     rows, cols = x.shape
     ptr, ld = _rows(x)
     if q is None:
         q = torch.empty(mcft_mx4_size(rows, cols), dtype=torch.uint8, device=x.device)
+    else:
+        _wants_mx4(q, rows, cols, "q is smaller than mcft_mx4_size(rows, cols)")
     _check(lib().mcft_mx4_quantize(ptr, rows, cols, ld, _MX4_DTYPE[x.dtype], _ptr(q), _stream(stream)))
     return q
 
 
 def mcft_mx4_dequantize(q, rows, cols, dtype=torch.bfloat16, y=None, stream=None):
     """The values [rows, cols] that the mx4 matrix q stands for, fp32 or bf16."""
+    _wants_mx4(q, rows, cols, "q is smaller than mcft_mx4_size(rows, cols)")
     if y is None:
         y = torch.empty((rows, cols), dtype=dtype, device=q.device)
+    else:
+        _wants(y.shape == (rows, cols), "y is [rows, cols]")
     ptr, ld = _rows(y)
     _check(lib().mcft_mx4_dequantize(_ptr(q), rows, cols, _MX4_DTYPE[y.dtype], ptr, ld, _stream(stream)))
     return y
@@ -633,8 +676,12 @@ def mcft_mx4_dequantize(q, rows, cols, dtype=torch.bfloat16, y=None, stream=None
 
 def mcft_mx4_matmul(a, b, M, N, K, dtype=torch.bfloat16, y=None, stream=None):
     """y [M, N] = A B^T of the mx4 matrices a [M, K] and b [N, K], fp32 or bf16."""
+    _wants_mx4(a, M, K, "a is smaller than mcft_mx4_size(M, K)")
+    _wants_mx4(b, N, K, "b is smaller than mcft_mx4_size(N, K)")
     if y is None:
         y = torch.empty((M, N), dtype=dtype, device=a.device)
+    else:
+        _wants(y.shape == (M, N), "y is [M, N]")
     ptr, ld = _rows(y)
     _check(lib().mcft_mx4_matmul(_ptr(a), _ptr(b), M, N, K, _MX4_DTYPE[y.dtype], ptr, ld, _stream(stream)))
     return y
@@ -648,8 +695,12 @@ def mcft_mx4_expert_size(desc: LayerDesc) -> int:
 
 def mcft_mx4_pack_expert(desc: LayerDesc, block, out=None, stream=None):
     """The mx4 expert block (uint8) of a packed expert block [W1 | W3 | W2] of the layer dtype."""
+    size = mcft_mx4_expert_size(desc)
+    _wants(block.dtype == torch_dtype(desc) and block.numel() == 3 * desc.w * desc.d, "block is [W1 | W3 | W2] of the layer dtype")
     if out is None:
-        out = torch.empty(mcft_mx4_expert_size(desc), dtype=torch.uint8, device=block.device)
+        out = torch.empty(size, dtype=torch.uint8, device=block.device)
+    else:
+        _wants(_nbytes(out) >= size, "out is smaller than mcft_mx4_expert_size")
     _check(lib().mcft_mx4_pack_expert(C.byref(desc), _ptr(block), _ptr(out), _stream(stream)))
     return out
 
@@ -665,8 +716,12 @@ def mcft_moe_forward_mx4(desc: LayerDesc, x, idx, gate, experts, shared=(), y=No
     """y [T, d] of the layer on mx4 expert blocks; an idx of -1 is no expert. ``experts`` and
     ``workspace`` as for mcft_moe_forward."""
     T = x.shape[0]
+    _wants(_is(x, torch_dtype(desc), T, desc.d), "x is [T, d] of the layer dtype")
+    _wants(_is(idx, torch.int32, T, desc.K) and _is(gate, torch.float32, T, desc.K), "idx is int32 [T, K], gate fp32 [T, K]")
     if y is None:
         y = torch.empty_like(x)
+    else:
+        _wants(_is(y, x.dtype, T, desc.d), "y is [T, d] of the layer dtype")
     if workspace is None:
         workspace = torch.empty(mcft_mx4_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
     ex = _ptr_array(experts, desc.E)
