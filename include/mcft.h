@@ -461,7 +461,7 @@ void mcft_stack_destroy(mcft_stack* stack);
  * mcft_mx4_dequantize: the values that q stands for, exact in either dtype but for subnormal bf16
  *   results, which round; y device [rows, cols], `ld` elements from row to row.
  * rows = 0 is a no-op. Asynchronous. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer, rows < 0,
- * cols < 1, ld < cols, an unknown dtype. */
+ * cols < 1, ld < cols, an unknown dtype; MCFT_ERR_UNSUPPORTED for rows > 2^31 - 129 or cols > 134215680. */
 mcft_status mcft_mx4_size(long long rows, long long cols, size_t* bytes);
 mcft_status mcft_mx4_quantize(const void* x, long long rows, long long cols, long long ld, int dtype,
                               void* q, mcft_stream_t stream);
@@ -472,7 +472,8 @@ mcft_status mcft_mx4_dequantize(const void* q, long long rows, long long cols, i
  * tensor cores (tcgen05 block-scaled MMAs), rounded once if y is bf16.
  *   y device [M, N] of dtype, `ldy` elements from row to row (16-byte rows are not required).
  * M = 0 or N = 0 is a no-op. Asynchronous; no workspace. Errors: MCFT_ERR_INVALID for a NULL or
- * misaligned pointer, M, N < 0, K < 1, ldy < N, an unknown dtype. */
+ * misaligned pointer, M, N < 0, K < 1, ldy < N, an unknown dtype; MCFT_ERR_UNSUPPORTED for K > 134215680 or
+ * more tiles than an int counts. */
 mcft_status mcft_mx4_matmul(const void* a, const void* b, int M, int N, int K, int dtype, void* y,
                             long long ldy, mcft_stream_t stream);
 

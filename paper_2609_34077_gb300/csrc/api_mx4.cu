@@ -9,10 +9,18 @@
 namespace mcft {
 namespace {
 
-mcft_status check_matrix(const void* q, long long rows, long long cols, int dtype, const void* x, long long ld) {
+// Rows: tiles are counted in ints. Columns: 2048 of them are a step of a grid's second extent (mx4_quant.cu), which ends at 65535.
+constexpr long long kMaxRows = INT_MAX - 128, kMaxCols = 65535LL * 2048;
+
+mcft_status check_size(long long rows, long long cols) {
   if (rows < 0 || cols < 1) return fail(MCFT_ERR_INVALID, "bad rows = %lld or cols = %lld", rows, cols);
-  if (rows > INT_MAX - 128 || cols > INT_MAX / 2)
-    return fail(MCFT_ERR_UNSUPPORTED, "rows = %lld or cols = %lld is too large", rows, cols);
+  if (rows > kMaxRows || cols > kMaxCols) return fail(MCFT_ERR_UNSUPPORTED, "rows = %lld or cols = %lld is too large", rows, cols);
+  return MCFT_OK;
+}
+
+mcft_status check_matrix(const void* q, long long rows, long long cols, int dtype, const void* x, long long ld) {
+  const mcft_status st = check_size(rows, cols);
+  if (st != MCFT_OK) return st;
   if (dtype != MCFT_F32 && dtype != MCFT_BF16) return fail(MCFT_ERR_INVALID, "unknown dtype %d", dtype);
   if (rows == 0) return MCFT_OK;
   if (!q || !x) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
@@ -64,7 +72,8 @@ extern "C" {
 
 mcft_status mcft_mx4_size(long long rows, long long cols, size_t* bytes) {
   if (!bytes) return fail(MCFT_ERR_INVALID, "bytes is NULL");
-  if (rows < 0 || cols < 1) return fail(MCFT_ERR_INVALID, "bad rows = %lld or cols = %lld", rows, cols);
+  const mcft_status st = check_size(rows, cols);
+  if (st != MCFT_OK) return st;
   *bytes = Mx4Layout(rows, cols).bytes();
   return MCFT_OK;
 }
@@ -92,6 +101,7 @@ mcft_status mcft_mx4_matmul(const void* a, const void* b, int M, int N, int K, i
                             mcft_stream_t stream) {
   NvtxRange nvtx_range("mcft_mx4_matmul");
   if (M < 0 || N < 0 || K < 1) return fail(MCFT_ERR_INVALID, "bad M = %d, N = %d or K = %d", M, N, K);
+  if (K > kMaxCols) return fail(MCFT_ERR_UNSUPPORTED, "K = %d is too large", K);
   if (dtype != MCFT_F32 && dtype != MCFT_BF16) return fail(MCFT_ERR_INVALID, "unknown dtype %d", dtype);
   if (M == 0 || N == 0) return MCFT_OK;
   if (!a || !b || !y) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
