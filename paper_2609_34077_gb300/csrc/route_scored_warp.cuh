@@ -171,7 +171,9 @@ __device__ inline void rank_scored_warp(const ScoredArgs& a, const float (&z)[PL
       second = fmaxf(fmaxf(second, b2), fminf(best, b));
       best = fmaxf(best, b);
     }
-    int gkey = sub == 0 && g < a.n_group ? ordered_int(a.group_top == 2 ? best + second : best) : kNone;
+    // (without a second eligible expert -infinity, also where the first one's value is +infinity and the sum would be NaN)
+    const float value = a.group_top == 2 && second > -INFINITY ? best + second : a.group_top == 2 ? second : best;
+    int gkey = sub == 0 && g < a.n_group ? ordered_int(value) : kNone;
     unsigned groups = 0;
     for (int k = 0; k < a.topk_group; ++k) {
       const int top = __reduce_max_sync(kAll, gkey);
