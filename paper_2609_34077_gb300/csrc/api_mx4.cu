@@ -186,6 +186,7 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   if (!x || !idx || !gate || !experts || !y || !workspace || (S > 0 && !shared))
     return fail(MCFT_ERR_INVALID, "NULL pointer argument");
   if (!aligned(x, 16) || !aligned(y, 16)) return fail(MCFT_ERR_INVALID, "x and y must be 16-byte aligned");
+  if (!aligned(idx, 4) || !aligned(gate, 4)) return fail(MCFT_ERR_INVALID, "misaligned idx or gate");
   if (!aligned(workspace, 256)) return fail(MCFT_ERR_INVALID, "workspace must be 256-byte aligned");
   const Mx4MoeLayout L(desc, T);
   if (ws_bytes < L.total) return fail(MCFT_ERR_INVALID, "workspace of %zu bytes, %zu needed", ws_bytes, L.total);

@@ -48,6 +48,8 @@ mcft_status mcft_route_scored(const mcft_scored_desc* desc, const void* x, int T
   if (st != MCFT_OK || T == 0) return st;
   if (!x || !w_router || !idx || !gate) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
   if (!aligned(x, 16) || !aligned(w_router, 16)) return fail(MCFT_ERR_INVALID, "x and w_router must be 16-byte aligned");
+  if (!aligned(bias, 4) || !aligned(idx, 4) || !aligned(gate, 4) || !aligned(logits, 4) || !aligned(load, 4))
+    return fail(MCFT_ERR_INVALID, "misaligned bias, idx, gate, logits or load");
   const ScoredArgs a{x, w_router, bias, T, desc->d, desc->E, desc->K, desc->n_group, desc->topk_group, desc->group_top,
                      desc->score, desc->gate, desc->scale, idx, gate, logits, load, device_error_word()};
   const cudaError_t e = launch_route_scored(a, desc->dtype, stream);
@@ -81,6 +83,8 @@ mcft_status mcft_route_scored_grad(const mcft_scored_desc* desc, const void* x, 
     return fail(MCFT_ERR_INVALID, "NULL pointer argument");
   if (!aligned(x, 16) || !aligned(w_router, 16) || !aligned(dx, 16) || !aligned(dw, 16))
     return fail(MCFT_ERR_INVALID, "x, w_router, dx and dw must be 16-byte aligned");
+  if (!aligned(idx, 4) || !aligned(gate, 4) || !aligned(logits, 4) || !aligned(dgate, 4))
+    return fail(MCFT_ERR_INVALID, "misaligned idx, gate, logits or dgate");
   if (!aligned(workspace, 256)) return fail(MCFT_ERR_INVALID, "workspace must be 256-byte aligned");
   const size_t need = scored_grad_workspace(T, desc->d, desc->E, desc->K, desc->dtype);
   if (ws_bytes < need) return fail(MCFT_ERR_INVALID, "workspace of %zu bytes, %zu needed", ws_bytes, need);
