@@ -129,6 +129,17 @@ def _stream(stream):
     return int(stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """What a call allocates, from the memory of the stream that its kernels run on: what that memory held before, and what takes it
+    once it is given back (a workspace: as the call returns), is in order with those kernels."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _ptr(t):
     if t is None or isinstance(t, int):
         return t
@@ -158,9 +169,9 @@ def mcft_route(desc: LayerDesc, x, w_router, mode, mask=None, prior=None, idx=No
     """idx [T,K] int32 and gate [T,K] fp32 (allocated on x's device if not given)."""
     T = x.shape[0]
     if idx is None:
-        idx = torch.empty((T, desc.K), dtype=torch.int32, device=x.device)
+        idx = _empty((T, desc.K), torch.int32, x.device, stream)
     if gate is None:
-        gate = torch.empty((T, desc.K), dtype=torch.float32, device=x.device)
+        gate = _empty((T, desc.K), torch.float32, x.device, stream)
     m = _host_array(mask, np.uint8, desc.E)
     if m is None and mask is not None:
         mb = bytes(int(v) for v in mask)
@@ -214,9 +225,9 @@ def mcft_moe_forward(desc: LayerDesc, x, idx, gate, experts, shared=(), y=None, 
     None; ``workspace``: uint8 device tensor (allocated if not given)."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty(x.shape, x.dtype, x.device, stream)
     if workspace is None:
-        workspace = torch.empty(mcft_moe_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
+        workspace = _empty(mcft_moe_workspace_size(desc, T), torch.uint8, x.device, stream)
     ex = _ptr_array(experts, desc.E)
     sh = _ptr_array(shared, desc.n_shared)
     _check(lib().mcft_moe_forward(C.byref(desc), _ptr(x), T, _ptr(idx), _ptr(gate),
@@ -236,10 +247,9 @@ def mcft_moe_forward_lora(desc: LayerDesc, x, idx, gate, experts, shared=(), exp
     """Layer forward with LoRA adapters (packed blocks, see include/mcft.h) on the experts."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty(x.shape, x.dtype, x.device, stream)
     if workspace is None:
-        workspace = torch.empty(mcft_moe_workspace_size_lora(desc, rank, T), dtype=torch.uint8,
-                                device=x.device)
+        workspace = _empty(mcft_moe_workspace_size_lora(desc, rank, T), torch.uint8, x.device, stream)
     ex = _ptr_array(experts, desc.E)
     sh = _ptr_array(shared, desc.n_shared)
     el = _ptr_array(expert_lora, desc.E)
@@ -257,7 +267,7 @@ def mcft_moe_forward_noalloc(desc: LayerDesc, x, idx, gate, experts, shared=(), 
     (for callers that cannot allocate device memory; decode-sized calls only)."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty(x.shape, x.dtype, x.device, stream)
     ex = _ptr_array(experts, desc.E)
     sh = _ptr_array(shared, desc.n_shared)
     _check(lib().mcft_moe_forward_noalloc(C.byref(desc), _ptr(x), T, _ptr(idx), _ptr(gate),
@@ -342,9 +352,9 @@ def mcft_moe_forward_cached(desc: LayerDesc, x, idx, gate, cache: Cache, layer, 
     """Decode forward of `layer` with experts from the cache, fetch driven on the device."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty(x.shape, x.dtype, x.device, compute_stream)
     if workspace is None:
-        workspace = torch.empty(mcft_moe_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
+        workspace = _empty(mcft_moe_workspace_size(desc, T), torch.uint8, x.device, compute_stream)
     sh = _ptr_array(shared, desc.n_shared)
     _check(lib().mcft_moe_forward_cached(C.byref(desc), _ptr(x), T, _ptr(idx), _ptr(gate),
                                          C.c_void_p(cache.handle), layer, sh.buffer_info()[0],
@@ -389,8 +399,7 @@ def mcft_residual_rmsnorm(desc: LayerDesc, x, y=None, gamma=None, eps=1e-5, u=No
     (allocated on x's device if not given) when gamma is given, else None."""
     T = x.shape[0]
     if gamma is not None and u is None:
-        u = torch.empty((T, desc.d), dtype=torch.bfloat16 if desc.dtype == MCFT_BF16 else torch.float32,
-                        device=x.device)
+        u = _empty((T, desc.d), torch.bfloat16 if desc.dtype == MCFT_BF16 else torch.float32, x.device, stream)
     _check(lib().mcft_residual_rmsnorm(C.byref(desc), _ptr(x), _ptr(y) if y is not None else None, T,
                                        _ptr(gamma) if gamma is not None else None, C.c_float(eps),
                                        _ptr(u) if gamma is not None else None, _stream(stream)))
@@ -517,8 +526,8 @@ def mcft_profile_read():
 def mcft_mask_sample(m_tilde, uniforms, e_keep, stream=None):
     """(mask [L, E] uint8, pi [L, E] fp32) from m~ and uniforms [L, E] (device tensors)."""
     L, E = m_tilde.shape
-    mask = torch.empty((L, E), dtype=torch.uint8, device=m_tilde.device)
-    pi = torch.empty((L, E), dtype=torch.float32, device=m_tilde.device)
+    mask = _empty((L, E), torch.uint8, m_tilde.device, stream)
+    pi = _empty((L, E), torch.float32, m_tilde.device, stream)
     _check(lib().mcft_mask_sample(_ptr(m_tilde), _ptr(uniforms), L, E, int(e_keep), _ptr(mask),
                                   _ptr(pi), _stream(stream)))
     return mask, pi
@@ -528,7 +537,7 @@ def mcft_gate_grad(desc: LayerDesc, dy, workspace, dgate=None, stream=None):
     """dL/dg [T, K] from dL/dy and the workspace of the forward of the same batch."""
     T = dy.shape[0]
     if dgate is None:
-        dgate = torch.empty((T, desc.K), dtype=torch.float32, device=dy.device)
+        dgate = _empty((T, desc.K), torch.float32, dy.device, stream)
     _check(lib().mcft_gate_grad(C.byref(desc), _ptr(dy), T, _ptr(workspace), workspace.numel(),
                                 _ptr(dgate), _stream(stream)))
     return dgate
@@ -539,7 +548,7 @@ def mcft_mask_grad(desc: LayerDesc, idx, gate, dgate, pi, dm=None, dm_tilde=None
     """(dL/dm [E], dL/dm~ [E]) of one layer (straight-through estimator, Eq. ste)."""
     T = idx.shape[0]
     if dm is None:
-        dm = torch.empty(desc.E, dtype=torch.float32, device=idx.device)
+        dm = _empty(desc.E, torch.float32, idx.device, stream)
     if dm_tilde is None:
         dm_tilde = torch.zeros(desc.E, dtype=torch.float32, device=idx.device)
     _check(lib().mcft_mask_grad(C.byref(desc), _ptr(idx), _ptr(gate), _ptr(dgate), T, _ptr(pi),
@@ -586,11 +595,11 @@ def mcft_route_scored(desc: ScoredDesc, x, w_router, bias=None, idx=None, gate=N
     _wants_router(desc, x, w_router)
     _wants(bias is None or _is(bias, torch.float32, desc.E), "bias is fp32 [E]")
     if idx is None:
-        idx = torch.empty((T, desc.K), dtype=torch.int32, device=x.device)
+        idx = _empty((T, desc.K), torch.int32, x.device, stream)
     else:
         _wants(_is(idx, torch.int32, T, desc.K), "idx is int32 [T, K]")
     if gate is None:
-        gate = torch.empty((T, desc.K), dtype=torch.float32, device=x.device)
+        gate = _empty((T, desc.K), torch.float32, x.device, stream)
     else:
         _wants(_is(gate, torch.float32, T, desc.K), "gate is fp32 [T, K]")
     _wants(logits is None or _is(logits, torch.float32, T, desc.E), "logits is fp32 [T, E]")
@@ -615,16 +624,16 @@ def mcft_route_scored_grad(desc: ScoredDesc, x, w_router, idx, gate, logits, dga
     _wants(_is(idx, torch.int32, T, desc.K) and _is(gate, torch.float32, T, desc.K) and _is(dgate, torch.float32, T, desc.K)
            and _is(logits, torch.float32, T, desc.E), "idx is int32 [T, K], gate and dgate fp32 [T, K], logits fp32 [T, E]")
     if dx is None:
-        dx = torch.empty_like(x)
+        dx = _empty(x.shape, x.dtype, x.device, stream)
     else:
         _wants(_is(dx, x.dtype, T, desc.d), "dx is [T, d] of the layer dtype")
     if dw is None:
         _wants(not accumulate, "accumulate adds to a dw that is given")
-        dw = torch.empty((desc.E, desc.d), dtype=torch.float32, device=x.device)
+        dw = _empty((desc.E, desc.d), torch.float32, x.device, stream)
     else:
         _wants(_is(dw, torch.float32, desc.E, desc.d), "dw is fp32 [E, d]")
     if workspace is None:
-        workspace = torch.empty(mcft_route_scored_grad_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
+        workspace = _empty(mcft_route_scored_grad_workspace_size(desc, T), torch.uint8, x.device, stream)
     _check(lib().mcft_route_scored_grad(C.byref(desc), _ptr(x), T, _ptr(w_router), _ptr(idx), _ptr(gate), _ptr(logits),
                                         _ptr(dgate), _ptr(dx), _ptr(dw), 1 if accumulate else 0, _ptr(workspace),
                                         workspace.numel(), _stream(stream)))
@@ -655,7 +664,7 @@ def mcft_mx4_quantize(x, q=None, stream=None):
     rows, cols = x.shape
     ptr, ld = _rows(x)
     if q is None:
-        q = torch.empty(mcft_mx4_size(rows, cols), dtype=torch.uint8, device=x.device)
+        q = _empty(mcft_mx4_size(rows, cols), torch.uint8, x.device, stream)
     else:
         _wants_mx4(q, rows, cols, "q is smaller than mcft_mx4_size(rows, cols)")
     _check(lib().mcft_mx4_quantize(ptr, rows, cols, ld, _MX4_DTYPE[x.dtype], _ptr(q), _stream(stream)))
@@ -666,7 +675,7 @@ def mcft_mx4_dequantize(q, rows, cols, dtype=torch.bfloat16, y=None, stream=None
     """The values [rows, cols] that the mx4 matrix q stands for, fp32 or bf16."""
     _wants_mx4(q, rows, cols, "q is smaller than mcft_mx4_size(rows, cols)")
     if y is None:
-        y = torch.empty((rows, cols), dtype=dtype, device=q.device)
+        y = _empty((rows, cols), dtype, q.device, stream)
     else:
         _wants(y.shape == (rows, cols), "y is [rows, cols]")
     ptr, ld = _rows(y)
@@ -679,7 +688,7 @@ def mcft_mx4_matmul(a, b, M, N, K, dtype=torch.bfloat16, y=None, stream=None):
     _wants_mx4(a, M, K, "a is smaller than mcft_mx4_size(M, K)")
     _wants_mx4(b, N, K, "b is smaller than mcft_mx4_size(N, K)")
     if y is None:
-        y = torch.empty((M, N), dtype=dtype, device=a.device)
+        y = _empty((M, N), dtype, a.device, stream)
     else:
         _wants(y.shape == (M, N), "y is [M, N]")
     ptr, ld = _rows(y)
@@ -698,7 +707,7 @@ def mcft_mx4_pack_expert(desc: LayerDesc, block, out=None, stream=None):
     size = mcft_mx4_expert_size(desc)
     _wants(block.dtype == torch_dtype(desc) and block.numel() == 3 * desc.w * desc.d, "block is [W1 | W3 | W2] of the layer dtype")
     if out is None:
-        out = torch.empty(size, dtype=torch.uint8, device=block.device)
+        out = _empty(size, torch.uint8, block.device, stream)
     else:
         _wants(_nbytes(out) >= size, "out is smaller than mcft_mx4_expert_size")
     _check(lib().mcft_mx4_pack_expert(C.byref(desc), _ptr(block), _ptr(out), _stream(stream)))
@@ -719,11 +728,11 @@ def mcft_moe_forward_mx4(desc: LayerDesc, x, idx, gate, experts, shared=(), y=No
     _wants(_is(x, torch_dtype(desc), T, desc.d), "x is [T, d] of the layer dtype")
     _wants(_is(idx, torch.int32, T, desc.K) and _is(gate, torch.float32, T, desc.K), "idx is int32 [T, K], gate fp32 [T, K]")
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty(x.shape, x.dtype, x.device, stream)
     else:
         _wants(_is(y, x.dtype, T, desc.d), "y is [T, d] of the layer dtype")
     if workspace is None:
-        workspace = torch.empty(mcft_mx4_workspace_size(desc, T), dtype=torch.uint8, device=x.device)
+        workspace = _empty(mcft_mx4_workspace_size(desc, T), torch.uint8, x.device, stream)
     ex = _ptr_array(experts, desc.E)
     sh = _ptr_array(shared, desc.n_shared)
     _check(lib().mcft_moe_forward_mx4(C.byref(desc), _ptr(x), T, _ptr(idx), _ptr(gate), ex.buffer_info()[0],
