@@ -479,9 +479,12 @@ mcft_status mcft_mx4_matmul(const void* a, const void* b, int M, int N, int K, i
 
 /* mcft_mx4_pack_expert: a packed expert block [W1 | W3 | W2] of the layer dtype to an mx4 expert block: each
  * row of the three matrices quantised, W1 and W3 interleaved 32 rows by 32, mcft_mx4_expert_size bytes, a
- * multiple of 512. Both 16-byte aligned device blocks. An mx4 block is one unit of cache traffic like any
- * expert block: mcft_cache_create takes its size as expert_bytes, mcft_fetch_experts brings it in.
- * Here and in the next two calls desc may have E up to 256 and K up to 16. Asynchronous. */
+ * multiple of 512. Both 16-byte aligned device blocks. Here and in the next two calls desc may have E up to
+ * 256 and K up to 16.
+ * An mx4 block is one unit of cache traffic like any expert block, within the cache's limits: up to 64 experts
+ * a layer, every id in [0, E) (an idx of -1 is an error to mcft_cache_step). mcft_cache_create takes its size as
+ * expert_bytes, mcft_fetch_experts brings it in; mcft_moe_forward_cached and mcft_stack_* take blocks of the layer
+ * dtype only. Asynchronous. */
 mcft_status mcft_mx4_expert_size(const mcft_layer_desc* desc, size_t* bytes);
 mcft_status mcft_mx4_pack_expert(const mcft_layer_desc* desc, const void* block, void* out,
                                  mcft_stream_t stream);
@@ -547,7 +550,8 @@ mcft_status mcft_route_scored(const mcft_scored_desc* desc, const void* x, int T
                               mcft_stream_t stream);
 
 /* mcft_route_scored_grad: gradients of a loss that reaches the router through the gates (the choice of
- * experts is piecewise constant), from dgate = dL/dgate (mcft_gate_grad's, for instance):
+ * experts is piecewise constant), from dgate = dL/dgate, the caller's own or mcft_gate_grad's (which goes up to 64
+ * experts and K = 8, as mcft_moe_forward does, and takes no idx of -1):
  *   dz = (d gate / d z)^T dgate,  dx = dz W,  dW = dz^T x.
  *   x, w_router, idx, gate, logits  as given to and written by mcft_route_scored; an idx of -1 contributes
  *            nothing and its gate and dgate are not read into the sum; another id outside [0, E) sets the

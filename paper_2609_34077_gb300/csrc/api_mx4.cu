@@ -9,7 +9,8 @@
 namespace mcft {
 namespace {
 
-// Rows: tiles are counted in ints. Columns: 2048 of them are a step of a grid's second extent (mx4_quant.cu), which ends at 65535.
+// Rows: tiles are counted in ints. Columns: 2048 of them are a step of a grid's second extent (mx4_quant.cu), which ends at
+// 65535.
 constexpr long long kMaxRows = INT_MAX - 128, kMaxCols = 65535LL * 2048;
 
 mcft_status check_size(long long rows, long long cols) {
@@ -236,8 +237,8 @@ mcft_status mcft_moe_forward_mx4(const mcft_layer_desc* desc, const void* x, int
   const ExpertBlock B(desc);
   const int tile_rows = T < 128 ? T : 128;
   // pairs of token tiles waste half a pair for each expert with an odd number of them: from four tiles an expert on average
-  // (d = 2048, w = 1408, E = 64, K = 6: 4096 tokens, three tiles, 196 us by single tiles and 202 by pairs; 16384 tokens 654
-  // and 644; d = 4096, w = 14336, E = 8, K = 2: 4096 tokens 530 and 487)
+  // (d = 2048, w = 1408, E = 64, K = 6: 4096 tokens, three tiles, 215 us by single tiles and 219 by pairs; 16384 tokens 736
+  // and 732; d = 4096, w = 14336, E = 8, K = 2: 4096 tokens 547 and 500)
   p.pairs = L.permuted && (long long)T * K >= 512LL * E;
   p.hdr = m.hdr;
   p.tiles = m.tiles;

@@ -15,17 +15,22 @@
 // drain the 256 accumulator columns into registers and give them back at once, so that the next tile's MMAs run
 // under the epilogue's arithmetic and stores (one accumulator: two of 256 columns and the scales do not fit into tensor
 // memory, and two of 192 were slower). An SM takes about 70 bytes a cycle in from L2, so a tile's copies take longer than
-// its MMAs (128 cycles for 128 x 256 x 64): 4096 x 14336 x 4096 75 us with the copies alone, 82 in all, 50 at the MMAs' rate.
+// its MMAs (128 cycles for 128 x 256 x 64): 4096 x 14336 x 4096 75 us with the copies alone, 82 in all, 50 at the rate of
+// these MMAs. (PTX has a K of 96 for this kind on sm_103a, half as fast again; the layout's 128-column chunks are not a
+// multiple of it, and the copies, which bound these tiles, would stay.)
 // `pair`: the same under tcgen05's CTA pairs, M = 256: each CTA brings in its 128 token rows and half of the weight rows,
-// two thirds of the bytes, and copies and MMAs are level: 72.7 us (6.6 PFLOP/s). `narrow` tiles of up to 128 weight rows
+// two thirds of the bytes, and copies and MMAs are level: 73.2 us (6.6 PFLOP/s). Results of any width and stride are turned
+// in registers, of which 300 bytes a thread spill: 4095 x 14335 x 4096 93 us. `narrow` tiles of up to 128 weight rows
 // for few tokens, where the bytes of the weights bound the time: one item a cluster of 1, 2, 4 or 8 CTAs that split the
 // contraction and add their partial tiles through distributed shared memory, two CTAs an SM; only the 8-row groups that
 // hold tokens are copied (the MMA's other rows read whatever is there, and nobody reads their results). 1 x 4096 x 14336:
-// 8.0 us a replayed graph's node, 4.6 at HBM's rate; the layer of 16 tokens on 8 experts of 4096 x 14336 109 us, its floor.
+// 8.0 us a replayed graph's node, 4.6 at HBM's rate; the layer of 16 tokens on 8 experts of 4096 x 14336 112 to 122 us, 109 at
+// HBM's rate.
 //
 // Warp 0 issues the copies (pair: warp 10 those of the tokens), warp 1 the tcgen05.cp and MMAs and owns the tensor memory
-// (pair: the second CTA's tells the first of its copies), warps 2-9 are the epilogue. Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again
-// with a limit) for its copies and MMAs in flight, frees the tensor memory and returns.
+// (pair: the second CTA's tells the first of its copies), warps 2-9 are the epilogue. Every wait is bounded: after 2 s the
+// kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (again with a limit) for its copies and MMAs in flight, frees the
+// tensor memory and returns.
 #include <algorithm>
 #include <type_traits>
 
@@ -122,9 +127,9 @@ __device__ __forceinline__ void arrive(uint64_t* bar) {
 __device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// Of bulk copies that have landed in this CTA's shared memory, as this thread has seen by an acquiring wait: released to the other
-// CTA by a fence that is restricted to shared memory. (A release of everything first waits for the SM's stores on their
-// way to global memory: 1250 cycles on average.)
+// Of bulk copies that have landed in this CTA's shared memory, as this thread has seen by an acquiring wait: released to the
+// other CTA by a fence that is restricted to shared memory. (A release of everything first waits for the SM's stores on
+// their way to global memory: 1250 cycles on average.)
 __device__ __forceinline__ void announce(uint32_t cluster_addr) {
   asm volatile(
       "fence.release.sync_restrict::shared::cta.cluster;\n\tmbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
@@ -745,7 +750,7 @@ cudaError_t launch_mx4_gemm(Mx4GemmArgs p, int epi, long long max_tiles, int til
   auto tiles_of = [&](int tn) { return (n_rows + tn - 1) / tn; };
   const bool wide = mx4_wide(max_tiles, n_rows, tile_rows, p.chunks);
   // CTA pairs pay where items follow one another on every SM and are long: 4096 x 14336 x 4096 82.4 us by single CTAs and
-  // 72.7 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
+  // 73.2 by pairs, 8192 x 8192 x 8192 169 and 146; but 4096 x 4096 x 1024 14.4 and 15.3, 1024 x 4096 x 4096 10.6 and 11.8.
   const bool pair = wide && p.pairs && wide_items(max_tiles, n_rows) > num_sms && p.chunks >= 16;
   p.split = 1;
   int grid;

@@ -138,7 +138,8 @@ __device__ __forceinline__ int peer_int(const int* p, uint32_t rank) {
 // One cluster: each CTA counts and places an eighth of the assignments.
 __global__ void __cluster_dims__(kPermCtas, 1, 1) __launch_bounds__(kPermThreads)
     mx4_permute_kernel(const __grid_constant__ Mx4MoeArgs a) {
-  __shared__ int cnt[kMaxMx4E + 1], next[kMaxMx4E], tile0[kMaxMx4E], wsum[8], wpairs[8], routed, routed_pairs;  // cnt[kMaxMx4E]: bad ids
+  __shared__ int cnt[kMaxMx4E + 1];  // (the last: bad ids)
+  __shared__ int next[kMaxMx4E], tile0[kMaxMx4E], wsum[8], wpairs[8], routed, routed_pairs;
   pdl_wait();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (x is complete: mx4_spread_kernel quantises it meanwhile)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;

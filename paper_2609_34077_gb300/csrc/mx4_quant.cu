@@ -55,10 +55,11 @@ __device__ __forceinline__ void load_block(const T* row, long long c, long long 
   }
 }
 
-// Rows that are aligned to their type only (the way back: not to 32 bytes): a warp's 8 rows by 128 columns pass through shared memory, so that its lanes
-// load and store neighbouring values. Value i of block b of row r stands at [r][b][i] in rows of 4 x 33 words: 32 lanes
-// that each take value i of their block meet 32 banks. 26800 x 4101: fp32 97 us there and 107 back, bf16 86 and 82; with a
-// block a lane 189 and 805, 88 and 647.
+// Rows that are aligned to their type only (the way back: not to 32 bytes): a warp's 8 rows by 128 columns pass through
+// shared memory, so that its lanes load and store neighbouring values. Value i of block b of row r stands at [r][b][i] in
+// rows of 4 x 33 words: 32 lanes that each take value i of their block meet 32 banks. 26800 x 4101: fp32 97 us there and 107
+// back, bf16 86 and 82 (where the bytes take 41: a value of two bytes a lane and load); with a block a lane 189 and 805, 88
+// and 647.
 constexpr int kTurnRow = 4 * 33, kTurnWords = 8 * kTurnRow;
 
 template <typename T>

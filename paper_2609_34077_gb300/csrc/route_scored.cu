@@ -1,7 +1,7 @@
 // Scored routing: z = W x, then route_scored_warp.cuh's choice of experts for each token.
 //
-// Few tokens (kFewT) and small weights: latency bounds it. A cluster of eight CTAs takes kFewTokens tokens: its 64 warps share the
-// experts, each streaming its rows of W once against all of the tokens (held in shared memory), and the logits meet
+// Few tokens (kFewT) and small weights: latency bounds it. A cluster of eight CTAs takes kFewTokens tokens: its 64 warps share
+// the experts, each streaming its rows of W once against all of the tokens (held in shared memory), and the logits meet
 // in the leader's shared memory, where one warp ranks a token. One token of d = 2048, E = 64: 5.2 us a replayed graph's
 // node, of which the 256 kB of W are 0.04 at HBM's rate; the rest is the launch, one round of loads, two cluster barriers
 // and the choice's chain of shuffles.

@@ -2,7 +2,7 @@
 // values c = s + bias, the best groups of experts, the K best of their experts by c (ties to the lower index, of
 // groups too), gates from s. Not part of the C ABI.
 //
-// A warp's instructions bound it (one token's are a chain of shuffles and reductions; other warps fill the gaps), so
+// One token's instructions are a chain of shuffles and reductions, whose gaps other warps fill; there are too many of both, so
 // the choice first narrows the field: the K-th largest of the 32 lanes' own maxima is a bound below which nothing can
 // be chosen, and what reaches it (K to about 2 K experts) is packed one to a lane, where a round of the choice is a
 // warp maximum and a ballot. 8192 tokens of 256 experts in 8 groups, forward: 70 us with all eight experts of every

@@ -19,11 +19,11 @@ __device__ __forceinline__ void store32_by16(void* p, const uint32_t* v) {
   q[1] = make_uint4(v[4], v[5], v[6], v[7]);
 }
 
-// 64 bytes u of each lane's own row to global memory, at `row` (NULL: none; ALIGN: bytes to which it is aligned, 32 or 16), by a whole warp. Two neighbouring lanes
-// first exchange halves, so that an instruction writes 64 contiguous bytes of 16 rows, not 32 of 32: each line that a
-// store touches takes the way through L1 that the copies into shared memory take too (mx4 product of 4096 x 14336 x
-// 4096: 16, 32, 64 and 128 bytes a row 109, 83.2, 82.2 and 83.8 us, the exchange of four lanes costing more than it
-// gives).
+// 64 bytes u of each lane's own row to global memory, at `row` (NULL: none; ALIGN: bytes to which it is aligned, 32 or 16),
+// by a whole warp. Two neighbouring lanes first exchange halves, so that an instruction writes 64 contiguous bytes of 16
+// rows, not 32 of 32: each line that a store touches takes the way through L1 that the copies into shared memory take too
+// (mx4 product of 4096 x 14336 x 4096: 16, 32, 64 and 128 bytes a row 109, 83.2, 82.2 and 83.8 us, the exchange of four
+// lanes costing more than it gives).
 template <int ALIGN = 32>
 __device__ __forceinline__ void store_rows64(void* row, uint32_t* u) {
   static_assert(ALIGN == 32 || ALIGN == 16, "alignment of the rows");

@@ -13,8 +13,10 @@
 // with one accumulator the logits of 4096-wide tokens came out 1.2e-6 short, which the gradient of large sigmoids shows.
 // There are few tiles, so a cluster of up to 8 CTAs splits a tile's contraction, each CTA puts its partial logits into its
 // shared memory, and each ranks its share of the tokens from the sum of its peers' rows, in the order of the peers.
-// 4096 tokens of d = 4096, E = 256, K = 8 in 8 groups: 23.5 us (floor 5.3, HBM: 34 MB of x and 2 of W), 8192 tokens 34:
-// after the loads (9 to 12 us at these sizes) the ranking, bound by its warps' instructions, is the larger part.
+// 4096 tokens of d = 4096, E = 256, K = 8 in 8 groups: 20.7 us a graph node (floor 5.3, HBM: 34 MB of x and 2 of W), 8192
+// tokens 34: the loads (9 to 12 us at these sizes), the cluster's barrier and the ranking follow one another. A capture of
+// the first shows neither end full: HBM 18 %, issue slots 40 % of the cycles in which an SM has the kernel, and a third of its
+// warps' cycles are the wait for the barrier.
 // dx and dw read W, x and (dw) dz along their contiguous index, which is not the contraction's: their shared-memory
 // tiles are MN-major operands (64 columns of 128 bytes, 128-byte swizzle), straight from the row-major tensors.
 #include <algorithm>
@@ -244,7 +246,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) scored_forward_kernel(const __
 
 // ---- dx = dz W ----
 // 128 tokens by 256 columns an item, persistent. 8192 tokens, E = 256, d = 4096: 26.6 us for 17.2 GFLOP as 34.4 (two
-// parts: 18 us at the tensor cores' rate) and 67 MB written (10 us); its epilogue and MMAs overlap in two accumulators.
+// parts: 18 us at the tensor cores' rate) and 67 MB written (10 us); its epilogue and MMAs overlap in two accumulators. Two
+// parts are within 2^-17 of the terms dz W; with three the step took 117 us where it takes 107, and dx, which rounds to
+// bf16, was as far from 64 bits.
 
 struct DxArgs {
   CUtensorMap dz, w;  // boxes of 64 columns by 128 tokens; of 64 columns by 64 experts
