@@ -570,6 +570,101 @@ mcft_status mcft_route_scored_grad(const mcft_scored_desc* desc, const void* x, 
                                    size_t ws_bytes, mcft_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * mx8: microscaled 8-bit floating point, the format of activation checkpoints (no counterpart in the paper; its Stage 2,
+ * Section 3.2, fine-tunes experts, whose backward pass wants the forward's activations, and the paper's setting,
+ * Section 1, is short of device memory: a checkpoint in this format takes 33/64 of bf16's bytes).
+ *
+ * A block of 32 values along a row is 32 e4m3 codes and one scale, the smallest power of two 2^s with max|x| <= 448 * 2^s,
+ * s in [-127, 127], held as s + 127 in a byte. Codes round to nearest even; none saturates. A block with a NaN or an infinity
+ * has the scale byte 0xff and reads back as NaN. An mx8 matrix [rows, cols] is row-major codes [rows, Cp], Cp = cols
+ * rounded up to 32 (codes past cols are 0), then row-major scales [rows, Cp / 32]: mcft_mx8_size bytes, 16-byte aligned.
+ *
+ * mcft_mx8_quantize: x device [rows, cols] of dtype (MCFT_F32 or MCFT_BF16), `ld` elements from row to row, any
+ *   alignment of its type (rows on 32 bytes are read faster); q device, mcft_mx8_size bytes out.
+ * mcft_mx8_dequantize: the values that q stands for, exact in either dtype but for subnormal bf16 results, which round;
+ *   y device [rows, cols], `ld` elements from row to row.
+ * rows = 0 is a no-op. Asynchronous. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer, rows < 0, cols < 1,
+ * ld < cols, an unknown dtype; MCFT_ERR_UNSUPPORTED for rows > 2^31 - 1, cols > 536862720 or ld > 2^40. */
+mcft_status mcft_mx8_size(long long rows, long long cols, size_t* bytes);
+mcft_status mcft_mx8_quantize(const void* x, long long rows, long long cols, long long ld, int dtype,
+                              void* q, mcft_stream_t stream);
+mcft_status mcft_mx8_dequantize(const void* q, long long rows, long long cols, int dtype, void* y,
+                                long long ld, mcft_stream_t stream);
+
+/* mcft_residual_rmsnorm_mx8: mcft_residual_rmsnorm for a program that trains, with what its backward pass wants:
+ *   v = x + y (v = x when y is NULL), r = 1 / sqrt(mean_j v[j]^2 + eps), u = gamma * v * r.
+ *   x      device [T, d] fp32;  y device [T, d] layer dtype, or NULL;  gamma device [d] layer dtype
+ *   out    device [T, d] fp32: v; may be x (then the stream is updated in place)
+ *   u      device [T, d] layer dtype
+ *   u8, x8 device mx8 [T, d]: u, before its rounding to the layer dtype, and v. u8 is the checkpoint of the block's input that
+ *          mcft_ffn_grad takes, x8 that of the stream that mcft_rmsnorm_grad takes
+ *   rstd   device [T] fp32: r
+ * Each output may be NULL, but not all. Of desc only d (at most 32768) and dtype are read. T = 0 is a no-op. Asynchronous; the
+ * same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (rstd 4 bytes, the
+ * others 16), a bad desc, T < 0, eps outside [0, 1]; MCFT_ERR_UNSUPPORTED for larger d, T > 2^24. */
+mcft_status mcft_residual_rmsnorm_mx8(const mcft_layer_desc* desc, const float* x, const void* y, int T,
+                                      const void* gamma, float eps, float* out, void* u, void* u8,
+                                      void* x8, float* rstd, mcft_stream_t stream);
+
+/* mcft_rmsnorm_grad: gradients of that norm, from du = dL/du and the gradient dres that reaches v past the norm. With
+ * n = v * rstd and g = gamma * du:
+ *   dx = dres + rstd (g - n mean_j(g[j] n[j])),  dgamma = sum_t du[t] n[t].
+ *   x, x8     v as fp32 [T, d] or as mx8: one of the two, the other NULL
+ *   rstd      as mcft_residual_rmsnorm_mx8 wrote it;  gamma as given to it
+ *   du        device [T, d] layer dtype;  dres device [T, d] fp32, or NULL (zero)
+ *   dx        device [T, d] fp32 out, may be dres; or NULL
+ *   dgamma    device [d] fp32 out, added to what it holds if accumulate is non-zero; or NULL
+ *   workspace device, mcft_rmsnorm_grad_workspace_size(desc, T) bytes, 256-byte aligned (dgamma NULL: not used), in use until
+ *             the call's kernels finish; enough for any smaller T
+ * T = 0 writes zeros to dgamma (unless accumulating). Asynchronous; the same bits whenever the inputs are the same. Errors as
+ * above, and for dx and dgamma both NULL or a workspace too small. */
+mcft_status mcft_rmsnorm_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
+mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const void* x8, const float* rstd,
+                              const void* gamma, const void* du, int T, const float* dres, float* dx,
+                              float* dgamma, int accumulate, void* workspace, size_t ws_bytes,
+                              mcft_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The dense gated feed-forward block: one packed expert block for every token (a shared expert, Section 3.1, or the dense
+ * layer that DeepSeek-V2-Lite begins with), forward and backward.
+ *
+ * mcft_ffn_forward: y = W2 (silu(W1 x) * (W3 x)).
+ *   x, y      device [T, d] layer dtype (y may not alias x)
+ *   block     device packed expert block [W1 | W3 | W2]
+ *   ckpt      device mx8 [T, 2w] out: g = W1 x and u = W3 x (g first), rounded from fp32, for mcft_ffn_grad; or NULL
+ *   workspace device, mcft_ffn_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
+ *             enough for any smaller T
+ * Of desc only d, w and dtype are read. bf16: fp32 sums, h rounded to bf16 once, y once; up to 64 tokens without a checkpoint
+ * run the decode kernels, the others tcgen05 products with SwiGLU and the checkpoint's rounding in the epilogue. fp32 layers
+ * are fp32 throughout. T = 0 is a no-op. Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID
+ * for a NULL or misaligned pointer (16 bytes), a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for T > 2^24 or
+ * d or w > 2^20. */
+mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
+mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, const void* block, void* y,
+                             void* ckpt, void* workspace, size_t ws_bytes, mcft_stream_t stream);
+
+/* mcft_ffn_grad: its gradients from dy = dL/dy. With s the logistic function, h = g s(g) u and dh = W2^T dy:
+ *   du = dh g s(g),  dg = dh u s(g) (1 + g (1 - s(g))),
+ *   dx = W1^T dg + W3^T du,  dW1 = dg^T x,  dW3 = du^T x,  dW2 = dy^T h   (sums over tokens).
+ *   dy        device [T, d] layer dtype
+ *   block     as given to the forward
+ *   x, x8     the forward's input, in the layer dtype or as mx8 [T, d]: one of the two, the other NULL
+ *   ckpt      what the forward wrote: g and u are its values, so no product is computed twice and neither has to be kept at
+ *             full size; or NULL: g and u are computed again from x or x8
+ *   dx        device [T, d] layer dtype out, or NULL
+ *   dblock    device out, packed like the block, of grad_dtype (MCFT_F32 or the layer dtype), added to what it holds if
+ *             accumulate is non-zero; or NULL (then x and x8 may both be NULL beside a ckpt)
+ *   workspace device, mcft_ffn_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
+ *             enough for any smaller T
+ * bf16 layers: dg, du and h are rounded to bf16 as operands, sums are fp32. T = 0 writes zeros to dblock (unless
+ * accumulating). Asynchronous; the same bits whenever the inputs are the same. Errors as above, and for dx and dblock both
+ * NULL or another grad_dtype. */
+mcft_status mcft_ffn_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
+mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, const void* block, const void* x,
+                          const void* x8, const void* ckpt, void* dx, void* dblock, int grad_dtype,
+                          int accumulate, void* workspace, size_t ws_bytes, mcft_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
  * mcft_device_error: synchronise `stream`, return and clear the device error word of the current
  * device: MCFT_OK, MCFT_ERR_INVALID (bad id, missing expert pointer) or MCFT_ERR_TIMEOUT. */
 mcft_status mcft_device_error(mcft_stream_t stream);

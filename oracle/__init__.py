@@ -19,8 +19,10 @@ Everything is a plain, slow, readable restatement of the paper's definitions in 
   and the next-layer prediction that drives expert prefetch; the cache's prefetch event is in
   ``cache``.
 * ``mx4``      - microscaled 4-bit floating point: rounding, products, the layer on rounded experts.
+* ``dense``    - the dense gated feed-forward block and the RMSNorm ahead of it, forward and backward, and microscaled 8-bit
+  floating point (checkpoints).
 * ``scored``   - scored routing (sigmoid or softmax scores, bias, groups) and its gradient.
 
 Pins (tests marked ``not gpu``) tie each function to something other than itself; see the tests.
 """
-from . import cache, ffn, mask, mx4, routing, scored, stack  # noqa: F401
+from . import cache, dense, ffn, mask, mx4, routing, scored, stack  # noqa: F401

@@ -1,0 +1,369 @@
+// C ABI of the dense gated feed-forward block, its 8-bit checkpoints and the RMSNorm ahead of it (include/mcft.h):
+// argument checks, workspaces and launches.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "api_check.h"
+#include "dense.h"
+#include "mx8.cuh"
+
+namespace mcft {
+namespace {
+
+constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
+constexpr int kFewTokens = 64;  // up to here the decode kernels: the weights are what there is to read
+
+mcft_status check_T(int T) {
+  if (T < 0) return fail(MCFT_ERR_INVALID, "T = %d < 0", T);
+  if (T > kMaxT) return fail(MCFT_ERR_UNSUPPORTED, "T = %d > %d", T, kMaxT);
+  return MCFT_OK;
+}
+
+mcft_status check_width(const char* name, int v) {
+  if (v <= 0 || v % 64) return fail(MCFT_ERR_INVALID, "%s = %d must be a positive multiple of 64", name, v);
+  if (v > kMaxWidth) return fail(MCFT_ERR_UNSUPPORTED, "%s = %d > %d", name, v, kMaxWidth);
+  return MCFT_OK;
+}
+
+mcft_status check_dtype(int dtype) {
+  return dtype == MCFT_F32 || dtype == MCFT_BF16 ? MCFT_OK : fail(MCFT_ERR_INVALID, "unknown dtype %d", dtype);
+}
+
+mcft_status check_ffn(const mcft_layer_desc* d, int T) {
+  if (!d) return fail(MCFT_ERR_INVALID, "desc is NULL");
+  mcft_status st = check_width("d", d->d);
+  if (st == MCFT_OK) st = check_width("w", d->w);
+  if (st == MCFT_OK) st = check_dtype(d->dtype);
+  return st == MCFT_OK ? check_T(T) : st;
+}
+
+mcft_status check_norm(const mcft_layer_desc* d, int T) {
+  if (!d) return fail(MCFT_ERR_INVALID, "desc is NULL");
+  mcft_status st = check_width("d", d->d);
+  if (st == MCFT_OK) st = check_dtype(d->dtype);
+  if (st == MCFT_OK && d->d > kMaxNormD) return fail(MCFT_ERR_UNSUPPORTED, "d = %d > %d", d->d, kMaxNormD);
+  return st == MCFT_OK ? check_T(T) : st;
+}
+
+mcft_status check_workspace(const void* p, size_t have, size_t need) {
+  if (!p && need) return fail(MCFT_ERR_INVALID, "workspace is NULL");
+  if (!aligned(p, 256)) return fail(MCFT_ERR_INVALID, "workspace must be 256-byte aligned");
+  if (have < need) return fail(MCFT_ERR_INVALID, "workspace of %zu bytes, %zu needed", have, need);
+  return MCFT_OK;
+}
+
+// Sections of a workspace, on 256 bytes each.
+struct Sections {
+  size_t total = 0;
+  size_t add(size_t bytes) {
+    const size_t at = total;
+    total += (bytes + 255) & ~size_t(255);
+    return at;
+  }
+};
+
+size_t elem(int dtype) { return dtype == MCFT_BF16 ? 2 : 4; }
+
+struct ForwardLayout {
+  size_t h, gu, planes;        // many tokens (gu: fp32 with a checkpoint)
+  size_t hdr, off, perm, done, few_h, few_o;
+  size_t total;
+};
+// Every section grows with T, so a workspace for T_max serves all smaller calls of either kind.
+ForwardLayout forward_layout(const mcft_layer_desc* d, int T) {
+  const size_t t = size_t(T), w = size_t(d->w), D = size_t(d->d);
+  ForwardLayout L{};
+  Sections many, few;
+  L.h = many.add(t * w * elem(d->dtype));
+  if (d->dtype == MCFT_F32) L.gu = many.add(t * 2 * w * 4);
+  const size_t up = d->dtype == MCFT_F32 ? dense_plane_bytes(1, t * 2 * w, d->d, d->dtype) : 0;
+  L.planes = many.add(std::max(up, dense_plane_bytes(1, t * D, d->w, d->dtype)));
+  const int n = d->dtype == MCFT_BF16 ? std::min(T, kFewTokens) : T;
+  L.hdr = few.add(sizeof(WsHeader));
+  L.off = few.add(2 * sizeof(int));
+  L.perm = few.add(size_t(n) * sizeof(int));
+  L.done = few.add((1 + kClaimSlots) * sizeof(int));
+  L.few_h = few.add(size_t(n) * w * elem(d->dtype));
+  // partial planes: 8 of up to 4 tokens, 2 of up to 16, one of more
+  size_t rows = size_t(n);
+  if (d->dtype == MCFT_BF16)
+    for (int i : {4, 16}) rows = std::max(rows, size_t(decode_ksplit(std::min(n, i))) * std::min(n, i));
+  L.few_o = few.add(rows * D * 4);
+  L.total = std::max(many.total, few.total);
+  return L;
+}
+
+struct GradLayout {
+  size_t x, h, dgu, gu, dh, planes, total;
+};
+GradLayout grad_layout(const mcft_layer_desc* d, int T) {
+  const size_t t = size_t(T), w = size_t(d->w), D = size_t(d->d), e = elem(d->dtype);
+  GradLayout L{};
+  Sections s;
+  L.x = s.add(t * D * e);
+  L.h = s.add(t * w * e);
+  L.dgu = s.add(t * 2 * w * e);
+  L.gu = s.add(t * 2 * w * 4);
+  if (d->dtype == MCFT_F32) L.dh = s.add(t * w * 4);
+  L.planes = s.add(std::max(dense_plane_bytes(3, t * D + 3 * w * D, std::max(T, 2 * d->w), d->dtype),
+                            d->dtype == MCFT_F32 ? dense_plane_bytes(1, t * 2 * w, d->d, d->dtype) : size_t(0)));
+  L.total = s.total;
+  return L;
+}
+
+// y = F(x) by the kernels that serve batches of few tokens (bf16), or fp32 ones of any size, as one expert that every token
+// takes.
+cudaError_t forward_few(const mcft_layer_desc* d, const void* x, int T, const void* block, void* y, char* ws,
+                        const ForwardLayout& L, cudaStream_t s) {
+  DenseFewArgs p{reinterpret_cast<WsHeader*>(ws + L.hdr), reinterpret_cast<int*>(ws + L.off),
+                 reinterpret_cast<int*>(ws + L.perm), reinterpret_cast<int*>(ws + L.done), T, 1 + kClaimSlots};
+  cudaError_t e = launch_dense_few(p, s);
+  if (e != cudaSuccess) return e;
+  FfnArgs a{};
+  a.x = x;
+  a.off = p.off;
+  a.perm = p.perm;
+  a.hdr = p.hdr;
+  a.done = p.done;
+  a.wblk[0] = block;
+  a.h = ws + L.few_h;
+  a.o = reinterpret_cast<float*>(ws + L.few_o);
+  a.o_plane = size_t(T) * d->d;
+  a.ksplit = d->dtype == MCFT_BF16 ? decode_ksplit(T) : 1;
+  a.T = T;
+  a.K = 1;
+  a.d = d->d;
+  a.w = d->w;
+  a.nseg = 1;
+  a.E = 1;
+  a.err = device_error_word();
+  e = d->dtype == MCFT_BF16 ? launch_ffn_decode(a, num_sms(), s, 3) : launch_ffn_rowwise(a, d->dtype, num_sms(), s, 3);
+  return e != cudaSuccess ? e : launch_dense_join(a.o, a.ksplit, a.o_plane, y, d->dtype, 0, s);
+}
+
+}  // namespace
+}  // namespace mcft
+
+using namespace mcft;
+
+extern "C" {
+
+mcft_status mcft_mx8_size(long long rows, long long cols, size_t* bytes) {
+  if (rows < 0 || cols < 1) return fail(MCFT_ERR_INVALID, "rows = %lld < 0 or cols = %lld < 1", rows, cols);
+  if (rows > INT_MAX || cols > 65535ll * 8192)
+    return fail(MCFT_ERR_UNSUPPORTED, "rows = %lld or cols = %lld is too large", rows, cols);
+  if (!bytes) return fail(MCFT_ERR_INVALID, "bytes is NULL");
+  *bytes = Mx8Layout(rows, cols).bytes();
+  return MCFT_OK;
+}
+
+static mcft_status mx8_call(const void* x, long long rows, long long cols, long long ld, int dtype, const void* q, bool back,
+                            mcft_stream_t stream) {
+  size_t bytes;
+  mcft_status st = mcft_mx8_size(rows, cols, &bytes);
+  if (st == MCFT_OK) st = check_dtype(dtype);
+  if (st != MCFT_OK) return st;
+  if (ld < cols) return fail(MCFT_ERR_INVALID, "ld = %lld < cols = %lld", ld, cols);
+  if (ld > (1ll << 40)) return fail(MCFT_ERR_UNSUPPORTED, "ld = %lld is too large", ld);
+  if (rows == 0) return MCFT_OK;
+  if (!x || !q) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
+  if (!aligned(x, uintptr_t(elem(dtype)))) return fail(MCFT_ERR_INVALID, "the matrix is not aligned to its type");
+  if (!aligned(q, 16)) return fail(MCFT_ERR_INVALID, "an mx8 matrix must be 16-byte aligned");
+  const cudaError_t e = launch_mx8_quant(Mx8Args{x, const_cast<void*>(q), rows, cols, ld}, dtype, back, stream);
+  return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "mx8 kernel launch");
+}
+
+mcft_status mcft_mx8_quantize(const void* x, long long rows, long long cols, long long ld, int dtype, void* q,
+                              mcft_stream_t stream) {
+  NvtxRange nvtx_range("mcft_mx8_quantize");
+  return mx8_call(x, rows, cols, ld, dtype, q, false, stream);
+}
+
+mcft_status mcft_mx8_dequantize(const void* q, long long rows, long long cols, int dtype, void* y, long long ld,
+                                mcft_stream_t stream) {
+  NvtxRange nvtx_range("mcft_mx8_dequantize");
+  return mx8_call(y, rows, cols, ld, dtype, q, true, stream);
+}
+
+mcft_status mcft_residual_rmsnorm_mx8(const mcft_layer_desc* desc, const float* x, const void* y, int T,
+                                      const void* gamma, float eps, float* out, void* u, void* u8, void* x8,
+                                      float* rstd, mcft_stream_t stream) {
+  NvtxRange nvtx_range("mcft_residual_rmsnorm_mx8");
+  const mcft_status st = check_norm(desc, T);
+  if (st != MCFT_OK) return st;
+  if (!(eps >= 0.f) || eps > 1.f) return fail(MCFT_ERR_INVALID, "eps = %g must be in [0, 1]", eps);
+  if (T == 0) return MCFT_OK;
+  if (!x || !gamma) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
+  if (!out && !u && !u8 && !x8 && !rstd) return fail(MCFT_ERR_INVALID, "every output is NULL");
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gamma, 16) || !aligned(out, 16) || !aligned(u, 16) ||
+      !aligned(u8, 16) || !aligned(x8, 16) || !aligned(rstd, 4))
+    return fail(MCFT_ERR_INVALID, "x, y, gamma, out, u, u8 and x8 must be 16-byte aligned, rstd 4-byte");
+  const Norm8Args a{x, y, gamma, out, u, static_cast<uint8_t*>(u8), static_cast<uint8_t*>(x8), rstd, T, desc->d, eps};
+  const cudaError_t e = launch_norm8(a, desc->dtype, stream);
+  return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "RMSNorm kernel launch");
+}
+
+mcft_status mcft_rmsnorm_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes) {
+  const mcft_status st = check_norm(desc, T_max);
+  if (st != MCFT_OK) return st;
+  if (!bytes) return fail(MCFT_ERR_INVALID, "bytes is NULL");
+  *bytes = T_max == 0 ? 0 : size_t(norm_grad_planes(T_max, desc->d)) * desc->d * sizeof(float);
+  return MCFT_OK;
+}
+
+mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const void* x8, const float* rstd,
+                              const void* gamma, const void* du, int T, const float* dres, float* dx, float* dgamma,
+                              int accumulate, void* workspace, size_t ws_bytes, mcft_stream_t stream) {
+  NvtxRange nvtx_range("mcft_rmsnorm_grad");
+  mcft_status st = check_norm(desc, T);
+  if (st != MCFT_OK) return st;
+  if (!dx && !dgamma) return fail(MCFT_ERR_INVALID, "dx and dgamma are both NULL");
+  if (!aligned(dx, 16) || !aligned(dgamma, 16)) return fail(MCFT_ERR_INVALID, "dx and dgamma must be 16-byte aligned");
+  if (T == 0) {
+    if (dgamma && !accumulate) {
+      const cudaError_t e = cudaMemsetAsync(dgamma, 0, sizeof(float) * size_t(desc->d), stream);
+      if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync");
+    }
+    return MCFT_OK;
+  }
+  if (!x == !x8) return fail(MCFT_ERR_INVALID, "one of x and x8 is wanted");
+  if (!rstd || !gamma || !du) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
+  if (!aligned(x, 16) || !aligned(x8, 16) || !aligned(gamma, 16) || !aligned(du, 16) || !aligned(dres, 16) || !aligned(rstd, 4))
+    return fail(MCFT_ERR_INVALID, "x, x8, gamma, du and dres must be 16-byte aligned, rstd 4-byte");
+  const size_t need = dgamma ? size_t(norm_grad_planes(T, desc->d)) * desc->d * sizeof(float) : 0;
+  st = check_workspace(workspace, ws_bytes, need);
+  if (st != MCFT_OK) return st;
+  const NormGradArgs a{x, static_cast<const uint8_t*>(x8), rstd, gamma, du, dres, dx, dgamma, static_cast<float*>(workspace),
+                       T, desc->d, accumulate};
+  const cudaError_t e = launch_norm_grad(a, desc->dtype, stream);
+  return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "RMSNorm gradient launch");
+}
+
+mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes) {
+  const mcft_status st = check_ffn(desc, T_max);
+  if (st != MCFT_OK) return st;
+  if (!bytes) return fail(MCFT_ERR_INVALID, "bytes is NULL");
+  *bytes = T_max == 0 ? 0 : forward_layout(desc, T_max).total;
+  return MCFT_OK;
+}
+
+mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, const void* block, void* y, void* ckpt,
+                             void* workspace, size_t ws_bytes, mcft_stream_t stream) {
+  NvtxRange nvtx_range("mcft_ffn_forward");
+  mcft_status st = check_ffn(desc, T);
+  if (st != MCFT_OK || T == 0) return st;
+  if (!x || !block || !y) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
+  if (!aligned(x, 16) || !aligned(block, 16) || !aligned(y, 16) || !aligned(ckpt, 16))
+    return fail(MCFT_ERR_INVALID, "x, block, y and ckpt must be 16-byte aligned");
+  const ForwardLayout L = forward_layout(desc, T);
+  st = check_workspace(workspace, ws_bytes, L.total);
+  if (st != MCFT_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  cudaError_t e;
+  if (!ckpt && (desc->dtype == MCFT_F32 || T <= kFewTokens)) {
+    e = forward_few(desc, x, T, block, y, ws, L, stream);
+    return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
+  }
+  const char* w13 = static_cast<const char*>(block);
+  const char* w2 = w13 + size_t(2) * desc->w * desc->d * elem(desc->dtype);
+  float* planes = reinterpret_cast<float*>(ws + L.planes);
+  if (desc->dtype == MCFT_BF16) {
+    e = launch_dense_up(DenseUpArgs{x, w13, T, desc->d, desc->w, ws + L.h, nullptr, static_cast<uint8_t*>(ckpt)}, stream);
+  } else {
+    float* gu = reinterpret_cast<float*>(ws + L.gu);
+    const DenseProduct up{x, w13, T, 2 * desc->w, desc->d, 0, 1, gu, MCFT_F32, 0};
+    e = launch_dense_products(&up, 1, MCFT_F32, planes, stream);
+    if (e == cudaSuccess)
+      e = launch_dense_act(DenseActArgs{gu, static_cast<uint8_t*>(ckpt), nullptr, reinterpret_cast<float*>(ws + L.h),
+                                        nullptr, T, desc->w}, stream);
+  }
+  if (e == cudaSuccess) {
+    const DenseProduct down{ws + L.h, w2, T, desc->d, desc->w, 0, 1, y, desc->dtype, 0};
+    e = launch_dense_products(&down, 1, desc->dtype, planes, stream);
+  }
+  return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
+}
+
+mcft_status mcft_ffn_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes) {
+  const mcft_status st = check_ffn(desc, T_max);
+  if (st != MCFT_OK) return st;
+  if (!bytes) return fail(MCFT_ERR_INVALID, "bytes is NULL");
+  *bytes = T_max == 0 ? 0 : grad_layout(desc, T_max).total;
+  return MCFT_OK;
+}
+
+mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, const void* block, const void* x, const void* x8,
+                          const void* ckpt, void* dx, void* dblock, int grad_dtype, int accumulate, void* workspace,
+                          size_t ws_bytes, mcft_stream_t stream) {
+  NvtxRange nvtx_range("mcft_ffn_grad");
+  mcft_status st = check_ffn(desc, T);
+  if (st != MCFT_OK) return st;
+  if (!dx && !dblock) return fail(MCFT_ERR_INVALID, "dx and dblock are both NULL");
+  if (dblock && grad_dtype != MCFT_F32 && grad_dtype != desc->dtype)
+    return fail(MCFT_ERR_INVALID, "the block's gradient is fp32 or of the layer dtype, not %d", grad_dtype);
+  if (!aligned(dx, 16) || !aligned(dblock, 16)) return fail(MCFT_ERR_INVALID, "dx and dblock must be 16-byte aligned");
+  const int d = desc->d, w = desc->w;
+  const size_t wd = size_t(w) * d;
+  if (T == 0) {
+    if (dblock && !accumulate) {
+      const cudaError_t e = cudaMemsetAsync(dblock, 0, 3 * wd * elem(grad_dtype), stream);
+      if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync");
+    }
+    return MCFT_OK;
+  }
+  if (!dy || !block) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
+  if (x && x8) return fail(MCFT_ERR_INVALID, "one of x and x8 is wanted, not both");
+  const bool want_x = dblock || !ckpt;
+  if (want_x && !x && !x8) return fail(MCFT_ERR_INVALID, "x and x8 are both NULL");
+  if (!aligned(dy, 16) || !aligned(block, 16) || !aligned(x, 16) || !aligned(x8, 16) || !aligned(ckpt, 16))
+    return fail(MCFT_ERR_INVALID, "dy, block, x, x8 and ckpt must be 16-byte aligned");
+  const GradLayout L = grad_layout(desc, T);
+  st = check_workspace(workspace, ws_bytes, L.total);
+  if (st != MCFT_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  const size_t eb = elem(desc->dtype);
+  const char* w13 = static_cast<const char*>(block);
+  const char* w2 = w13 + 2 * wd * eb;
+  float* planes = reinterpret_cast<float*>(ws + L.planes);
+  float* gu = ckpt ? nullptr : reinterpret_cast<float*>(ws + L.gu);
+  cudaError_t e = cudaSuccess;
+  if (want_x && x8) {
+    e = launch_mx8_quant(Mx8Args{ws + L.x, const_cast<void*>(x8), T, d, d}, desc->dtype, true, stream);
+    x = ws + L.x;
+  }
+  if (desc->dtype == MCFT_BF16) {
+    if (e == cudaSuccess && gu) e = launch_dense_up(DenseUpArgs{x, w13, T, d, w, nullptr, gu, nullptr}, stream);
+    if (e == cudaSuccess)
+      e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), gu, ws + L.h, ws + L.dgu}, stream);
+  } else {
+    if (e == cudaSuccess && gu) {
+      const DenseProduct up{x, w13, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0};
+      e = launch_dense_products(&up, 1, MCFT_F32, planes, stream);
+    }
+    float* dh = reinterpret_cast<float*>(ws + L.dh);
+    if (e == cudaSuccess) {
+      const DenseProduct back{dy, w2, T, w, d, 0, 0, dh, MCFT_F32, 0};
+      e = launch_dense_products(&back, 1, MCFT_F32, planes, stream);
+    }
+    if (e == cudaSuccess)
+      e = launch_dense_act_grad(DenseActArgs{gu, static_cast<const uint8_t*>(ckpt), dh, reinterpret_cast<float*>(ws + L.h),
+                                             reinterpret_cast<float*>(ws + L.dgu), T, w}, stream);
+  }
+  if (e == cudaSuccess) {
+    DenseProduct p[kMaxProducts];
+    int n = 0;
+    if (dblock) {
+      char* out = static_cast<char*>(dblock);
+      p[n++] = DenseProduct{ws + L.dgu, x, 2 * w, d, T, 1, 0, out, grad_dtype, accumulate};
+      p[n++] = DenseProduct{dy, ws + L.h, d, w, T, 1, 0, out + 2 * wd * elem(grad_dtype), grad_dtype, accumulate};
+    }
+    if (dx) p[n++] = DenseProduct{ws + L.dgu, w13, T, d, 2 * w, 0, 0, dx, desc->dtype, 0};
+    for (int i = n - 1; i > 0 && p[i].k > p[i - 1].k; --i) std::swap(p[i], p[i - 1]);  // the longest contraction first
+    e = launch_dense_products(p, n, desc->dtype, planes, stream);
+  }
+  return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward gradient launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,114 @@
+// Launchers of the dense feed-forward block, its 8-bit checkpoints and the RMSNorm ahead of it, shared by api_dense.cu and
+// the kernels. Not part of the C ABI.
+#pragma once
+
+#include "internal.h"
+
+namespace mcft {
+
+int num_sms();
+
+struct Mx8Args {
+  const void* x;  // [R, C], ld elements from row to row (the way back: written)
+  void* q;
+  long long R, C, ld;
+};
+cudaError_t launch_mx8_quant(const Mx8Args& a, int dtype, bool back, cudaStream_t s);
+
+constexpr int kMaxNormD = 32768;  // what 1024 threads hold of a row
+
+struct Norm8Args {
+  const float* x;     // [T, d]
+  const void* y;      // [T, d] layer dtype or NULL
+  const void* gamma;  // [d] layer dtype
+  float* out;         // [T, d] x + y, or NULL
+  void* u;            // [T, d] layer dtype or NULL
+  uint8_t *u8, *x8;   // mx8 [T, d] of u and of x + y, or NULL
+  float* rstd;        // [T] or NULL
+  int T, d;
+  float eps;
+};
+cudaError_t launch_norm8(const Norm8Args& a, int dtype, cudaStream_t s);
+
+struct NormGradArgs {
+  const float* x;     // [T, d], or NULL and
+  const uint8_t* x8;  // mx8 [T, d]
+  const float* rstd;
+  const void *gamma, *du;
+  const float* dres;  // [T, d] or NULL
+  float* dx;          // [T, d] or NULL
+  float* dgamma;      // [d] or NULL
+  float* part;        // [norm_grad_planes(T, d)][d]
+  int T, d, accumulate;
+};
+int norm_grad_planes(int T, int d);
+cudaError_t launch_norm_grad(const NormGradArgs& a, int dtype, cudaStream_t s);
+
+// ---- products ----
+
+// One product C = A B of a launch: rows of C are A's, columns B's, summed over `k`. Operands are row-major matrices of the
+// layer dtype; `a_t`: A is given as [k, rows]; `b_t`: B is given as [columns, k] (else [k, columns]).
+struct DenseProduct {
+  const void *a, *b;
+  int rows, cols, k, a_t, b_t;
+  void* out;       // [rows, cols] of out_dtype, row-major
+  int out_dtype, accumulate;
+};
+constexpr int kMaxProducts = 3;
+constexpr int kDenseTile = 256;  // rows and columns of a bf16 tile
+
+// Fp32 partial sums of products whose contraction is split.
+struct DensePlan {
+  int splits[kMaxProducts], per[kMaxProducts];  // parts of a contraction, steps of each
+  size_t plane[kMaxProducts];                   // where its planes begin, in floats
+  size_t floats;
+};
+// Most bytes that the planes of a launch of `n` products take, whose outputs number `outs` in all and whose contractions
+// are at most `k` long: grows with each, so that it covers smaller calls too.
+size_t dense_plane_bytes(int n, size_t outs, int k, int dtype);
+cudaError_t launch_dense_products(const DenseProduct* p, int n, int dtype, float* planes, cudaStream_t s);
+
+// Sum of `n` fp32 planes [count] into out.
+cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* out, int out_dtype, int accumulate,
+                              cudaStream_t s);
+
+// Gate and up projections of [W1 ; W3] and what follows them, bf16: h = silu(g) u, or g and u in fp32 ([T, 2w], g first).
+struct DenseUpArgs {
+  const void *x, *w13;
+  int T, d, w;
+  void* h;         // [T, w] bf16, or NULL and
+  float* gu;       // [T, 2w] fp32
+  uint8_t* ckpt;   // mx8 [T, 2w] of g and u, or NULL
+};
+cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s);
+
+// dh = dy W2 and what follows it, bf16: dg | du [T, 2w] and h [T, w], from mx8 or fp32 g and u.
+struct DenseUpGradArgs {
+  const void *dy, *w2;
+  int T, d, w;
+  const uint8_t* ckpt;
+  const float* gu;
+  void *h, *dgu;
+};
+cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s);
+
+// The same two steps on fp32 values that products have left in memory.
+struct DenseActArgs {
+  const float* gu;      // [T, 2w], or NULL and
+  const uint8_t* ckpt;  // mx8 [T, 2w]: written by the forward (or NULL), read by the gradient
+  const float* dh;      // [T, w]: the gradient
+  float *h, *dgu;       // [T, w]; [T, 2w]
+  int T, w;
+};
+cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s);
+cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s);
+
+// What the decode kernels expect of a permutation, for one expert that all T tokens take in order.
+struct DenseFewArgs {
+  WsHeader* hdr;
+  int *off, *perm, *done;
+  int T, ndone;
+};
+cudaError_t launch_dense_few(const DenseFewArgs& a, cudaStream_t s);
+
+}  // namespace mcft

@@ -1,0 +1,568 @@
+// Products of the dense gated feed-forward block on the tensor cores (tcgen05 on CTA pairs, TMA, bf16 operands, fp32
+// accumulators), with what follows each in its epilogue:
+//   up       g = x W1^T, u = x W3^T;                h = silu(g) u, and mx8 checkpoints of g and u
+//   up_grad  dh = dy W2;                            dg, du, h from dh and the checkpoints
+//   out      C = A B of up to three problems: y = h W2^T, or dx = [dg | du] [W1 ; W3], d[W1 ; W3] = [dg | du]^T x and
+//            dW2 = dy^T h in one launch, whose tiles fill the SMs together.
+// A tile is 256 rows x 256 columns (up: 128 of g and the same 128 of u), one MMA of M = 256 a step, issued by the pair's
+// leader over both CTAs' shared memory: each CTA brings in its 128 rows of A and 128 of B's columns, 64 of the contraction
+// a stage, 7 stages of 32 KB. Operands are taken as they lie in memory: one whose contiguous index is the contraction's is a
+// K-major operand (a box of 64 x 128), another an MN-major one (two boxes of 64 x 64), so nothing is transposed.
+//   warp 0 (both CTAs) copies; the loads of both complete on the leader's full[s];
+//   warp 1 of the leader issues the MMAs; their commits arrive on empty[s] and tfull[b] of both CTAs;
+//   warps 2-9 (both CTAs) are the epilogue of the CTA's 128 rows, a row a lane: four lane quarters of TMEM by two halves of
+//   the columns, 32 columns (one mx8 block) at a time. Two accumulators of 256 columns let the next tile's MMAs run meanwhile.
+// A persistent grid strides over the tiles, rows fastest inside groups of row tiles that share L2. Tiles of problems that do
+// not fill the pairs are split along the contraction into fp32 planes, which dense_join_kernel adds up in order.
+// Rows and columns past a matrix's end are zeros that TMA fills in, and are not stored.
+// Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (bounded) for its copies and MMAs
+// in flight, frees TMEM and returns.
+#include <string.h>
+
+#include <algorithm>
+
+#include "dense.h"
+#include "dense_act.cuh"
+#include "mx8.cuh"
+#include "row_store.cuh"
+#include "tc_ptx.cuh"
+
+namespace mcft {
+namespace {
+
+constexpr int BK = 64;
+constexpr int kTile = kDenseTile;  // rows, and columns of accumulators
+constexpr int kThreads = 64 + 256;
+constexpr int kEpiWarps = 8;
+constexpr int kStages = 7;
+constexpr int kHalfBytes = 128 * BK * 2;  // a CTA's part of an operand in a stage
+constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kTmemCols = 2 * kTile;
+constexpr int kUpCols = kTile / 2;  // columns of h of an up tile
+// instruction descriptor without the operands' order: D fp32, A and B bf16, N = 256, M = 256
+constexpr uint32_t kIdesc =
+    (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
+constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
+
+enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_OUT = 2 };
+
+struct Problem {
+  CUtensorMap a, b, b1;  // b1: rank 1's columns of an up tile
+  void* out;
+  float* planes;         // splits > 1: fp32 [splits][M][N] instead of out
+  int M, N, kblocks, per, splits, mt, nt, group, first;
+  int a_mn, b_mn, out_f32, accumulate, wide;
+};
+
+struct Params {
+  Problem p[kMaxProducts];
+  int n, items;
+  unsigned* err;
+  // up, up_grad
+  uint8_t* ckpt;
+  float* gu;
+  uint16_t *h, *dgu;
+  int w, wide_h, wide_dgu, wide_ckpt;
+};
+static_assert(sizeof(Params) <= 4096, "kernel parameters");
+
+struct Ctl {
+  uint64_t full[kStages], empty[kStages], tfull[2], tempty[2], drain;
+  uint32_t tmem_base;
+  int abort;
+};
+constexpr int kSmem = kStages * kStageBytes + 1024 + int(sizeof(Ctl));
+static_assert(kSmem <= 227 * 1024, "shared memory");
+
+struct Item {
+  const Problem* p;
+  int mt, nt, split, k0, k1;
+};
+
+__device__ __forceinline__ Item item_at(const Params& q, int item) {
+  Item t;
+  int i = 0;
+  while (i + 1 < q.n && item >= q.p[i + 1].first) ++i;
+  t.p = &q.p[i];
+  const int local = item - t.p->first, tiles = t.p->mt * t.p->nt;
+  t.split = local / tiles;
+  const int tile = local - t.split * tiles, G = t.p->group;
+  const int g = tile / (G * t.p->nt), r = tile - g * G * t.p->nt, size = min(G, t.p->mt - g * G);
+  t.nt = r / size;
+  t.mt = g * G + r % size;
+  t.k0 = t.split * t.p->per;
+  t.k1 = min(t.k0 + t.p->per, t.p->kblocks);
+  return t;
+}
+
+// Operand of a stage: K-major rows of 128 bytes, or two boxes of 64 contiguous rows by 64 of the contraction.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn) {
+  const uint64_t lead = mn ? uint64_t((BK * 128) >> 4) : 1u;
+  return uint64_t((saddr >> 4) & 0x3FFFu) | (lead << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) |
+         (uint64_t(2) << 61);
+}
+
+__device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap* map, bool mn, int k, int at, uint32_t bar) {
+  if (mn) {
+    tma_load_2d_pair(to, map, at, k, bar);
+    tma_load_2d_pair(to + kHalfBytes / 2, map, at + 64, k, bar);
+  } else {
+    tma_load_2d_pair(to, map, k, at, bar);
+  }
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  tmem_ld16(taddr, r);
+  tmem_ld16(taddr + 16, r + 16);
+}
+
+// 64 bytes of each lane's row (NULL: none).
+__device__ __forceinline__ void put64(void* row, uint32_t* u, int wide) {
+  if (wide) store_rows64<32>(row, u);
+  else store_rows64<16>(row, u);
+}
+
+// A row's 32 values to a block of the checkpoint.
+__device__ __forceinline__ void put_mx8(uint8_t* code, uint8_t* scale, const uint32_t* bits, int wide) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) m = max(m, bits[i] & 0x7fffffffu);
+  const uint32_t s = mx8_scale(m);
+  const float k = mx8_inverse(s);
+  uint32_t c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    c[i] = mx8_quad(__uint_as_float(bits[4 * i]) * k, __uint_as_float(bits[4 * i + 1]) * k,
+                    __uint_as_float(bits[4 * i + 2]) * k, __uint_as_float(bits[4 * i + 3]) * k);
+  if (wide) store32(code, c);
+  else store32_by16(code, c);
+  *scale = uint8_t(s);
+}
+
+__device__ __forceinline__ void get_mx8(const uint8_t* code, uint32_t scale, float* v) {
+  const uint4 a = ldg16(code), b = ldg16(code + 16);
+  const uint32_t c[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const float unit = mx8_unit(scale);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) mx8_values(c[i], v + 4 * i);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] *= unit;
+}
+
+template <int EPI>
+__device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_t taddr, int row, int half) {
+  const Problem& p = *t.p;
+  const bool in = row < p.M;
+  const size_t r = size_t(in ? row : 0);
+  if constexpr (EPI == EPI_UP) {
+    const size_t w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
+#pragma unroll 1
+    for (int c = half * 64; c < half * 64 + 64; c += 32) {
+      const int col = t.nt * kUpCols + c;
+      if (col >= q.w) break;
+      uint32_t g[32], u[32];
+      tmem_ld32(taddr + c, g);
+      tmem_ld32(taddr + kUpCols + c, u);
+      tmem_ld_wait();
+      if (q.gu) {
+        float* to = in ? q.gu + r * 2 * w + col : nullptr;
+        put64(to, g, 1);
+        put64(to ? to + 16 : nullptr, g + 16, 1);
+        to = to ? to + w : nullptr;
+        put64(to, u, 1);
+        put64(to ? to + 16 : nullptr, u + 16, 1);
+        continue;
+      }
+      if (q.ckpt && in) {
+        uint8_t* code = q.ckpt + r * 2 * w + col;
+        uint8_t* scale = q.ckpt + scales + r * 2 * nb + col / 32;
+        put_mx8(code, scale, g, q.wide_ckpt);
+        put_mx8(code + w, scale + nb, u, q.wide_ckpt);
+      }
+      uint32_t h[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        h[i] = pack2bf(swiglu(__uint_as_float(g[2 * i]), __uint_as_float(u[2 * i])),
+                       swiglu(__uint_as_float(g[2 * i + 1]), __uint_as_float(u[2 * i + 1])));
+      put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
+    }
+  } else if constexpr (EPI == EPI_UP_GRAD) {
+    const size_t w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
+#pragma unroll 1
+    for (int c = half * 128; c < half * 128 + 128; c += 32) {
+      const int col = t.nt * kTile + c;
+      if (col >= q.w) break;
+      float g[32], u[32];
+      if (q.ckpt) {
+        const uint8_t* code = q.ckpt + r * 2 * w + col;
+        const uint8_t* scale = q.ckpt + scales + r * 2 * nb + col / 32;
+        get_mx8(code, __ldg(scale), g);
+        get_mx8(code + w, __ldg(scale + nb), u);
+      } else {
+        const float4* from = reinterpret_cast<const float4*>(q.gu + r * 2 * w + col);
+        const float4* more = reinterpret_cast<const float4*>(q.gu + r * 2 * w + w + col);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float4 a = __ldg(from + i), b = __ldg(more + i);
+          g[4 * i] = a.x; g[4 * i + 1] = a.y; g[4 * i + 2] = a.z; g[4 * i + 3] = a.w;
+          u[4 * i] = b.x; u[4 * i + 1] = b.y; u[4 * i + 2] = b.z; u[4 * i + 3] = b.w;
+        }
+      }
+      uint32_t dh[32];
+      tmem_ld32(taddr + c, dh);
+      tmem_ld_wait();
+      uint32_t h[16], dg[16], du[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const SwigluGrad lo(g[2 * i], u[2 * i], __uint_as_float(dh[2 * i]));
+        const SwigluGrad hi(g[2 * i + 1], u[2 * i + 1], __uint_as_float(dh[2 * i + 1]));
+        h[i] = pack2bf(lo.h, hi.h);
+        dg[i] = pack2bf(lo.dg, hi.dg);
+        du[i] = pack2bf(lo.du, hi.du);
+      }
+      put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
+      uint16_t* to = in ? q.dgu + r * 2 * w + col : nullptr;
+      put64(to, dg, q.wide_dgu);
+      put64(to ? to + w : nullptr, du, q.wide_dgu);
+    }
+  } else {
+    const size_t N = size_t(p.N);
+#pragma unroll 1
+    for (int c = half * 128; c < half * 128 + 128; c += 32) {
+      const int col = t.nt * kTile + c;
+      if (col >= p.N) break;
+      uint32_t v[32];
+      tmem_ld32(taddr + c, v);
+      tmem_ld_wait();
+      const size_t at = r * N + col;
+      if (p.splits > 1 || p.out_f32) {
+        float* base = p.splits > 1 ? p.planes + size_t(t.split) * p.M * N : static_cast<float*>(p.out);
+        float* to = in ? base + at : nullptr;
+        if (p.accumulate && p.splits == 1 && in) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 o = reinterpret_cast<const float4*>(to)[i];
+            v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + o.x);
+            v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + o.y);
+            v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + o.z);
+            v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + o.w);
+          }
+        }
+        put64(to, v, p.wide);
+        put64(to ? to + 16 : nullptr, v + 16, p.wide);
+      } else {
+        uint16_t* to = in ? static_cast<uint16_t*>(p.out) + at : nullptr;
+        uint32_t o[16] = {};
+        if (p.accumulate && in) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(to)[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
+          if (p.accumulate) {
+            lo += bf16lo(o[i]);
+            hi += bf16hi(o[i]);
+          }
+          o[i] = pack2bf(lo, hi);
+        }
+        put64(to, o, p.wide);
+      }
+    }
+  }
+}
+
+template <int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    dense_gemm_kernel(const __grid_constant__ Params q) {
+  pdl_wait();
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;  // the same offsets in both CTAs
+  Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + kStages * kStageBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const bool leader = rank == 0;
+  if (threadIdx.x == 0) {
+    ctl->abort = 0;
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->tfull[b], 1);
+      mbar_init(&ctl->tempty[b], 2 * kEpiWarps);
+    }
+    mbar_init(&ctl->drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  cluster_sync();  // barriers initialised and TMEM allocated in both CTAs
+  tc_fence_after();
+
+  const uint32_t tmem = ctl->tmem_base;
+  const int items = q.items, cid = int(blockIdx.x >> 1), ncl = int(gridDim.x >> 1);
+  volatile int* abort = &ctl->abort;
+
+  if (warp == 0) {
+    if (cid < items && elect_one()) {
+      const uint32_t fb0 = peer_addr(&ctl->full[0], 0);
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      for (int item = cid; item < items && !*abort; item += ncl) {
+        const Item t = item_at(q, item);
+        const int arow = t.mt * kTile + int(rank) * 128;
+        const CUtensorMap* mb = EPI == EPI_UP && rank ? &t.p->b1 : &t.p->b;
+        const int brow = EPI == EPI_UP ? t.nt * kUpCols : t.nt * kTile + int(rank) * 128;
+        const bool a_mn = EPI == EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_OUT && t.p->b_mn);
+        for (int kb = t.k0; kb < t.k1; ++kb) {
+          if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, q.err)) break;
+          const uint32_t sa = base + uint32_t(s) * kStageBytes, fb = fb0 + uint32_t(s) * 8u;
+          if (leader) mbar_expect_tx(&ctl->full[s], 2 * kStageBytes);
+          load_operand(sa, &t.p->a, a_mn, kb * BK, arow, fb);
+          load_operand(sa + kHalfBytes, mb, b_mn, kb * BK, brow, fb);
+          if (issued < kStages) ++issued;
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      // Stages still in flight: the leader waits for their bytes (both CTAs'), the peer until the leader's MMAs consumed
+      // them, oldest first; after the first wait that runs out the rest are skipped.
+      for (int i = 0; i < issued; ++i) {
+        const int j = s - (issued - i);
+        uint64_t* ring = leader ? ctl->full : ctl->empty;
+        if (!mbar_wait_drain_cl(&ring[j < 0 ? j + kStages : j], j < 0 ? ph ^ 1u : ph, q.err)) break;
+      }
+    }
+  } else if (warp == 1) {
+    if (leader && cid < items && elect_one()) {
+      int s = 0;
+      uint32_t ph = 0, lt = 0;
+      for (int item = cid; item < items && !*abort; item += ncl) {
+        const Item t = item_at(q, item);
+        const bool a_mn = EPI == EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_OUT && t.p->b_mn);
+        const uint32_t idesc = kIdesc | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
+        // 16 of the contraction: 32 bytes of each K-major row, or 16 rows of 128 bytes
+        const uint64_t ka = a_mn ? (16 * 128) >> 4 : 32 >> 4, kb_ = b_mn ? (16 * 128) >> 4 : 32 >> 4;
+        const uint32_t b = lt & 1u;
+        if (!mbar_wait_cl(&ctl->tempty[b], ((lt >> 1) & 1u) ^ 1u, abort, q.err)) break;
+        tc_fence_after();
+        const uint32_t dt = tmem + b * kTile;
+        bool ok = true;
+        for (int kb = t.k0; kb < t.k1; ++kb) {
+          if (!mbar_wait_cl(&ctl->full[s], ph, abort, q.err)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t sa = base + uint32_t(s) * kStageBytes;
+          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + kHalfBytes, b_mn);
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)
+            tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (kb != t.k0 || k != 0) ? 1u : 0u);
+          tc_commit_pair_both(&ctl->empty[s]);
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        if (!ok) break;
+        tc_commit_pair_both(&ctl->tfull[b]);
+        ++lt;
+      }
+      tc_commit_pair(&ctl->drain);  // arrives once every MMA issued above has completed
+      mbar_wait_drain_cl(&ctl->drain, 0, q.err);
+    }
+  } else {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;  // TMEM lanes this warp may access, columns it takes
+    uint32_t lt = 0;
+    for (int item = cid; item < items; item += ncl) {
+      const Item t = item_at(q, item);
+      const uint32_t b = lt & 1u;
+      int ok = 1;
+      if (lane == 0) ok = mbar_wait_cl(&ctl->tfull[b], (lt >> 1) & 1u, abort, q.err) ? 1 : 0;
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) break;
+      tc_fence_after();
+      epilogue<EPI>(q, t, tmem + b * kTile + (uint32_t(quarter * 32) << 16),
+                    t.mt * kTile + int(rank) * 128 + quarter * 32 + lane, half);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(peer_addr(&ctl->tempty[b], 0));
+      ++lt;
+    }
+  }
+
+  tc_fence_before();
+  cluster_sync();  // the leader's MMAs drained, every copy landed, both epilogues done
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// bf16 matrix [rows, cols] row-major; a box of 64 columns (128 bytes, one swizzle span) and box_rows rows.
+bool encode(CUtensorMap* m, const void* base, size_t cols, size_t rows, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {cols * 2};
+  const cuuint32_t box[2] = {BK, cuuint32_t(box_rows)};
+  const cuuint32_t es[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+
+constexpr size_t kGroupBytes = size_t(24) << 20;  // of A that the row tiles of a group read
+
+void shape(Problem& p, int M, int N, int K, int tile_cols) {
+  p.M = M;
+  p.N = N;
+  p.kblocks = (K + BK - 1) / BK;
+  p.per = p.kblocks;
+  p.splits = 1;
+  p.mt = (M + kTile - 1) / kTile;
+  p.nt = (N + tile_cols - 1) / tile_cols;
+  p.group = int(std::clamp<size_t>(kGroupBytes / (size_t(kTile) * K * 2), 1, 4096));
+}
+
+template <int EPI>
+int pairs_at_once() {
+  static SmemOptIn smem;
+  static ResidentClusters resident;
+  const void* fn = reinterpret_cast<const void*>(dense_gemm_kernel<EPI>);
+  if (smem.allow(fn, kSmem) != cudaSuccess) return 0;
+  return resident.get(fn, num_sms() & ~1, kThreads, kSmem);
+}
+
+template <int EPI>
+cudaError_t launch(Params& q, int kid, cudaStream_t s) {
+  q.err = device_error_word();
+  q.items = 0;
+  for (int i = 0; i < q.n; ++i) {
+    q.p[i].first = q.items;
+    q.items += q.p[i].mt * q.p[i].nt * q.p[i].splits;
+  }
+  const int pairs = pairs_at_once<EPI>();
+  if (pairs < 1) return cudaErrorInvalidConfiguration;
+  prof_begin(kid, s);
+  const cudaError_t e = launch_pdl(dense_gemm_kernel<EPI>, dim3(unsigned(2 * std::min(pairs, q.items))), dim3(kThreads), kSmem, s, q);
+  prof_end(kid, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
+  Params q;
+  memset(&q, 0, sizeof(q));
+  q.n = 1;
+  Problem& p = q.p[0];
+  shape(p, a.T, a.w, a.d, kUpCols);
+  const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
+  if (!encode(&p.a, a.x, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, w1, size_t(a.d), size_t(a.w), 128) ||
+      !encode(&p.b1, w1 + size_t(a.w) * a.d, size_t(a.d), size_t(a.w), 128))
+    return cudaErrorInvalidValue;
+  q.w = a.w;
+  q.h = static_cast<uint16_t*>(a.h);
+  q.gu = a.gu;
+  q.ckpt = a.ckpt;
+  q.wide_h = wide(a.h);
+  q.wide_ckpt = wide(a.ckpt);
+  return launch<EPI_UP>(q, kProfDenseUp, s);
+}
+
+cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
+  Params q;
+  memset(&q, 0, sizeof(q));
+  q.n = 1;
+  Problem& p = q.p[0];
+  shape(p, a.T, a.w, a.d, kTile);
+  p.b_mn = 1;
+  if (!encode(&p.a, a.dy, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, a.w2, size_t(a.w), size_t(a.d), 64))
+    return cudaErrorInvalidValue;
+  q.w = a.w;
+  q.ckpt = const_cast<uint8_t*>(a.ckpt);
+  q.gu = const_cast<float*>(a.gu);
+  q.h = static_cast<uint16_t*>(a.h);
+  q.dgu = static_cast<uint16_t*>(a.dgu);
+  q.wide_h = wide(a.h);
+  q.wide_dgu = wide(a.dgu);
+  return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
+}
+
+// Splits where the tiles leave pairs idle: parts of at least 4 steps (below that an item is mostly its fill and its
+// stores), as short as they can be with all items running at once.
+DensePlan dense_tc_plan(const DenseProduct* in, int n) {
+  DensePlan plan = {};
+  Problem p[kMaxProducts];
+  int tiles = 0, longest = 1;
+  for (int i = 0; i < n; ++i) {
+    shape(p[i], in[i].rows, in[i].cols, in[i].k, kTile);
+    tiles += p[i].mt * p[i].nt;
+    longest = std::max(longest, p[i].kblocks);
+    plan.splits[i] = 1;
+    plan.per[i] = p[i].kblocks;
+  }
+  const int pairs = num_sms() / 2;
+  if (tiles >= pairs) return plan;
+  for (int unit = 4; unit <= longest; ++unit) {
+    long long items = 0;
+    for (int i = 0; i < n; ++i) items += (long long)p[i].mt * p[i].nt * ((p[i].kblocks + unit - 1) / unit);
+    if (items > pairs && unit < longest) continue;
+    for (int i = 0; i < n; ++i) {
+      plan.splits[i] = (p[i].kblocks + unit - 1) / unit;
+      plan.per[i] = (p[i].kblocks + plan.splits[i] - 1) / plan.splits[i];
+      plan.splits[i] = (p[i].kblocks + plan.per[i] - 1) / plan.per[i];
+      plan.plane[i] = plan.floats;
+      if (plan.splits[i] > 1) plan.floats += size_t(plan.splits[i]) * in[i].rows * in[i].cols;
+    }
+    break;
+  }
+  return plan;
+}
+
+cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaStream_t s) {
+  Params q;
+  memset(&q, 0, sizeof(q));
+  q.n = n;
+  const DensePlan plan = dense_tc_plan(in, n);
+  for (int i = 0; i < n; ++i) {
+    const DenseProduct& d = in[i];
+    Problem& p = q.p[i];
+    shape(p, d.rows, d.cols, d.k, kTile);
+    p.splits = plan.splits[i];
+    p.per = plan.per[i];
+    p.a_mn = d.a_t;
+    p.b_mn = !d.b_t;
+    const size_t M = size_t(d.rows), N = size_t(d.cols), K = size_t(d.k);
+    if (!(d.a_t ? encode(&p.a, d.a, M, K, 64) : encode(&p.a, d.a, K, M, 128)) ||
+        !(d.b_t ? encode(&p.b, d.b, K, N, 128) : encode(&p.b, d.b, N, K, 64)))
+      return cudaErrorInvalidValue;
+    p.out = d.out;
+    p.planes = planes + plan.plane[i];
+    p.out_f32 = d.out_dtype == MCFT_F32;
+    p.accumulate = d.accumulate;
+    p.wide = p.splits > 1 ? wide(planes) : wide(d.out);
+  }
+  cudaError_t e = launch<EPI_OUT>(q, kProfDenseOut, s);
+  for (int i = 0; i < n && e == cudaSuccess; ++i)
+    if (plan.splits[i] > 1)
+      e = launch_dense_join(planes + plan.plane[i], plan.splits[i], size_t(in[i].rows) * in[i].cols, in[i].out,
+                            in[i].out_dtype, in[i].accumulate, s);
+  return e;
+}
+
+}  // namespace mcft

@@ -1,0 +1,288 @@
+// RMSNorm of the fp32 stream with the residual's addition and 8-bit (mx8) outputs, and its gradient.
+//
+//   v = x + y,  r = 1 / sqrt(mean_j v[j]^2 + eps),  u = v r gamma;  u and v also as mx8 (mx8.cuh)
+//   with n = v r and g = du gamma:  dx = dres + r (g - n mean_j(g[j] n[j])),  dgamma = sum_t du n
+//
+// A row belongs to a team of 8 to 1024 threads (a power of two) that hold it in registers, 8 neighbouring values
+// a thread and step, so every value is read once; four neighbouring lanes hold a block of mx8. Sums go through a
+// shuffle tree and then over warps in order: the same bits every time. Both are bound by HBM.
+// The gradient's CTAs stride over rows and keep their share of dgamma in registers; the shares are added in order by
+// a second kernel.
+#include "dense.h"
+#include "mx8.cuh"
+
+namespace mcft {
+namespace {
+
+template <typename T>
+__device__ __forceinline__ void load8(const void* p, size_t i, float* v) {
+  if constexpr (sizeof(T) == 2) {
+    unpack8(*reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + i), v);
+  } else {
+    const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + i);
+    const float4 a = q[0], b = q[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(void* p, size_t i, const float* v) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p) + i) =
+        make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
+  } else {
+    float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + i);
+    q[0] = make_float4(v[0], v[1], v[2], v[3]);
+    q[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// The eight values of a lane as a quarter of an mx8 block; `at`: of the first value in the codes. All lanes of a warp call it.
+__device__ __forceinline__ void store_mx8(uint8_t* q, size_t scales, size_t at, const float* v, bool ok) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, mag(v[i]));
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  const uint32_t s = mx8_scale(m);
+  const float k = mx8_inverse(s);
+  if (!ok) return;
+  *reinterpret_cast<uint2*>(q + at) = make_uint2(mx8_quad(v[0] * k, v[1] * k, v[2] * k, v[3] * k),
+                                                 mx8_quad(v[4] * k, v[5] * k, v[6] * k, v[7] * k));
+  if ((threadIdx.x & 3) == 0) q[scales + at / 32] = uint8_t(s);
+}
+
+// Sum over a team of 2^lg threads. part: 32 floats that no other sum of the CTA is using.
+__device__ __forceinline__ float team_sum(float s, int lg, float* part) {
+  const int n = lg < 5 ? 1 << lg : 32;
+  for (int o = n >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lg <= 5) return s;
+  const int warp = threadIdx.x >> 5, per = 1 << (lg - 5), w0 = warp & ~(per - 1);
+  if ((threadIdx.x & 31) == 0) part[warp] = s;
+  __syncthreads();
+  s = part[w0];
+  for (int w = 1; w < per; ++w) s += part[w0 + w];
+  return s;
+}
+
+template <typename T, int NG, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ Norm8Args a, int lg) {
+  pdl_wait();
+  __shared__ float part[32];
+  const int lane = threadIdx.x & ((1 << lg) - 1), groups = a.d / 8;
+  const long long row = (long long)blockIdx.x * (blockDim.x >> lg) + (threadIdx.x >> lg);
+  const bool in = row < a.T;
+  const size_t base = size_t(in ? row : 0) * a.d, scales = size_t(a.T) * a.d;
+  float v[NG][8];
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const int c = lane + (j << lg);
+    if (in && c < groups) {
+      load8<float>(a.x, base + c * 8, v[j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+    }
+  }
+  if (a.y) {
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      const int c = lane + (j << lg);
+      if (in && c < groups) {
+        float y[8];
+        load8<T>(a.y, base + c * 8, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] += y[i];
+      }
+    }
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const int c = lane + (j << lg);
+    const bool ok = in && c < groups;
+    if (ok && a.out) store8<float>(a.out, base + c * 8, v[j]);
+    if (a.x8) store_mx8(a.x8, scales, base + c * 8, v[j], ok);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss = fmaf(v[j][i], v[j][i], ss);
+  }
+  const float r = 1.0f / sqrtf(team_sum(ss, lg, part) / float(a.d) + a.eps);
+  if (in && lane == 0 && a.rstd) a.rstd[row] = r;
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const int c = lane + (j << lg);
+    const bool ok = in && c < groups;
+    float g[8] = {};
+    if (ok) load8<T>(a.gamma, size_t(c) * 8, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = v[j][i] * r * g[i];
+    if (ok && a.u) store8<T>(a.u, base + c * 8, g);
+    if (a.u8) store_mx8(a.u8, scales, base + c * 8, g, ok);
+  }
+}
+
+template <typename T, int NG, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm_grad_kernel(const __grid_constant__ NormGradArgs a, int lg) {
+  pdl_wait();
+  __shared__ float part[2][32];
+  __shared__ float share[THREADS == 256 && NG == 1 ? 2048 : 1];  // several teams: [team][8 values of a thread]
+  const int lane = threadIdx.x & ((1 << lg) - 1), team = threadIdx.x >> lg, teams = blockDim.x >> lg, groups = a.d / 8;
+  const size_t scales = size_t(a.T) * a.d;
+  const float over_d = 1.0f / float(a.d);
+  float dg[NG][8] = {};
+  int turn = 0;
+  for (long long row0 = (long long)blockIdx.x * teams; row0 < a.T; row0 += (long long)gridDim.x * teams, turn ^= 1) {
+    const long long row = row0 + team;
+    const bool in = row < a.T;
+    const size_t base = size_t(in ? row : 0) * a.d;
+    const float r = in ? a.rstd[row] : 0.f;
+    float n[NG][8], g[NG][8], res[NG][8];
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      const int c = lane + (j << lg);
+      const bool ok = in && c < groups;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[j][i] = g[j][i] = res[j][i] = 0.f;
+      if (ok) {
+        const size_t at = base + c * 8;
+        if (a.x8) {
+          const uint2 q = *reinterpret_cast<const uint2*>(a.x8 + at);
+          const float unit = mx8_unit(a.x8[scales + at / 32]);
+          mx8_values(q.x, n[j]);
+          mx8_values(q.y, n[j] + 4);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) n[j][i] *= unit;
+        } else {
+          load8<float>(a.x, at, n[j]);
+        }
+        load8<T>(a.du, at, g[j]);
+        if (a.dres) load8<float>(a.dres, at, res[j]);
+      }
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      const int c = lane + (j << lg);
+      float gam[8] = {};
+      if (c < groups) load8<T>(a.gamma, size_t(c) * 8, gam);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        n[j][i] *= r;
+        dg[j][i] = fmaf(g[j][i], n[j][i], dg[j][i]);
+        g[j][i] *= gam[i];
+        dot = fmaf(g[j][i], n[j][i], dot);
+      }
+    }
+    dot = team_sum(dot, lg, part[turn]) * over_d;
+    if (a.dx && in) {
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        const int c = lane + (j << lg);
+        if (c < groups) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) res[j][i] = fmaf(r, fmaf(-n[j][i], dot, g[j][i]), res[j][i]);
+          store8<float>(a.dx, base + c * 8, res[j]);
+        }
+      }
+    }
+  }
+  if (!a.dgamma) return;
+  float* plane = a.part + size_t(blockIdx.x) * a.d;
+  if (teams == 1) {
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      const int c = lane + (j << lg);
+      if (c < groups) store8<float>(plane, size_t(c) * 8, dg[j]);
+    }
+  } else if constexpr (THREADS == 256 && NG == 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) share[threadIdx.x * 8 + i] = dg[0][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.d; c += 256) {
+      float s = 0.f;
+      for (int t = 0; t < teams; ++t) s += share[(t << (lg + 3)) + c];
+      plane[c] = s;
+    }
+  }
+}
+
+// 32 columns a CTA: a warp adds up every 32nd plane of them, then the warps' sums are added in order.
+__global__ void __launch_bounds__(1024) norm_planes_kernel(const __grid_constant__ NormGradArgs a, int planes) {
+  pdl_wait();
+  __shared__ float sum[32][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = int(blockIdx.x) * 32 + lane;
+  float s = 0.f;
+  for (int p = warp; p < planes; p += 32) s += a.part[size_t(p) * a.d + c];
+  sum[warp][lane] = s;
+  __syncthreads();
+  if (warp) return;
+  s = a.accumulate ? a.dgamma[c] : 0.f;
+#pragma unroll
+  for (int w = 0; w < 32; ++w) s += sum[w][lane];
+  a.dgamma[c] = s;
+}
+
+// How a row is shared out: 2^lg threads of 8 values, `steps` of them each.
+struct Teams {
+  int lg, steps, threads;
+  explicit Teams(int d) {
+    const int groups = d / 8;
+    lg = 3;
+    while (lg < 8 && (1 << lg) < groups) ++lg;  // up to 2048 values: one step
+    steps = 1;
+    if ((1 << lg) < groups) {
+      steps = 2;
+      while (lg < 10 && (2 << lg) < groups) ++lg;
+      if ((2 << lg) < groups) steps = 4;
+    }
+    threads = lg > 8 ? 1 << lg : 256;
+  }
+  int rows() const { return threads >> lg; }
+};
+
+template <typename T>
+cudaError_t forward(const Norm8Args& a, cudaStream_t s) {
+  const Teams t(a.d);
+  const dim3 grid{unsigned((a.T + t.rows() - 1) / t.rows())};
+  auto* k = t.steps == 1 ? norm8_kernel<T, 1, 256>
+            : t.steps == 2 ? (t.threads == 256 ? norm8_kernel<T, 2, 256> : norm8_kernel<T, 2, 1024>)
+                           : norm8_kernel<T, 4, 1024>;
+  return launch_pdl(k, grid, dim3(unsigned(t.threads)), 0, s, a, t.lg);
+}
+
+template <typename T>
+cudaError_t backward(const NormGradArgs& a, cudaStream_t s) {
+  const Teams t(a.d);
+  const int planes = norm_grad_planes(a.T, a.d);
+  auto* k = t.steps == 1 ? norm_grad_kernel<T, 1, 256>
+            : t.steps == 2 ? (t.threads == 256 ? norm_grad_kernel<T, 2, 256> : norm_grad_kernel<T, 2, 1024>)
+                           : norm_grad_kernel<T, 4, 1024>;
+  const cudaError_t e = launch_pdl(k, dim3(unsigned(planes)), dim3(unsigned(t.threads)), 0, s, a, t.lg);
+  if (e != cudaSuccess || !a.dgamma) return e;
+  return launch_pdl(norm_planes_kernel, dim3(unsigned(a.d / 32)), dim3(1024), 0, s, a, planes);
+}
+
+}  // namespace
+
+cudaError_t launch_norm8(const Norm8Args& a, int dtype, cudaStream_t s) {
+  prof_begin(kProfNorm8, s);
+  const cudaError_t e = dtype == MCFT_BF16 ? forward<uint16_t>(a, s) : forward<float>(a, s);
+  prof_end(kProfNorm8, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+int norm_grad_planes(int T, int d) {
+  const Teams t(d);
+  const int rows = (T + t.rows() - 1) / t.rows(), most = num_sms() * (1024 / t.threads);
+  return rows < most ? rows : most;
+}
+
+cudaError_t launch_norm_grad(const NormGradArgs& a, int dtype, cudaStream_t s) {
+  prof_begin(kProfNormGrad, s);
+  const cudaError_t e = dtype == MCFT_BF16 ? backward<uint16_t>(a, s) : backward<float>(a, s);
+  prof_end(kProfNormGrad, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace mcft

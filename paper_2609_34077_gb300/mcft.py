@@ -66,6 +66,16 @@ SIGNATURES = {
     "mcft_mx4_pack_expert": (_i, [_vp, _vp, _vp, _vp]),
     "mcft_mx4_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
     "mcft_moe_forward_mx4": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mcft_mx8_size": (_i, [_ll, _ll, C.POINTER(_sz)]),
+    "mcft_mx8_quantize": (_i, [_vp, _ll, _ll, _ll, _i, _vp, _vp]),
+    "mcft_mx8_dequantize": (_i, [_vp, _ll, _ll, _i, _vp, _ll, _vp]),
+    "mcft_residual_rmsnorm_mx8": (_i, [_vp, _vp, _vp, _i, _vp, C.c_float, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mcft_rmsnorm_grad_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
+    "mcft_rmsnorm_grad": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "mcft_ffn_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
+    "mcft_ffn_forward": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mcft_ffn_grad_workspace_size": (_i, [_vp, _i, C.POINTER(_sz)]),
+    "mcft_ffn_grad": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _sz, _vp]),
     "mcft_device_error": (_i, [_vp]),
     "mcft_test_inject": (_i, [_i, _i, C.c_ulonglong, _i]),
     "mcft_profile_enable": (_i, [_i]),
@@ -739,3 +749,167 @@ def mcft_moe_forward_mx4(desc: LayerDesc, x, idx, gate, experts, shared=(), y=No
                                       sh.buffer_info()[0], _ptr(y), _ptr(workspace), workspace.numel(),
                                       _stream(stream)))
     return y
+
+
+def _size_of(call, *args) -> int:
+    n = C.c_size_t(0)
+    _check(call(*args, C.byref(n)))
+    return n.value
+
+
+def mcft_mx8_size(rows: int, cols: int) -> int:
+    return _size_of(lib().mcft_mx8_size, int(rows), int(cols))
+
+
+def _wants_mx8(q, rows, cols, what):
+    _wants(q.dtype == torch.uint8 and (rows <= 0 or cols <= 0 or q.numel() >= rows * -(-cols // 32) * 33), what)
+
+
+def mcft_mx8_quantize(x, q=None, stream=None):
+    """The mx8 matrix (a uint8 tensor of mcft_mx8_size bytes) of x [rows, cols], fp32 or bf16."""
+    rows, cols = x.shape
+    ptr, ld = _rows(x)
+    if q is None:
+        q = _empty(mcft_mx8_size(rows, cols), torch.uint8, x.device, stream)
+    else:
+        _wants_mx8(q, rows, cols, "q is uint8 of mcft_mx8_size(rows, cols) bytes")
+    _check(lib().mcft_mx8_quantize(ptr, rows, cols, ld, _MX4_DTYPE[x.dtype], _ptr(q), _stream(stream)))
+    return q
+
+
+def mcft_mx8_dequantize(q, rows, cols, dtype=torch.bfloat16, y=None, stream=None):
+    """The values [rows, cols] that the mx8 matrix q stands for, fp32 or bf16."""
+    _wants_mx8(q, rows, cols, "q is uint8 of mcft_mx8_size(rows, cols) bytes")
+    if y is None:
+        y = _empty((rows, cols), dtype, q.device, stream)
+    else:
+        _wants(y.shape == (rows, cols), "y is [rows, cols]")
+    ptr, ld = _rows(y)
+    _check(lib().mcft_mx8_dequantize(_ptr(q), rows, cols, _MX4_DTYPE[y.dtype], ptr, ld, _stream(stream)))
+    return y
+
+
+def mcft_residual_rmsnorm_mx8(desc: LayerDesc, x, y=None, gamma=None, eps=1e-5, out=None, u=None, u8=None, x8=None,
+                              rstd=None, stream=None):
+    """(out [T, d] fp32 = x + y, u [T, d] of the layer dtype, its mx8 matrix u8, rstd [T] fp32), allocated on x's
+    device if not given (out=x updates the stream in place); writes x8, the mx8 matrix of out, where given."""
+    T, d, dtype = x.shape[0], desc.d, torch_dtype(desc)
+    _wants(_is(x, torch.float32, T, d), "x is fp32 [T, d]")
+    _wants(y is None or _is(y, dtype, T, d), "y is [T, d] of the layer dtype")
+    _wants(gamma is not None and _is(gamma, dtype, d), "gamma is [d] of the layer dtype")
+    if out is None:
+        out = _empty((T, d), torch.float32, x.device, stream)
+    else:
+        _wants(_is(out, torch.float32, T, d), "out is fp32 [T, d]")
+    if u is None:
+        u = _empty((T, d), dtype, x.device, stream)
+    else:
+        _wants(_is(u, dtype, T, d), "u is [T, d] of the layer dtype")
+    if u8 is None:
+        u8 = _empty(mcft_mx8_size(T, d), torch.uint8, x.device, stream)
+    else:
+        _wants_mx8(u8, T, d, "u8 is uint8 of mcft_mx8_size(T, d) bytes")
+    if x8 is not None:
+        _wants_mx8(x8, T, d, "x8 is uint8 of mcft_mx8_size(T, d) bytes")
+    if rstd is None:
+        rstd = _empty((T,), torch.float32, x.device, stream)
+    else:
+        _wants(_is(rstd, torch.float32, T), "rstd is fp32 [T]")
+    _check(lib().mcft_residual_rmsnorm_mx8(C.byref(desc), _ptr(x), _ptr(y), T, _ptr(gamma), C.c_float(eps), _ptr(out),
+                                           _ptr(u), _ptr(u8), _ptr(x8), _ptr(rstd), _stream(stream)))
+    return out, u, u8, rstd
+
+
+def mcft_rmsnorm_grad_workspace_size(desc: LayerDesc, T_max: int) -> int:
+    return _size_of(lib().mcft_rmsnorm_grad_workspace_size, C.byref(desc), int(T_max))
+
+
+def mcft_rmsnorm_grad(desc: LayerDesc, gamma, rstd, du, dres=None, x=None, x8=None, dx=None, dgamma=None,
+                      accumulate=False, workspace=None, stream=None):
+    """(dx [T, d] fp32, dgamma [d] fp32) from du = dL/du, the stream's gradient dres past the norm, and the normalised
+    stream as fp32 x or as its mx8 matrix x8; dgamma is added to if accumulate."""
+    T, d, dtype = du.shape[0], desc.d, torch_dtype(desc)
+    _wants(_is(du, dtype, T, d) and _is(gamma, dtype, d), "du is [T, d] and gamma [d] of the layer dtype")
+    _wants(_is(rstd, torch.float32, T), "rstd is fp32 [T]")
+    _wants((x is None) != (x8 is None), "one of x and x8 is wanted")
+    _wants(x is None or _is(x, torch.float32, T, d), "x is fp32 [T, d]")
+    if x8 is not None:
+        _wants_mx8(x8, T, d, "x8 is uint8 of mcft_mx8_size(T, d) bytes")
+    _wants(dres is None or _is(dres, torch.float32, T, d), "dres is fp32 [T, d]")
+    if dx is None:
+        dx = _empty((T, d), torch.float32, du.device, stream)
+    else:
+        _wants(_is(dx, torch.float32, T, d), "dx is fp32 [T, d]")
+    if dgamma is None:
+        _wants(not accumulate, "accumulate adds to a dgamma that is given")
+        dgamma = _empty((d,), torch.float32, du.device, stream)
+    else:
+        _wants(_is(dgamma, torch.float32, d), "dgamma is fp32 [d]")
+    if workspace is None:
+        workspace = _empty(mcft_rmsnorm_grad_workspace_size(desc, T), torch.uint8, du.device, stream)
+    _check(lib().mcft_rmsnorm_grad(C.byref(desc), _ptr(x), _ptr(x8), _ptr(rstd), _ptr(gamma), _ptr(du), T, _ptr(dres),
+                                   _ptr(dx), _ptr(dgamma), 1 if accumulate else 0, _ptr(workspace), _nbytes(workspace),
+                                   _stream(stream)))
+    return dx, dgamma
+
+
+def _wants_block(desc, block):
+    _wants(block.dtype == torch_dtype(desc) and block.numel() == 3 * desc.w * desc.d, "block is [W1 | W3 | W2] of the layer dtype")
+
+
+def mcft_ffn_workspace_size(desc: LayerDesc, T_max: int) -> int:
+    return _size_of(lib().mcft_ffn_workspace_size, C.byref(desc), int(T_max))
+
+
+def mcft_ffn_forward(desc: LayerDesc, x, block, y=None, ckpt=None, workspace=None, stream=None):
+    """y [T, d] = W2 (silu(W1 x) * (W3 x)) of the packed block; writes the checkpoint of both projections (the mx8 matrix
+    [T, 2w]) to ckpt where given."""
+    T, dtype = x.shape[0], torch_dtype(desc)
+    _wants(_is(x, dtype, T, desc.d), "x is [T, d] of the layer dtype")
+    _wants_block(desc, block)
+    if y is None:
+        y = _empty(x.shape, dtype, x.device, stream)
+    else:
+        _wants(_is(y, dtype, T, desc.d), "y is [T, d] of the layer dtype")
+    if ckpt is not None:
+        _wants_mx8(ckpt, T, 2 * desc.w, "ckpt is uint8 of mcft_mx8_size(T, 2 w) bytes")
+    if workspace is None:
+        workspace = _empty(mcft_ffn_workspace_size(desc, T), torch.uint8, x.device, stream)
+    _check(lib().mcft_ffn_forward(C.byref(desc), _ptr(x), T, _ptr(block), _ptr(y), _ptr(ckpt), _ptr(workspace),
+                                  _nbytes(workspace), _stream(stream)))
+    return y
+
+
+def mcft_ffn_grad_workspace_size(desc: LayerDesc, T_max: int) -> int:
+    return _size_of(lib().mcft_ffn_grad_workspace_size, C.byref(desc), int(T_max))
+
+
+def mcft_ffn_grad(desc: LayerDesc, dy, block, x=None, x8=None, ckpt=None, dx=None, dblock=None, grad_dtype=None,
+                  accumulate=False, workspace=None, stream=None):
+    """(dx [T, d] of the layer dtype, dblock packed like the block) from dL/dy, the input as x or as its mx8 matrix x8, and
+    the forward's ckpt (None: both projections are computed again). dblock is of grad_dtype (a given dblock's, else the
+    layer's) and added to if accumulate."""
+    T, dtype = dy.shape[0], torch_dtype(desc)
+    _wants(_is(dy, dtype, T, desc.d), "dy is [T, d] of the layer dtype")
+    _wants_block(desc, block)
+    _wants((x is None) != (x8 is None), "one of x and x8 is wanted")
+    _wants(x is None or _is(x, dtype, T, desc.d), "x is [T, d] of the layer dtype")
+    if x8 is not None:
+        _wants_mx8(x8, T, desc.d, "x8 is uint8 of mcft_mx8_size(T, d) bytes")
+    if ckpt is not None:
+        _wants_mx8(ckpt, T, 2 * desc.w, "ckpt is uint8 of mcft_mx8_size(T, 2 w) bytes")
+    if dx is None:
+        dx = _empty(dy.shape, dtype, dy.device, stream)
+    else:
+        _wants(_is(dx, dtype, T, desc.d), "dx is [T, d] of the layer dtype")
+    if dblock is None:
+        _wants(not accumulate, "accumulate adds to a dblock that is given")
+        dblock = _empty((3 * desc.w * desc.d,), grad_dtype or dtype, dy.device, stream)
+    _wants(dblock.numel() == 3 * desc.w * desc.d and dblock.dtype in (torch.float32, dtype)
+           and grad_dtype in (None, dblock.dtype), "dblock is [dW1 | dW3 | dW2], fp32 or of the layer dtype")
+    if workspace is None:
+        workspace = _empty(mcft_ffn_grad_workspace_size(desc, T), torch.uint8, dy.device, stream)
+    _check(lib().mcft_ffn_grad(C.byref(desc), _ptr(dy), T, _ptr(block), _ptr(x), _ptr(x8), _ptr(ckpt), _ptr(dx), _ptr(dblock),
+                               _MX4_DTYPE[dblock.dtype], 1 if accumulate else 0, _ptr(workspace), _nbytes(workspace),
+                               _stream(stream)))
+    return dx, dblock
