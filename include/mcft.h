@@ -575,8 +575,8 @@ mcft_status mcft_route_scored_grad(const mcft_scored_desc* desc, const void* x, 
  * Section 1, is short of device memory: a checkpoint in this format takes 33/64 of bf16's bytes).
  *
  * A block of 32 values along a row is 32 e4m3 codes and one scale, the smallest power of two 2^s with max|x| <= 448 * 2^s,
- * s in [-127, 127], held as s + 127 in a byte. Codes round to nearest even; none saturates. A block with a NaN or an infinity
- * has the scale byte 0xff and reads back as NaN. An mx8 matrix [rows, cols] is row-major codes [rows, Cp], Cp = cols
+ * s in [-127, 127], held as s + 127 in a byte. Codes round to nearest even, none saturates (but values that would round to
+ * 2^128 are held as 1.875 * 2^127). A block with a NaN or an infinity has the scale byte 0xff and reads back as NaN. An mx8 matrix [rows, cols] is row-major codes [rows, Cp], Cp = cols
  * rounded up to 32 (codes past cols are 0), then row-major scales [rows, Cp / 32]: mcft_mx8_size bytes, 16-byte aligned.
  *
  * mcft_mx8_quantize: x device [rows, cols] of dtype (MCFT_F32 or MCFT_BF16), `ld` elements from row to row, any

@@ -2,7 +2,8 @@
 
 mx8, from the definition: blocks of 32 along a row under 2^s, s the smallest in [-127, 127] with max|x| <= 448 * 2^s; values
 rounded to the nearest e4m3 number (sign, four exponent bits of bias 7, three mantissa bits, subnormals of 2^-9, 448 the largest),
-ties to the even code; a block with a NaN or an infinity is NaN."""
+ties to the even code, or to 1.875 * 2^127 where that would be 2^128 (fp32 and bf16 end below); a block with a NaN or an infinity
+is NaN."""
 from __future__ import annotations
 
 import numpy as np
@@ -36,7 +37,7 @@ def mx8(x):
     v = np.where(ok, v, 0.0)
     s = scale_exponent(np.abs(v).max(2, keepdims=True))
     unit = np.ldexp(1.0, s)
-    code = round_to_grid(np.abs(v) / unit)
+    code = np.where(s == 120, np.minimum(round_to_grid(np.abs(v) / unit), 0x77), round_to_grid(np.abs(v) / unit))
     values = np.where(ok, np.copysign(GRID[code] * unit, v), np.nan).reshape(R, -1)[:, :C]
     codes = np.where(np.signbit(v), code + 128, code).reshape(R, -1)
     return values, codes.astype(np.uint8), np.where(ok, s + 127, 255)[..., 0].astype(np.uint8)

@@ -212,14 +212,15 @@ __global__ void __launch_bounds__(256) dense_act_kernel(const __grid_constant__ 
       uint8_t* q = const_cast<uint8_t*>(a.ckpt);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const float* v = half ? u : g;
+        float v[8];
         uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) m = max(m, mag(v[k]));
+        for (int k = 0; k < 8; ++k) m = max(m, mag(v[k] = half ? u[k] : g[k]));
         m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
         m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
         const uint32_t s = mx8_scale(m);
         const float k = mx8_inverse(s);
+        mx8_below_top<8>(v, s);
         const size_t to = at + half * w;
         if (in) {
           *reinterpret_cast<uint2*>(q + to) = make_uint2(mx8_quad(v[0] * k, v[1] * k, v[2] * k, v[3] * k),

@@ -129,11 +129,13 @@ __device__ __forceinline__ void put_mx8(uint8_t* code, uint8_t* scale, const uin
   for (int i = 0; i < 32; ++i) m = max(m, bits[i] & 0x7fffffffu);
   const uint32_t s = mx8_scale(m);
   const float k = mx8_inverse(s);
+  float v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(bits[i]);
+  mx8_below_top<32>(v, s);
   uint32_t c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    c[i] = mx8_quad(__uint_as_float(bits[4 * i]) * k, __uint_as_float(bits[4 * i + 1]) * k,
-                    __uint_as_float(bits[4 * i + 2]) * k, __uint_as_float(bits[4 * i + 3]) * k);
+  for (int i = 0; i < 8; ++i) c[i] = mx8_quad(v[4 * i] * k, v[4 * i + 1] * k, v[4 * i + 2] * k, v[4 * i + 3] * k);
   if (wide) store32(code, c);
   else store32_by16(code, c);
   *scale = uint8_t(s);

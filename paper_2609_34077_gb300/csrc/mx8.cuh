@@ -1,8 +1,9 @@
 // Microscaled 8-bit floating point (mx8): the format's arithmetic and its layout in memory. Not part of the C ABI.
 //
 // A block is 32 values along a row: e4m3 codes under one power-of-two scale, held as its exponent + 127. The scale is
-// the smallest 2^s, s in [-127, 127], with max|x| <= 448 * 2^s, so that no code saturates; codes round to nearest even. A
-// block with a NaN or an infinity gets the scale byte 0xff: all its values read back as NaN.
+// the smallest 2^s, s in [-127, 127], with max|x| <= 448 * 2^s, so that no code saturates; codes round to nearest even, but
+// to 1.875 * 2^127 where that would be 2^128, which no fp32 is. A block with a NaN or an infinity gets the scale byte 0xff:
+// all its values read back as NaN.
 //
 // A matrix [R, C] is row-major codes [R, Cp] with Cp = C rounded up to 32 (zeros past C), then row-major scales
 // [R, Cp / 32]. A value has four significant bits, so bf16 holds it exactly (but for bf16's subnormals).
@@ -31,6 +32,14 @@ __device__ __forceinline__ float mx8_inverse(uint32_t scale) {
 }
 __device__ __forceinline__ float mx8_unit(uint32_t scale) {
   return scale == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(scale ? scale << 23 : 0x00400000u);
+}
+// Values of a block under the largest scale that there is, kept from rounding to 2^128.
+template <int N>
+__device__ __forceinline__ void mx8_below_top(float* v, uint32_t scale) {
+  if (scale != 247u) return;  // (fp32 values end below 256 * 2^120)
+  const float top = __uint_as_float(0x7f700000u);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = fminf(fmaxf(v[i], -top), top);
 }
 // Two codes, `lo` in the low byte: round to nearest even.
 __device__ __forceinline__ uint32_t mx8_pair(float lo, float hi) {

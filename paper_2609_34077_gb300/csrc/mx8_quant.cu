@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(kThreads) mx8_quantize_kernel(const __grid_con
   for (int i = 0; i < 32; ++i) m = max(m, mag(v[i]));
   const uint32_t s = mx8_scale(m);
   const float inv = mx8_inverse(s);
+  mx8_below_top<32>(v, s);
   uint32_t code[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) code[i] = mx8_quad(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
@@ -135,6 +136,7 @@ __global__ void __launch_bounds__(kThreads) mx8_quantize_any_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t s = mx8_scale(__reduce_max_sync(0xffffffffu, mag(v[i])));
+      mx8_below_top<1>(v + i, s);
       const uint32_t q = mx8_pair(v[i] * mx8_inverse(s), 0.f);
       if (g + i < n) out[(g + i) * 32 + lane] = uint8_t(q);
       if (lane == g + i) scale = s;

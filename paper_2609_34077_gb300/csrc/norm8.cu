@@ -6,6 +6,8 @@
 // A row belongs to a team of 8 to 1024 threads (a power of two) that hold it in registers, 8 neighbouring values
 // a thread and step, so every value is read once; four neighbouring lanes hold a block of mx8. Sums go through a
 // shuffle tree and then over warps in order: the same bits every time. Both are bound by HBM.
+// The forward keeps what the sum of squares, r and the products drop, and rounds u once: a code of u8 is then the code of
+// the exact u, where an error of 2^-23 moved one in a million of them across the middle between two codes.
 // The gradient's CTAs stride over rows and keep their share of dgamma in registers; the shares are added in order by
 // a second kernel.
 #include "dense.h"
@@ -39,18 +41,63 @@ __device__ __forceinline__ void store8(void* p, size_t i, const float* v) {
 }
 
 // The eight values of a lane as a quarter of an mx8 block; `at`: of the first value in the codes. All lanes of a warp call it.
-__device__ __forceinline__ void store_mx8(uint8_t* q, size_t scales, size_t at, const float* v, bool ok) {
+__device__ __forceinline__ void store_mx8(uint8_t* q, size_t scales, size_t at, const float* from, bool ok) {
+  float v[8];
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, mag(v[i]));
+  for (int i = 0; i < 8; ++i) m = max(m, mag(v[i] = from[i]));
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
   const uint32_t s = mx8_scale(m);
   const float k = mx8_inverse(s);
   if (!ok) return;
+  mx8_below_top<8>(v, s);
   *reinterpret_cast<uint2*>(q + at) = make_uint2(mx8_quad(v[0] * k, v[1] * k, v[2] * k, v[3] * k),
                                                  mx8_quad(v[4] * k, v[5] * k, v[6] * k, v[7] * k));
   if ((threadIdx.x & 3) == 0) q[scales + at / 32] = uint8_t(s);
+}
+
+// An fp32 sum with what its additions dropped (compensated summation; Knuth's exact sum of two).
+struct Sum2 {
+  float hi, lo;
+  __device__ __forceinline__ void add(float h, float l) {
+    const float t = hi + h, z = t - hi;
+    lo += (hi - (t - z)) + (h - z) + l;
+    hi = t;
+  }
+  __device__ __forceinline__ void square(float v) {
+    const float p = v * v;
+    add(p, fmaf(v, v, -p));
+  }
+};
+
+__device__ __forceinline__ Sum2 team_sum(Sum2 s, int lg, float2* part) {
+  const int n = lg < 5 ? 1 << lg : 32;
+  for (int o = n >> 1; o > 0; o >>= 1) {
+    const float h = __shfl_xor_sync(0xffffffffu, s.hi, o), l = __shfl_xor_sync(0xffffffffu, s.lo, o);
+    s.add(h, l);
+  }
+  if (lg <= 5) return s;
+  const int warp = threadIdx.x >> 5, per = 1 << (lg - 5), w0 = warp & ~(per - 1);
+  if ((threadIdx.x & 31) == 0) part[warp] = make_float2(s.hi, s.lo);
+  __syncthreads();
+  s = Sum2{part[w0].x, part[w0].y};
+  for (int w = 1; w < per; ++w) s.add(part[w0 + w].x, part[w0 + w].y);
+  return s;
+}
+
+// 1 / sqrt(sum / d + eps) as an fp32 number and what is left of it: the rounded root corrected once by its residual.
+// (A sum that overflowed has nothing left to correct.)
+__device__ __forceinline__ float2 rstd_of(Sum2 s, int d, float eps) {
+  const float n = float(d), lo = fabsf(s.hi) < INFINITY ? s.lo : 0.f;
+  const float q = s.hi / n, ql = fabsf(q) < INFINITY ? (fmaf(-q, n, s.hi) + lo) / n : 0.f;
+  Sum2 m{q, ql};
+  m.add(eps, 0.f);
+  const float r = 1.0f / sqrtf(m.hi);
+  if (!(fabsf(m.hi) < INFINITY) || !(r < INFINITY)) return make_float2(r, 0.f);
+  const float t = r * r, te = fmaf(r, r, -t);
+  const float off = fmaf(m.hi, t, -1.0f) + fmaf(m.hi, te, m.lo * t);
+  return make_float2(r, -0.5f * r * off);
 }
 
 // Sum over a team of 2^lg threads. part: 32 floats that no other sum of the CTA is using.
@@ -69,7 +116,7 @@ __device__ __forceinline__ float team_sum(float s, int lg, float* part) {
 template <typename T, int NG, int THREADS>
 __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ Norm8Args a, int lg) {
   pdl_wait();
-  __shared__ float part[32];
+  __shared__ float2 part[32];
   const int lane = threadIdx.x & ((1 << lg) - 1), groups = a.d / 8;
   const long long row = (long long)blockIdx.x * (blockDim.x >> lg) + (threadIdx.x >> lg);
   const bool in = row < a.T;
@@ -97,7 +144,7 @@ __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ 
       }
     }
   }
-  float ss = 0.f;
+  Sum2 ss{0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int c = lane + (j << lg);
@@ -105,10 +152,10 @@ __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ 
     if (ok && a.out) store8<float>(a.out, base + c * 8, v[j]);
     if (a.x8) store_mx8(a.x8, scales, base + c * 8, v[j], ok);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(v[j][i], v[j][i], ss);
+    for (int i = 0; i < 8; ++i) ss.square(v[j][i]);
   }
-  const float r = 1.0f / sqrtf(team_sum(ss, lg, part) / float(a.d) + a.eps);
-  if (in && lane == 0 && a.rstd) a.rstd[row] = r;
+  const float2 r = rstd_of(team_sum(ss, lg, part), a.d, a.eps);
+  if (in && lane == 0 && a.rstd) a.rstd[row] = r.x + r.y;
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int c = lane + (j << lg);
@@ -116,7 +163,11 @@ __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ 
     float g[8] = {};
     if (ok) load8<T>(a.gamma, size_t(c) * 8, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = v[j][i] * r * g[i];
+    for (int i = 0; i < 8; ++i) {  // gamma v r with what the two products and r drop: rounded once
+      const float t = v[j][i] * r.x, u = t * g[i];
+      const float rest = fmaf(v[j][i], r.y, fmaf(v[j][i], r.x, -t));
+      g[i] = u + (fabsf(u) < INFINITY ? fmaf(rest, g[i], fmaf(t, g[i], -u)) : 0.f);
+    }
     if (ok && a.u) store8<T>(a.u, base + c * 8, g);
     if (a.u8) store_mx8(a.u8, scales, base + c * 8, g, ok);
   }
