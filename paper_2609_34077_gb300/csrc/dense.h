@@ -55,14 +55,9 @@ struct DenseProduct {
   int out_dtype, accumulate;
 };
 constexpr int kMaxProducts = 3;
-constexpr int kDenseTile = 256;  // rows and columns of a bf16 tile
+constexpr int kDenseTile = 256;       // rows and columns of a bf16 tile
+constexpr int kDensePlaneTiles = 2;  // tiles' worth of split sums that a pair of SMs may leave in memory
 
-// Fp32 partial sums of products whose contraction is split.
-struct DensePlan {
-  int splits[kMaxProducts], per[kMaxProducts];  // parts of a contraction, steps of each
-  size_t plane[kMaxProducts];                   // where its planes begin, in floats
-  size_t floats;
-};
 // Most bytes that the planes of a launch of `n` products take, whose outputs number `outs` in all and whose contractions
 // are at most `k` long: grows with each, so that it covers smaller calls too.
 size_t dense_plane_bytes(int n, size_t outs, int k, int dtype);

@@ -13,7 +13,6 @@
 
 namespace mcft {
 
-DensePlan dense_tc_plan(const DenseProduct* p, int n);
 cudaError_t launch_dense_tc(const DenseProduct* p, int n, float* planes, cudaStream_t s);
 
 namespace {
@@ -247,8 +246,12 @@ cudaError_t launch_act(const DenseActArgs& a, cudaStream_t s) {
 }
 
 // Parts of a contraction such that the tiles make up to about three CTAs an SM, of at least 128 elements.
-DensePlan f32_plan(const DenseProduct* p, int n) {
-  DensePlan plan = {};
+struct F32Plan {
+  int splits[kMaxProducts], per[kMaxProducts];  // parts of a contraction, elements of each
+  size_t plane[kMaxProducts], floats;
+};
+F32Plan f32_plan(const DenseProduct* p, int n) {
+  F32Plan plan = {};
   for (int i = 0; i < n; ++i) {
     const long long tiles = (long long)((p[i].rows + TM - 1) / TM) * ((p[i].cols + TN - 1) / TN);
     const int want = int(std::max(1ll, 3ll * num_sms() / tiles)), most = std::max(1, p[i].k / 128);
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(256) dense_few_kernel(const __grid_constant__ 
 size_t dense_plane_bytes(int n, size_t outs, int k, int dtype) {
   // items that run at once, and the most parts of a contraction
   const size_t sms = size_t(num_sms());
-  const size_t items = dtype == MCFT_BF16 ? sms / 2 * kDenseTile * kDenseTile : size_t(n) * (3 * sms) * TM * TN;
+  const size_t items = dtype == MCFT_BF16 ? sms / 2 * kDensePlaneTiles * kDenseTile * kDenseTile : size_t(n) * (3 * sms) * TM * TN;
   const size_t parts = dtype == MCFT_BF16 ? size_t(k) / (4 * 64) + 2 : size_t(k) / 128 + 2;
   return std::min(items, parts * outs) * sizeof(float);
 }
@@ -296,7 +299,7 @@ cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* ou
 
 cudaError_t launch_dense_products(const DenseProduct* p, int n, int dtype, float* planes, cudaStream_t s) {
   if (dtype == MCFT_BF16) return launch_dense_tc(p, n, planes, s);
-  const DensePlan plan = f32_plan(p, n);
+  const F32Plan plan = f32_plan(p, n);
   for (int i = 0; i < n; ++i) {
     const bool split = plan.splits[i] > 1;
     const F32Params q{static_cast<const float*>(p[i].a), static_cast<const float*>(p[i].b),

@@ -4,9 +4,9 @@
 //   up_grad  dh = dy W2;                            dg, du, h from dh and the checkpoints
 //   out      C = A B of up to three problems: y = h W2^T, or dx = [dg | du] [W1 ; W3], d[W1 ; W3] = [dg | du]^T x and
 //            dW2 = dy^T h in one launch, whose tiles fill the SMs together.
-// A tile is 256 rows x 256 columns (up: 128 of g and the same 128 of u), one MMA of M = 256 a step, issued by the pair's
-// leader over both CTAs' shared memory: each CTA brings in its 128 rows of A and 128 of B's columns, 64 of the contraction
-// a stage, 7 stages of 32 KB. Operands are taken as they lie in memory: one whose contiguous index is the contraction's is a
+// A tile is 256 rows x 256 or 128 columns (up: half of them of g, the same ones of u), one MMA of M = 256 a step, issued by the
+// pair's leader over both CTAs' shared memory: each CTA brings in its 128 rows of A and its half of B's columns, 64 of the
+// contraction a stage, 7 stages of 32 KB or 9 of 24. Operands are taken as they lie in memory: one whose contiguous index is the contraction's is a
 // K-major operand (a box of 64 x 128), another an MN-major one (two boxes of 64 x 64), so nothing is transposed.
 //   warp 0 (both CTAs) copies; the loads of both complete on the leader's full[s];
 //   warp 1 of the leader issues the MMAs; their commits arrive on empty[s] and tfull[b] of both CTAs;
@@ -31,17 +31,15 @@ namespace mcft {
 namespace {
 
 constexpr int BK = 64;
-constexpr int kTile = kDenseTile;  // rows, and columns of accumulators
+constexpr int kTile = kDenseTile;  // rows, and most columns
 constexpr int kThreads = 64 + 256;
 constexpr int kEpiWarps = 8;
-constexpr int kStages = 7;
-constexpr int kHalfBytes = 128 * BK * 2;  // a CTA's part of an operand in a stage
-constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kABytes = 128 * BK * 2;  // a CTA's rows of A in a stage
+constexpr int kRingBytes = 7 * (kABytes + 128 * BK * 2);
+constexpr int kMaxStages = 9;
 constexpr int kTmemCols = 2 * kTile;
-constexpr int kUpCols = kTile / 2;  // columns of h of an up tile
-// instruction descriptor without the operands' order: D fp32, A and B bf16, N = 256, M = 256
-constexpr uint32_t kIdesc =
-    (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
+// instruction descriptor without N and the operands' order: D fp32, A and B bf16, M = 256
+constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 4) << 24);
 constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
 
 enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_OUT = 2 };
@@ -57,6 +55,7 @@ struct Problem {
 struct Params {
   Problem p[kMaxProducts];
   int n, items;
+  int cols;  // of a tile: 256 or 128
   unsigned* err;
   // up, up_grad
   uint8_t* ckpt;
@@ -67,11 +66,11 @@ struct Params {
 static_assert(sizeof(Params) <= 4096, "kernel parameters");
 
 struct Ctl {
-  uint64_t full[kStages], empty[kStages], tfull[2], tempty[2], drain;
+  uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2], drain;
   uint32_t tmem_base;
   int abort;
 };
-constexpr int kSmem = kStages * kStageBytes + 1024 + int(sizeof(Ctl));
+constexpr int kSmem = kRingBytes + 1024 + int(sizeof(Ctl));
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
 struct Item {
@@ -102,10 +101,11 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn) {
          (uint64_t(2) << 61);
 }
 
-__device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap* map, bool mn, int k, int at, uint32_t bar) {
+__device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap* map, bool mn, int rows, int k, int at,
+                                             uint32_t bar) {
   if (mn) {
     tma_load_2d_pair(to, map, at, k, bar);
-    tma_load_2d_pair(to + kHalfBytes / 2, map, at + 64, k, bar);
+    if (rows > 64) tma_load_2d_pair(to + 64 * BK * 2, map, at + 64, k, bar);
   } else {
     tma_load_2d_pair(to, map, k, at, bar);
   }
@@ -114,6 +114,12 @@ __device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap* map
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   tmem_ld16(taddr, r);
   tmem_ld16(taddr + 16, r + 16);
+}
+
+// Of tensor memory that this warp has read, once tcgen05.fence::before_thread_sync has ordered those reads before it: a
+// relaxed arrival (a release would first wait for the stores of the rows).
+__device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // 64 bytes of each lane's row (NULL: none).
@@ -159,12 +165,12 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
   if constexpr (EPI == EPI_UP) {
     const size_t w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
 #pragma unroll 1
-    for (int c = half * 64; c < half * 64 + 64; c += 32) {
-      const int col = t.nt * kUpCols + c;
+    for (int c = half * (q.cols / 4); c < (half + 1) * (q.cols / 4); c += 32) {
+      const int col = t.nt * (q.cols / 2) + c;
       if (col >= q.w) break;
       uint32_t g[32], u[32];
       tmem_ld32(taddr + c, g);
-      tmem_ld32(taddr + kUpCols + c, u);
+      tmem_ld32(taddr + q.cols / 2 + c, u);
       tmem_ld_wait();
       if (q.gu) {
         float* to = in ? q.gu + r * 2 * w + col : nullptr;
@@ -191,8 +197,8 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
   } else if constexpr (EPI == EPI_UP_GRAD) {
     const size_t w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
 #pragma unroll 1
-    for (int c = half * 128; c < half * 128 + 128; c += 32) {
-      const int col = t.nt * kTile + c;
+    for (int c = half * (q.cols / 2); c < (half + 1) * (q.cols / 2); c += 32) {
+      const int col = t.nt * q.cols + c;
       if (col >= q.w) break;
       float g[32], u[32];
       if (q.ckpt) {
@@ -230,8 +236,8 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
   } else {
     const size_t N = size_t(p.N);
 #pragma unroll 1
-    for (int c = half * 128; c < half * 128 + 128; c += 32) {
-      const int col = t.nt * kTile + c;
+    for (int c = half * (q.cols / 2); c < (half + 1) * (q.cols / 2); c += 32) {
+      const int col = t.nt * q.cols + c;
       if (col >= p.N) break;
       uint32_t v[32];
       tmem_ld32(taddr + c, v);
@@ -277,17 +283,16 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
 template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     dense_gemm_kernel(const __grid_constant__ Params q) {
-  pdl_wait();
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;  // the same offsets in both CTAs
-  Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + kStages * kStageBytes);
+  Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + kRingBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
   if (threadIdx.x == 0) {
     ctl->abort = 0;
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(&ctl->full[s], 1);
       mbar_init(&ctl->empty[s], 1);
     }
@@ -308,8 +313,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   tc_fence_before();
   cluster_sync();  // barriers initialised and TMEM allocated in both CTAs
   tc_fence_after();
+  pdl_wait();  // (nothing above reads memory)
 
   const uint32_t tmem = ctl->tmem_base;
+  const int half_cols = q.cols / 2, stage_bytes = kABytes + half_cols * BK * 2, stages = min(kMaxStages, kRingBytes / stage_bytes);
   const int items = q.items, cid = int(blockIdx.x >> 1), ncl = int(gridDim.x >> 1);
   volatile int* abort = &ctl->abort;
 
@@ -322,16 +329,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const Item t = item_at(q, item);
         const int arow = t.mt * kTile + int(rank) * 128;
         const CUtensorMap* mb = EPI == EPI_UP && rank ? &t.p->b1 : &t.p->b;
-        const int brow = EPI == EPI_UP ? t.nt * kUpCols : t.nt * kTile + int(rank) * 128;
+        const int brow = EPI == EPI_UP ? t.nt * half_cols : t.nt * q.cols + int(rank) * half_cols;
         const bool a_mn = EPI == EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_OUT && t.p->b_mn);
         for (int kb = t.k0; kb < t.k1; ++kb) {
           if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, q.err)) break;
-          const uint32_t sa = base + uint32_t(s) * kStageBytes, fb = fb0 + uint32_t(s) * 8u;
-          if (leader) mbar_expect_tx(&ctl->full[s], 2 * kStageBytes);
-          load_operand(sa, &t.p->a, a_mn, kb * BK, arow, fb);
-          load_operand(sa + kHalfBytes, mb, b_mn, kb * BK, brow, fb);
-          if (issued < kStages) ++issued;
-          if (++s == kStages) {
+          const uint32_t sa = base + uint32_t(s * stage_bytes), fb = fb0 + uint32_t(s) * 8u;
+          if (leader) mbar_expect_tx(&ctl->full[s], 2u * uint32_t(stage_bytes));
+          load_operand(sa, &t.p->a, a_mn, 128, kb * BK, arow, fb);
+          load_operand(sa + kABytes, mb, b_mn, half_cols, kb * BK, brow, fb);
+          if (issued < stages) ++issued;
+          if (++s == stages) {
             s = 0;
             ph ^= 1u;
           }
@@ -342,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int i = 0; i < issued; ++i) {
         const int j = s - (issued - i);
         uint64_t* ring = leader ? ctl->full : ctl->empty;
-        if (!mbar_wait_drain_cl(&ring[j < 0 ? j + kStages : j], j < 0 ? ph ^ 1u : ph, q.err)) break;
+        if (!mbar_wait_drain_cl(&ring[j < 0 ? j + stages : j], j < 0 ? ph ^ 1u : ph, q.err)) break;
       }
     }
   } else if (warp == 1) {
@@ -352,7 +359,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int item = cid; item < items && !*abort; item += ncl) {
         const Item t = item_at(q, item);
         const bool a_mn = EPI == EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_OUT && t.p->b_mn);
-        const uint32_t idesc = kIdesc | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
+        const uint32_t idesc = kIdesc | (uint32_t(q.cols >> 3) << 17) | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
         // 16 of the contraction: 32 bytes of each K-major row, or 16 rows of 128 bytes
         const uint64_t ka = a_mn ? (16 * 128) >> 4 : 32 >> 4, kb_ = b_mn ? (16 * 128) >> 4 : 32 >> 4;
         const uint32_t b = lt & 1u;
@@ -366,13 +373,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             break;
           }
           tc_fence_after();
-          const uint32_t sa = base + uint32_t(s) * kStageBytes;
-          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + kHalfBytes, b_mn);
+          const uint32_t sa = base + uint32_t(s * stage_bytes);
+          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + kABytes, b_mn);
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k)
             tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (kb != t.k0 || k != 0) ? 1u : 0u);
           tc_commit_pair_both(&ctl->empty[s]);
-          if (++s == kStages) {
+          if (++s == stages) {
             s = 0;
             ph ^= 1u;
           }
@@ -399,7 +406,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     t.mt * kTile + int(rank) * 128 + quarter * 32 + lane, half);
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(peer_addr(&ctl->tempty[b], 0));
+      if (lane == 0) arrive_relaxed(peer_addr(&ctl->tempty[b], 0));
       ++lt;
     }
   }
@@ -440,6 +447,62 @@ void shape(Problem& p, int M, int N, int K, int tile_cols) {
   p.group = int(std::clamp<size_t>(kGroupBytes / (size_t(kTile) * K * 2), 1, 4096));
 }
 
+// What a launch's items take, in steps of 64 of the contraction by 256 columns (0.29 us): the longest pair's share of them,
+// where pair i has items i, i + pairs, ...; an item takes at least what its epilogue does.
+struct Plan {
+  int cols, per[kMaxProducts];
+  double time;
+};
+struct Sizes {
+  int M, N, kblocks;
+};
+constexpr int kLeastPart = 4;  // steps: below that an item is mostly its fill and its stores
+constexpr double kJoin = 10;   // a launch more, beside the planes' bytes
+
+double plan_time(const Sizes* z, int n, int up, int cols, const int* per, int pairs) {
+  const double step = cols == kTile ? 1.0 : 0.56, epilogue = (cols == kTile ? 4.0 : 2.0) * (up ? 1.5 : 1.0), fill = 5.0;
+  double total = 0, longest = 0, planes = 0;
+  long long items = 0;
+  for (int i = 0; i < n; ++i) {
+    const long long tiles = (long long)((z[i].M + kTile - 1) / kTile) * ((z[i].N * (up ? 2 : 1) + cols - 1) / cols);
+    const int splits = (z[i].kblocks + per[i] - 1) / per[i];
+    const double one = std::max(per[i] * step, epilogue);
+    total += one * tiles * splits;
+    longest = std::max(longest, one);
+    items += tiles * splits;
+    if (splits > 1) planes += double(splits) * z[i].M * z[i].N;
+  }
+  // whole rounds where there are few, their mean where there are many
+  const double rounds = double((items + pairs - 1) / pairs), mean = total / items;
+  const double busy = rounds <= 3 ? std::max(longest, mean * rounds) : std::max(total / pairs + longest / 2, longest);
+  return fill + busy + epilogue + (planes > 0 ? kJoin + planes * 8 / 1.7e6 : 0);
+}
+
+// Tile width, and (splittable) parts of the contractions, by the least time.
+Plan choose(const Sizes* z, int n, int up, bool splittable, int pairs) {
+  Plan best{};
+  int longest = 1;
+  for (int i = 0; i < n; ++i) longest = std::max(longest, z[i].kblocks);
+  for (int cols = kTile; cols >= 128; cols /= 2) {
+    for (int parts = 1; parts <= (splittable ? 32 : 1); ++parts) {
+      const int unit = (longest + parts - 1) / parts;
+      if (parts > 1 && unit < kLeastPart) break;
+      Plan p{cols, {}, 0};
+      size_t planes = 0;
+      for (int i = 0; i < n; ++i) {
+        const int splits = (z[i].kblocks + unit - 1) / unit;
+        p.per[i] = (z[i].kblocks + splits - 1) / splits;
+        const int made = (z[i].kblocks + p.per[i] - 1) / p.per[i];
+        if (made > 1) planes += size_t(made) * z[i].M * z[i].N;
+      }
+      if (planes > size_t(pairs) * kDensePlaneTiles * kTile * kTile) break;
+      p.time = plan_time(z, n, up, cols, p.per, pairs);
+      if (best.cols == 0 || p.time < best.time) best = p;
+    }
+  }
+  return best;
+}
+
 template <int EPI>
 int pairs_at_once() {
   static SmemOptIn smem;
@@ -472,10 +535,12 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
   memset(&q, 0, sizeof(q));
   q.n = 1;
   Problem& p = q.p[0];
-  shape(p, a.T, a.w, a.d, kUpCols);
+  const Sizes z{a.T, a.w, (a.d + BK - 1) / BK};
+  q.cols = choose(&z, 1, 1, false, num_sms() / 2).cols;
+  shape(p, a.T, a.w, a.d, q.cols / 2);
   const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
-  if (!encode(&p.a, a.x, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, w1, size_t(a.d), size_t(a.w), 128) ||
-      !encode(&p.b1, w1 + size_t(a.w) * a.d, size_t(a.d), size_t(a.w), 128))
+  if (!encode(&p.a, a.x, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, w1, size_t(a.d), size_t(a.w), q.cols / 2) ||
+      !encode(&p.b1, w1 + size_t(a.w) * a.d, size_t(a.d), size_t(a.w), q.cols / 2))
     return cudaErrorInvalidValue;
   q.w = a.w;
   q.h = static_cast<uint16_t*>(a.h);
@@ -491,7 +556,9 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   memset(&q, 0, sizeof(q));
   q.n = 1;
   Problem& p = q.p[0];
-  shape(p, a.T, a.w, a.d, kTile);
+  const Sizes z{a.T, a.w, (a.d + BK - 1) / BK};
+  q.cols = choose(&z, 1, 0, false, num_sms() / 2).cols;
+  shape(p, a.T, a.w, a.d, q.cols);
   p.b_mn = 1;
   if (!encode(&p.a, a.dy, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, a.w2, size_t(a.w), size_t(a.d), 64))
     return cudaErrorInvalidValue;
@@ -505,65 +572,39 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
 }
 
-// Splits where the tiles leave pairs idle: parts of at least 4 steps (below that an item is mostly its fill and its
-// stores), as short as they can be with all items running at once.
-DensePlan dense_tc_plan(const DenseProduct* in, int n) {
-  DensePlan plan = {};
-  Problem p[kMaxProducts];
-  int tiles = 0, longest = 1;
-  for (int i = 0; i < n; ++i) {
-    shape(p[i], in[i].rows, in[i].cols, in[i].k, kTile);
-    tiles += p[i].mt * p[i].nt;
-    longest = std::max(longest, p[i].kblocks);
-    plan.splits[i] = 1;
-    plan.per[i] = p[i].kblocks;
-  }
-  const int pairs = num_sms() / 2;
-  if (tiles >= pairs) return plan;
-  for (int unit = 4; unit <= longest; ++unit) {
-    long long items = 0;
-    for (int i = 0; i < n; ++i) items += (long long)p[i].mt * p[i].nt * ((p[i].kblocks + unit - 1) / unit);
-    if (items > pairs && unit < longest) continue;
-    for (int i = 0; i < n; ++i) {
-      plan.splits[i] = (p[i].kblocks + unit - 1) / unit;
-      plan.per[i] = (p[i].kblocks + plan.splits[i] - 1) / plan.splits[i];
-      plan.splits[i] = (p[i].kblocks + plan.per[i] - 1) / plan.per[i];
-      plan.plane[i] = plan.floats;
-      if (plan.splits[i] > 1) plan.floats += size_t(plan.splits[i]) * in[i].rows * in[i].cols;
-    }
-    break;
-  }
-  return plan;
-}
-
 cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaStream_t s) {
   Params q;
   memset(&q, 0, sizeof(q));
   q.n = n;
-  const DensePlan plan = dense_tc_plan(in, n);
+  Sizes z[kMaxProducts];
+  for (int i = 0; i < n; ++i) z[i] = Sizes{in[i].rows, in[i].cols, (in[i].k + BK - 1) / BK};
+  const Plan plan = choose(z, n, 0, true, num_sms() / 2);
+  q.cols = plan.cols;
+  size_t used = 0;
   for (int i = 0; i < n; ++i) {
     const DenseProduct& d = in[i];
     Problem& p = q.p[i];
-    shape(p, d.rows, d.cols, d.k, kTile);
-    p.splits = plan.splits[i];
+    shape(p, d.rows, d.cols, d.k, plan.cols);
     p.per = plan.per[i];
+    p.splits = (p.kblocks + p.per - 1) / p.per;
     p.a_mn = d.a_t;
     p.b_mn = !d.b_t;
     const size_t M = size_t(d.rows), N = size_t(d.cols), K = size_t(d.k);
     if (!(d.a_t ? encode(&p.a, d.a, M, K, 64) : encode(&p.a, d.a, K, M, 128)) ||
-        !(d.b_t ? encode(&p.b, d.b, K, N, 128) : encode(&p.b, d.b, N, K, 64)))
+        !(d.b_t ? encode(&p.b, d.b, K, N, plan.cols / 2) : encode(&p.b, d.b, N, K, 64)))
       return cudaErrorInvalidValue;
     p.out = d.out;
-    p.planes = planes + plan.plane[i];
+    p.planes = planes + used;
+    if (p.splits > 1) used += size_t(p.splits) * M * N;
     p.out_f32 = d.out_dtype == MCFT_F32;
     p.accumulate = d.accumulate;
     p.wide = p.splits > 1 ? wide(planes) : wide(d.out);
   }
   cudaError_t e = launch<EPI_OUT>(q, kProfDenseOut, s);
   for (int i = 0; i < n && e == cudaSuccess; ++i)
-    if (plan.splits[i] > 1)
-      e = launch_dense_join(planes + plan.plane[i], plan.splits[i], size_t(in[i].rows) * in[i].cols, in[i].out,
-                            in[i].out_dtype, in[i].accumulate, s);
+    if (q.p[i].splits > 1)
+      e = launch_dense_join(q.p[i].planes, q.p[i].splits, size_t(in[i].rows) * in[i].cols, in[i].out, in[i].out_dtype,
+                            in[i].accumulate, s);
   return e;
 }
 

@@ -6,10 +6,13 @@
 // A row belongs to a team of 8 to 1024 threads (a power of two) that hold it in registers, 8 neighbouring values
 // a thread and step, so every value is read once; four neighbouring lanes hold a block of mx8. Sums go through a
 // shuffle tree and then over warps in order: the same bits every time. Both are bound by HBM.
-// The forward keeps what the sum of squares, r and the products drop, and rounds u once: a code of u8 is then the code of
-// the exact u, where an error of 2^-23 moved one in a million of them across the middle between two codes.
+// The forward adds the threads' sums of squares with what the additions drop (a thread's own 8 to 32 terms are summed in fp32: the
+// errors of a row's hundreds of threads average out), keeps what r and the products drop, and rounds u once: a code of u8 is
+// then nearly always that of the exact u, where an error of 2^-23 moved one in a million across the middle between two codes.
 // The gradient's CTAs stride over rows and keep their share of dgamma in registers; the shares are added in order by
 // a second kernel.
+#include <type_traits>
+
 #include "dense.h"
 #include "mx8.cuh"
 
@@ -64,10 +67,6 @@ struct Sum2 {
     const float t = hi + h, z = t - hi;
     lo += (hi - (t - z)) + (h - z) + l;
     hi = t;
-  }
-  __device__ __forceinline__ void square(float v) {
-    const float p = v * v;
-    add(p, fmaf(v, v, -p));
   }
 };
 
@@ -144,7 +143,7 @@ __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ 
       }
     }
   }
-  Sum2 ss{0.f, 0.f};
+  float ss = 0.f;
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int c = lane + (j << lg);
@@ -152,9 +151,9 @@ __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ 
     if (ok && a.out) store8<float>(a.out, base + c * 8, v[j]);
     if (a.x8) store_mx8(a.x8, scales, base + c * 8, v[j], ok);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss.square(v[j][i]);
+    for (int i = 0; i < 8; ++i) ss = fmaf(v[j][i], v[j][i], ss);
   }
-  const float2 r = rstd_of(team_sum(ss, lg, part), a.d, a.eps);
+  const float2 r = rstd_of(team_sum(Sum2{ss, 0.f}, lg, part), a.d, a.eps);
   if (in && lane == 0 && a.rstd) a.rstd[row] = r.x + r.y;
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
@@ -173,8 +172,43 @@ __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ 
   }
 }
 
-template <typename T, int NG, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_grad_kernel(const __grid_constant__ NormGradArgs a, int lg) {
+// Eight neighbouring values as they lie in memory, to be read again instead of kept unpacked.
+struct RawF32 {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p, size_t i) {
+    a = __ldcs(reinterpret_cast<const float4*>(p + i));
+    b = __ldcs(reinterpret_cast<const float4*>(p + i) + 1);
+  }
+  __device__ __forceinline__ void values(float* v) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+};
+struct RawBf16 {
+  uint4 q;
+  __device__ __forceinline__ void load(const uint16_t* p, size_t i) { q = __ldcs(reinterpret_cast<const uint4*>(p + i)); }
+  __device__ __forceinline__ void values(float* v) const { unpack8(q, v); }
+};
+struct RawMx8 {
+  uint2 q;
+  uint32_t scale;
+  __device__ __forceinline__ void load(const uint8_t* p, size_t scales, size_t i) {
+    q = __ldcs(reinterpret_cast<const uint2*>(p + i));
+    scale = __ldg(p + scales + i / 32);
+  }
+  __device__ __forceinline__ void values(float* v) const {
+    const float unit = mx8_unit(scale);
+    mx8_values(q.x, v);
+    mx8_values(q.y, v + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= unit;
+  }
+};
+template <typename T>
+using Raw = std::conditional_t<sizeof(T) == 2, RawBf16, RawF32>;
+
+template <typename T, bool X8, int NG, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? (X8 ? 4 : 2) : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a, int lg) {
   pdl_wait();
   __shared__ float part[2][32];
   __shared__ float share[THREADS == 256 && NG == 1 ? 2048 : 1];  // several teams: [team][8 values of a thread]
@@ -187,42 +221,35 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const __grid_constan
     const long long row = row0 + team;
     const bool in = row < a.T;
     const size_t base = size_t(in ? row : 0) * a.d;
-    const float r = in ? a.rstd[row] : 0.f;
-    float n[NG][8], g[NG][8], res[NG][8];
+    std::conditional_t<X8, RawMx8, RawF32> x[NG];
+    Raw<T> du[NG];
+    RawF32 res[NG];
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
       const int c = lane + (j << lg);
-      const bool ok = in && c < groups;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) n[j][i] = g[j][i] = res[j][i] = 0.f;
-      if (ok) {
-        const size_t at = base + c * 8;
-        if (a.x8) {
-          const uint2 q = *reinterpret_cast<const uint2*>(a.x8 + at);
-          const float unit = mx8_unit(a.x8[scales + at / 32]);
-          mx8_values(q.x, n[j]);
-          mx8_values(q.y, n[j] + 4);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) n[j][i] *= unit;
-        } else {
-          load8<float>(a.x, at, n[j]);
-        }
-        load8<T>(a.du, at, g[j]);
-        if (a.dres) load8<float>(a.dres, at, res[j]);
-      }
+      const size_t at = base + (c < groups ? c : 0) * 8;  // (threads past the row's end read its beginning)
+      if constexpr (X8) x[j].load(a.x8, scales, at);
+      else x[j].load(a.x, at);
+      du[j].load(static_cast<const T*>(a.du), at);
+      if (a.dres) res[j].load(a.dres, at);
+      else res[j] = RawF32{};
     }
+    const float r = a.rstd[in ? row : 0];
     float dot = 0.f;
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
       const int c = lane + (j << lg);
-      float gam[8] = {};
-      if (c < groups) load8<T>(a.gamma, size_t(c) * 8, gam);
+      if (in && c < groups) {
+        float n[8], g[8], gam[8];
+        x[j].values(n);
+        du[j].values(g);
+        load8<T>(a.gamma, size_t(c) * 8, gam);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        n[j][i] *= r;
-        dg[j][i] = fmaf(g[j][i], n[j][i], dg[j][i]);
-        g[j][i] *= gam[i];
-        dot = fmaf(g[j][i], n[j][i], dot);
+        for (int i = 0; i < 8; ++i) {
+          const float m = n[i] * r;
+          dg[j][i] = fmaf(g[i], m, dg[j][i]);
+          dot = fmaf(g[i] * gam[i], m, dot);
+        }
       }
     }
     dot = team_sum(dot, lg, part[turn]) * over_d;
@@ -231,9 +258,14 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const __grid_constan
       for (int j = 0; j < NG; ++j) {
         const int c = lane + (j << lg);
         if (c < groups) {
+          float n[8], g[8], gam[8], v[8];
+          x[j].values(n);
+          du[j].values(g);
+          res[j].values(v);
+          load8<T>(a.gamma, size_t(c) * 8, gam);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) res[j][i] = fmaf(r, fmaf(-n[j][i], dot, g[j][i]), res[j][i]);
-          store8<float>(a.dx, base + c * 8, res[j]);
+          for (int i = 0; i < 8; ++i) v[i] = fmaf(r, fmaf(-(n[i] * r), dot, g[i] * gam[i]), v[i]);
+          store8<float>(a.dx, base + c * 8, v);
         }
       }
     }
@@ -302,13 +334,13 @@ cudaError_t forward(const Norm8Args& a, cudaStream_t s) {
   return launch_pdl(k, grid, dim3(unsigned(t.threads)), 0, s, a, t.lg);
 }
 
-template <typename T>
+template <typename T, bool X8>
 cudaError_t backward(const NormGradArgs& a, cudaStream_t s) {
   const Teams t(a.d);
   const int planes = norm_grad_planes(a.T, a.d);
-  auto* k = t.steps == 1 ? norm_grad_kernel<T, 1, 256>
-            : t.steps == 2 ? (t.threads == 256 ? norm_grad_kernel<T, 2, 256> : norm_grad_kernel<T, 2, 1024>)
-                           : norm_grad_kernel<T, 4, 1024>;
+  auto* k = t.steps == 1 ? norm_grad_kernel<T, X8, 1, 256>
+            : t.steps == 2 ? (t.threads == 256 ? norm_grad_kernel<T, X8, 2, 256> : norm_grad_kernel<T, X8, 2, 1024>)
+                           : norm_grad_kernel<T, X8, 4, 1024>;
   const cudaError_t e = launch_pdl(k, dim3(unsigned(planes)), dim3(unsigned(t.threads)), 0, s, a, t.lg);
   if (e != cudaSuccess || !a.dgamma) return e;
   return launch_pdl(norm_planes_kernel, dim3(unsigned(a.d / 32)), dim3(1024), 0, s, a, planes);
@@ -331,7 +363,8 @@ int norm_grad_planes(int T, int d) {
 
 cudaError_t launch_norm_grad(const NormGradArgs& a, int dtype, cudaStream_t s) {
   prof_begin(kProfNormGrad, s);
-  const cudaError_t e = dtype == MCFT_BF16 ? backward<uint16_t>(a, s) : backward<float>(a, s);
+  const cudaError_t e = dtype == MCFT_BF16 ? (a.x8 ? backward<uint16_t, true>(a, s) : backward<uint16_t, false>(a, s))
+                                           : (a.x8 ? backward<float, true>(a, s) : backward<float, false>(a, s));
   prof_end(kProfNormGrad, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
