@@ -13,7 +13,8 @@ namespace mcft {
 namespace {
 
 constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
-constexpr int kFewTokens = 64;  // up to here the decode kernels: the weights are what there is to read
+
+constexpr int kFewTokensF32 = 32;  // fp32: up to here the kernels that read each weight row once for 8 tokens
 
 mcft_status check_T(int T) {
   if (T < 0) return fail(MCFT_ERR_INVALID, "T = %d < 0", T);
@@ -67,31 +68,26 @@ struct Sections {
 size_t elem(int dtype) { return dtype == MCFT_BF16 ? 2 : 4; }
 
 struct ForwardLayout {
-  size_t h, gu, planes;        // many tokens (gu: fp32 with a checkpoint)
-  size_t hdr, off, perm, done, few_h, few_o;
+  size_t h, gu, planes;   // products
+  size_t hdr, off, perm;  // fp32 without a checkpoint: h, and what its kernels expect of a permutation
   size_t total;
 };
-// Every section grows with T, so a workspace for T_max serves all smaller calls of either kind.
+// Every section grows with T, so a workspace for T_max serves all smaller calls.
 ForwardLayout forward_layout(const mcft_layer_desc* d, int T) {
   const size_t t = size_t(T), w = size_t(d->w), D = size_t(d->d);
+  const bool f32 = d->dtype == MCFT_F32;
   ForwardLayout L{};
-  Sections many, few;
-  L.h = many.add(t * w * elem(d->dtype));
-  if (d->dtype == MCFT_F32) L.gu = many.add(t * 2 * w * 4);
-  const size_t up = d->dtype == MCFT_F32 ? dense_plane_bytes(1, t * 2 * w, d->d, d->dtype) : 0;
-  L.planes = many.add(std::max(up, dense_plane_bytes(1, t * D, d->w, d->dtype)));
-  const int n = d->dtype == MCFT_BF16 ? std::min(T, kFewTokens) : T;
-  L.hdr = few.add(sizeof(WsHeader));
-  L.off = few.add(2 * sizeof(int));
-  L.perm = few.add(size_t(n) * sizeof(int));
-  L.done = few.add((1 + kClaimSlots) * sizeof(int));
-  L.few_h = few.add(size_t(n) * w * elem(d->dtype));
-  // partial planes: 8 of up to 4 tokens, 2 of up to 16, one of more
-  size_t rows = size_t(n);
-  if (d->dtype == MCFT_BF16)
-    for (int i : {4, 16}) rows = std::max(rows, size_t(decode_ksplit(std::min(n, i))) * std::min(n, i));
-  L.few_o = few.add(rows * D * 4);
-  L.total = std::max(many.total, few.total);
+  Sections s;
+  L.h = s.add(t * w * elem(d->dtype));
+  if (f32) {
+    L.hdr = s.add(sizeof(WsHeader));
+    L.off = s.add(2 * sizeof(int));
+    L.perm = s.add(t * sizeof(int));
+    L.gu = s.add(t * 2 * w * 4);
+  }
+  const size_t up = f32 ? dense_plane_bytes(1, t * 2 * w, d->d, d->dtype) : 0;
+  L.planes = s.add(std::max(up, dense_plane_bytes(1, t * D, d->w, d->dtype)));
+  L.total = s.total;
   return L;
 }
 
@@ -113,25 +109,23 @@ GradLayout grad_layout(const mcft_layer_desc* d, int T) {
   return L;
 }
 
-// y = F(x) by the kernels that serve batches of few tokens (bf16), or fp32 ones of any size, as one expert that every token
-// takes.
-cudaError_t forward_few(const mcft_layer_desc* d, const void* x, int T, const void* block, void* y, char* ws,
+// fp32: y = F(x) by the expert kernels, as one expert that every token takes.
+cudaError_t forward_f32(const mcft_layer_desc* d, const void* x, int T, const void* block, void* y, char* ws,
                         const ForwardLayout& L, cudaStream_t s) {
-  DenseFewArgs p{reinterpret_cast<WsHeader*>(ws + L.hdr), reinterpret_cast<int*>(ws + L.off),
-                 reinterpret_cast<int*>(ws + L.perm), reinterpret_cast<int*>(ws + L.done), T, 1 + kClaimSlots};
-  cudaError_t e = launch_dense_few(p, s);
+  const DensePlaceArgs p{reinterpret_cast<WsHeader*>(ws + L.hdr), reinterpret_cast<int*>(ws + L.off),
+                         reinterpret_cast<int*>(ws + L.perm), T};
+  const cudaError_t e = launch_dense_place(p, s);
   if (e != cudaSuccess) return e;
   FfnArgs a{};
   a.x = x;
   a.off = p.off;
   a.perm = p.perm;
   a.hdr = p.hdr;
-  a.done = p.done;
   a.wblk[0] = block;
-  a.h = ws + L.few_h;
-  a.o = reinterpret_cast<float*>(ws + L.few_o);
+  a.h = ws + L.h;
+  a.o = static_cast<float*>(y);
   a.o_plane = size_t(T) * d->d;
-  a.ksplit = d->dtype == MCFT_BF16 ? decode_ksplit(T) : 1;
+  a.ksplit = 1;
   a.T = T;
   a.K = 1;
   a.d = d->d;
@@ -139,8 +133,7 @@ cudaError_t forward_few(const mcft_layer_desc* d, const void* x, int T, const vo
   a.nseg = 1;
   a.E = 1;
   a.err = device_error_word();
-  e = d->dtype == MCFT_BF16 ? launch_ffn_decode(a, num_sms(), s, 3) : launch_ffn_rowwise(a, d->dtype, num_sms(), s, 3);
-  return e != cudaSuccess ? e : launch_dense_join(a.o, a.ksplit, a.o_plane, y, d->dtype, 0, s);
+  return launch_ffn_rowwise(a, MCFT_F32, num_sms(), s, 3);
 }
 
 }  // namespace
@@ -262,8 +255,9 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   if (st != MCFT_OK) return st;
   char* ws = static_cast<char*>(workspace);
   cudaError_t e;
-  if (!ckpt && (desc->dtype == MCFT_F32 || T <= kFewTokens)) {
-    e = forward_few(desc, x, T, block, y, ws, L, stream);
+  if (!ckpt && T <= (desc->dtype == MCFT_F32 ? kFewTokensF32 : kFewTokens)) {
+    e = desc->dtype == MCFT_F32 ? forward_f32(desc, x, T, block, y, ws, L, stream)
+                                : launch_dense_few(DenseFewArgs{x, block, ws + L.h, y, T, desc->d, desc->w}, stream);
     return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
   }
   const char* w13 = static_cast<const char*>(block);

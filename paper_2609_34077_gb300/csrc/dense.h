@@ -98,12 +98,21 @@ struct DenseActArgs {
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s);
 cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s);
 
-// What the decode kernels expect of a permutation, for one expert that all T tokens take in order.
+// The whole block for up to kFewTokens tokens, bf16: h [T, w] is scratch.
+constexpr int kFewTokens = 8;
 struct DenseFewArgs {
-  WsHeader* hdr;
-  int *off, *perm, *done;
-  int T, ndone;
+  const void *x, *block;
+  void *h, *y;
+  int T, d, w;
 };
 cudaError_t launch_dense_few(const DenseFewArgs& a, cudaStream_t s);
+
+// What the fp32 expert kernels expect of a permutation, for one expert that all T tokens take in order.
+struct DensePlaceArgs {
+  WsHeader* hdr;
+  int *off, *perm;
+  int T;
+};
+cudaError_t launch_dense_place(const DensePlaceArgs& a, cudaStream_t s);
 
 }  // namespace mcft

@@ -1,10 +1,11 @@
 // Products of the dense block in fp32 (CUDA-core multiply-adds, no TF32), the element-wise steps between them, and the sum
 // of split products' planes.
 //
-// A CTA of 128 threads computes 128 x 64 outputs, 8 x 8 a thread, 16 of the contraction a step in two shared buffers;
-// operands are taken as they lie in memory, whichever index is contiguous, and stand in shared memory by contraction
-// index, so a step's 16-byte loads feed 16 multiply-adds each. A step's 16 products are summed first and then added to the
-// total: one running sum's error grows with the square root of its length.
+// A CTA of 128 threads computes 128 x 64 outputs, 8 x 8 a thread, by packed multiply-adds (two columns an instruction), 16 of
+// the contraction a step in two shared buffers. Operands are taken as they lie in memory, whichever index is contiguous, and stand
+// in shared memory by contraction index, so a step's four 16-byte loads feed 64 multiply-adds. After 128 elements the
+// sums are added to totals in shared memory, a place a thread: one running sum's error grows with the square root of its
+// length. Up to three products make one launch; contractions are split into planes by a rule on the rounds that the CTAs make.
 #include <algorithm>
 
 #include "dense.h"
@@ -19,13 +20,33 @@ namespace {
 
 constexpr int TM = 128, TN = 64, TK = 16, kThreads = 128;
 constexpr int kPitchA = TM + 4, kPitchB = TN + 4;
+constexpr int kRun = 128;  // of the contraction between additions to the totals
+constexpr int kF32Smem = (2 * TK * (kPitchA + kPitchB) + TM * TN) * 4;
 
-struct F32Params {
+struct F32Problem {
   const float *a, *b;
   float* out;
   size_t plane;  // elements between split planes
-  int M, N, K, a_t, b_t, per, accumulate;
+  int M, N, K, a_t, b_t, per, accumulate, mt, tiles, first;
 };
+struct F32Params {
+  F32Problem p[kMaxProducts];
+  int n;
+};
+
+__device__ __forceinline__ uint64_t twice(float v) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ float2 halves(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
 
 // A step's tile of an operand with `R` rows: from memory to registers, four neighbouring values a load.
 // contiguous: the contraction is the contiguous index.
@@ -58,23 +79,28 @@ __device__ __forceinline__ void put(float* to, const float4* v, bool contiguous)
   }
 }
 
-__global__ void __launch_bounds__(kThreads) dense_f32_kernel(const __grid_constant__ F32Params p) {
+__global__ void __launch_bounds__(kThreads, 3) dense_f32_kernel(const __grid_constant__ F32Params params) {
   pdl_wait();
-  __shared__ float4 sa4[2][TK * kPitchA / 4], sb4[2][TK * kPitchB / 4];
-  const int m0 = int(blockIdx.x) * TM, n0 = int(blockIdx.y) * TN;
-  const int k0 = int(blockIdx.z) * p.per, k1 = min(k0 + p.per, p.K);
+  extern __shared__ __align__(16) float smem[];  // [2][TK][A | B], then totals [16][threads][4]
+  float4* totals = reinterpret_cast<float4*>(smem + 2 * TK * (kPitchA + kPitchB)) + threadIdx.x;
+  int i = 0;
+  while (i + 1 < params.n && int(blockIdx.x) >= params.p[i + 1].first) ++i;
+  const F32Problem& p = params.p[i];
+  const int local = int(blockIdx.x) - p.first, split = local / p.tiles, tile = local - split * p.tiles;
+  const int m0 = tile % p.mt * TM, n0 = tile / p.mt * TN;
+  const int k0 = split * p.per, k1 = min(k0 + p.per, p.K);
   const bool ca = !p.a_t, cb = p.b_t;
   const int lda = ca ? p.K : p.M, ldb = cb ? p.K : p.N;
   // thread's rows tm + 0..3 and 64 + tm + 0..3, columns tn + 0..3 and 32 + tn + 0..3
   const int tm = int(threadIdx.x >> 3) * 4, tn = int(threadIdx.x & 7) * 4;
   float4 va[TM * TK / 4 / kThreads], vb[TN * TK / 4 / kThreads];
-  float acc[8][8] = {};
+  uint64_t acc[8][4] = {};
   fetch<TM>(va, p.a, ca, m0, p.M, k0, k1, lda);
   fetch<TN>(vb, p.b, cb, n0, p.N, k0, k1, ldb);
-  int buf = 0;
-  for (int k = k0; k < k1; k += TK, buf ^= 1) {
-    float* sa = reinterpret_cast<float*>(sa4[buf]);
-    float* sb = reinterpret_cast<float*>(sb4[buf]);
+  bool kept = false;  // something in the totals
+  for (int k = k0, step = 0; k < k1; k += TK, ++step) {
+    float* sa = smem + (step & 1) * TK * (kPitchA + kPitchB);
+    float* sb = sa + TK * kPitchA;
     put<TM, kPitchA>(sa, va, ca);
     put<TN, kPitchB>(sb, vb, cb);
     __syncthreads();  // (the buffer of the step before last has been read by all)
@@ -82,37 +108,55 @@ __global__ void __launch_bounds__(kThreads) dense_f32_kernel(const __grid_consta
       fetch<TM>(va, p.a, ca, m0, p.M, k + TK, k1, lda);
       fetch<TN>(vb, p.b, cb, n0, p.N, k + TK, k1, ldb);
     }
-    float sum[8][8];
 #pragma unroll
     for (int kk = 0; kk < TK; ++kk) {
-      float x[8], y[8];
+      float x[8];
+      ulonglong2 y[2];
       *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(sa + kk * kPitchA + tm);
       *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(sa + kk * kPitchA + 64 + tm);
-      *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(sb + kk * kPitchB + tn);
-      *reinterpret_cast<float4*>(y + 4) = *reinterpret_cast<const float4*>(sb + kk * kPitchB + 32 + tn);
+      y[0] = *reinterpret_cast<const ulonglong2*>(sb + kk * kPitchB + tn);
+      y[1] = *reinterpret_cast<const ulonglong2*>(sb + kk * kPitchB + 32 + tn);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[i][j] = kk == 0 ? x[i] * y[j] : fmaf(x[i], y[j], sum[i][j]);
+      for (int r = 0; r < 8; ++r) {
+        const uint64_t xx = twice(x[r]);
+        fma2(acc[r][0], xx, y[0].x);
+        fma2(acc[r][1], xx, y[0].y);
+        fma2(acc[r][2], xx, y[1].x);
+        fma2(acc[r][3], xx, y[1].y);
+      }
     }
+    if ((step + 1) % (kRun / TK) == 0 && k + TK < k1) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+      for (int r = 0; r < 8; ++r)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[i][j] += sum[i][j];
+        for (int h = 0; h < 2; ++h) {
+          const float2 a = halves(acc[r][2 * h]), b = halves(acc[r][2 * h + 1]);
+          float4 t = kept ? totals[(2 * r + h) * kThreads] : make_float4(0.f, 0.f, 0.f, 0.f);
+          t.x += a.x;
+          t.y += a.y;
+          t.z += b.x;
+          t.w += b.y;
+          totals[(2 * r + h) * kThreads] = t;
+          acc[r][2 * h] = acc[r][2 * h + 1] = 0;
+        }
+      kept = true;
+    }
   }
-  float* out = p.out + size_t(blockIdx.z) * p.plane;
+  float* out = p.out + size_t(split) * p.plane;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int m = m0 + tm + (i & 3) + (i >> 2) * 64;
+  for (int r = 0; r < 8; ++r) {
+    const int m = m0 + tm + (r & 3) + (r >> 2) * 64;
     if (m >= p.M) continue;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int n = n0 + tn + h * 32;
       if (n >= p.N) continue;
       float4* to = reinterpret_cast<float4*>(out + size_t(m) * p.N + n);
-      float4 v = make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
-      if (p.accumulate) {
-        const float4 o = *to;
+      const float2 a = halves(acc[r][2 * h]), b = halves(acc[r][2 * h + 1]);
+      float4 v = make_float4(a.x, a.y, b.x, b.y);
+      for (int from = 0; from < 2; ++from) {
+        if (from ? !p.accumulate : !kept) continue;
+        const float4 o = from ? *to : totals[(2 * r + h) * kThreads];
         v.x += o.x;
         v.y += o.y;
         v.z += o.z;
@@ -245,26 +289,50 @@ cudaError_t launch_act(const DenseActArgs& a, cudaStream_t s) {
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-// Parts of a contraction such that the tiles make up to about three CTAs an SM, of at least 128 elements.
+// Parts of the contractions: what the fullest SM computes (CTAs on one SM share its multiply-adds), at 40 ns for an element of
+// a tile's contraction, beside the planes' way to memory and back and the launches that add them up.
 struct F32Plan {
-  int splits[kMaxProducts], per[kMaxProducts];  // parts of a contraction, elements of each
-  size_t plane[kMaxProducts], floats;
+  int per[kMaxProducts], splits[kMaxProducts];
 };
 F32Plan f32_plan(const DenseProduct* p, int n) {
-  F32Plan plan = {};
-  for (int i = 0; i < n; ++i) {
-    const long long tiles = (long long)((p[i].rows + TM - 1) / TM) * ((p[i].cols + TN - 1) / TN);
-    const int want = int(std::max(1ll, 3ll * num_sms() / tiles)), most = std::max(1, p[i].k / 128);
-    const int parts = std::min({want, most, 64});
-    plan.per[i] = ((p[i].k + parts - 1) / parts + TK - 1) / TK * TK;
-    plan.splits[i] = (p[i].k + plan.per[i] - 1) / plan.per[i];
-    plan.plane[i] = plan.floats;
-    if (plan.splits[i] > 1) plan.floats += size_t(plan.splits[i]) * p[i].rows * p[i].cols;
+  F32Plan best{};
+  double least = 0;
+  int longest = 1;
+  const int sms = num_sms();
+  for (int i = 0; i < n; ++i) longest = std::max(longest, p[i].k);
+  for (int parts = 1; parts <= 32; ++parts) {
+    const int unit = std::max(kRun, ((longest + parts - 1) / parts + TK - 1) / TK * TK);
+    F32Plan plan{};
+    double work = 0, planes = 0;
+    long long items = 0;
+    int joins = 0, most = 0;
+    for (int i = 0; i < n; ++i) {
+      const long long tiles = (long long)((p[i].rows + TM - 1) / TM) * ((p[i].cols + TN - 1) / TN);
+      const int want = (p[i].k + unit - 1) / unit;
+      plan.per[i] = ((p[i].k + want - 1) / want + TK - 1) / TK * TK;
+      plan.splits[i] = (p[i].k + plan.per[i] - 1) / plan.per[i];
+      items += tiles * plan.splits[i];
+      work += double(tiles) * p[i].k;
+      most = std::max(most, plan.per[i]);
+      if (plan.splits[i] > 1) {
+        planes += double(plan.splits[i]) * p[i].rows * p[i].cols;
+        ++joins;
+      }
+    }
+    if (planes > double(n) * 3 * sms * TM * TN) break;
+    const double rounds = double((items + sms - 1) / sms), mean = work / items;
+    const double busy = rounds <= 6 ? std::max(double(most), rounds * mean) : work / sms + most / 2;
+    const double time = busy * 0.040 + planes * 8 / 4e6 + joins * 4;
+    if (parts == 1 || time < least) {
+      least = time;
+      best = plan;
+    }
+    if (unit == kRun) break;
   }
-  return plan;
+  return best;
 }
 
-__global__ void __launch_bounds__(256) dense_few_kernel(const __grid_constant__ DenseFewArgs a) {
+__global__ void __launch_bounds__(256) dense_place_kernel(const __grid_constant__ DensePlaceArgs a) {
   pdl_wait();
   const int i = int(blockIdx.x) * 256 + int(threadIdx.x);
   if (i == 0) {
@@ -273,7 +341,6 @@ __global__ void __launch_bounds__(256) dense_few_kernel(const __grid_constant__ 
     a.off[1] = a.T;
   }
   if (i < a.T) a.perm[i] = i;
-  if (i < a.ndone) a.done[i] = 0;
 }
 
 }  // namespace
@@ -282,7 +349,7 @@ size_t dense_plane_bytes(int n, size_t outs, int k, int dtype) {
   // items that run at once, and the most parts of a contraction
   const size_t sms = size_t(num_sms());
   const size_t items = dtype == MCFT_BF16 ? sms / 2 * kDensePlaneTiles * kDenseTile * kDenseTile : size_t(n) * (3 * sms) * TM * TN;
-  const size_t parts = dtype == MCFT_BF16 ? size_t(k) / (4 * 64) + 2 : size_t(k) / 128 + 2;
+  const size_t parts = dtype == MCFT_BF16 ? size_t(k) / (4 * 64) + 2 : size_t(k) / kRun + 2;
   return std::min(items, parts * outs) * sizeof(float);
 }
 
@@ -300,31 +367,39 @@ cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* ou
 cudaError_t launch_dense_products(const DenseProduct* p, int n, int dtype, float* planes, cudaStream_t s) {
   if (dtype == MCFT_BF16) return launch_dense_tc(p, n, planes, s);
   const F32Plan plan = f32_plan(p, n);
+  F32Params q{};
+  q.n = n;
+  size_t used = 0;
+  int items = 0;
   for (int i = 0; i < n; ++i) {
     const bool split = plan.splits[i] > 1;
-    const F32Params q{static_cast<const float*>(p[i].a), static_cast<const float*>(p[i].b),
-                      split ? planes + plan.plane[i] : static_cast<float*>(p[i].out), size_t(p[i].rows) * p[i].cols,
-                      p[i].rows, p[i].cols, p[i].k, p[i].a_t, p[i].b_t, plan.per[i], split ? 0 : p[i].accumulate};
-    const dim3 grid{unsigned((p[i].rows + TM - 1) / TM), unsigned((p[i].cols + TN - 1) / TN), unsigned(plan.splits[i])};
-    prof_begin(kProfDenseF32, s);
-    cudaError_t e = launch_pdl(dense_f32_kernel, grid, dim3(kThreads), 0, s, q);
-    prof_end(kProfDenseF32, s);
-    if (e == cudaSuccess) e = cudaGetLastError();
-    if (e == cudaSuccess && split)
-      e = launch_dense_join(planes + plan.plane[i], plan.splits[i], q.plane, p[i].out, MCFT_F32, p[i].accumulate, s);
-    if (e != cudaSuccess) return e;
+    const int mt = (p[i].rows + TM - 1) / TM, tiles = mt * ((p[i].cols + TN - 1) / TN);
+    q.p[i] = F32Problem{static_cast<const float*>(p[i].a), static_cast<const float*>(p[i].b),
+                        split ? planes + used : static_cast<float*>(p[i].out), size_t(p[i].rows) * p[i].cols, p[i].rows,
+                        p[i].cols, p[i].k, p[i].a_t, p[i].b_t, plan.per[i], split ? 0 : p[i].accumulate, mt, tiles, items};
+    items += tiles * plan.splits[i];
+    if (split) used += size_t(plan.splits[i]) * q.p[i].plane;
   }
-  return cudaSuccess;
+  static SmemOptIn smem;
+  cudaError_t e = smem.allow(reinterpret_cast<const void*>(dense_f32_kernel), kF32Smem);
+  if (e != cudaSuccess) return e;
+  prof_begin(kProfDenseF32, s);
+  e = launch_pdl(dense_f32_kernel, dim3(unsigned(items)), dim3(kThreads), kF32Smem, s, q);
+  prof_end(kProfDenseF32, s);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  for (int i = 0; i < n && e == cudaSuccess; ++i)
+    if (plan.splits[i] > 1)
+      e = launch_dense_join(q.p[i].out, plan.splits[i], q.p[i].plane, p[i].out, MCFT_F32, p[i].accumulate, s);
+  return e;
 }
 
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s) { return launch_act<false>(a, s); }
 cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s) { return launch_act<true>(a, s); }
 
-cudaError_t launch_dense_few(const DenseFewArgs& a, cudaStream_t s) {
-  const int n = std::max(a.T, a.ndone);
-  prof_begin(kProfDenseFew, s);
-  const cudaError_t e = launch_pdl(dense_few_kernel, dim3(unsigned((n + 255) / 256)), dim3(256), 0, s, a);
-  prof_end(kProfDenseFew, s);
+cudaError_t launch_dense_place(const DensePlaceArgs& a, cudaStream_t s) {
+  prof_begin(kProfDensePlace, s);
+  const cudaError_t e = launch_pdl(dense_place_kernel, dim3(unsigned((a.T + 255) / 256)), dim3(256), 0, s, a);
+  prof_end(kProfDensePlace, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -36,7 +36,7 @@ constexpr int kThreads = 64 + 256;
 constexpr int kEpiWarps = 8;
 constexpr int kABytes = 128 * BK * 2;  // a CTA's rows of A in a stage
 constexpr int kRingBytes = 7 * (kABytes + 128 * BK * 2);
-constexpr int kMaxStages = 9;
+constexpr int kMaxStages = 16;
 constexpr int kTmemCols = 2 * kTile;
 // instruction descriptor without N and the operands' order: D fp32, A and B bf16, M = 256
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 4) << 24);
@@ -55,7 +55,8 @@ struct Problem {
 struct Params {
   Problem p[kMaxProducts];
   int n, items;
-  int cols;  // of a tile: 256 or 128
+  int cols;    // of a tile: 256 or 128
+  int a_rows;  // of A that the first CTA of a pair brings in, where no A has more than its 128; else 0: 128 each
   unsigned* err;
   // up, up_grad
   uint8_t* ckpt;
@@ -316,7 +317,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   pdl_wait();  // (nothing above reads memory)
 
   const uint32_t tmem = ctl->tmem_base;
-  const int half_cols = q.cols / 2, stage_bytes = kABytes + half_cols * BK * 2, stages = min(kMaxStages, kRingBytes / stage_bytes);
+  // Few rows: the others of the MMA's A are whatever follows in shared memory, and so are sums that nobody reads. (The last
+  // stage's must still lie in the ring.)
+  const int a_bytes = q.a_rows ? q.a_rows * BK * 2 : kABytes, b_bytes = q.cols / 2 * BK * 2, stage_bytes = a_bytes + b_bytes;
+  const int half_cols = q.cols / 2, stages = min(kMaxStages, (kRingBytes - (kABytes - a_bytes)) / stage_bytes);
   const int items = q.items, cid = int(blockIdx.x >> 1), ncl = int(gridDim.x >> 1);
   volatile int* abort = &ctl->abort;
 
@@ -334,9 +338,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int kb = t.k0; kb < t.k1; ++kb) {
           if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, q.err)) break;
           const uint32_t sa = base + uint32_t(s * stage_bytes), fb = fb0 + uint32_t(s) * 8u;
-          if (leader) mbar_expect_tx(&ctl->full[s], 2u * uint32_t(stage_bytes));
-          load_operand(sa, &t.p->a, a_mn, 128, kb * BK, arow, fb);
-          load_operand(sa + kABytes, mb, b_mn, half_cols, kb * BK, brow, fb);
+          if (leader) mbar_expect_tx(&ctl->full[s], uint32_t(q.a_rows ? stage_bytes + b_bytes : 2 * stage_bytes));
+          if (leader || !q.a_rows) load_operand(sa, &t.p->a, a_mn, 128, kb * BK, arow, fb);
+          load_operand(sa + a_bytes, mb, b_mn, half_cols, kb * BK, brow, fb);
           if (issued < stages) ++issued;
           if (++s == stages) {
             s = 0;
@@ -374,7 +378,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
           tc_fence_after();
           const uint32_t sa = base + uint32_t(s * stage_bytes);
-          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + kABytes, b_mn);
+          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + a_bytes, b_mn);
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k)
             tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (kb != t.k0 || k != 0) ? 1u : 0u);
@@ -503,6 +507,9 @@ Plan choose(const Sizes* z, int n, int up, bool splittable, int pairs) {
   return best;
 }
 
+// Rows of A (as they lie in memory: K-major) of a launch's first CTAs, where that is all there are.
+int few_rows(int M) { return M <= 128 ? (M + 7) & ~7 : 0; }
+
 template <int EPI>
 int pairs_at_once() {
   static SmemOptIn smem;
@@ -539,7 +546,8 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
   q.cols = choose(&z, 1, 1, false, num_sms() / 2).cols;
   shape(p, a.T, a.w, a.d, q.cols / 2);
   const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
-  if (!encode(&p.a, a.x, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, w1, size_t(a.d), size_t(a.w), q.cols / 2) ||
+  q.a_rows = few_rows(a.T);
+  if (!encode(&p.a, a.x, size_t(a.d), size_t(a.T), q.a_rows ? q.a_rows : 128) || !encode(&p.b, w1, size_t(a.d), size_t(a.w), q.cols / 2) ||
       !encode(&p.b1, w1 + size_t(a.w) * a.d, size_t(a.d), size_t(a.w), q.cols / 2))
     return cudaErrorInvalidValue;
   q.w = a.w;
@@ -560,7 +568,8 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   q.cols = choose(&z, 1, 0, false, num_sms() / 2).cols;
   shape(p, a.T, a.w, a.d, q.cols);
   p.b_mn = 1;
-  if (!encode(&p.a, a.dy, size_t(a.d), size_t(a.T), 128) || !encode(&p.b, a.w2, size_t(a.w), size_t(a.d), 64))
+  q.a_rows = few_rows(a.T);
+  if (!encode(&p.a, a.dy, size_t(a.d), size_t(a.T), q.a_rows ? q.a_rows : 128) || !encode(&p.b, a.w2, size_t(a.w), size_t(a.d), 64))
     return cudaErrorInvalidValue;
   q.w = a.w;
   q.ckpt = const_cast<uint8_t*>(a.ckpt);
@@ -582,6 +591,10 @@ cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaSt
   q.cols = plan.cols;
   size_t used = 0;
   for (int i = 0; i < n; ++i) {
+    const int r = in[i].a_t ? 0 : few_rows(in[i].rows);
+    q.a_rows = i == 0 ? r : q.a_rows && r ? std::max(q.a_rows, r) : 0;
+  }
+  for (int i = 0; i < n; ++i) {
     const DenseProduct& d = in[i];
     Problem& p = q.p[i];
     shape(p, d.rows, d.cols, d.k, plan.cols);
@@ -590,7 +603,7 @@ cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaSt
     p.a_mn = d.a_t;
     p.b_mn = !d.b_t;
     const size_t M = size_t(d.rows), N = size_t(d.cols), K = size_t(d.k);
-    if (!(d.a_t ? encode(&p.a, d.a, M, K, 64) : encode(&p.a, d.a, K, M, 128)) ||
+    if (!(d.a_t ? encode(&p.a, d.a, M, K, 64) : encode(&p.a, d.a, K, M, q.a_rows ? q.a_rows : 128)) ||
         !(d.b_t ? encode(&p.b, d.b, K, N, plan.cols / 2) : encode(&p.b, d.b, N, K, 64)))
       return cudaErrorInvalidValue;
     p.out = d.out;
