@@ -634,9 +634,11 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  *   ckpt      device mx8 [T, 2w] out: g = W1 x and u = W3 x (g first), rounded from fp32, for mcft_ffn_grad; or NULL
  *   workspace device, mcft_ffn_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
- * Of desc only d, w and dtype are read. bf16: fp32 sums, h rounded to bf16 once, y once; up to 64 tokens without a checkpoint
- * run the decode kernels, the others tcgen05 products with SwiGLU and the checkpoint's rounding in the epilogue. fp32 layers
- * are fp32 throughout. T = 0 is a no-op. Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID
+ * Of desc only d, w and dtype are read. bf16: fp32 sums, h rounded to bf16 once, y once; tcgen05 products with SwiGLU and the
+ * checkpoint's rounding in the epilogue, a weight-streaming pair of kernels for few tokens. fp32 layers: operands of the
+ * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones), and six
+ * products of them on the tensor cores make each fp32 one, in fp32 sums of short runs; few tokens take CUDA-core fp32
+ * arithmetic. T = 0 is a no-op. Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID
  * for a NULL or misaligned pointer (16 bytes), a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for T > 2^24 or
  * d or w > 2^20. */
 mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);

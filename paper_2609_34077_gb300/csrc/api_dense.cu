@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
 
-constexpr int kFewTokensF32 = 32;  // fp32: up to here the kernels that read each weight row once for 8 tokens
+constexpr int kFewTokensF32 = 8;  // fp32: up to here the kernels that read each weight row once for 8 tokens
 
 mcft_status check_T(int T) {
   if (T < 0) return fail(MCFT_ERR_INVALID, "T = %d < 0", T);
@@ -68,8 +68,9 @@ struct Sections {
 size_t elem(int dtype) { return dtype == MCFT_BF16 ? 2 : 4; }
 
 struct ForwardLayout {
-  size_t h, gu, planes;   // products
-  size_t hdr, off, perm;  // fp32 without a checkpoint: h, and what its kernels expect of a permutation
+  size_t h, planes;       // h: bf16, or fp32 in parts (few tokens: as it is)
+  size_t gu, x, block;    // fp32: the projections, and operands in parts
+  size_t hdr, off, perm;  // fp32, few tokens: what the expert kernels expect of a permutation
   size_t total;
 };
 // Every section grows with T, so a workspace for T_max serves all smaller calls.
@@ -78,33 +79,44 @@ ForwardLayout forward_layout(const mcft_layer_desc* d, int T) {
   const bool f32 = d->dtype == MCFT_F32;
   ForwardLayout L{};
   Sections s;
-  L.h = s.add(t * w * elem(d->dtype));
+  L.h = s.add(t * w * (f32 ? 6 : 2));
+  size_t planes = dense_plane_bytes(t * D, d->w);
   if (f32) {
     L.hdr = s.add(sizeof(WsHeader));
     L.off = s.add(2 * sizeof(int));
     L.perm = s.add(t * sizeof(int));
     L.gu = s.add(t * 2 * w * 4);
+    L.x = s.add(t * D * 6);
+    L.block = s.add(3 * w * D * 6);
+    planes = std::max(planes, dense_plane_bytes(t * 2 * w, d->d));
   }
-  const size_t up = f32 ? dense_plane_bytes(1, t * 2 * w, d->d, d->dtype) : 0;
-  L.planes = s.add(std::max(up, dense_plane_bytes(1, t * D, d->w, d->dtype)));
+  L.planes = s.add(planes);
   L.total = s.total;
   return L;
 }
 
 struct GradLayout {
-  size_t x, h, dgu, gu, dh, planes, total;
+  size_t x8, x, dy, block;  // x8: its values; fp32: operands in parts
+  size_t gu, dh, h, dgu, planes, total;
 };
 GradLayout grad_layout(const mcft_layer_desc* d, int T) {
-  const size_t t = size_t(T), w = size_t(d->w), D = size_t(d->d), e = elem(d->dtype);
+  const size_t t = size_t(T), w = size_t(d->w), D = size_t(d->d);
+  const bool f32 = d->dtype == MCFT_F32;
   GradLayout L{};
   Sections s;
-  L.x = s.add(t * D * e);
-  L.h = s.add(t * w * e);
-  L.dgu = s.add(t * 2 * w * e);
+  L.x8 = s.add(t * D * elem(d->dtype));
+  L.h = s.add(t * w * (f32 ? 6 : 2));
+  L.dgu = s.add(t * 2 * w * (f32 ? 6 : 2));
   L.gu = s.add(t * 2 * w * 4);
-  if (d->dtype == MCFT_F32) L.dh = s.add(t * w * 4);
-  L.planes = s.add(std::max(dense_plane_bytes(3, t * D + 3 * w * D, std::max(T, 2 * d->w), d->dtype),
-                            d->dtype == MCFT_F32 ? dense_plane_bytes(1, t * 2 * w, d->d, d->dtype) : size_t(0)));
+  size_t planes = dense_plane_bytes(t * D + 3 * w * D, std::max(T, 2 * d->w));
+  if (f32) {
+    L.dh = s.add(t * w * 4);
+    L.x = s.add(t * D * 6);
+    L.dy = s.add(t * D * 6);
+    L.block = s.add(3 * w * D * 6);
+    planes = std::max(planes, dense_plane_bytes(t * 2 * w, d->d));
+  }
+  L.planes = s.add(planes);
   L.total = s.total;
   return L;
 }
@@ -263,19 +275,26 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   const char* w13 = static_cast<const char*>(block);
   const char* w2 = w13 + size_t(2) * desc->w * desc->d * elem(desc->dtype);
   float* planes = reinterpret_cast<float*>(ws + L.planes);
+  const int d = desc->d, w = desc->w;
+  const size_t wd = size_t(w) * d;
   if (desc->dtype == MCFT_BF16) {
-    e = launch_dense_up(DenseUpArgs{x, w13, T, desc->d, desc->w, ws + L.h, nullptr, static_cast<uint8_t*>(ckpt)}, stream);
+    e = launch_dense_up(DenseUpArgs{x, w13, T, d, w, ws + L.h, nullptr, static_cast<uint8_t*>(ckpt)}, stream);
+    if (e == cudaSuccess) {
+      const DenseProduct down{ws + L.h, w2, T, d, w, 0, 1, y, MCFT_BF16, 0, 0, 0};
+      e = launch_dense_products(&down, 1, planes, stream);
+    }
   } else {
     float* gu = reinterpret_cast<float*>(ws + L.gu);
-    const DenseProduct up{x, w13, T, 2 * desc->w, desc->d, 0, 1, gu, MCFT_F32, 0};
-    e = launch_dense_products(&up, 1, MCFT_F32, planes, stream);
+    uint16_t *x3 = reinterpret_cast<uint16_t*>(ws + L.x), *block3 = reinterpret_cast<uint16_t*>(ws + L.block),
+             *h3 = reinterpret_cast<uint16_t*>(ws + L.h);
+    const size_t nx = size_t(T) * d;
+    e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(x), static_cast<const float*>(block)}, {x3, block3}, {nx, 3 * wd}}, stream);
+    const DenseProduct up{x3, block3, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0, nx, 3 * wd};
+    if (e == cudaSuccess) e = launch_dense_split_products(&up, 1, planes, stream);
     if (e == cudaSuccess)
-      e = launch_dense_act(DenseActArgs{gu, static_cast<uint8_t*>(ckpt), nullptr, reinterpret_cast<float*>(ws + L.h),
-                                        nullptr, T, desc->w}, stream);
-  }
-  if (e == cudaSuccess) {
-    const DenseProduct down{ws + L.h, w2, T, desc->d, desc->w, 0, 1, y, desc->dtype, 0};
-    e = launch_dense_products(&down, 1, desc->dtype, planes, stream);
+      e = launch_dense_act(DenseActArgs{gu, static_cast<uint8_t*>(ckpt), nullptr, h3, nullptr, T, w}, stream);
+    const DenseProduct down{h3, block3 + 2 * wd, T, d, w, 0, 1, y, MCFT_F32, 0, size_t(T) * w, 3 * wd};
+    if (e == cudaSuccess) e = launch_dense_split_products(&down, 1, planes, stream);
   }
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
 }
@@ -324,38 +343,55 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   float* gu = ckpt ? nullptr : reinterpret_cast<float*>(ws + L.gu);
   cudaError_t e = cudaSuccess;
   if (want_x && x8) {
-    e = launch_mx8_quant(Mx8Args{ws + L.x, const_cast<void*>(x8), T, d, d}, desc->dtype, true, stream);
-    x = ws + L.x;
+    e = launch_mx8_quant(Mx8Args{ws + L.x8, const_cast<void*>(x8), T, d, d}, desc->dtype, true, stream);
+    x = ws + L.x8;
   }
+  // the last products' operands: bf16, or fp32 in parts
+  const void *dgu = ws + L.dgu, *h = ws + L.h, *xs = x, *dys = dy, *w13s = w13;
+  size_t part_gu = 0, part_h = 0, part_x = 0, part_w = 0;
+  auto* products = launch_dense_products;
   if (desc->dtype == MCFT_BF16) {
     if (e == cudaSuccess && gu) e = launch_dense_up(DenseUpArgs{x, w13, T, d, w, nullptr, gu, nullptr}, stream);
     if (e == cudaSuccess)
       e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), gu, ws + L.h, ws + L.dgu}, stream);
   } else {
+    products = launch_dense_split_products;
+    uint16_t *x3 = reinterpret_cast<uint16_t*>(ws + L.x), *dy3 = reinterpret_cast<uint16_t*>(ws + L.dy),
+             *block3 = reinterpret_cast<uint16_t*>(ws + L.block);
+    part_gu = size_t(T) * 2 * w;
+    part_h = size_t(T) * w;
+    part_x = size_t(T) * d;
+    part_w = 3 * wd;
+    if (e == cudaSuccess)
+      e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(dy), static_cast<const float*>(block), static_cast<const float*>(x)},
+                                            {dy3, block3, x3}, {part_x, part_w, want_x ? part_x : 0}}, stream);
+    xs = x3;
+    dys = dy3;
+    w13s = block3;
     if (e == cudaSuccess && gu) {
-      const DenseProduct up{x, w13, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0};
-      e = launch_dense_products(&up, 1, MCFT_F32, planes, stream);
+      const DenseProduct up{xs, w13s, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0, part_x, part_w};
+      e = products(&up, 1, planes, stream);
     }
     float* dh = reinterpret_cast<float*>(ws + L.dh);
     if (e == cudaSuccess) {
-      const DenseProduct back{dy, w2, T, w, d, 0, 0, dh, MCFT_F32, 0};
-      e = launch_dense_products(&back, 1, MCFT_F32, planes, stream);
+      const DenseProduct back{dys, block3 + 2 * wd, T, w, d, 0, 0, dh, MCFT_F32, 0, part_x, part_w};
+      e = products(&back, 1, planes, stream);
     }
     if (e == cudaSuccess)
-      e = launch_dense_act_grad(DenseActArgs{gu, static_cast<const uint8_t*>(ckpt), dh, reinterpret_cast<float*>(ws + L.h),
-                                             reinterpret_cast<float*>(ws + L.dgu), T, w}, stream);
+      e = launch_dense_act_grad(DenseActArgs{gu, static_cast<const uint8_t*>(ckpt), dh, reinterpret_cast<uint16_t*>(ws + L.h),
+                                             reinterpret_cast<uint16_t*>(ws + L.dgu), T, w}, stream);
   }
   if (e == cudaSuccess) {
     DenseProduct p[kMaxProducts];
     int n = 0;
     if (dblock) {
       char* out = static_cast<char*>(dblock);
-      p[n++] = DenseProduct{ws + L.dgu, x, 2 * w, d, T, 1, 0, out, grad_dtype, accumulate};
-      p[n++] = DenseProduct{dy, ws + L.h, d, w, T, 1, 0, out + 2 * wd * elem(grad_dtype), grad_dtype, accumulate};
+      p[n++] = DenseProduct{dgu, xs, 2 * w, d, T, 1, 0, out, grad_dtype, accumulate, part_gu, part_x};
+      p[n++] = DenseProduct{dys, h, d, w, T, 1, 0, out + 2 * wd * elem(grad_dtype), grad_dtype, accumulate, part_x, part_h};
     }
-    if (dx) p[n++] = DenseProduct{ws + L.dgu, w13, T, d, 2 * w, 0, 0, dx, desc->dtype, 0};
+    if (dx) p[n++] = DenseProduct{dgu, w13s, T, d, 2 * w, 0, 0, dx, desc->dtype, 0, part_gu, part_w};
     for (int i = n - 1; i > 0 && p[i].k > p[i - 1].k; --i) std::swap(p[i], p[i - 1]);  // the longest contraction first
-    e = launch_dense_products(p, n, desc->dtype, planes, stream);
+    e = products(p, n, planes, stream);
   }
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward gradient launch");
 }

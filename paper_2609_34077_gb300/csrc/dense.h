@@ -46,22 +46,32 @@ cudaError_t launch_norm_grad(const NormGradArgs& a, int dtype, cudaStream_t s);
 
 // ---- products ----
 
-// One product C = A B of a launch: rows of C are A's, columns B's, summed over `k`. Operands are row-major matrices of the
-// layer dtype; `a_t`: A is given as [k, rows]; `b_t`: B is given as [columns, k] (else [k, columns]).
+// One product C = A B of a launch: rows of C are A's, columns B's, summed over `k`. Operands are row-major matrices;
+// `a_t`: A is given as [k, rows]; `b_t`: B is given as [columns, k] (else [k, columns]). Elements are bf16, or fp32
+// split into three bf16 parts (launch_dense_split), a_part and b_part elements from part to part.
 struct DenseProduct {
   const void *a, *b;
   int rows, cols, k, a_t, b_t;
   void* out;       // [rows, cols] of out_dtype, row-major
   int out_dtype, accumulate;
+  size_t a_part, b_part;
 };
 constexpr int kMaxProducts = 3;
-constexpr int kDenseTile = 256;       // rows and columns of a bf16 tile
-constexpr int kDensePlaneTiles = 2;  // tiles' worth of split sums that a pair of SMs may leave in memory
 
-// Most bytes that the planes of a launch of `n` products take, whose outputs number `outs` in all and whose contractions
-// are at most `k` long: grows with each, so that it covers smaller calls too.
-size_t dense_plane_bytes(int n, size_t outs, int k, int dtype);
-cudaError_t launch_dense_products(const DenseProduct* p, int n, int dtype, float* planes, cudaStream_t s);
+// Most bytes that the planes of a launch's split products take, whose outputs number `outs` in all and whose contractions are at
+// most `k` long: grows with both, so that it covers smaller calls too.
+size_t dense_plane_bytes(size_t outs, int k);
+cudaError_t launch_dense_products(const DenseProduct* p, int n, float* planes, cudaStream_t s);         // bf16
+cudaError_t launch_dense_split_products(const DenseProduct* p, int n, float* planes, cudaStream_t s);   // fp32 in parts
+
+// fp32 values as three bf16 ones, each the rounding of what the ones before leave (24 bits, but for the last of very small
+// values): parts [3][n], for up to three arrays.
+struct DenseSplitArgs {
+  const float* x[3];
+  uint16_t* parts[3];
+  size_t n[3];
+};
+cudaError_t launch_dense_split(const DenseSplitArgs& a, cudaStream_t s);
 
 // Sum of `n` fp32 planes [count] into out.
 cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* out, int out_dtype, int accumulate,
@@ -92,7 +102,7 @@ struct DenseActArgs {
   const float* gu;      // [T, 2w], or NULL and
   const uint8_t* ckpt;  // mx8 [T, 2w]: written by the forward (or NULL), read by the gradient
   const float* dh;      // [T, w]: the gradient
-  float *h, *dgu;       // [T, w]; [T, 2w]
+  uint16_t *h, *dgu;    // [T, w]; [T, 2w]: in three parts
   int T, w;
 };
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s);

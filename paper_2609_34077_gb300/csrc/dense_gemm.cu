@@ -10,7 +10,7 @@
 // K-major operand (a box of 64 x 128), another an MN-major one (two boxes of 64 x 64), so nothing is transposed.
 //   warp 0 (both CTAs) copies; the loads of both complete on the leader's full[s];
 //   warp 1 of the leader issues the MMAs; their commits arrive on empty[s] and tfull[b] of both CTAs;
-//   warps 2-9 (both CTAs) are the epilogue of the CTA's 128 rows, a row a lane: four lane quarters of TMEM by two halves of
+//   the other warps (both CTAs) are the epilogue of the CTA's 128 rows, a row a lane: four lane quarters of TMEM by shares of
 //   the columns, 32 columns (one mx8 block) at a time. Two accumulators of 256 columns let the next tile's MMAs run meanwhile.
 // A persistent grid strides over the tiles, rows fastest inside groups of row tiles that share L2. Tiles of problems that do
 // not fill the pairs are split along the contraction into fp32 planes, which dense_join_kernel adds up in order.
@@ -31,9 +31,7 @@ namespace mcft {
 namespace {
 
 constexpr int BK = 64;
-constexpr int kTile = kDenseTile;  // rows, and most columns
-constexpr int kThreads = 64 + 256;
-constexpr int kEpiWarps = 8;
+constexpr int kTile = 256;  // rows, and most columns
 constexpr int kABytes = 128 * BK * 2;  // a CTA's rows of A in a stage
 constexpr int kRingBytes = 7 * (kABytes + 128 * BK * 2);
 constexpr int kMaxStages = 16;
@@ -42,7 +40,14 @@ constexpr int kTmemCols = 2 * kTile;
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 4) << 24);
 constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
 
-enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_OUT = 2 };
+enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_OUT = 2, EPI_PARTS = 3 };  // EPI_PARTS: out, of operands in parts
+
+// Epilogue warps: four lane quarters of TMEM by so many shares of the columns (operands in parts: so that a thread's 64 sums fit
+// its registers).
+template <int EPI>
+constexpr int kShares = EPI == EPI_PARTS ? 4 : 2;
+template <int EPI>
+constexpr int kThreads = 64 + 128 * kShares<EPI>;
 
 struct Problem {
   CUtensorMap a, b, b1;  // b1: rank 1's columns of an up tile
@@ -95,6 +100,18 @@ __device__ __forceinline__ Item item_at(const Params& q, int item) {
   return t;
 }
 
+// Operands in three bf16 parts (h, m, l): six products whose sum is the fp32 one but for 2^-26 of it, in the order h l, l h, m m,
+// h m, m h, h h. The tensor cores cut an accumulator's last bits, always towards zero, at every step: that costs little while
+// it holds only the small products' sum, and an accumulator holds kRun steps of the contraction only, whose sums the
+// epilogue's threads add up in fp32 registers (512 tokens through 1024 x 1408: y 2.4e-6 off 64 bits with accumulators of whole
+// contractions).
+constexpr int kPasses = 6;
+constexpr int kRun = 4;
+__device__ __forceinline__ int part_of(bool b, int pass) {
+  constexpr uint32_t kA = 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8, kB = 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8;
+  return int(((b ? kB : kA) >> (2 * pass)) & 3u);
+}
+
 // Operand of a stage: K-major rows of 128 bytes, or two boxes of 64 contiguous rows by 64 of the contraction.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn) {
   const uint64_t lead = mn ? uint64_t((BK * 128) >> 4) : 1u;
@@ -102,13 +119,21 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn) {
          (uint64_t(2) << 61);
 }
 
-__device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap* map, bool mn, int rows, int k, int at,
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2,
+                                                 uint32_t bar_cluster) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar_cluster)
+      : "memory");
+}
+__device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap* map, bool mn, int rows, int k, int at, int part,
                                              uint32_t bar) {
   if (mn) {
-    tma_load_2d_pair(to, map, at, k, bar);
-    if (rows > 64) tma_load_2d_pair(to + 64 * BK * 2, map, at + 64, k, bar);
+    tma_load_3d_pair(to, map, at, k, part, bar);
+    if (rows > 64) tma_load_3d_pair(to + 64 * BK * 2, map, at + 64, k, part, bar);
   } else {
-    tma_load_2d_pair(to, map, k, at, bar);
+    tma_load_3d_pair(to, map, k, at, part, bar);
   }
 }
 
@@ -156,6 +181,46 @@ __device__ __forceinline__ void get_mx8(const uint8_t* code, uint32_t scale, flo
   for (int i = 0; i < 8; ++i) mx8_values(c[i], v + 4 * i);
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] *= unit;
+}
+
+// 32 columns of a row of C, or of its plane.
+__device__ __forceinline__ void put_out(const Item& t, int row, int col, uint32_t* v) {
+  const Problem& p = *t.p;
+  const bool in = row < p.M;
+  const size_t N = size_t(p.N), at = size_t(in ? row : 0) * N + col;
+  if (p.splits > 1 || p.out_f32) {
+    float* base = p.splits > 1 ? p.planes + size_t(t.split) * p.M * N : static_cast<float*>(p.out);
+    float* to = in ? base + at : nullptr;
+    if (p.accumulate && p.splits == 1 && in) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 o = reinterpret_cast<const float4*>(to)[i];
+        v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + o.x);
+        v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + o.y);
+        v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + o.z);
+        v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + o.w);
+      }
+    }
+    put64(to, v, p.wide);
+    put64(to ? to + 16 : nullptr, v + 16, p.wide);
+  } else {
+    uint16_t* to = in ? static_cast<uint16_t*>(p.out) + at : nullptr;
+    uint32_t o[16] = {};
+    if (p.accumulate && in) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(to)[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
+      if (p.accumulate) {
+        lo += bf16lo(o[i]);
+        hi += bf16hi(o[i]);
+      }
+      o[i] = pack2bf(lo, hi);
+    }
+    put64(to, o, p.wide);
+  }
 }
 
 template <int EPI>
@@ -235,7 +300,6 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
       put64(to ? to + w : nullptr, du, q.wide_dgu);
     }
   } else {
-    const size_t N = size_t(p.N);
 #pragma unroll 1
     for (int c = half * (q.cols / 2); c < (half + 1) * (q.cols / 2); c += 32) {
       const int col = t.nt * q.cols + c;
@@ -243,46 +307,13 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
       uint32_t v[32];
       tmem_ld32(taddr + c, v);
       tmem_ld_wait();
-      const size_t at = r * N + col;
-      if (p.splits > 1 || p.out_f32) {
-        float* base = p.splits > 1 ? p.planes + size_t(t.split) * p.M * N : static_cast<float*>(p.out);
-        float* to = in ? base + at : nullptr;
-        if (p.accumulate && p.splits == 1 && in) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float4 o = reinterpret_cast<const float4*>(to)[i];
-            v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + o.x);
-            v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + o.y);
-            v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + o.z);
-            v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + o.w);
-          }
-        }
-        put64(to, v, p.wide);
-        put64(to ? to + 16 : nullptr, v + 16, p.wide);
-      } else {
-        uint16_t* to = in ? static_cast<uint16_t*>(p.out) + at : nullptr;
-        uint32_t o[16] = {};
-        if (p.accumulate && in) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(to)[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
-          if (p.accumulate) {
-            lo += bf16lo(o[i]);
-            hi += bf16hi(o[i]);
-          }
-          o[i] = pack2bf(lo, hi);
-        }
-        put64(to, o, p.wide);
-      }
+      put_out(t, row, col, v);
     }
   }
 }
 
 template <int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
     dense_gemm_kernel(const __grid_constant__ Params q) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -299,7 +330,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&ctl->tfull[b], 1);
-      mbar_init(&ctl->tempty[b], 2 * kEpiWarps);
+      mbar_init(&ctl->tempty[b], 2 * 4 * kShares<EPI>);
     }
     mbar_init(&ctl->drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -334,13 +365,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int arow = t.mt * kTile + int(rank) * 128;
         const CUtensorMap* mb = EPI == EPI_UP && rank ? &t.p->b1 : &t.p->b;
         const int brow = EPI == EPI_UP ? t.nt * half_cols : t.nt * q.cols + int(rank) * half_cols;
-        const bool a_mn = EPI == EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_OUT && t.p->b_mn);
-        for (int kb = t.k0; kb < t.k1; ++kb) {
+        const bool a_mn = EPI >= EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI >= EPI_OUT && t.p->b_mn);
+        // operands in parts: all six products of kRun steps, then those of the next
+        int kb = t.k0, pass = 0, r0 = t.k0;
+        for (int left = (EPI == EPI_PARTS ? kPasses : 1) * (t.k1 - t.k0); left > 0; --left) {
           if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, q.err)) break;
+          const int pa = EPI == EPI_PARTS ? part_of(false, pass) : 0, pb = EPI == EPI_PARTS ? part_of(true, pass) : 0;
           const uint32_t sa = base + uint32_t(s * stage_bytes), fb = fb0 + uint32_t(s) * 8u;
           if (leader) mbar_expect_tx(&ctl->full[s], uint32_t(q.a_rows ? stage_bytes + b_bytes : 2 * stage_bytes));
-          if (leader || !q.a_rows) load_operand(sa, &t.p->a, a_mn, 128, kb * BK, arow, fb);
-          load_operand(sa + a_bytes, mb, b_mn, half_cols, kb * BK, brow, fb);
+          if (leader || !q.a_rows) load_operand(sa, &t.p->a, a_mn, 128, kb * BK, arow, pa, fb);
+          load_operand(sa + a_bytes, mb, b_mn, half_cols, kb * BK, brow, pb, fb);
+          ++kb;
+          if (EPI == EPI_PARTS && kb == min(r0 + kRun, t.k1)) {
+            if (++pass == kPasses) {
+              pass = 0;
+              r0 = kb;
+            }
+            kb = r0;
+          }
           if (issued < stages) ++issued;
           if (++s == stages) {
             s = 0;
@@ -362,35 +404,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       uint32_t ph = 0, lt = 0;
       for (int item = cid; item < items && !*abort; item += ncl) {
         const Item t = item_at(q, item);
-        const bool a_mn = EPI == EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_OUT && t.p->b_mn);
+        const bool a_mn = EPI >= EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI >= EPI_OUT && t.p->b_mn);
         const uint32_t idesc = kIdesc | (uint32_t(q.cols >> 3) << 17) | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
         // 16 of the contraction: 32 bytes of each K-major row, or 16 rows of 128 bytes
         const uint64_t ka = a_mn ? (16 * 128) >> 4 : 32 >> 4, kb_ = b_mn ? (16 * 128) >> 4 : 32 >> 4;
-        const uint32_t b = lt & 1u;
-        if (!mbar_wait_cl(&ctl->tempty[b], ((lt >> 1) & 1u) ^ 1u, abort, q.err)) break;
-        tc_fence_after();
-        const uint32_t dt = tmem + b * kTile;
         bool ok = true;
-        for (int kb = t.k0; kb < t.k1; ++kb) {
-          if (!mbar_wait_cl(&ctl->full[s], ph, abort, q.err)) {
+        // an accumulator's steps: all of the item's, or the products of a run of them
+        for (int k0 = t.k0; k0 < t.k1 && ok; k0 = EPI == EPI_PARTS ? k0 + kRun : t.k1) {
+          const int n = EPI == EPI_PARTS ? kPasses * min(kRun, t.k1 - k0) : t.k1 - k0;
+          const uint32_t b = lt & 1u;
+          if (!mbar_wait_cl(&ctl->tempty[b], ((lt >> 1) & 1u) ^ 1u, abort, q.err)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t sa = base + uint32_t(s * stage_bytes);
-          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + a_bytes, b_mn);
+          const uint32_t dt = tmem + b * kTile;
+          for (int i = 0; i < n; ++i) {
+            if (!mbar_wait_cl(&ctl->full[s], ph, abort, q.err)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sa = base + uint32_t(s * stage_bytes);
+            const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + a_bytes, b_mn);
 #pragma unroll
-          for (int k = 0; k < BK / 16; ++k)
-            tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (kb != t.k0 || k != 0) ? 1u : 0u);
-          tc_commit_pair_both(&ctl->empty[s]);
-          if (++s == stages) {
-            s = 0;
-            ph ^= 1u;
+            for (int k = 0; k < BK / 16; ++k)
+              tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (i != 0 || k != 0) ? 1u : 0u);
+            tc_commit_pair_both(&ctl->empty[s]);
+            if (++s == stages) {
+              s = 0;
+              ph ^= 1u;
+            }
           }
+          if (!ok) break;
+          tc_commit_pair_both(&ctl->tfull[b]);
+          ++lt;
         }
         if (!ok) break;
-        tc_commit_pair_both(&ctl->tfull[b]);
-        ++lt;
       }
       tc_commit_pair(&ctl->drain);  // arrives once every MMA issued above has completed
       mbar_wait_drain_cl(&ctl->drain, 0, q.err);
@@ -400,18 +450,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     uint32_t lt = 0;
     for (int item = cid; item < items; item += ncl) {
       const Item t = item_at(q, item);
-      const uint32_t b = lt & 1u;
-      int ok = 1;
-      if (lane == 0) ok = mbar_wait_cl(&ctl->tfull[b], (lt >> 1) & 1u, abort, q.err) ? 1 : 0;
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) break;
-      tc_fence_after();
-      epilogue<EPI>(q, t, tmem + b * kTile + (uint32_t(quarter * 32) << 16),
-                    t.mt * kTile + int(rank) * 128 + quarter * 32 + lane, half);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_relaxed(peer_addr(&ctl->tempty[b], 0));
-      ++lt;
+      const int row = t.mt * kTile + int(rank) * 128 + quarter * 32 + lane;
+      auto begin = [&](uint32_t& taddr) {
+        const uint32_t b = lt & 1u;
+        int ok = 1;
+        if (lane == 0) ok = mbar_wait_cl(&ctl->tfull[b], (lt >> 1) & 1u, abort, q.err) ? 1 : 0;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        tc_fence_after();
+        taddr = tmem + b * kTile + (uint32_t(quarter * 32) << 16);
+        return ok != 0;
+      };
+      auto end = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_relaxed(peer_addr(&ctl->tempty[lt & 1u], 0));
+        ++lt;
+      };
+      uint32_t taddr;
+      if constexpr (EPI == EPI_PARTS) {
+        const int share = q.cols / kShares<EPI>, c0 = half * share;  // 64 or 32 columns
+        float sum[2][32];
+        bool ok = true;
+        for (int k0 = t.k0; k0 < t.k1 && ok; k0 += kRun) {
+          ok = begin(taddr);
+          if (!ok) break;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (c * 16 >= share) continue;
+            uint32_t v[16];
+            tmem_ld16(taddr + c0 + c * 16, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float& to = sum[c / 2][c % 2 * 16 + i];
+              to = k0 == t.k0 ? __uint_as_float(v[i]) : to + __uint_as_float(v[i]);
+            }
+          }
+          end();
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int col = t.nt * q.cols + c0 + c * 32;
+          if (c * 32 >= share || col >= t.p->N) continue;
+          put_out(t, row, col, reinterpret_cast<uint32_t*>(sum[c]));
+        }
+      } else {
+        if (!begin(taddr)) break;
+        epilogue<EPI>(q, t, taddr, row, half);
+        end();
+      }
     }
   }
 
@@ -423,15 +511,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-// bf16 matrix [rows, cols] row-major; a box of 64 columns (128 bytes, one swizzle span) and box_rows rows.
-bool encode(CUtensorMap* m, const void* base, size_t cols, size_t rows, int box_rows) {
+// bf16 matrix [rows, cols] row-major, in one part or three (`part` elements apart); a box of 64 columns (128 bytes, one swizzle
+// span) and box_rows rows.
+bool encode(CUtensorMap* m, const void* base, size_t cols, size_t rows, int box_rows, size_t part = 0) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
-  const cuuint64_t dims[2] = {cols, rows};
-  const cuuint64_t strides[1] = {cols * 2};
-  const cuuint32_t box[2] = {BK, cuuint32_t(box_rows)};
-  const cuuint32_t es[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+  const cuuint64_t dims[3] = {cols, rows, part ? 3u : 1u};
+  const cuuint64_t strides[2] = {cols * 2, part ? part * 2 : cols * rows * 2};
+  const cuuint32_t box[3] = {BK, cuuint32_t(box_rows), 1};
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -460,17 +549,18 @@ struct Plan {
 struct Sizes {
   int M, N, kblocks;
 };
+constexpr size_t kPlaneTiles = 2;  // tiles' worth of split sums that a pair may leave in memory
 constexpr int kLeastPart = 4;  // steps: below that an item is mostly its fill and its stores
 constexpr double kJoin = 10;   // a launch more, beside the planes' bytes
 
-double plan_time(const Sizes* z, int n, int up, int cols, const int* per, int pairs) {
+double plan_time(const Sizes* z, int n, int up, int passes, int cols, const int* per, int pairs) {
   const double step = cols == kTile ? 1.0 : 0.56, epilogue = (cols == kTile ? 4.0 : 2.0) * (up ? 1.5 : 1.0), fill = 5.0;
   double total = 0, longest = 0, planes = 0;
   long long items = 0;
   for (int i = 0; i < n; ++i) {
     const long long tiles = (long long)((z[i].M + kTile - 1) / kTile) * ((z[i].N * (up ? 2 : 1) + cols - 1) / cols);
     const int splits = (z[i].kblocks + per[i] - 1) / per[i];
-    const double one = std::max(per[i] * step, epilogue);
+    const double one = std::max(passes * per[i] * step, epilogue);
     total += one * tiles * splits;
     longest = std::max(longest, one);
     items += tiles * splits;
@@ -483,7 +573,7 @@ double plan_time(const Sizes* z, int n, int up, int cols, const int* per, int pa
 }
 
 // Tile width, and (splittable) parts of the contractions, by the least time.
-Plan choose(const Sizes* z, int n, int up, bool splittable, int pairs) {
+Plan choose(const Sizes* z, int n, int up, bool splittable, int passes, int pairs) {
   Plan best{};
   int longest = 1;
   for (int i = 0; i < n; ++i) longest = std::max(longest, z[i].kblocks);
@@ -499,8 +589,8 @@ Plan choose(const Sizes* z, int n, int up, bool splittable, int pairs) {
         const int made = (z[i].kblocks + p.per[i] - 1) / p.per[i];
         if (made > 1) planes += size_t(made) * z[i].M * z[i].N;
       }
-      if (planes > size_t(pairs) * kDensePlaneTiles * kTile * kTile) break;
-      p.time = plan_time(z, n, up, cols, p.per, pairs);
+      if (parts > 1 && planes > size_t(pairs) * kPlaneTiles * kTile * kTile) break;
+      p.time = plan_time(z, n, up, passes, cols, p.per, pairs);
       if (best.cols == 0 || p.time < best.time) best = p;
     }
   }
@@ -516,7 +606,7 @@ int pairs_at_once() {
   static ResidentClusters resident;
   const void* fn = reinterpret_cast<const void*>(dense_gemm_kernel<EPI>);
   if (smem.allow(fn, kSmem) != cudaSuccess) return 0;
-  return resident.get(fn, num_sms() & ~1, kThreads, kSmem);
+  return resident.get(fn, num_sms() & ~1, kThreads<EPI>, kSmem);
 }
 
 template <int EPI>
@@ -530,7 +620,7 @@ cudaError_t launch(Params& q, int kid, cudaStream_t s) {
   const int pairs = pairs_at_once<EPI>();
   if (pairs < 1) return cudaErrorInvalidConfiguration;
   prof_begin(kid, s);
-  const cudaError_t e = launch_pdl(dense_gemm_kernel<EPI>, dim3(unsigned(2 * std::min(pairs, q.items))), dim3(kThreads), kSmem, s, q);
+  const cudaError_t e = launch_pdl(dense_gemm_kernel<EPI>, dim3(unsigned(2 * std::min(pairs, q.items))), dim3(kThreads<EPI>), kSmem, s, q);
   prof_end(kid, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -543,7 +633,7 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
   q.n = 1;
   Problem& p = q.p[0];
   const Sizes z{a.T, a.w, (a.d + BK - 1) / BK};
-  q.cols = choose(&z, 1, 1, false, num_sms() / 2).cols;
+  q.cols = choose(&z, 1, 1, false, 1, num_sms() / 2).cols;
   shape(p, a.T, a.w, a.d, q.cols / 2);
   const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
   q.a_rows = few_rows(a.T);
@@ -565,7 +655,7 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   q.n = 1;
   Problem& p = q.p[0];
   const Sizes z{a.T, a.w, (a.d + BK - 1) / BK};
-  q.cols = choose(&z, 1, 0, false, num_sms() / 2).cols;
+  q.cols = choose(&z, 1, 0, false, 1, num_sms() / 2).cols;
   shape(p, a.T, a.w, a.d, q.cols);
   p.b_mn = 1;
   q.a_rows = few_rows(a.T);
@@ -581,13 +671,15 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
 }
 
-cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaStream_t s) {
+namespace {
+
+cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes, cudaStream_t s) {
   Params q;
   memset(&q, 0, sizeof(q));
   q.n = n;
   Sizes z[kMaxProducts];
   for (int i = 0; i < n; ++i) z[i] = Sizes{in[i].rows, in[i].cols, (in[i].k + BK - 1) / BK};
-  const Plan plan = choose(z, n, 0, true, num_sms() / 2);
+  const Plan plan = choose(z, n, 0, true, passes, num_sms() / 2);
   q.cols = plan.cols;
   size_t used = 0;
   for (int i = 0; i < n; ++i) {
@@ -603,8 +695,9 @@ cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaSt
     p.a_mn = d.a_t;
     p.b_mn = !d.b_t;
     const size_t M = size_t(d.rows), N = size_t(d.cols), K = size_t(d.k);
-    if (!(d.a_t ? encode(&p.a, d.a, M, K, 64) : encode(&p.a, d.a, K, M, q.a_rows ? q.a_rows : 128)) ||
-        !(d.b_t ? encode(&p.b, d.b, K, N, plan.cols / 2) : encode(&p.b, d.b, N, K, 64)))
+    const size_t pa = passes > 1 ? d.a_part : 0, pb = passes > 1 ? d.b_part : 0;
+    if (!(d.a_t ? encode(&p.a, d.a, M, K, 64, pa) : encode(&p.a, d.a, K, M, q.a_rows ? q.a_rows : 128, pa)) ||
+        !(d.b_t ? encode(&p.b, d.b, K, N, plan.cols / 2, pb) : encode(&p.b, d.b, N, K, 64, pb)))
       return cudaErrorInvalidValue;
     p.out = d.out;
     p.planes = planes + used;
@@ -613,12 +706,26 @@ cudaError_t launch_dense_tc(const DenseProduct* in, int n, float* planes, cudaSt
     p.accumulate = d.accumulate;
     p.wide = p.splits > 1 ? wide(planes) : wide(d.out);
   }
-  cudaError_t e = launch<EPI_OUT>(q, kProfDenseOut, s);
+  cudaError_t e = passes > 1 ? launch<EPI_PARTS>(q, kProfDenseOut, s) : launch<EPI_OUT>(q, kProfDenseOut, s);
   for (int i = 0; i < n && e == cudaSuccess; ++i)
     if (q.p[i].splits > 1)
       e = launch_dense_join(q.p[i].planes, q.p[i].splits, size_t(in[i].rows) * in[i].cols, in[i].out, in[i].out_dtype,
                             in[i].accumulate, s);
   return e;
+}
+
+}  // namespace
+
+size_t dense_plane_bytes(size_t outs, int k) {
+  const size_t items = size_t(num_sms()) / 2 * kPlaneTiles * kTile * kTile, parts = size_t(k) / (kLeastPart * BK) + 2;
+  return std::min(items, parts * outs) * sizeof(float);
+}
+
+cudaError_t launch_dense_products(const DenseProduct* p, int n, float* planes, cudaStream_t s) {
+  return launch_out(p, n, 1, planes, s);
+}
+cudaError_t launch_dense_split_products(const DenseProduct* p, int n, float* planes, cudaStream_t s) {
+  return launch_out(p, n, kPasses, planes, s);
 }
 
 }  // namespace mcft
