@@ -107,7 +107,7 @@ GradLayout grad_layout(const mcft_layer_desc* d, int T) {
   L.x8 = s.add(t * D * elem(d->dtype));
   L.h = s.add(t * w * (f32 ? 6 : 2));
   L.dgu = s.add(t * 2 * w * (f32 ? 6 : 2));
-  L.gu = s.add(t * 2 * w * 4);
+  if (f32) L.gu = s.add(t * 2 * w * 4);
   size_t planes = dense_plane_bytes(t * D + 3 * w * D, std::max(T, 2 * d->w));
   if (f32) {
     L.dh = s.add(t * w * 4);
@@ -278,7 +278,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   const int d = desc->d, w = desc->w;
   const size_t wd = size_t(w) * d;
   if (desc->dtype == MCFT_BF16) {
-    e = launch_dense_up(DenseUpArgs{x, w13, T, d, w, ws + L.h, nullptr, static_cast<uint8_t*>(ckpt)}, stream);
+    e = launch_dense_up(DenseUpArgs{x, w13, T, d, w, ws + L.h, static_cast<uint8_t*>(ckpt)}, stream);
     if (e == cudaSuccess) {
       const DenseProduct down{ws + L.h, w2, T, d, w, 0, 1, y, MCFT_BF16, 0, 0, 0};
       e = launch_dense_products(&down, 1, planes, stream);
@@ -340,7 +340,7 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   const char* w13 = static_cast<const char*>(block);
   const char* w2 = w13 + 2 * wd * eb;
   float* planes = reinterpret_cast<float*>(ws + L.planes);
-  float* gu = ckpt ? nullptr : reinterpret_cast<float*>(ws + L.gu);
+  float* gu = ckpt || desc->dtype == MCFT_BF16 ? nullptr : reinterpret_cast<float*>(ws + L.gu);
   cudaError_t e = cudaSuccess;
   if (want_x && x8) {
     e = launch_mx8_quant(Mx8Args{ws + L.x8, const_cast<void*>(x8), T, d, d}, desc->dtype, true, stream);
@@ -351,9 +351,8 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   size_t part_gu = 0, part_h = 0, part_x = 0, part_w = 0;
   auto* products = launch_dense_products;
   if (desc->dtype == MCFT_BF16) {
-    if (e == cudaSuccess && gu) e = launch_dense_up(DenseUpArgs{x, w13, T, d, w, nullptr, gu, nullptr}, stream);
     if (e == cudaSuccess)
-      e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), gu, ws + L.h, ws + L.dgu}, stream);
+      e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), x, w13, ws + L.h, ws + L.dgu}, stream);
   } else {
     products = launch_dense_split_products;
     uint16_t *x3 = reinterpret_cast<uint16_t*>(ws + L.x), *dy3 = reinterpret_cast<uint16_t*>(ws + L.dy),

@@ -77,22 +77,21 @@ cudaError_t launch_dense_split(const DenseSplitArgs& a, cudaStream_t s);
 cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* out, int out_dtype, int accumulate,
                               cudaStream_t s);
 
-// Gate and up projections of [W1 ; W3] and what follows them, bf16: h = silu(g) u, or g and u in fp32 ([T, 2w], g first).
+// Gate and up projections of [W1 ; W3] and what follows them, bf16: h = silu(g) u [T, w].
 struct DenseUpArgs {
   const void *x, *w13;
   int T, d, w;
-  void* h;         // [T, w] bf16, or NULL and
-  float* gu;       // [T, 2w] fp32
-  uint8_t* ckpt;   // mx8 [T, 2w] of g and u, or NULL
+  void* h;
+  uint8_t* ckpt;  // mx8 [T, 2w] of g and u, or NULL
 };
 cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s);
 
-// dh = dy W2 and what follows it, bf16: dg | du [T, 2w] and h [T, w], from mx8 or fp32 g and u.
+// dh = dy W2 and what follows it, bf16: dg | du [T, 2w] and h [T, w], from the checkpoint of g and u, or (NULL) from x.
 struct DenseUpGradArgs {
   const void *dy, *w2;
   int T, d, w;
   const uint8_t* ckpt;
-  const float* gu;
+  const void *x, *w13;
   void *h, *dgu;
 };
 cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s);

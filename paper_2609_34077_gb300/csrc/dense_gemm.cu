@@ -2,6 +2,7 @@
 // accumulators), with what follows each in its epilogue:
 //   up       g = x W1^T, u = x W3^T;                h = silu(g) u, and mx8 checkpoints of g and u
 //   up_grad  dh = dy W2;                            dg, du, h from dh and the checkpoints
+//   both     g, u and dh of a tile one after the other, dg, du and h from them: the gradient without checkpoints
 //   out      C = A B of up to three problems: y = h W2^T, or dx = [dg | du] [W1 ; W3], d[W1 ; W3] = [dg | du]^T x and
 //            dW2 = dy^T h in one launch, whose tiles fill the SMs together.
 // A tile is 256 rows x 256 or 128 columns (up: half of them of g, the same ones of u), one MMA of M = 256 a step, issued by the
@@ -40,7 +41,8 @@ constexpr int kTmemCols = 2 * kTile;
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 4) << 24);
 constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
 
-enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_OUT = 2, EPI_PARTS = 3 };  // EPI_PARTS: out, of operands in parts
+// EPI_BOTH: up and up_grad in one, from x; EPI_PARTS: out, of operands in parts
+enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_BOTH = 2, EPI_OUT = 3, EPI_PARTS = 4 };
 
 // Epilogue warps: four lane quarters of TMEM by so many shares of the columns (operands in parts: so that a thread's 64 sums fit
 // its registers).
@@ -65,7 +67,6 @@ struct Params {
   unsigned* err;
   // up, up_grad
   uint8_t* ckpt;
-  float* gu;
   uint16_t *h, *dgu;
   int w, wide_h, wide_dgu, wide_ckpt;
 };
@@ -106,7 +107,7 @@ __device__ __forceinline__ Item item_at(const Params& q, int item) {
 // epilogue's threads add up in fp32 registers (512 tokens through 1024 x 1408: y 2.4e-6 off 64 bits with accumulators of whole
 // contractions).
 constexpr int kPasses = 6;
-constexpr int kRun = 4;
+constexpr int kRun = 3;
 __device__ __forceinline__ int part_of(bool b, int pass) {
   constexpr uint32_t kA = 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8, kB = 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8;
   return int(((b ? kB : kA) >> (2 * pass)) & 3u);
@@ -173,14 +174,42 @@ __device__ __forceinline__ void put_mx8(uint8_t* code, uint8_t* scale, const uin
   *scale = uint8_t(s);
 }
 
-__device__ __forceinline__ void get_mx8(const uint8_t* code, uint32_t scale, float* v) {
-  const uint4 a = ldg16(code), b = ldg16(code + 16);
-  const uint32_t c[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  const float unit = mx8_unit(scale);
+// A row's block of the checkpoint, as it lies in memory.
+struct RawBlock {
+  uint4 a, b;
+  uint32_t scale;
+  __device__ __forceinline__ void load(const uint8_t* code, const uint8_t* s) {
+    a = ldg16(code);
+    b = ldg16(code + 16);
+    scale = __ldg(s);
+  }
+  __device__ __forceinline__ void values(float* v) const {
+    const uint32_t c[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const float unit = mx8_unit(scale);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) mx8_values(c[i], v + 4 * i);
+    for (int i = 0; i < 8; ++i) mx8_values(c[i], v + 4 * i);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] *= unit;
+    for (int i = 0; i < 32; ++i) v[i] *= unit;
+  }
+};
+
+// 32 columns of a row: h, dg and du from g, u and dh.
+__device__ __forceinline__ void put_grads(const Params& q, bool in, size_t r, int col, const float* g, const float* u,
+                                          const uint32_t* dh) {
+  const size_t w = size_t(q.w);
+  uint32_t h[16], dg[16], du[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const SwigluGrad lo(g[2 * i], u[2 * i], __uint_as_float(dh[2 * i]));
+    const SwigluGrad hi(g[2 * i + 1], u[2 * i + 1], __uint_as_float(dh[2 * i + 1]));
+    h[i] = pack2bf(lo.h, hi.h);
+    dg[i] = pack2bf(lo.dg, hi.dg);
+    du[i] = pack2bf(lo.du, hi.du);
+  }
+  put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
+  uint16_t* to = in ? q.dgu + r * 2 * w + col : nullptr;
+  put64(to, dg, q.wide_dgu);
+  put64(to ? to + w : nullptr, du, q.wide_dgu);
 }
 
 // 32 columns of a row of C, or of its plane.
@@ -238,15 +267,6 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
       tmem_ld32(taddr + c, g);
       tmem_ld32(taddr + q.cols / 2 + c, u);
       tmem_ld_wait();
-      if (q.gu) {
-        float* to = in ? q.gu + r * 2 * w + col : nullptr;
-        put64(to, g, 1);
-        put64(to ? to + 16 : nullptr, g + 16, 1);
-        to = to ? to + w : nullptr;
-        put64(to, u, 1);
-        put64(to ? to + 16 : nullptr, u + 16, 1);
-        continue;
-      }
       if (q.ckpt && in) {
         uint8_t* code = q.ckpt + r * 2 * w + col;
         uint8_t* scale = q.ckpt + scales + r * 2 * nb + col / 32;
@@ -260,44 +280,17 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
                        swiglu(__uint_as_float(g[2 * i + 1]), __uint_as_float(u[2 * i + 1])));
       put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
     }
-  } else if constexpr (EPI == EPI_UP_GRAD) {
-    const size_t w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
+  } else if constexpr (EPI == EPI_BOTH) {
 #pragma unroll 1
-    for (int c = half * (q.cols / 2); c < (half + 1) * (q.cols / 2); c += 32) {
-      const int col = t.nt * q.cols + c;
+    for (int c = half * (q.cols / 4); c < (half + 1) * (q.cols / 4); c += 32) {
+      const int col = t.nt * (q.cols / 2) + c;
       if (col >= q.w) break;
-      float g[32], u[32];
-      if (q.ckpt) {
-        const uint8_t* code = q.ckpt + r * 2 * w + col;
-        const uint8_t* scale = q.ckpt + scales + r * 2 * nb + col / 32;
-        get_mx8(code, __ldg(scale), g);
-        get_mx8(code + w, __ldg(scale + nb), u);
-      } else {
-        const float4* from = reinterpret_cast<const float4*>(q.gu + r * 2 * w + col);
-        const float4* more = reinterpret_cast<const float4*>(q.gu + r * 2 * w + w + col);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float4 a = __ldg(from + i), b = __ldg(more + i);
-          g[4 * i] = a.x; g[4 * i + 1] = a.y; g[4 * i + 2] = a.z; g[4 * i + 3] = a.w;
-          u[4 * i] = b.x; u[4 * i + 1] = b.y; u[4 * i + 2] = b.z; u[4 * i + 3] = b.w;
-        }
-      }
-      uint32_t dh[32];
-      tmem_ld32(taddr + c, dh);
+      uint32_t g[32], u[32], dh[32];
+      tmem_ld32(taddr + c, g);
+      tmem_ld32(taddr + q.cols / 2 + c, u);
+      tmem_ld32(taddr + q.cols + c, dh);
       tmem_ld_wait();
-      uint32_t h[16], dg[16], du[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const SwigluGrad lo(g[2 * i], u[2 * i], __uint_as_float(dh[2 * i]));
-        const SwigluGrad hi(g[2 * i + 1], u[2 * i + 1], __uint_as_float(dh[2 * i + 1]));
-        h[i] = pack2bf(lo.h, hi.h);
-        dg[i] = pack2bf(lo.dg, hi.dg);
-        du[i] = pack2bf(lo.du, hi.du);
-      }
-      put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
-      uint16_t* to = in ? q.dgu + r * 2 * w + col : nullptr;
-      put64(to, dg, q.wide_dgu);
-      put64(to ? to + w : nullptr, du, q.wide_dgu);
+      put_grads(q, in, r, col, reinterpret_cast<const float*>(g), reinterpret_cast<const float*>(u), dh);
     }
   } else {
 #pragma unroll 1
@@ -310,6 +303,39 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
       put_out(t, row, col, v);
     }
   }
+}
+
+// up_grad's epilogue: the checkpoint's blocks are asked for before the accumulator is there (`wait` returns its address, or
+// false), then each a step ahead.
+template <typename Wait>
+__device__ __forceinline__ bool epilogue_up_grad(const Params& q, const Item& t, int row, int half, Wait wait) {
+  const Problem& p = *t.p;
+  const bool in = row < p.M;
+  const size_t r = size_t(in ? row : 0), w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
+  const int c0 = half * (q.cols / 2), c1 = min(c0 + q.cols / 2, q.w - t.nt * q.cols);
+  RawBlock rg, ru;
+  auto ask = [&](int c) {
+    const int col = t.nt * q.cols + c;
+    const uint8_t* code = q.ckpt + r * 2 * w + col;
+    const uint8_t* scale = q.ckpt + scales + r * 2 * nb + col / 32;
+    rg.load(code, scale);
+    ru.load(code + w, scale + nb);
+  };
+  if (c0 < c1) ask(c0);
+  uint32_t taddr;
+  if (!wait(taddr)) return false;
+#pragma unroll 1
+  for (int c = c0; c < c1; c += 32) {
+    uint32_t dh[32];
+    tmem_ld32(taddr + c, dh);
+    float g[32], u[32];
+    rg.values(g);
+    ru.values(u);
+    if (c + 32 < c1) ask(c + 32);
+    tmem_ld_wait();
+    put_grads(q, in, r, t.nt * q.cols + c, g, u, dh);
+  }
+  return true;
 }
 
 template <int EPI>
@@ -346,6 +372,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
   cluster_sync();  // barriers initialised and TMEM allocated in both CTAs
   tc_fence_after();
   pdl_wait();  // (nothing above reads memory)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (every CTA of this grid is running: they take no slot of it)
 
   const uint32_t tmem = ctl->tmem_base;
   // Few rows: the others of the MMA's A are whatever follows in shared memory, and so are sums that nobody reads. (The last
@@ -363,30 +390,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
       for (int item = cid; item < items && !*abort; item += ncl) {
         const Item t = item_at(q, item);
         const int arow = t.mt * kTile + int(rank) * 128;
-        const CUtensorMap* mb = EPI == EPI_UP && rank ? &t.p->b1 : &t.p->b;
-        const int brow = EPI == EPI_UP ? t.nt * half_cols : t.nt * q.cols + int(rank) * half_cols;
-        const bool a_mn = EPI >= EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI >= EPI_OUT && t.p->b_mn);
-        // operands in parts: all six products of kRun steps, then those of the next
-        int kb = t.k0, pass = 0, r0 = t.k0;
-        for (int left = (EPI == EPI_PARTS ? kPasses : 1) * (t.k1 - t.k0); left > 0; --left) {
-          if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, q.err)) break;
-          const int pa = EPI == EPI_PARTS ? part_of(false, pass) : 0, pb = EPI == EPI_PARTS ? part_of(true, pass) : 0;
-          const uint32_t sa = base + uint32_t(s * stage_bytes), fb = fb0 + uint32_t(s) * 8u;
-          if (leader) mbar_expect_tx(&ctl->full[s], uint32_t(q.a_rows ? stage_bytes + b_bytes : 2 * stage_bytes));
-          if (leader || !q.a_rows) load_operand(sa, &t.p->a, a_mn, 128, kb * BK, arow, pa, fb);
-          load_operand(sa + a_bytes, mb, b_mn, half_cols, kb * BK, brow, pb, fb);
-          ++kb;
-          if (EPI == EPI_PARTS && kb == min(r0 + kRun, t.k1)) {
-            if (++pass == kPasses) {
-              pass = 0;
-              r0 = kb;
+        // both: x by [W1 ; W3], then dy by W2, whose columns are half as many
+        for (int phase = 0; phase < (EPI == EPI_BOTH ? 2 : 1); ++phase) {
+          const Problem* p = EPI == EPI_BOTH ? &q.p[phase] : t.p;
+          const bool up = EPI == EPI_UP || (EPI == EPI_BOTH && phase == 0), back = EPI == EPI_UP_GRAD || (EPI == EPI_BOTH && phase == 1);
+          const CUtensorMap* mb = up && rank ? &p->b1 : &p->b;
+          const int b_cols = EPI == EPI_BOTH && phase ? half_cols / 2 : half_cols;
+          const int brow = up ? t.nt * half_cols : EPI == EPI_BOTH ? t.nt * half_cols + int(rank) * b_cols : t.nt * q.cols + int(rank) * half_cols;
+          const bool a_mn = EPI >= EPI_OUT && p->a_mn, b_mn = back || (EPI >= EPI_OUT && p->b_mn);
+          const uint32_t bytes = 2u * uint32_t(b_cols * BK * 2) + uint32_t(q.a_rows ? a_bytes : 2 * a_bytes);
+          // operands in parts: all six products of kRun steps, then those of the next
+          int kb = t.k0, pass = 0, r0 = t.k0;
+          for (int left = (EPI == EPI_PARTS ? kPasses : 1) * (t.k1 - t.k0); left > 0; --left) {
+            if (!mbar_wait_cl(&ctl->empty[s], ph ^ 1u, abort, q.err)) break;
+            const int pa = EPI == EPI_PARTS ? part_of(false, pass) : 0, pb = EPI == EPI_PARTS ? part_of(true, pass) : 0;
+            const uint32_t sa = base + uint32_t(s * stage_bytes), fb = fb0 + uint32_t(s) * 8u;
+            if (leader) mbar_expect_tx(&ctl->full[s], bytes);
+            if (leader || !q.a_rows) load_operand(sa, &p->a, a_mn, 128, kb * BK, arow, pa, fb);
+            load_operand(sa + a_bytes, mb, b_mn, b_cols, kb * BK, brow, pb, fb);
+            ++kb;
+            if (EPI == EPI_PARTS && kb == min(r0 + kRun, t.k1)) {
+              if (++pass == kPasses) {
+                pass = 0;
+                r0 = kb;
+              }
+              kb = r0;
             }
-            kb = r0;
-          }
-          if (issued < stages) ++issued;
-          if (++s == stages) {
-            s = 0;
-            ph ^= 1u;
+            if (issued < stages) ++issued;
+            if (++s == stages) {
+              s = 0;
+              ph ^= 1u;
+            }
           }
         }
       }
@@ -404,36 +438,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
       uint32_t ph = 0, lt = 0;
       for (int item = cid; item < items && !*abort; item += ncl) {
         const Item t = item_at(q, item);
-        const bool a_mn = EPI >= EPI_OUT && t.p->a_mn, b_mn = EPI == EPI_UP_GRAD || (EPI >= EPI_OUT && t.p->b_mn);
-        const uint32_t idesc = kIdesc | (uint32_t(q.cols >> 3) << 17) | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
         // 16 of the contraction: 32 bytes of each K-major row, or 16 rows of 128 bytes
-        const uint64_t ka = a_mn ? (16 * 128) >> 4 : 32 >> 4, kb_ = b_mn ? (16 * 128) >> 4 : 32 >> 4;
+        const bool a_mn = EPI >= EPI_OUT && t.p->a_mn;
+        const uint64_t ka = a_mn ? (16 * 128) >> 4 : 32 >> 4;
         bool ok = true;
         // an accumulator's steps: all of the item's, or the products of a run of them
         for (int k0 = t.k0; k0 < t.k1 && ok; k0 = EPI == EPI_PARTS ? k0 + kRun : t.k1) {
           const int n = EPI == EPI_PARTS ? kPasses * min(kRun, t.k1 - k0) : t.k1 - k0;
-          const uint32_t b = lt & 1u;
-          if (!mbar_wait_cl(&ctl->tempty[b], ((lt >> 1) & 1u) ^ 1u, abort, q.err)) {
+          const uint32_t b = EPI == EPI_BOTH ? 0u : lt & 1u, turn = EPI == EPI_BOTH ? lt : lt >> 1;
+          if (!mbar_wait_cl(&ctl->tempty[b], (turn & 1u) ^ 1u, abort, q.err)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t dt = tmem + b * kTile;
-          for (int i = 0; i < n; ++i) {
-            if (!mbar_wait_cl(&ctl->full[s], ph, abort, q.err)) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
-            const uint32_t sa = base + uint32_t(s * stage_bytes);
-            const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + a_bytes, b_mn);
+          for (int phase = 0; phase < (EPI == EPI_BOTH ? 2 : 1) && ok; ++phase) {
+            const bool b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_BOTH && phase == 1) || (EPI >= EPI_OUT && t.p->b_mn);
+            const int cols = EPI == EPI_BOTH && phase ? half_cols : q.cols;
+            const uint32_t idesc = kIdesc | (uint32_t(cols >> 3) << 17) | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
+            const uint64_t kb_ = b_mn ? (16 * 128) >> 4 : 32 >> 4;
+            const uint32_t dt = tmem + (EPI == EPI_BOTH ? uint32_t(phase * q.cols) : b * kTile);
+            for (int i = 0; i < n; ++i) {
+              if (!mbar_wait_cl(&ctl->full[s], ph, abort, q.err)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              const uint32_t sa = base + uint32_t(s * stage_bytes);
+              const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + a_bytes, b_mn);
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k)
-              tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (i != 0 || k != 0) ? 1u : 0u);
-            tc_commit_pair_both(&ctl->empty[s]);
-            if (++s == stages) {
-              s = 0;
-              ph ^= 1u;
+              for (int k = 0; k < BK / 16; ++k)
+                tc_mma_pair(dt, da + uint64_t(k) * ka, db + uint64_t(k) * kb_, idesc, (i != 0 || k != 0) ? 1u : 0u);
+              tc_commit_pair_both(&ctl->empty[s]);
+              if (++s == stages) {
+                s = 0;
+                ph ^= 1u;
+              }
             }
           }
           if (!ok) break;
@@ -452,9 +491,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
       const Item t = item_at(q, item);
       const int row = t.mt * kTile + int(rank) * 128 + quarter * 32 + lane;
       auto begin = [&](uint32_t& taddr) {
-        const uint32_t b = lt & 1u;
+        const uint32_t b = EPI == EPI_BOTH ? 0u : lt & 1u, turn = EPI == EPI_BOTH ? lt : lt >> 1;
         int ok = 1;
-        if (lane == 0) ok = mbar_wait_cl(&ctl->tfull[b], (lt >> 1) & 1u, abort, q.err) ? 1 : 0;
+        if (lane == 0) ok = mbar_wait_cl(&ctl->tfull[b], turn & 1u, abort, q.err) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         tc_fence_after();
         taddr = tmem + b * kTile + (uint32_t(quarter * 32) << 16);
@@ -463,7 +502,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
       auto end = [&] {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_relaxed(peer_addr(&ctl->tempty[lt & 1u], 0));
+        if (lane == 0) arrive_relaxed(peer_addr(&ctl->tempty[EPI == EPI_BOTH ? 0u : lt & 1u], 0));
         ++lt;
       };
       uint32_t taddr;
@@ -495,6 +534,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
           if (c * 32 >= share || col >= t.p->N) continue;
           put_out(t, row, col, reinterpret_cast<uint32_t*>(sum[c]));
         }
+      } else if constexpr (EPI == EPI_UP_GRAD) {
+        if (!epilogue_up_grad(q, t, row, half, begin)) break;
+        end();
       } else {
         if (!begin(taddr)) break;
         epilogue<EPI>(q, t, taddr, row, half);
@@ -642,7 +684,6 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
     return cudaErrorInvalidValue;
   q.w = a.w;
   q.h = static_cast<uint16_t*>(a.h);
-  q.gu = a.gu;
   q.ckpt = a.ckpt;
   q.wide_h = wide(a.h);
   q.wide_ckpt = wide(a.ckpt);
@@ -652,23 +693,32 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
 cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   Params q;
   memset(&q, 0, sizeof(q));
-  q.n = 1;
-  Problem& p = q.p[0];
   const Sizes z{a.T, a.w, (a.d + BK - 1) / BK};
-  q.cols = choose(&z, 1, 0, false, 1, num_sms() / 2).cols;
-  shape(p, a.T, a.w, a.d, q.cols);
-  p.b_mn = 1;
-  q.a_rows = few_rows(a.T);
-  if (!encode(&p.a, a.dy, size_t(a.d), size_t(a.T), q.a_rows ? q.a_rows : 128) || !encode(&p.b, a.w2, size_t(a.w), size_t(a.d), 64))
-    return cudaErrorInvalidValue;
+  const size_t d = size_t(a.d), w = size_t(a.w), T = size_t(a.T);
+  const int rows = few_rows(a.T), box = rows ? rows : 128;
+  q.a_rows = rows;
   q.w = a.w;
-  q.ckpt = const_cast<uint8_t*>(a.ckpt);
-  q.gu = const_cast<float*>(a.gu);
   q.h = static_cast<uint16_t*>(a.h);
   q.dgu = static_cast<uint16_t*>(a.dgu);
   q.wide_h = wide(a.h);
   q.wide_dgu = wide(a.dgu);
-  return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
+  q.n = 1;
+  if (a.ckpt) {
+    q.cols = choose(&z, 1, 0, false, 1, num_sms() / 2).cols;
+    shape(q.p[0], a.T, a.w, a.d, q.cols);
+    if (!encode(&q.p[0].a, a.dy, d, T, box) || !encode(&q.p[0].b, a.w2, w, d, 64)) return cudaErrorInvalidValue;
+    q.ckpt = const_cast<uint8_t*>(a.ckpt);
+    return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
+  }
+  // g, u and dh of 128 columns in one accumulator each
+  q.cols = kTile;
+  const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
+  shape(q.p[0], a.T, a.w, a.d, kTile / 2);
+  shape(q.p[1], a.T, a.w, a.d, kTile / 2);
+  if (!encode(&q.p[0].a, a.x, d, T, box) || !encode(&q.p[0].b, w1, d, w, 128) || !encode(&q.p[0].b1, w1 + w * d, d, w, 128) ||
+      !encode(&q.p[1].a, a.dy, d, T, box) || !encode(&q.p[1].b, a.w2, w, d, 64))
+    return cudaErrorInvalidValue;
+  return launch<EPI_BOTH>(q, kProfDenseUpGrad, s);
 }
 
 namespace {
