@@ -34,7 +34,6 @@ namespace {
 constexpr int BK = 64;
 constexpr int kTile = 256;  // rows, and most columns
 constexpr int kABytes = 128 * BK * 2;  // a CTA's rows of A in a stage
-constexpr int kRingBytes = 7 * (kABytes + 128 * BK * 2);
 constexpr int kMaxStages = 16;
 constexpr int kTmemCols = 2 * kTile;
 // instruction descriptor without N and the operands' order: D fp32, A and B bf16, M = 256
@@ -44,12 +43,21 @@ constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
 // EPI_BOTH: up and up_grad in one, from x; EPI_PARTS: out, of operands in parts
 enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_BOTH = 2, EPI_OUT = 3, EPI_PARTS = 4 };
 
-// Epilogue warps: four lane quarters of TMEM by so many shares of the columns (operands in parts: so that a thread's 64 sums fit
-// its registers).
+// Epilogue warps: four lane quarters of TMEM by so many shares of the columns. up_grad: eight warps do not hide the latencies of 45
+// instructions a value, the checkpoint's loads and three outputs; operands in parts: a thread's 64 sums fit its registers.
 template <int EPI>
-constexpr int kShares = EPI == EPI_PARTS ? 4 : 2;
+constexpr int kShares = EPI == EPI_UP_GRAD || EPI == EPI_PARTS ? 4 : 2;
 template <int EPI>
 constexpr int kThreads = 64 + 128 * kShares<EPI>;
+// up_grad's rows go to memory through 3 KB of shared memory a warp and TMA: a lane's own row in 64-byte stores keeps the way to L1
+// busy (rows 4 or 8 KB apart meet in few sets). The others' epilogues end before their products, for which the stages that the
+// room would cost count more (five in place of seven: up 49 -> 53 us at 1000 x 4096 x 4096).
+template <int EPI>
+constexpr int kStageOut = EPI == EPI_UP_GRAD ? 3072 : 0;
+template <int EPI>
+constexpr int kStaging = kStageOut<EPI> * 4 * kShares<EPI>;
+template <int EPI>
+constexpr int kRingBytes = 7 * (EPI == EPI_UP_GRAD ? 24576 : 32768);
 
 struct Problem {
   CUtensorMap a, b, b1;  // b1: rank 1's columns of an up tile
@@ -66,6 +74,7 @@ struct Params {
   int a_rows;  // of A that the first CTA of a pair brings in, where no A has more than its 128; else 0: 128 each
   unsigned* err;
   // up, up_grad
+  CUtensorMap to_h, to_dgu;  // up_grad: boxes of 32 rows by 32 bytes
   uint8_t* ckpt;
   uint16_t *h, *dgu;
   int w, wide_h, wide_dgu, wide_ckpt;
@@ -77,8 +86,9 @@ struct Ctl {
   uint32_t tmem_base;
   int abort;
 };
-constexpr int kSmem = kRingBytes + 1024 + int(sizeof(Ctl));
-static_assert(kSmem <= 227 * 1024, "shared memory");
+template <int EPI>
+constexpr int kSmem = kRingBytes<EPI> + kStaging<EPI> + 1024 + int(sizeof(Ctl));
+static_assert(kSmem<EPI_UP_GRAD> <= 227 * 1024 && kSmem<EPI_OUT> <= 227 * 1024, "shared memory");
 
 struct Item {
   const Problem* p;
@@ -149,6 +159,37 @@ __device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// A warp's way to memory: three pieces of 1 KB, boxes of 32 rows by 32 bytes, sent together.
+struct Stage {
+  uint32_t addr;  // shared memory, on 1024 bytes
+  // Once the last boxes have been read.
+  __device__ __forceinline__ static void free() {
+    if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+  }
+  // 32 bytes of each lane's row to a piece: the 32-byte swizzle.
+  __device__ __forceinline__ void put(int i, const uint32_t* v) const {
+    const uint32_t lane = threadIdx.x & 31u, at = addr + uint32_t(i) * 1024u + lane * 32u, flip = ((lane >> 2) & 1u) << 4;
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + (flip ^ (k << 4))), "r"(v[4 * k]), "r"(v[4 * k + 1]),
+                   "r"(v[4 * k + 2]), "r"(v[4 * k + 3])
+                   : "memory");
+  }
+  // What every lane has written can be copied now, by the one lane that gets true.
+  __device__ __forceinline__ static bool ready() {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    return (threadIdx.x & 31) == 0;
+  }
+  __device__ __forceinline__ void send(int i, const CUtensorMap* map, int col, int row0) const {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(col), "r"(row0), "r"(addr + uint32_t(i) * 1024u)
+                 : "memory");
+  }
+};
+
 // 64 bytes of each lane's row (NULL: none).
 __device__ __forceinline__ void put64(void* row, uint32_t* u, int wide) {
   if (wide) store_rows64<32>(row, u);
@@ -176,22 +217,50 @@ __device__ __forceinline__ void put_mx8(uint8_t* code, uint8_t* scale, const uin
 
 // A row's block of the checkpoint, as it lies in memory.
 struct RawBlock {
-  uint4 a, b;
-  uint32_t scale;
-  __device__ __forceinline__ void load(const uint8_t* code, const uint8_t* s) {
-    a = ldg16(code);
-    b = ldg16(code + 16);
+  uint32_t c[8], scale;
+  __device__ __forceinline__ void load(const uint8_t* code, const uint8_t* s, int wide) {
+    if (wide) {
+      asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]), "=r"(c[4]), "=r"(c[5]), "=r"(c[6]), "=r"(c[7])
+                   : "l"(code));
+    } else {
+      const uint4 a = ldg16(code), b = ldg16(code + 16);
+      c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
+      c[4] = b.x; c[5] = b.y; c[6] = b.z; c[7] = b.w;
+    }
     scale = __ldg(s);
   }
-  __device__ __forceinline__ void values(float* v) const {
-    const uint32_t c[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    const float unit = mx8_unit(scale);
+  // Four of them.
+  __device__ __forceinline__ void values(int i, float unit, float* v) const {
+    mx8_values(c[i], v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mx8_values(c[i], v + 4 * i);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] *= unit;
+    for (int k = 0; k < 4; ++k) v[k] *= unit;
   }
 };
+
+// 16 columns of a warp's rows: h, dg and du.
+struct Grads {
+  uint32_t h[8], dg[8], du[8];
+  __device__ __forceinline__ void set(int i, float g0, float u0, float dh0, float g1, float u1, float dh1) {
+    const SwigluGrad lo(g0, u0, dh0), hi(g1, u1, dh1);
+    h[i] = pack2bf(lo.h, hi.h);
+    dg[i] = pack2bf(lo.dg, hi.dg);
+    du[i] = pack2bf(lo.du, hi.du);
+  }
+  __device__ __forceinline__ void put(const Params& q, Stage& st, int row0, int col) const {
+    st.free();
+    st.put(0, h);
+    st.put(1, dg);
+    st.put(2, du);
+    if (st.ready()) {
+      st.send(0, &q.to_h, col, row0);
+      st.send(1, &q.to_dgu, col, row0);
+      st.send(2, &q.to_dgu, q.w + col, row0);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+};
+__device__ __forceinline__ float as_float(uint32_t v) { return __uint_as_float(v); }
 
 // 32 columns of a row: h, dg and du from g, u and dh.
 __device__ __forceinline__ void put_grads(const Params& q, bool in, size_t r, int col, const float* g, const float* u,
@@ -305,35 +374,55 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
   }
 }
 
-// up_grad's epilogue: the checkpoint's blocks are asked for before the accumulator is there (`wait` returns its address, or
-// false), then each a step ahead.
+// up_grad's epilogue: the checkpoint's first blocks are asked for before the accumulator is there (`wait` gives its address, or
+// false).
 template <typename Wait>
-__device__ __forceinline__ bool epilogue_up_grad(const Params& q, const Item& t, int row, int half, Wait wait) {
+__device__ __forceinline__ bool epilogue_up_grad(const Params& q, const Item& t, int next, int row0, int c0, int c1, Stage& st,
+                                                 Wait wait) {
   const Problem& p = *t.p;
-  const bool in = row < p.M;
-  const size_t r = size_t(in ? row : 0), w = size_t(q.w), nb = w / 32, scales = size_t(p.M) * 2 * w;
-  const int c0 = half * (q.cols / 2), c1 = min(c0 + q.cols / 2, q.w - t.nt * q.cols);
+  const int row = row0 + int(threadIdx.x & 31), first = t.nt * q.cols;
+  const size_t r = size_t(row < p.M ? row : 0), w = size_t(q.w), nb = w / 32;
+  const uint8_t* codes = q.ckpt + r * 2 * w + first;
+  const uint8_t* scales = q.ckpt + size_t(p.M) * 2 * w + r * 2 * nb + first / 32;
+  if (row0 >= p.M) c1 = c0;
   RawBlock rg, ru;
   auto ask = [&](int c) {
-    const int col = t.nt * q.cols + c;
-    const uint8_t* code = q.ckpt + r * 2 * w + col;
-    const uint8_t* scale = q.ckpt + scales + r * 2 * nb + col / 32;
-    rg.load(code, scale);
-    ru.load(code + w, scale + nb);
+    rg.load(codes + c, scales + c / 32, q.wide_ckpt);
+    ru.load(codes + w + c, scales + nb + c / 32, q.wide_ckpt);
   };
   if (c0 < c1) ask(c0);
+  // the next item's on their way to L2 (64 or 32 bytes a row and half of it)
+  if (next < q.items) {
+    const Item n = item_at(q, next);
+    const int nrow = row + (n.mt - t.mt) * kTile, at = n.nt * q.cols + c0;
+    if (nrow < p.M && at < q.w) {
+      const uint8_t* from = q.ckpt + size_t(nrow) * 2 * w + at;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(from));
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(from + w));
+    }
+  }
   uint32_t taddr;
   if (!wait(taddr)) return false;
 #pragma unroll 1
   for (int c = c0; c < c1; c += 32) {
-    uint32_t dh[32];
-    tmem_ld32(taddr + c, dh);
-    float g[32], u[32];
-    rg.values(g);
-    ru.values(u);
-    if (c + 32 < c1) ask(c + 32);
-    tmem_ld_wait();
-    put_grads(q, in, r, t.nt * q.cols + c, g, u, dh);
+    if (c != c0) ask(c);
+    const float kg = mx8_unit(rg.scale), ku = mx8_unit(ru.scale);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint32_t dh[16];
+      tmem_ld16(taddr + c + 16 * k, dh);
+      tmem_ld_wait();
+      Grads d;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float g[4], u[4];
+        rg.values(4 * k + i, kg, g);
+        ru.values(4 * k + i, ku, u);
+        d.set(2 * i, g[0], u[0], as_float(dh[4 * i]), g[1], u[1], as_float(dh[4 * i + 1]));
+        d.set(2 * i + 1, g[2], u[2], as_float(dh[4 * i + 2]), g[3], u[3], as_float(dh[4 * i + 3]));
+      }
+      d.put(q, st, row0, first + c + 16 * k);
+    }
   }
   return true;
 }
@@ -344,7 +433,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;  // the same offsets in both CTAs
-  Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + kRingBytes);
+  Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + kRingBytes<EPI> + kStaging<EPI>);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
@@ -378,7 +467,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
   // Few rows: the others of the MMA's A are whatever follows in shared memory, and so are sums that nobody reads. (The last
   // stage's must still lie in the ring.)
   const int a_bytes = q.a_rows ? q.a_rows * BK * 2 : kABytes, b_bytes = q.cols / 2 * BK * 2, stage_bytes = a_bytes + b_bytes;
-  const int half_cols = q.cols / 2, stages = min(kMaxStages, (kRingBytes - (kABytes - a_bytes)) / stage_bytes);
+  const int half_cols = q.cols / 2, stages = min(kMaxStages, (kRingBytes<EPI> - (kABytes - a_bytes)) / stage_bytes);
   const int items = q.items, cid = int(blockIdx.x >> 1), ncl = int(gridDim.x >> 1);
   volatile int* abort = &ctl->abort;
 
@@ -486,6 +575,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
     }
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2;  // TMEM lanes this warp may access, columns it takes
+    Stage st{base + uint32_t(kRingBytes<EPI>) + uint32_t((warp - 2) * kStageOut<EPI>)};
     uint32_t lt = 0;
     for (int item = cid; item < items; item += ncl) {
       const Item t = item_at(q, item);
@@ -535,7 +625,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
           put_out(t, row, col, reinterpret_cast<uint32_t*>(sum[c]));
         }
       } else if constexpr (EPI == EPI_UP_GRAD) {
-        if (!epilogue_up_grad(q, t, row, half, begin)) break;
+        const int share = q.cols / kShares<EPI>, c0 = half * share;
+        if (!epilogue_up_grad(q, t, item + ncl, row - lane, c0, min(c0 + share, t.p->N - t.nt * q.cols), st, begin)) break;
         end();
       } else {
         if (!begin(taddr)) break;
@@ -543,6 +634,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
         end();
       }
     }
+    if (kStaging<EPI> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // the rows are in memory
   }
 
   tc_fence_before();
@@ -567,6 +659,18 @@ bool encode(CUtensorMap* m, const void* base, size_t cols, size_t rows, int box_
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// An output of bf16 [rows, cols], by boxes of 32 rows of 32 bytes.
+bool encode_out(CUtensorMap* m, void* base, size_t cols, size_t rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {cols * 2};
+  const cuuint32_t box[2] = {16, 32};
+  const cuuint32_t es[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
 
 constexpr size_t kGroupBytes = size_t(24) << 20;  // of A that the row tiles of a group read
@@ -583,7 +687,8 @@ void shape(Problem& p, int M, int N, int K, int tile_cols) {
 }
 
 // What a launch's items take, in steps of 64 of the contraction by 256 columns (0.29 us): the longest pair's share of them,
-// where pair i has items i, i + pairs, ...; an item takes at least what its epilogue does.
+// where pair i has items i, i + pairs, ...; an item takes at least what its epilogue does. A step by 128 columns takes 0.78 of
+// that: the copies from L2 bound it. Few rows: the weights' way from HBM bounds both.
 struct Plan {
   int cols, per[kMaxProducts];
   double time;
@@ -596,7 +701,9 @@ constexpr int kLeastPart = 4;  // steps: below that an item is mostly its fill a
 constexpr double kJoin = 10;   // a launch more, beside the planes' bytes
 
 double plan_time(const Sizes* z, int n, int up, int passes, int cols, const int* per, int pairs) {
-  const double step = cols == kTile ? 1.0 : 0.56, epilogue = (cols == kTile ? 4.0 : 2.0) * (up ? 1.5 : 1.0), fill = 5.0;
+  const bool few = n == 1 && z[0].M <= 128;
+  const double step = few ? (cols == kTile ? 1.3 : 0.65) : cols == kTile ? 1.0 : 0.78;
+  const double epilogue = (cols == kTile ? 4.0 : 2.0) * (up ? 1.5 : 1.0), fill = 5.0;
   double total = 0, longest = 0, planes = 0;
   long long items = 0;
   for (int i = 0; i < n; ++i) {
@@ -647,8 +754,8 @@ int pairs_at_once() {
   static SmemOptIn smem;
   static ResidentClusters resident;
   const void* fn = reinterpret_cast<const void*>(dense_gemm_kernel<EPI>);
-  if (smem.allow(fn, kSmem) != cudaSuccess) return 0;
-  return resident.get(fn, num_sms() & ~1, kThreads<EPI>, kSmem);
+  if (smem.allow(fn, kSmem<EPI>) != cudaSuccess) return 0;
+  return resident.get(fn, num_sms() & ~1, kThreads<EPI>, kSmem<EPI>);
 }
 
 template <int EPI>
@@ -662,7 +769,7 @@ cudaError_t launch(Params& q, int kid, cudaStream_t s) {
   const int pairs = pairs_at_once<EPI>();
   if (pairs < 1) return cudaErrorInvalidConfiguration;
   prof_begin(kid, s);
-  const cudaError_t e = launch_pdl(dense_gemm_kernel<EPI>, dim3(unsigned(2 * std::min(pairs, q.items))), dim3(kThreads<EPI>), kSmem, s, q);
+  const cudaError_t e = launch_pdl(dense_gemm_kernel<EPI>, dim3(unsigned(2 * std::min(pairs, q.items))), dim3(kThreads<EPI>), kSmem<EPI>, s, q);
   prof_end(kid, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -707,7 +814,9 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
     q.cols = choose(&z, 1, 0, false, 1, num_sms() / 2).cols;
     shape(q.p[0], a.T, a.w, a.d, q.cols);
     if (!encode(&q.p[0].a, a.dy, d, T, box) || !encode(&q.p[0].b, a.w2, w, d, 64)) return cudaErrorInvalidValue;
+    if (!encode_out(&q.to_h, a.h, w, T) || !encode_out(&q.to_dgu, a.dgu, 2 * w, T)) return cudaErrorInvalidValue;
     q.ckpt = const_cast<uint8_t*>(a.ckpt);
+    q.wide_ckpt = wide(a.ckpt);
     return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
   }
   // g, u and dh of 128 columns in one accumulator each
