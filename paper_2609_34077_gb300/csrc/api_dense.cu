@@ -14,6 +14,11 @@ namespace {
 
 constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
 
+// bf16: up to here the kernels that stream the weights. Graph nodes against the products', 2048 x 1408 and 4096 x 14336: 8 tokens
+// 10.5 and 72 us (20.6 and 71), 16 14.4 and 90 (20.7 and 72), 32 17.7 and 106 (20.6 and 72).
+bool few_tokens(int T, size_t weights) {
+  return T <= 8 || (T <= 16 && weights <= (size_t(48) << 20)) || (T <= 32 && weights <= (size_t(20) << 20));
+}
 constexpr int kFewTokensF32 = 8;  // fp32: up to here the kernels that read each weight row once for 8 tokens
 
 mcft_status check_T(int T) {
@@ -267,7 +272,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   if (st != MCFT_OK) return st;
   char* ws = static_cast<char*>(workspace);
   cudaError_t e;
-  if (!ckpt && T <= (desc->dtype == MCFT_F32 ? kFewTokensF32 : kFewTokens)) {
+  if (!ckpt && (desc->dtype == MCFT_F32 ? T <= kFewTokensF32 : few_tokens(T, size_t(3) * desc->w * desc->d))) {
     e = desc->dtype == MCFT_F32 ? forward_f32(desc, x, T, block, y, ws, L, stream)
                                 : launch_dense_few(DenseFewArgs{x, block, ws + L.h, y, T, desc->d, desc->w}, stream);
     return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
@@ -342,17 +347,19 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   float* planes = reinterpret_cast<float*>(ws + L.planes);
   float* gu = ckpt || desc->dtype == MCFT_BF16 ? nullptr : reinterpret_cast<float*>(ws + L.gu);
   cudaError_t e = cudaSuccess;
-  if (want_x && x8) {
+  const bool later = ckpt && desc->dtype == MCFT_BF16;  // x's values are wanted after the next kernel only, which writes them
+  if (want_x && x8 && !later) {
     e = launch_mx8_quant(Mx8Args{ws + L.x8, const_cast<void*>(x8), T, d, d}, desc->dtype, true, stream);
-    x = ws + L.x8;
   }
+  if (want_x && x8) x = ws + L.x8;
   // the last products' operands: bf16, or fp32 in parts
   const void *dgu = ws + L.dgu, *h = ws + L.h, *xs = x, *dys = dy, *w13s = w13;
   size_t part_gu = 0, part_h = 0, part_x = 0, part_w = 0;
   auto* products = launch_dense_products;
   if (desc->dtype == MCFT_BF16) {
     if (e == cudaSuccess)
-      e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), x, w13, ws + L.h, ws + L.dgu}, stream);
+      e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), x, w13, ws + L.h, ws + L.dgu,
+                                               want_x && later ? static_cast<const uint8_t*>(x8) : nullptr, ws + L.x8}, stream);
   } else {
     products = launch_dense_split_products;
     uint16_t *x3 = reinterpret_cast<uint16_t*>(ws + L.x), *dy3 = reinterpret_cast<uint16_t*>(ws + L.dy),

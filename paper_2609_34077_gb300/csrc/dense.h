@@ -8,6 +8,13 @@ namespace mcft {
 
 int num_sms();
 
+// Waits for the kernels ahead in the stream, then lets the next one be launched: its CTAs start as this grid's last ones leave
+// room, and wait in the same way before they touch memory.
+__device__ __forceinline__ void pdl_begin() {
+  pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 struct Mx8Args {
   const void* x;  // [R, C], ld elements from row to row (the way back: written)
   void* q;
@@ -93,6 +100,8 @@ struct DenseUpGradArgs {
   const uint8_t* ckpt;
   const void *x, *w13;
   void *h, *dgu;
+  const uint8_t* x8;  // with a checkpoint: mx8 [T, d] to be written out as bf16 besides (on 32 bytes), or NULL
+  void* x8_values;
 };
 cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s);
 
@@ -107,8 +116,7 @@ struct DenseActArgs {
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s);
 cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s);
 
-// The whole block for up to kFewTokens tokens, bf16: h [T, w] is scratch.
-constexpr int kFewTokens = 8;
+// The whole block for few tokens (at most 32), bf16: h [T, w] is scratch.
 struct DenseFewArgs {
   const void *x, *block;
   void *h, *y;

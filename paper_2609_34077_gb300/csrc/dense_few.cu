@@ -38,10 +38,7 @@ __global__ void __launch_bounds__(kWarps * 32) dense_few_kernel(const __grid_con
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int part = int(blockIdx.x) % p.parts, unit = int(blockIdx.x) / p.parts;
   if (p.parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-  if (UP) {
-    pdl_wait();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  }
+  if (UP) pdl_begin();
   const int steps = p.K / 32, stride = p.parts * kWarps, first = part * kWarps + warp;
   // up: a row of W1 and the same of W3; down: rows g and g + 8 of the tile
   const uint16_t* row0 = p.w + size_t(unit * kOuts + g) * p.K + q * 8;
@@ -58,7 +55,7 @@ __global__ void __launch_bounds__(kWarps * 32) dense_few_kernel(const __grid_con
   };
   float acc[NT][4] = {};
   ask(0, first);
-  if (!UP) pdl_wait();
+  if (!UP) pdl_begin();
   auto batch = [&](int buf, int s0) {
     uint4 b[kBatch][NT];
 #pragma unroll

@@ -76,8 +76,9 @@ struct Params {
   // up, up_grad
   CUtensorMap to_h, to_dgu;  // up_grad: boxes of 32 rows by 32 bytes
   uint8_t* ckpt;
-  uint16_t *h, *dgu;
-  int w, wide_h, wide_dgu, wide_ckpt;
+  const uint8_t* x8;  // up_grad: mx8 [T, d] whose values go to x, for the products after it
+  uint16_t *h, *dgu, *x;
+  int d, w, wide_h, wide_dgu, wide_ckpt;
 };
 static_assert(sizeof(Params) <= 4096, "kernel parameters");
 
@@ -89,6 +90,10 @@ struct Ctl {
 template <int EPI>
 constexpr int kSmem = kRingBytes<EPI> + kStaging<EPI> + 1024 + int(sizeof(Ctl));
 static_assert(kSmem<EPI_UP_GRAD> <= 227 * 1024 && kSmem<EPI_OUT> <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+}
 
 struct Item {
   const Problem* p;
@@ -374,6 +379,25 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
   }
 }
 
+// The values of an mx8 matrix of whole blocks, a block a thread: what the epilogue's threads do until the first tile is there.
+__device__ __forceinline__ void mx8_to_bf16(const uint8_t* q, uint16_t* x, size_t blocks, size_t first, size_t step) {
+  for (size_t b = first; b < blocks; b += step) {
+    RawBlock r;
+    r.load(q + b * 32, q + blocks * 32 + b, 0);
+    const float unit = mx8_unit(r.scale);
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[4];
+      r.values(i, unit, v);
+      w[2 * i] = pack2bf(v[0], v[1]);
+      w[2 * i + 1] = pack2bf(v[2], v[3]);
+    }
+    store32(x + b * 32, w);
+    store32(x + b * 32 + 16, w + 8);
+  }
+}
+
 // up_grad's epilogue: the checkpoint's first blocks are asked for before the accumulator is there (`wait` gives its address, or
 // false).
 template <typename Wait>
@@ -437,6 +461,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
+  if (threadIdx.x == 32) {
+    prefetch_map(&q.p[0].a);
+    prefetch_map(&q.p[0].b);
+    if (EPI == EPI_UP || EPI == EPI_BOTH) prefetch_map(&q.p[0].b1);
+  }
   if (threadIdx.x == 0) {
     ctl->abort = 0;
     for (int s = 0; s < kMaxStages; ++s) {
@@ -460,8 +489,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
   tc_fence_before();
   cluster_sync();  // barriers initialised and TMEM allocated in both CTAs
   tc_fence_after();
-  pdl_wait();  // (nothing above reads memory)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (every CTA of this grid is running: they take no slot of it)
+  pdl_begin();  // (nothing above reads memory)
 
   const uint32_t tmem = ctl->tmem_base;
   // Few rows: the others of the MMA's A are whatever follows in shared memory, and so are sums that nobody reads. (The last
@@ -575,6 +603,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
     }
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2;  // TMEM lanes this warp may access, columns it takes
+    if (EPI == EPI_UP_GRAD && q.x8) {
+      const size_t n = size_t(kThreads<EPI> - 64);
+      mx8_to_bf16(q.x8, q.x, size_t(q.p[0].M) * (q.d / 32), blockIdx.x * n + threadIdx.x - 64, gridDim.x * n);
+    }
     Stage st{base + uint32_t(kRingBytes<EPI>) + uint32_t((warp - 2) * kStageOut<EPI>)};
     uint32_t lt = 0;
     for (int item = cid; item < items; item += ncl) {
@@ -817,6 +849,9 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
     if (!encode_out(&q.to_h, a.h, w, T) || !encode_out(&q.to_dgu, a.dgu, 2 * w, T)) return cudaErrorInvalidValue;
     q.ckpt = const_cast<uint8_t*>(a.ckpt);
     q.wide_ckpt = wide(a.ckpt);
+    q.x8 = a.x8;
+    q.x = static_cast<uint16_t*>(a.x8_values);
+    q.d = a.d;
     return launch<EPI_UP_GRAD>(q, kProfDenseUpGrad, s);
   }
   // g, u and dh of 128 columns in one accumulator each

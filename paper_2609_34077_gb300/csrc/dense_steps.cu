@@ -32,7 +32,7 @@ __device__ __forceinline__ void put_parts(uint16_t* to, size_t stride, const flo
 }
 
 __global__ void __launch_bounds__(256) dense_split_kernel(const __grid_constant__ DenseSplitArgs a) {
-  pdl_wait();
+  pdl_begin();
   const size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 8;
   int k = 0;
   size_t at = i;
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(256) dense_split_kernel(const __grid_constant_
 // out = sum of n planes, in order (+ out): four values a thread.
 template <typename T>
 __global__ void __launch_bounds__(256) dense_join_kernel(const float* planes, int n, size_t count, void* out, int accumulate) {
-  pdl_wait();
+  pdl_begin();
   const size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 4;
   if (i >= count) return;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(256) dense_join_kernel(const float* planes, in
 // Element-wise steps: eight values of g and u a thread, four neighbouring lanes an mx8 block.
 template <bool GRAD>
 __global__ void __launch_bounds__(256) dense_act_kernel(const __grid_constant__ DenseActArgs a) {
-  pdl_wait();
+  pdl_begin();
   const size_t w = size_t(a.w), per = w / 8, i = size_t(blockIdx.x) * 256 + threadIdx.x;
   const bool in = i < size_t(a.T) * per;
   const size_t row = in ? i / per : 0, c = in ? (i - row * per) * 8 : 0;
@@ -163,7 +163,7 @@ cudaError_t launch_act(const DenseActArgs& a, cudaStream_t s) {
 }
 
 __global__ void __launch_bounds__(256) dense_place_kernel(const __grid_constant__ DensePlaceArgs a) {
-  pdl_wait();
+  pdl_begin();
   const int i = int(blockIdx.x) * 256 + int(threadIdx.x);
   if (i == 0) {
     *a.hdr = WsHeader{0, 1, a.T, 0};

@@ -40,7 +40,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t* c) {
 // One block a thread: 2^lg_tx threads along a row.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx8_quantize_kernel(const __grid_constant__ Mx8Args a, int lg_tx) {
-  pdl_wait();
+  pdl_begin();
   const long long r = (long long)blockIdx.x * (kThreads >> lg_tx) + (threadIdx.x >> lg_tx);
   const size_t b = (size_t(blockIdx.y) << lg_tx) + (threadIdx.x & ((1u << lg_tx) - 1u));
   const Mx8Layout L(a.R, a.C);
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) mx8_quantize_kernel(const __grid_con
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx8_dequantize_kernel(const __grid_constant__ Mx8Args a, int lg_tx) {
-  pdl_wait();
+  pdl_begin();
   const long long r = (long long)blockIdx.x * (kThreads >> lg_tx) + (threadIdx.x >> lg_tx);
   const size_t b = (size_t(blockIdx.y) << lg_tx) + (threadIdx.x & ((1u << lg_tx) - 1u));
   const Mx8Layout L(a.R, a.C);
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) mx8_dequantize_kernel(const __grid_c
 // 32 blocks of a row a warp, a value of each a lane.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx8_quantize_any_kernel(const __grid_constant__ Mx8Args a, int lg_tx) {
-  pdl_wait();
+  pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long r = (long long)blockIdx.x * ((kThreads / 32) >> lg_tx) + (warp >> lg_tx);
   const size_t b0 = ((size_t(blockIdx.y) << lg_tx) + (warp & ((1 << lg_tx) - 1))) * 32;
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads) mx8_quantize_any_kernel(const __grid
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx8_dequantize_any_kernel(const __grid_constant__ Mx8Args a, int lg_tx) {
-  pdl_wait();
+  pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long r = (long long)blockIdx.x * ((kThreads / 32) >> lg_tx) + (warp >> lg_tx);
   const size_t b0 = ((size_t(blockIdx.y) << lg_tx) + (warp & ((1 << lg_tx) - 1))) * 32;

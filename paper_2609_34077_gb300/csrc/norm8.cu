@@ -114,7 +114,7 @@ __device__ __forceinline__ float team_sum(float s, int lg, float* part) {
 
 template <typename T, int NG, int THREADS>
 __global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ Norm8Args a, int lg) {
-  pdl_wait();
+  pdl_begin();
   __shared__ float2 part[32];
   const int lane = threadIdx.x & ((1 << lg) - 1), groups = a.d / 8;
   const long long row = (long long)blockIdx.x * (blockDim.x >> lg) + (threadIdx.x >> lg);
@@ -209,7 +209,7 @@ using Raw = std::conditional_t<sizeof(T) == 2, RawBf16, RawF32>;
 
 template <typename T, bool X8, int NG, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? (X8 ? 4 : 2) : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a, int lg) {
-  pdl_wait();
+  pdl_begin();
   __shared__ float part[2][32];
   __shared__ float share[THREADS == 256 && NG == 1 ? 2048 : 1];  // several teams: [team][8 values of a thread]
   const int lane = threadIdx.x & ((1 << lg) - 1), team = threadIdx.x >> lg, teams = blockDim.x >> lg, groups = a.d / 8;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? (X8 ? 4 : 2) : 1) no
 
 // 32 columns a CTA: a warp adds up every 32nd plane of them, then the warps' sums are added in order.
 __global__ void __launch_bounds__(1024) norm_planes_kernel(const __grid_constant__ NormGradArgs a, int planes) {
-  pdl_wait();
+  pdl_begin();
   __shared__ float sum[32][33];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = int(blockIdx.x) * 32 + lane;
   float s = 0.f;

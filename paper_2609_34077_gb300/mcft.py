@@ -770,7 +770,7 @@ def mcft_mx8_quantize(x, q=None, stream=None):
     rows, cols = x.shape
     ptr, ld = _rows(x)
     if q is None:
-        q = _empty(mcft_mx8_size(rows, cols), torch.uint8, x.device, stream)
+        q = _empty(rows * -(-cols // 32) * 33, torch.uint8, x.device, stream)
     else:
         _wants_mx8(q, rows, cols, "q is uint8 of mcft_mx8_size(rows, cols) bytes")
     _check(lib().mcft_mx8_quantize(ptr, rows, cols, ld, _MX4_DTYPE[x.dtype], _ptr(q), _stream(stream)))
@@ -806,7 +806,7 @@ def mcft_residual_rmsnorm_mx8(desc: LayerDesc, x, y=None, gamma=None, eps=1e-5, 
     else:
         _wants(_is(u, dtype, T, d), "u is [T, d] of the layer dtype")
     if u8 is None:
-        u8 = _empty(mcft_mx8_size(T, d), torch.uint8, x.device, stream)
+        u8 = _empty(T * -(-d // 32) * 33, torch.uint8, x.device, stream)
     else:
         _wants_mx8(u8, T, d, "u8 is uint8 of mcft_mx8_size(T, d) bytes")
     if x8 is not None:
