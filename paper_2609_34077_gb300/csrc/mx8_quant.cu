@@ -2,8 +2,9 @@
 // as codes and scale.
 //  * Rows whose values begin on 32 bytes: a block of 32 values a thread, so that nothing crosses lanes and every access is
 //    a whole sector.
-//  * Other rows: a value of each block a lane, 32 blocks of a row a warp; the largest magnitude comes from one reduction
-//    instruction, and loads and stores are of neighbouring values.
+//  * Other rows: four neighbouring values a lane, 32 blocks of a row a warp; the largest magnitude comes from three shuffles.
+//    Values of two bytes that begin off a word are read in whole words and shifted (but for a row's ends, which are not all
+//    its own).
 #include "dense.h"
 #include "mx8.cuh"
 #include "row_store.cuh"
@@ -112,7 +113,49 @@ __global__ void __launch_bounds__(kThreads) mx8_dequantize_kernel(const __grid_c
   }
 }
 
-// 32 blocks of a row a warp, a value of each a lane.
+// Values c..c+3 of a row of C (zeros past it).
+template <typename T>
+__device__ __forceinline__ void load4(const T* row, long long c, long long C, float* v) {
+  const T* p = row + c;
+  if (c + 4 > C || (sizeof(T) == 2 && c == 0)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = c + i < C ? load1(p + i) : 0.f;
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __ldg(p + i);
+  } else {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~uintptr_t(3));
+    uint32_t a = __ldg(w), b = __ldg(w + 1);
+    if (at & 2) {  // (the words' other halves are the row's values c - 1 and, unless it ends there, c + 4)
+      const uint32_t e = c + 4 < C ? __ldg(w + 2) : uint32_t(*reinterpret_cast<const uint16_t*>(p + 3));
+      a = __funnelshift_r(a, b, 16);
+      b = __funnelshift_r(b, e, 16);
+    }
+    v[0] = bf16lo(a);
+    v[1] = bf16hi(a);
+    v[2] = bf16lo(b);
+    v[3] = bf16hi(b);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* row, long long c, long long C, const float* v) {
+  T* p = row + c;
+  if (c + 4 > C || sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < C) store1(p + i, v[i]);
+  } else if (reinterpret_cast<uintptr_t>(p) & 2) {
+    store1(p, v[0]);
+    *reinterpret_cast<uint32_t*>(p + 1) = pack2bf(v[1], v[2]);
+    store1(p + 3, v[3]);
+  } else {
+    reinterpret_cast<uint32_t*>(p)[0] = pack2bf(v[0], v[1]);
+    reinterpret_cast<uint32_t*>(p)[1] = pack2bf(v[2], v[3]);
+  }
+}
+
+// 32 blocks of a row a warp, four at a time, four neighbouring values a lane.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx8_quantize_any_kernel(const __grid_constant__ Mx8Args a, int lg_tx) {
   pdl_begin();
@@ -122,27 +165,30 @@ __global__ void __launch_bounds__(kThreads) mx8_quantize_any_kernel(const __grid
   const Mx8Layout L(a.R, a.C);
   if (r >= a.R || b0 >= L.blocks) return;
   const T* row = static_cast<const T*>(a.x) + r * a.ld;
-  uint8_t* out = static_cast<uint8_t*>(a.q) + (size_t(r) * L.blocks + b0) * 32;
+  uint8_t* out = static_cast<uint8_t*>(a.q);
+  const size_t at = size_t(r) * L.blocks + b0;
   const int n = int(min(size_t(32), L.blocks - b0));
-  uint32_t scale = 0;
 #pragma unroll 1
-  for (int g = 0; g < n; g += 8) {
-    float v[8];
+  for (int g = 0; g < n; g += 8) {  // two groups of four blocks: their loads in flight together
+    float v[2][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const long long c = (long long)(b0 + g + i) * 32 + lane;
-      v[i] = c < a.C ? load1(row + c) : 0.f;
-    }
+    for (int k = 0; k < 2; ++k) load4(row, (long long)(b0 + g + 4 * k) * 32 + lane * 4, a.C, v[k]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t s = mx8_scale(__reduce_max_sync(0xffffffffu, mag(v[i])));
-      mx8_below_top<1>(v + i, s);
-      const uint32_t q = mx8_pair(v[i] * mx8_inverse(s), 0.f);
-      if (g + i < n) out[(g + i) * 32 + lane] = uint8_t(q);
-      if (lane == g + i) scale = s;
+    for (int k = 0; k < 2; ++k) {
+      uint32_t m = max(max(mag(v[k][0]), mag(v[k][1])), max(mag(v[k][2]), mag(v[k][3])));
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const uint32_t s = mx8_scale(m);
+      const float inv = mx8_inverse(s);
+      mx8_below_top<4>(v[k], s);
+      const int b = g + 4 * k + (lane >> 3);
+      if (b < n) {
+        *reinterpret_cast<uint32_t*>(out + (at + b) * 32 + (lane & 7) * 4) =
+            mx8_quad(v[k][0] * inv, v[k][1] * inv, v[k][2] * inv, v[k][3] * inv);
+        if ((lane & 7) == 0) out[L.scales() + at + b] = uint8_t(s);
+      }
     }
   }
-  if (lane < n) static_cast<uint8_t*>(a.q)[L.scales() + size_t(r) * L.blocks + b0 + lane] = uint8_t(scale);
 }
 
 template <typename T>
@@ -157,19 +203,25 @@ __global__ void __launch_bounds__(kThreads) mx8_dequantize_any_kernel(const __gr
   const uint8_t* q = static_cast<const uint8_t*>(a.q);
   const size_t at = size_t(r) * L.blocks + b0;
   const int n = int(min(size_t(32), L.blocks - b0));
-  const uint32_t scale = lane < n ? __ldg(q + L.scales() + at + lane) : 0u;
 #pragma unroll 1
   for (int g = 0; g < n; g += 8) {
-    uint32_t code[8];
+    uint32_t code[2] = {}, scale[2] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) code[i] = g + i < n ? __ldg(q + (at + g + i) * 32 + lane) : 0u;
+    for (int k = 0; k < 2; ++k) {
+      const int b = g + 4 * k + (lane >> 3);
+      if (b < n) {
+        code[k] = __ldg(reinterpret_cast<const uint32_t*>(q + (at + b) * 32 + (lane & 7) * 4));
+        scale[k] = __ldg(q + L.scales() + at + b);
+      }
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float unit = mx8_unit(__shfl_sync(0xffffffffu, scale, g + i));
+    for (int k = 0; k < 2; ++k) {
+      const float unit = mx8_unit(scale[k]);
       float v[4];
-      mx8_values(code[i], v);
-      const long long c = (long long)(b0 + g + i) * 32 + lane;
-      if (c < a.C) store1(row + c, v[0] * unit);
+      mx8_values(code[k], v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] *= unit;
+      store4(row, (long long)(b0 + g + 4 * k) * 32 + lane * 4, a.C, v);
     }
   }
 }

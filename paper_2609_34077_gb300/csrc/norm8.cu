@@ -113,7 +113,7 @@ __device__ __forceinline__ float team_sum(float s, int lg, float* part) {
 }
 
 template <typename T, int NG, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm8_kernel(const __grid_constant__ Norm8Args a, int lg) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1024 / THREADS) norm8_kernel(const __grid_constant__ Norm8Args a, int lg) {
   pdl_begin();
   __shared__ float2 part[32];
   const int lane = threadIdx.x & ((1 << lg) - 1), groups = a.d / 8;
@@ -209,7 +209,7 @@ using Raw = std::conditional_t<sizeof(T) == 2, RawBf16, RawF32>;
 
 template <typename T, bool X8, int NG, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? (X8 ? 4 : 2) : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a, int lg) {
-  pdl_begin();
+  pdl_wait();
   __shared__ float part[2][32];
   __shared__ float share[THREADS == 256 && NG == 1 ? 2048 : 1];  // several teams: [team][8 values of a thread]
   const int lane = threadIdx.x & ((1 << lg) - 1), team = threadIdx.x >> lg, teams = blockDim.x >> lg, groups = a.d / 8;
@@ -309,15 +309,20 @@ __global__ void __launch_bounds__(1024) norm_planes_kernel(const __grid_constant
 // How a row is shared out: 2^lg threads of 8 values, `steps` of them each.
 struct Teams {
   int lg, steps, threads;
-  explicit Teams(int d) {
+  // The forward's threads hold four steps from 8192 values on (two CTAs an SM, one of them storing while the other loads: 2000 x
+  // 16384 96 us where one CTA of 1024 threads takes 116); the gradient's have no registers for that below 16384.
+  Teams(int d, bool grad) {
     const int groups = d / 8;
     lg = 3;
     while (lg < 8 && (1 << lg) < groups) ++lg;  // up to 2048 values: one step
     steps = 1;
     if ((1 << lg) < groups) {
       steps = 2;
-      while (lg < 10 && (2 << lg) < groups) ++lg;
-      if ((2 << lg) < groups) steps = 4;
+      while (lg < (grad ? 10 : 9) && (2 << lg) < groups) ++lg;
+      if ((2 << lg) < groups) {
+        steps = 4;
+        while ((4 << lg) < groups) ++lg;
+      }
     }
     threads = lg > 8 ? 1 << lg : 256;
   }
@@ -326,17 +331,18 @@ struct Teams {
 
 template <typename T>
 cudaError_t forward(const Norm8Args& a, cudaStream_t s) {
-  const Teams t(a.d);
+  const Teams t(a.d, false);
   const dim3 grid{unsigned((a.T + t.rows() - 1) / t.rows())};
   auto* k = t.steps == 1 ? norm8_kernel<T, 1, 256>
-            : t.steps == 2 ? (t.threads == 256 ? norm8_kernel<T, 2, 256> : norm8_kernel<T, 2, 1024>)
-                           : norm8_kernel<T, 4, 1024>;
+            : t.steps == 2 ? (t.threads == 256 ? norm8_kernel<T, 2, 256> : norm8_kernel<T, 2, 512>)
+            : t.threads == 512 ? norm8_kernel<T, 4, 512>
+                               : norm8_kernel<T, 4, 1024>;
   return launch_pdl(k, grid, dim3(unsigned(t.threads)), 0, s, a, t.lg);
 }
 
 template <typename T, bool X8>
 cudaError_t backward(const NormGradArgs& a, cudaStream_t s) {
-  const Teams t(a.d);
+  const Teams t(a.d, true);
   const int planes = norm_grad_planes(a.T, a.d);
   auto* k = t.steps == 1 ? norm_grad_kernel<T, X8, 1, 256>
             : t.steps == 2 ? (t.threads == 256 ? norm_grad_kernel<T, X8, 2, 256> : norm_grad_kernel<T, X8, 2, 1024>)
@@ -356,7 +362,7 @@ cudaError_t launch_norm8(const Norm8Args& a, int dtype, cudaStream_t s) {
 }
 
 int norm_grad_planes(int T, int d) {
-  const Teams t(d);
+  const Teams t(d, true);
   const int rows = (T + t.rows() - 1) / t.rows(), most = num_sms() * (1024 / t.threads);
   return rows < most ? rows : most;
 }
