@@ -32,7 +32,8 @@
  *    cudaDeviceReset() destroys the context those addresses belong to: after one, no mcft call may
  *    be made on that device in the same process, and handles created before it are invalid.
  *  - Layouts are row-major. dtype MCFT_BF16 means bf16 x, weights and y (fp32 accumulation);
- *    MCFT_F32 means fp32 everywhere (CUDA-core arithmetic, no TF32).
+ *    MCFT_F32 means fp32 everywhere (CUDA-core arithmetic, no TF32; the products of mcft_ffn_* are
+ *    sums of products of bf16 parts that together hold the operands' 24 bits).
  */
 #ifndef MCFT_H
 #define MCFT_H

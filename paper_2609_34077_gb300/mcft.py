@@ -751,6 +751,12 @@ def mcft_moe_forward_mx4(desc: LayerDesc, x, idx, gate, experts, shared=(), y=No
     return y
 
 
+def _wants_here(*tensors):
+    """The library takes addresses on the current device: a tensor of another one, or of the host, is refused."""
+    here = torch.cuda.current_device()
+    _wants(all(t is None or t.get_device() == here for t in tensors), "every tensor is on the current CUDA device")
+
+
 def _size_of(call, *args) -> int:
     n = C.c_size_t(0)
     _check(call(*args, C.byref(n)))
@@ -773,6 +779,7 @@ def mcft_mx8_quantize(x, q=None, stream=None):
         q = _empty(rows * -(-cols // 32) * 33, torch.uint8, x.device, stream)
     else:
         _wants_mx8(q, rows, cols, "q is uint8 of mcft_mx8_size(rows, cols) bytes")
+    _wants_here(x, q)
     _check(lib().mcft_mx8_quantize(ptr, rows, cols, ld, _MX4_DTYPE[x.dtype], _ptr(q), _stream(stream)))
     return q
 
@@ -785,6 +792,7 @@ def mcft_mx8_dequantize(q, rows, cols, dtype=torch.bfloat16, y=None, stream=None
     else:
         _wants(y.shape == (rows, cols), "y is [rows, cols]")
     ptr, ld = _rows(y)
+    _wants_here(q, y)
     _check(lib().mcft_mx8_dequantize(_ptr(q), rows, cols, _MX4_DTYPE[y.dtype], ptr, ld, _stream(stream)))
     return y
 
@@ -815,6 +823,7 @@ def mcft_residual_rmsnorm_mx8(desc: LayerDesc, x, y=None, gamma=None, eps=1e-5, 
         rstd = _empty((T,), torch.float32, x.device, stream)
     else:
         _wants(_is(rstd, torch.float32, T), "rstd is fp32 [T]")
+    _wants_here(x, y, gamma, out, u, u8, x8, rstd)
     _check(lib().mcft_residual_rmsnorm_mx8(C.byref(desc), _ptr(x), _ptr(y), T, _ptr(gamma), C.c_float(eps), _ptr(out),
                                            _ptr(u), _ptr(u8), _ptr(x8), _ptr(rstd), _stream(stream)))
     return out, u, u8, rstd
@@ -847,6 +856,7 @@ def mcft_rmsnorm_grad(desc: LayerDesc, gamma, rstd, du, dres=None, x=None, x8=No
         _wants(_is(dgamma, torch.float32, d), "dgamma is fp32 [d]")
     if workspace is None:
         workspace = _empty(mcft_rmsnorm_grad_workspace_size(desc, T), torch.uint8, du.device, stream)
+    _wants_here(du, gamma, rstd, x, x8, dres, dx, dgamma, workspace)
     _check(lib().mcft_rmsnorm_grad(C.byref(desc), _ptr(x), _ptr(x8), _ptr(rstd), _ptr(gamma), _ptr(du), T, _ptr(dres),
                                    _ptr(dx), _ptr(dgamma), 1 if accumulate else 0, _ptr(workspace), _nbytes(workspace),
                                    _stream(stream)))
@@ -875,6 +885,7 @@ def mcft_ffn_forward(desc: LayerDesc, x, block, y=None, ckpt=None, workspace=Non
         _wants_mx8(ckpt, T, 2 * desc.w, "ckpt is uint8 of mcft_mx8_size(T, 2 w) bytes")
     if workspace is None:
         workspace = _empty(mcft_ffn_workspace_size(desc, T), torch.uint8, x.device, stream)
+    _wants_here(x, block, y, ckpt, workspace)
     _check(lib().mcft_ffn_forward(C.byref(desc), _ptr(x), T, _ptr(block), _ptr(y), _ptr(ckpt), _ptr(workspace),
                                   _nbytes(workspace), _stream(stream)))
     return y
@@ -909,6 +920,7 @@ def mcft_ffn_grad(desc: LayerDesc, dy, block, x=None, x8=None, ckpt=None, dx=Non
            and grad_dtype in (None, dblock.dtype), "dblock is [dW1 | dW3 | dW2], fp32 or of the layer dtype")
     if workspace is None:
         workspace = _empty(mcft_ffn_grad_workspace_size(desc, T), torch.uint8, dy.device, stream)
+    _wants_here(dy, block, x, x8, ckpt, dx, dblock, workspace)
     _check(lib().mcft_ffn_grad(C.byref(desc), _ptr(dy), T, _ptr(block), _ptr(x), _ptr(x8), _ptr(ckpt), _ptr(dx), _ptr(dblock),
                                _MX4_DTYPE[dblock.dtype], 1 if accumulate else 0, _ptr(workspace), _nbytes(workspace),
                                _stream(stream)))

@@ -11,7 +11,8 @@ from tests.test_gpu_canary import Guarded
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
-SHAPES = [(1, 64, 64), (1, 2048, 1408), (2, 192, 320), (4, 64, 4096), (5, 4096, 64), (16, 960, 704), (17, 128, 192), (64, 320, 128),
+# (1 to 8, 16 and 32 tokens by the weights' size: the streaming kernels, with clusters where there are few rows)
+SHAPES = [(1, 64, 64), (1, 2048, 1408), (8, 512, 2048), (9, 256, 64), (24, 64, 832), (32, 704, 1024), (33, 704, 1024), (9, 4096, 4096), (2, 192, 320), (4, 64, 4096), (5, 4096, 64), (16, 960, 704), (17, 128, 192), (64, 320, 128),
           (65, 64, 64), (65, 64, 4096), (127, 192, 448), (128, 256, 256), (129, 448, 192), (256, 512, 384), (257, 320, 704),
           (300, 1024, 1408), (1023, 960, 704), (3000, 64, 64), (2100, 512, 1408)]
 
@@ -241,3 +242,43 @@ def test_a_block_trained_from_its_checkpoints():
     assert rel(out, s.detach()) < 2.0 ** -7
     for got, leaf, room in zip((grad, *dblocks, *dgammas), leaves, (2, 2, 1, 2, 1)):
         assert rel(got, leaf.grad) < room * 2.0 ** -4
+
+
+def test_offsets_past_32_bits():
+    """70000 tokens by 2 x 30720: the checkpoint, dg and du pass 2^32 elements. The last tokens' rows are those of a call on them
+    alone up to the order of sums (both within their bounds of the oracle); dW sums over all tokens, of which only the last four
+    have a gradient."""
+    T, d, w, n = 70_000, 64, 30720, 4
+    c = Case(n, d, w, BF16)
+    D = desc(c)
+    x = torch.randn(T, d, device="cuda").to(BF16)
+    dy = torch.zeros(T, d, dtype=BF16, device="cuda")
+    x[-n:], dy[-n:] = c.x, c.dy
+    ckpt = torch.empty(M.mcft_mx8_size(T, 2 * w), dtype=torch.uint8, device="cuda")
+    y = M.mcft_ffn_forward(D, x, c.block, ckpt=ckpt)
+    near(y[-n:], *c.forward(), "y")
+    gu = M.mcft_mx8_dequantize(ckpt, T, 2 * w, BF16)[-n:]
+    g, u, eg, eu = c.projections(f64(c.x))
+    want, room = np.concatenate((g, u), 1), np.concatenate((eg, eu), 1)
+    near(gu, want, room + 0.5 * oracle.dense.mx8_step(np.abs(want) + room), "checkpoint")
+    dx, db = M.mcft_ffn_grad(D, dy, c.block, x=x, ckpt=ckpt)
+    gu = f64(gu)
+    (wx, rx), (wb, rb) = c.gradient(f64(c.x), gu[:, :w], gu[:, w:])
+    near(dx[-n:], wx, rx, "dx")
+    near(db, wb, rb, "dblock")
+    assert not dx[:-n].any()
+    M.mcft_device_error()
+
+
+def test_tensors_of_the_host_are_refused():
+    c = Case(5, 128, 192, BF16)
+    D = desc(c)
+    gamma = torch.ones(128, dtype=BF16, device="cuda")
+    calls = [lambda: M.mcft_mx8_quantize(c.x.cpu()), lambda: M.mcft_mx8_dequantize(M.mcft_mx8_quantize(c.x).cpu(), 5, 128),
+             lambda: M.mcft_ffn_forward(D, c.x, c.block.cpu()), lambda: M.mcft_ffn_grad(D, c.dy, c.block, x=c.x.cpu()),
+             lambda: M.mcft_residual_rmsnorm_mx8(D, c.x.float(), None, gamma.cpu()),
+             lambda: M.mcft_rmsnorm_grad(D, gamma, torch.ones(5), c.dy, x=c.x.float())]
+    for i, call in enumerate(calls):
+        with pytest.raises(M.MCFTError) as e:
+            call()
+        assert e.value.status == M.MCFT_ERR_INVALID, i

@@ -206,3 +206,26 @@ def test_same_bits_on_a_stream_and_replayed(T, d):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(kept, want))
     M.mcft_device_error()
+
+
+def test_offsets_past_32_bits():
+    T, d = 132_000, 32768  # 4.3e9 values
+    D = desc_of(d, BF16)
+    x = torch.zeros(T, d, device="cuda")
+    last, _, gamma, du, _ = (t.cuda() for t in make(2, d, BF16, 5))
+    x[-2:] = last
+    u8 = torch.empty(M.mcft_mx8_size(T, d), dtype=torch.uint8, device="cuda")
+    M._check(M.lib().mcft_residual_rmsnorm_mx8(M.C.byref(D), x.data_ptr(), None, T, gamma.data_ptr(), M.C.c_float(1e-5), None, None,
+                                               u8.data_ptr(), None, None, M._stream(None)))
+    _, _, want, rstd = M.mcft_residual_rmsnorm_mx8(D, last, None, gamma)
+    n = T * d
+    assert torch.equal(u8[n - 2 * d: n], want[:2 * d]) and torch.equal(u8[n + n // 32 - d // 16:], want[2 * d:])
+    del u8
+    grad, dg = M.mcft_rmsnorm_grad(D, gamma, rstd, du, x=last)
+    big = torch.zeros(T, d, dtype=BF16, device="cuda")
+    big[-2:] = du
+    r = torch.ones(T, device="cuda")
+    r[-2:] = rstd
+    M.mcft_rmsnorm_grad(D, gamma, r, big, x=x, dx=x)
+    assert torch.equal(x[-2:], grad) and not x[:100].any()
+    M.mcft_device_error()
