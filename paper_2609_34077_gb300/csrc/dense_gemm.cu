@@ -2,7 +2,7 @@
 // accumulators), with what follows each in its epilogue:
 //   up       g = x W1^T, u = x W3^T;                h = silu(g) u, and mx8 checkpoints of g and u
 //   up_grad  dh = dy W2;                            dg, du, h from dh and the checkpoints
-//   both     g, u and dh of a tile one after the other, dg, du and h from them: the gradient without checkpoints
+//   both     dh, g and u of a tile one after the other, dg, du and h from them: the gradient without checkpoints
 //   out      C = A B of up to three problems: y = h W2^T, or dx = [dg | du] [W1 ; W3], d[W1 ; W3] = [dg | du]^T x and
 //            dW2 = dy^T h in one launch, whose tiles fill the SMs together.
 // A tile is 256 rows x 256 or 128 columns (up: half of them of g, the same ones of u), one MMA of M = 256 a step, issued by the
@@ -49,15 +49,15 @@ template <int EPI>
 constexpr int kShares = EPI == EPI_UP_GRAD || EPI == EPI_PARTS ? 4 : 2;
 template <int EPI>
 constexpr int kThreads = 64 + 128 * kShares<EPI>;
-// up_grad's rows go to memory through 3 KB of shared memory a warp and TMA: a lane's own row in 64-byte stores keeps the way to L1
+// up_grad's rows go to memory through 2 KB of shared memory a warp and TMA: a lane's own row in 64-byte stores keeps the way to L1
 // busy (rows 4 or 8 KB apart meet in few sets). The others' epilogues end before their products, for which the stages that the
 // room would cost count more (five in place of seven: up 49 -> 53 us at 1000 x 4096 x 4096).
 template <int EPI>
-constexpr int kStageOut = EPI == EPI_UP_GRAD ? 3072 : 0;
+constexpr int kStageOut = EPI == EPI_UP_GRAD ? 2048 : 0;
 template <int EPI>
 constexpr int kStaging = kStageOut<EPI> * 4 * kShares<EPI>;
 template <int EPI>
-constexpr int kRingBytes = 7 * (EPI == EPI_UP_GRAD ? 24576 : 32768);
+constexpr int kRingBytes = (EPI == EPI_UP_GRAD ? 6 : 7) * 32768;
 
 struct Problem {
   CUtensorMap a, b, b1;  // b1: rank 1's columns of an up tile
@@ -164,7 +164,7 @@ __device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-// A warp's way to memory: three pieces of 1 KB, boxes of 32 rows by 32 bytes, sent together.
+// A warp's way to memory: two pieces of 1 KB, boxes of 32 rows by 32 bytes.
 struct Stage {
   uint32_t addr;  // shared memory, on 1024 bytes
   // Once the last boxes have been read.
@@ -256,11 +256,15 @@ struct Grads {
     st.free();
     st.put(0, h);
     st.put(1, dg);
-    st.put(2, du);
     if (st.ready()) {
       st.send(0, &q.to_h, col, row0);
       st.send(1, &q.to_dgu, col, row0);
-      st.send(2, &q.to_dgu, q.w + col, row0);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    st.free();
+    st.put(0, du);
+    if (st.ready()) {
+      st.send(0, &q.to_dgu, q.w + col, row0);
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
   }
@@ -327,7 +331,7 @@ __device__ __forceinline__ void put_out(const Item& t, int row, int col, uint32_
 }
 
 template <int EPI>
-__device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_t taddr, int row, int half) {
+__device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_t taddr, int row, int half, int dh_turn) {
   const Problem& p = *t.p;
   const bool in = row < p.M;
   const size_t r = size_t(in ? row : 0);
@@ -362,7 +366,7 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
       uint32_t g[32], u[32], dh[32];
       tmem_ld32(taddr + c, g);
       tmem_ld32(taddr + q.cols / 2 + c, u);
-      tmem_ld32(taddr + q.cols + c, dh);
+      tmem_ld32(taddr + q.cols + dh_turn * (q.cols / 2) + c, dh);
       tmem_ld_wait();
       put_grads(q, in, r, col, reinterpret_cast<const float*>(g), reinterpret_cast<const float*>(u), dh);
     }
@@ -507,12 +511,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
       for (int item = cid; item < items && !*abort; item += ncl) {
         const Item t = item_at(q, item);
         const int arow = t.mt * kTile + int(rank) * 128;
-        // both: x by [W1 ; W3], then dy by W2, whose columns are half as many
+        // both: dy by W2, whose columns are half as many, then x by [W1 ; W3]
         for (int phase = 0; phase < (EPI == EPI_BOTH ? 2 : 1); ++phase) {
-          const Problem* p = EPI == EPI_BOTH ? &q.p[phase] : t.p;
-          const bool up = EPI == EPI_UP || (EPI == EPI_BOTH && phase == 0), back = EPI == EPI_UP_GRAD || (EPI == EPI_BOTH && phase == 1);
+          const Problem* p = EPI == EPI_BOTH ? &q.p[1 - phase] : t.p;
+          const bool up = EPI == EPI_UP || (EPI == EPI_BOTH && phase), back = EPI == EPI_UP_GRAD || (EPI == EPI_BOTH && !phase);
           const CUtensorMap* mb = up && rank ? &p->b1 : &p->b;
-          const int b_cols = EPI == EPI_BOTH && phase ? half_cols / 2 : half_cols;
+          const int b_cols = EPI == EPI_BOTH && back ? half_cols / 2 : half_cols;
           const int brow = up ? t.nt * half_cols : EPI == EPI_BOTH ? t.nt * half_cols + int(rank) * b_cols : t.nt * q.cols + int(rank) * half_cols;
           const bool a_mn = EPI >= EPI_OUT && p->a_mn, b_mn = back || (EPI >= EPI_OUT && p->b_mn);
           const uint32_t bytes = 2u * uint32_t(b_cols * BK * 2) + uint32_t(q.a_rows ? a_bytes : 2 * a_bytes);
@@ -563,17 +567,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
         for (int k0 = t.k0; k0 < t.k1 && ok; k0 = EPI == EPI_PARTS ? k0 + kRun : t.k1) {
           const int n = EPI == EPI_PARTS ? kPasses * min(kRun, t.k1 - k0) : t.k1 - k0;
           const uint32_t b = EPI == EPI_BOTH ? 0u : lt & 1u, turn = EPI == EPI_BOTH ? lt : lt >> 1;
-          if (!mbar_wait_cl(&ctl->tempty[b], (turn & 1u) ^ 1u, abort, q.err)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
           for (int phase = 0; phase < (EPI == EPI_BOTH ? 2 : 1) && ok; ++phase) {
-            const bool b_mn = EPI == EPI_UP_GRAD || (EPI == EPI_BOTH && phase == 1) || (EPI >= EPI_OUT && t.p->b_mn);
-            const int cols = EPI == EPI_BOTH && phase ? half_cols : q.cols;
+            // (both: the epilogue before last is done with this dh, or the last one's g and u would not have been begun)
+            const bool back = EPI == EPI_BOTH && phase == 0;
+            if (!back) {
+              ok = mbar_wait_cl(&ctl->tempty[b], (turn & 1u) ^ 1u, abort, q.err);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            const bool b_mn = EPI == EPI_UP_GRAD || back || (EPI >= EPI_OUT && t.p->b_mn);
+            const int cols = back ? half_cols : q.cols;
             const uint32_t idesc = kIdesc | (uint32_t(cols >> 3) << 17) | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u);
             const uint64_t kb_ = b_mn ? (16 * 128) >> 4 : 32 >> 4;
-            const uint32_t dt = tmem + (EPI == EPI_BOTH ? uint32_t(phase * q.cols) : b * kTile);
+            const uint32_t dt = tmem + (back ? uint32_t(q.cols) + (lt & 1u) * uint32_t(half_cols) : b * kTile);
             for (int i = 0; i < n; ++i) {
               if (!mbar_wait_cl(&ctl->full[s], ph, abort, q.err)) {
                 ok = false;
@@ -662,7 +668,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
         end();
       } else {
         if (!begin(taddr)) break;
-        epilogue<EPI>(q, t, taddr, row, half);
+        epilogue<EPI>(q, t, taddr, row, half, int(lt & 1u));
         end();
       }
     }
