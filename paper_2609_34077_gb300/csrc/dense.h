@@ -80,9 +80,17 @@ struct DenseSplitArgs {
 };
 cudaError_t launch_dense_split(const DenseSplitArgs& a, cudaStream_t s);
 
-// Sum of `n` fp32 planes [count] into out.
-cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* out, int out_dtype, int accumulate,
-                              cudaStream_t s);
+// Sums of fp32 planes, n of [count] each, into out: those of a launch's products together.
+struct DenseJoinArgs {
+  struct {
+    const float* planes;
+    void* out;
+    size_t count;
+    int n, out_f32, accumulate, blocks;  // blocks: CTAs, filled in
+  } p[kMaxProducts];
+  int products;
+};
+cudaError_t launch_dense_join(const DenseJoinArgs& a, cudaStream_t s);
 
 // Gate and up projections of [W1 ; W3] and what follows them, bf16: h = silu(g) u [T, w].
 struct DenseUpArgs {

@@ -907,10 +907,18 @@ cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes,
     p.wide = p.splits > 1 ? wide(planes) : wide(d.out);
   }
   cudaError_t e = passes > 1 ? launch<EPI_PARTS>(q, kProfDenseOut, s) : launch<EPI_OUT>(q, kProfDenseOut, s);
-  for (int i = 0; i < n && e == cudaSuccess; ++i)
-    if (q.p[i].splits > 1)
-      e = launch_dense_join(q.p[i].planes, q.p[i].splits, size_t(in[i].rows) * in[i].cols, in[i].out, in[i].out_dtype,
-                            in[i].accumulate, s);
+  DenseJoinArgs join{};
+  for (int i = 0; i < n; ++i) {
+    if (q.p[i].splits == 1) continue;
+    auto& j = join.p[join.products++];
+    j.planes = q.p[i].planes;
+    j.out = in[i].out;
+    j.count = size_t(in[i].rows) * in[i].cols;
+    j.n = q.p[i].splits;
+    j.out_f32 = in[i].out_dtype == MCFT_F32;
+    j.accumulate = in[i].accumulate;
+  }
+  if (e == cudaSuccess && join.products) e = launch_dense_join(join, s);
   return e;
 }
 

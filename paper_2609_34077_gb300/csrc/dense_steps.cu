@@ -44,41 +44,50 @@ __global__ void __launch_bounds__(256) dense_split_kernel(const __grid_constant_
   put_parts(a.parts[k] + at, a.n[k], v);
 }
 
-// out = sum of n planes, in order (+ out): four values a thread.
-template <typename T>
-__global__ void __launch_bounds__(256) dense_join_kernel(const float* planes, int n, size_t count, void* out, int accumulate) {
+// out = sum of n planes (+ out), four values a thread: slice i of SLICES adds planes i, i + SLICES, .. in order, and the first adds
+// the slices' sums in order. One slice for all planes of a few values waits for one load after another (two joins of 6 rows, width
+// 10368: 16 us by one slice, 12 by eight); many values fill the SMs by themselves (512 x 2048 and as many more: 15 us by one slice,
+// 25 by two).
+template <int SLICES>
+__global__ void __launch_bounds__(256) dense_join_kernel(const __grid_constant__ DenseJoinArgs a) {
   pdl_begin();
-  const size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (i >= count) return;
+  __shared__ float4 part[SLICES > 1 ? 256 : 1];
+  int k = 0, block = int(blockIdx.x);
+  while (k + 1 < a.products && block >= a.p[k].blocks) block -= a.p[k++].blocks;
+  const auto p = a.p[k];
+  constexpr int across = 256 / SLICES;
+  const int slice = int(threadIdx.x) / across, lane = int(threadIdx.x) - slice * across;
+  const size_t i = (size_t(block) * across + lane) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int k = 0; k < n; ++k) {
-    const float4 v = *reinterpret_cast<const float4*>(planes + size_t(k) * count + i);
+  auto add = [&](const float4& v) {
     s.x += v.x;
     s.y += v.y;
     s.z += v.z;
     s.w += v.w;
+  };
+  if (i < p.count) {
+#pragma unroll 4
+    for (int n = slice; n < p.n; n += SLICES) add(*reinterpret_cast<const float4*>(p.planes + size_t(n) * p.count + i));
   }
-  if constexpr (sizeof(T) == 2) {
-    uint2* to = reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + i);
-    if (accumulate) {
+  if constexpr (SLICES > 1) {
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (slice) return;
+#pragma unroll
+    for (int n = 1; n < SLICES; ++n) add(part[n * across + lane]);
+  }
+  if (i >= p.count) return;
+  if (p.out_f32) {
+    float4* to = reinterpret_cast<float4*>(static_cast<float*>(p.out) + i);
+    if (p.accumulate) add(*to);
+    *to = s;
+  } else {
+    uint2* to = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + i);
+    if (p.accumulate) {
       const uint2 o = *to;
-      s.x += bf16lo(o.x);
-      s.y += bf16hi(o.x);
-      s.z += bf16lo(o.y);
-      s.w += bf16hi(o.y);
+      add(make_float4(bf16lo(o.x), bf16hi(o.x), bf16lo(o.y), bf16hi(o.y)));
     }
     *to = make_uint2(pack2bf(s.x, s.y), pack2bf(s.z, s.w));
-  } else {
-    float4* to = reinterpret_cast<float4*>(static_cast<float*>(out) + i);
-    if (accumulate) {
-      const float4 o = *to;
-      s.x += o.x;
-      s.y += o.y;
-      s.z += o.z;
-      s.w += o.w;
-    }
-    *to = s;
   }
 }
 
@@ -175,13 +184,24 @@ __global__ void __launch_bounds__(256) dense_place_kernel(const __grid_constant_
 
 }  // namespace
 
-cudaError_t launch_dense_join(const float* planes, int n, size_t count, void* out, int out_dtype, int accumulate,
-                              cudaStream_t s) {
+cudaError_t launch_dense_join(const DenseJoinArgs& args, cudaStream_t s) {
+  DenseJoinArgs a = args;
+  int most = 1, blocks = 0;
+  size_t threads = 0;
+  for (int i = 0; i < a.products; ++i) {
+    most = most > a.p[i].n ? most : a.p[i].n;
+    threads += a.p[i].count / 4;
+  }
+  const int slices = threads > 40000 ? 1 : most > 4 ? 8 : most > 2 ? 4 : 2;
+  for (int i = 0; i < a.products; ++i) {
+    a.p[i].blocks = int((a.p[i].count / 4 + 256 / slices - 1) / (256 / slices));
+    blocks += a.p[i].blocks;
+  }
   prof_begin(kProfDenseJoin, s);
-  const dim3 grid{unsigned((count / 4 + 255) / 256)};
-  const cudaError_t e = out_dtype == MCFT_BF16
-      ? launch_pdl(dense_join_kernel<uint16_t>, grid, dim3(256), 0, s, planes, n, count, out, accumulate)
-      : launch_pdl(dense_join_kernel<float>, grid, dim3(256), 0, s, planes, n, count, out, accumulate);
+  const auto kernel = slices == 1 ? dense_join_kernel<1> : slices == 2 ? dense_join_kernel<2>
+                                : slices == 4           ? dense_join_kernel<4>
+                                                        : dense_join_kernel<8>;
+  const cudaError_t e = launch_pdl(kernel, dim3(unsigned(blocks)), dim3(256), 0, s, a);
   prof_end(kProfDenseJoin, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
