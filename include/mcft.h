@@ -577,8 +577,9 @@ mcft_status mcft_route_scored_grad(const mcft_scored_desc* desc, const void* x, 
  *
  * A block of 32 values along a row is 32 e4m3 codes and one scale, the smallest power of two 2^s with max|x| <= 448 * 2^s,
  * s in [-127, 127], held as s + 127 in a byte. Codes round to nearest even, none saturates (but values that would round to
- * 2^128 are held as 1.875 * 2^127). A block with a NaN or an infinity has the scale byte 0xff and reads back as NaN. An mx8 matrix [rows, cols] is row-major codes [rows, Cp], Cp = cols
- * rounded up to 32 (codes past cols are 0), then row-major scales [rows, Cp / 32]: mcft_mx8_size bytes, 16-byte aligned.
+ * 2^128 are held as 1.875 * 2^127). A block with a NaN or an infinity has the scale byte 0xff and reads back as NaN. An mx8
+ * matrix [rows, cols] is row-major codes [rows, Cp], Cp = cols rounded up to 32 (codes past cols are 0), then row-major scales
+ * [rows, Cp / 32]: mcft_mx8_size bytes, 16-byte aligned.
  *
  * mcft_mx8_quantize: x device [rows, cols] of dtype (MCFT_F32 or MCFT_BF16), `ld` elements from row to row, any
  *   alignment of its type (rows on 32 bytes are read faster); q device, mcft_mx8_size bytes out.
@@ -640,8 +641,8 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones), and six
  * products of them on the tensor cores make each fp32 one, in fp32 sums of short runs; few tokens take CUDA-core fp32
  * arithmetic. T = 0 is a no-op. Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID
- * for a NULL or misaligned pointer (16 bytes), a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for T > 2^24 or
- * d or w > 2^20. */
+ * for a NULL or misaligned pointer (16 bytes), y at x's address, a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED
+ * for T > 2^24 or d or w > 2^20. */
 mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
 mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, const void* block, void* y,
                              void* ckpt, void* workspace, size_t ws_bytes, mcft_stream_t stream);
@@ -659,9 +660,10 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
  *             accumulate is non-zero; or NULL (then x and x8 may both be NULL beside a ckpt)
  *   workspace device, mcft_ffn_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
- * bf16 layers: dg, du and h are rounded to bf16 as operands, sums are fp32. T = 0 writes zeros to dblock (unless
- * accumulating). Asynchronous; the same bits whenever the inputs are the same. Errors as above, and for dx and dblock both
- * NULL or another grad_dtype. */
+ * Neither output may overlap an input or the other: both are written while the inputs are read. bf16 layers: dg, du and h are
+ * rounded to bf16 as operands, sums are fp32. T = 0 writes zeros to dblock (unless accumulating). Asynchronous; the same bits
+ * whenever the inputs are the same. Errors as above, and for dx and dblock both NULL, another grad_dtype, or an output at an
+ * input's address. */
 mcft_status mcft_ffn_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
 mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, const void* block, const void* x,
                           const void* x8, const void* ckpt, void* dx, void* dblock, int grad_dtype,

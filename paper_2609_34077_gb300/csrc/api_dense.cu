@@ -270,6 +270,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   const ForwardLayout L = forward_layout(desc, T);
   st = check_workspace(workspace, ws_bytes, L.total);
   if (st != MCFT_OK) return st;
+  if (y == x) return fail(MCFT_ERR_INVALID, "y may not be x");
   char* ws = static_cast<char*>(workspace);
   cudaError_t e;
   if (!ckpt && (desc->dtype == MCFT_F32 ? T <= kFewTokensF32 : few_tokens(T, size_t(3) * desc->w * desc->d))) {
@@ -340,6 +341,10 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   const GradLayout L = grad_layout(desc, T);
   st = check_workspace(workspace, ws_bytes, L.total);
   if (st != MCFT_OK) return st;
+  for (const void* out : {static_cast<const void*>(dx), static_cast<const void*>(dblock)})
+    if (out && (out == dy || out == block || out == x || out == x8 || out == ckpt))
+      return fail(MCFT_ERR_INVALID, "dx and dblock may not be inputs");
+  if (dx == dblock) return fail(MCFT_ERR_INVALID, "dx and dblock are the same");
   char* ws = static_cast<char*>(workspace);
   const size_t eb = elem(desc->dtype);
   const char* w13 = static_cast<const char*>(block);

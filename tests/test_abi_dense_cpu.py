@@ -129,6 +129,19 @@ def test_refusals_of_its_gradient_too():
     assert call(T=0, dy=None, block=None, x=None, ckpt=None, dblock=None, ws=None) == M.MCFT_OK
 
 
+def test_outputs_at_an_inputs_address_are_refused():
+    at = [C.c_void_p(1 << 20 | i << 12) for i in range(9)]
+    n, D = 1 << 40, C.byref(desc())
+    x, block, y, ckpt, ws = at[:5]
+    assert M.lib().mcft_ffn_forward(D, x, 3, block, x, ckpt, ws, n, None) == BAD
+    assert b"y may not be x" in M.lib().mcft_last_error()
+    dx, dblock = at[5:7]
+    for out in ((y, dblock), (dx, y), (x, dblock), (dx, x), (dx, block), (ckpt, dblock), (dx, dx)):
+        assert M.lib().mcft_ffn_grad(D, y, 3, block, x, None, ckpt, *out, M.MCFT_BF16, 0, ws, n, None) == BAD
+        assert b"may not be inputs" in M.lib().mcft_last_error() or b"are the same" in M.lib().mcft_last_error()
+    assert M.lib().mcft_ffn_grad(D, y, 3, block, None, x, ckpt, x, None, M.MCFT_BF16, 0, ws, n, None) == BAD
+
+
 def test_the_binding_refuses_tensors_of_other_sizes():
     D, b, f = desc(), torch.bfloat16, torch.float32
     x, block, g = torch.zeros(5, 128, dtype=b), torch.zeros(3 * 128 * 192, dtype=b), torch.zeros(128, dtype=b)
