@@ -119,7 +119,7 @@ GradLayout grad_layout(const mcft_layer_desc* d, int T) {
     L.x = s.add(t * D * 6);
     L.dy = s.add(t * D * 6);
     L.block = s.add(3 * w * D * 6);
-    planes = std::max(planes, dense_plane_bytes(t * 2 * w, d->d));
+    planes = std::max(planes, dense_plane_bytes(t * 3 * w, d->d));
   }
   L.planes = s.add(planes);
   L.total = s.total;
@@ -379,14 +379,11 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
     xs = x3;
     dys = dy3;
     w13s = block3;
-    if (e == cudaSuccess && gu) {
-      const DenseProduct up{xs, w13s, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0, part_x, part_w};
-      e = products(&up, 1, planes, stream);
-    }
     float* dh = reinterpret_cast<float*>(ws + L.dh);
     if (e == cudaSuccess) {
-      const DenseProduct back{dys, block3 + 2 * wd, T, w, d, 0, 0, dh, MCFT_F32, 0, part_x, part_w};
-      e = products(&back, 1, planes, stream);
+      const DenseProduct back_up[2] = {{dys, block3 + 2 * wd, T, w, d, 0, 0, dh, MCFT_F32, 0, part_x, part_w},
+                                       {xs, w13s, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0, part_x, part_w}};
+      e = products(back_up, gu ? 2 : 1, planes, stream);
     }
     if (e == cudaSuccess)
       e = launch_dense_act_grad(DenseActArgs{gu, static_cast<const uint8_t*>(ckpt), dh, reinterpret_cast<uint16_t*>(ws + L.h),
