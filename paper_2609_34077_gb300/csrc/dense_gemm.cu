@@ -784,6 +784,40 @@ Plan choose(const Sizes* z, int n, int up, bool splittable, int passes, int pair
   return best;
 }
 
+// A product whose last round of tiles would leave many pairs idle: its last row tiles as a product of their own, in parts that
+// are short enough to fill that round (rows: of the tail; 0: none). Only there are planes to be joined: y of 4096 x 4096 by
+// 14336 293 us without, 258 + 6 with; 5000 x 1024 by 4096 48 and 36 + 5. Rows' sums then differ in their order, by where they are.
+struct Tail {
+  int rows, per;
+};
+Tail tail_of(const Sizes& z, const Plan& plan, int passes, int pairs) {
+  Tail best{0, 0};
+  const int mt = (z.M + kTile - 1) / kTile, nt = (z.N + plan.cols - 1) / plan.cols;
+  const long long tiles = (long long)mt * nt;
+  if (plan.per[0] < z.kblocks || tiles <= pairs || tiles > 16ll * pairs) return best;
+  const double step = passes * (plan.cols == kTile ? 1.0 : 0.78);
+  double least = 0.97 * step * z.kblocks * double((tiles + pairs - 1) / pairs);
+  for (int m = 1; m < mt && m * nt <= 2 * pairs; ++m) {
+    const int rows = z.M - (mt - m) * kTile, first = (mt - m) * nt;
+    for (int parts = 2; parts <= 4; ++parts) {
+      const int per = (z.kblocks + parts - 1) / parts, made = (z.kblocks + per - 1) / per, all = first + m * nt * made;
+      const size_t planes = size_t(made) * rows * z.N;
+      if (per < 2 * kLeastPart || planes > size_t(pairs) * kPlaneTiles * kTile * kTile) continue;
+      double longest = 0;
+      for (int i = 0; i < pairs; ++i) {
+        const int whole = (first - i + pairs - 1) / pairs, items = (all - i + pairs - 1) / pairs;
+        longest = std::max(longest, step * (double(whole) * z.kblocks + double(items - whole) * per));
+      }
+      const double time = longest + kJoin + double(planes) * 8 / 1.7e6;
+      if (time < least) {
+        least = time;
+        best = Tail{rows, per};
+      }
+    }
+  }
+  return best;
+}
+
 // Rows of A (as they lie in memory: K-major) of a launch's first CTAs, where that is all there are.
 int few_rows(int M) { return M <= 128 ? (M + 7) & ~7 : 0; }
 
@@ -876,10 +910,25 @@ namespace {
 cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes, cudaStream_t s) {
   Params q;
   memset(&q, 0, sizeof(q));
-  q.n = n;
   Sizes z[kMaxProducts];
   for (int i = 0; i < n; ++i) z[i] = Sizes{in[i].rows, in[i].cols, (in[i].k + BK - 1) / BK};
-  const Plan plan = choose(z, n, 0, true, passes, num_sms() / 2);
+  Plan plan = choose(z, n, 0, true, passes, num_sms() / 2);
+  DenseProduct two[2];
+  if (n == 1 && !in[0].a_t) {
+    const Tail tail = tail_of(z[0], plan, passes, num_sms() / 2);
+    if (tail.rows) {
+      two[0] = two[1] = in[0];
+      const size_t rows = size_t(in[0].rows - tail.rows), elem = in[0].out_dtype == MCFT_F32 ? 4 : 2;
+      two[0].rows = int(rows);
+      two[1].rows = tail.rows;
+      two[1].a = static_cast<const uint16_t*>(in[0].a) + rows * in[0].k;
+      two[1].out = static_cast<char*>(in[0].out) + rows * in[0].cols * elem;
+      plan.per[1] = tail.per;
+      in = two;
+      n = 2;
+    }
+  }
+  q.n = n;
   q.cols = plan.cols;
   size_t used = 0;
   for (int i = 0; i < n; ++i) {

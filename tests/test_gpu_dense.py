@@ -90,6 +90,21 @@ def test_gradient(T, d, w, dtype, form):
         assert bool((outs[skip] == 3.0).all())
 
 
+@pytest.mark.parametrize("T,d,w,dtype", [(19999, 64, 2048, BF16), (19999, 64, 1024, F32)])
+def test_last_row_tiles_in_parts(T, d, w, dtype):
+    """One round of tiles and a little more: the last ones' sums are split and joined."""
+    c = Case(T, d, w, dtype)
+    D = desc(c)
+    guards = [Guarded(T * d * c.x.element_size()), Guarded(M.mcft_ffn_workspace_size(D, T))]
+    y = M.mcft_ffn_forward(D, c.x, c.block, y=guards[0].view(dtype, (T, d)), workspace=guards[1].view())
+    M.mcft_device_error()
+    for g in guards:
+        g.check("forward")
+    near(y, *c.forward(), "y")
+    again = M.mcft_ffn_forward(D, c.x, c.block)
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("T,d,w", [(3, 128, 192), (200, 320, 448)])
 def test_buffers_on_16_bytes(T, d, w):
     """Every tensor 16 bytes past a 32-byte boundary: the same bits."""
