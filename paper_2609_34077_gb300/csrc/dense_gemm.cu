@@ -7,14 +7,18 @@
 //            dW2 = dy^T h in one launch, whose tiles fill the SMs together.
 // A tile is 256 rows x 256 or 128 columns (up: half of them of g, the same ones of u), one MMA of M = 256 a step, issued by the
 // pair's leader over both CTAs' shared memory: each CTA brings in its 128 rows of A and its half of B's columns, 64 of the
-// contraction a stage, 7 stages of 32 KB or 9 of 24. Operands are taken as they lie in memory: one whose contiguous index is the contraction's is a
-// K-major operand (a box of 64 x 128), another an MN-major one (two boxes of 64 x 64), so nothing is transposed.
+// contraction a stage, 7 stages of 32 KB or 9 of 24 (up_grad: 6 or 8; few rows: up to 16). Operands are taken as they lie in
+// memory: one whose contiguous index is the contraction's is a K-major operand (a box of 64 x 128), another an MN-major one (two
+// boxes of 64 x 64), so nothing is transposed.
 //   warp 0 (both CTAs) copies; the loads of both complete on the leader's full[s];
 //   warp 1 of the leader issues the MMAs; their commits arrive on empty[s] and tfull[b] of both CTAs;
 //   the other warps (both CTAs) are the epilogue of the CTA's 128 rows, a row a lane: four lane quarters of TMEM by shares of
 //   the columns, 32 columns (one mx8 block) at a time. Two accumulators of 256 columns let the next tile's MMAs run meanwhile.
 // A persistent grid strides over the tiles, rows fastest inside groups of row tiles that share L2. Tiles of problems that do
 // not fill the pairs are split along the contraction into fp32 planes, which dense_join_kernel adds up in order.
+// Bound by the tensor pipe where there are rows enough, by HBM for few. Measured in bursts, TFLOP/s: 4096 tokens, 4096 x 14336 up
+// 1910 and y 1770; 4096 x 8192 up with a checkpoint 1780, up_grad 1450, both 1630, dx and the block's gradient 1730; parts (1024
+// tokens, 2048 x 4096 fp32) 1660 of bf16 products. 16 tokens, 4096 x 14336: 46 + 30 us, 5.1 and 3.9 TB/s with both ends of the launches.
 // Rows and columns past a matrix's end are zeros that TMA fills in, and are not stored.
 // Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (bounded) for its copies and MMAs
 // in flight, frees TMEM and returns.

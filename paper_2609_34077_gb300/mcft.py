@@ -754,7 +754,9 @@ def mcft_moe_forward_mx4(desc: LayerDesc, x, idx, gate, experts, shared=(), y=No
 def _wants_here(*tensors):
     """The library takes addresses on the current device: a tensor of another one, or of the host, is refused."""
     here = torch.cuda.current_device()
-    _wants(all(t is None or t.get_device() == here for t in tensors), "every tensor is on the current CUDA device")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            _wants(False, "every tensor is on the current CUDA device")
 
 
 def _size_of(call, *args) -> int:
