@@ -90,6 +90,24 @@ def test_gradient(T, d, w, dtype, form):
         assert bool((outs[skip] == 3.0).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [5, 300])
+def test_input_gradient_from_the_checkpoint_alone(T, dtype):
+    """dx wants neither x nor its mx8 matrix beside a checkpoint."""
+    c = Case(T, 192, 320, dtype)
+    D = desc(c)
+    ckpt = torch.empty(M.mcft_mx8_size(T, 640), dtype=torch.uint8, device="cuda")
+    M.mcft_ffn_forward(D, c.x, c.block, ckpt=ckpt)
+    ws = torch.empty(M.mcft_ffn_grad_workspace_size(D, T), dtype=torch.uint8, device="cuda")
+    dx = torch.empty_like(c.x)
+    M._check(M.lib().mcft_ffn_grad(M.C.byref(D), c.dy.data_ptr(), T, c.block.data_ptr(), None, None, ckpt.data_ptr(), dx.data_ptr(),
+                                   None, M.MCFT_F32, 0, ws.data_ptr(), ws.numel(), M._stream(None)))
+    M.mcft_device_error()
+    gu = f64(M.mcft_mx8_dequantize(ckpt, T, 640, F32))
+    (want, room), _ = c.gradient(f64(c.x), gu[:, :320], gu[:, 320:])
+    near(dx, want, room, "dx")
+
+
 @pytest.mark.parametrize("T,d,w,dtype", [(19999, 64, 2048, BF16), (19999, 64, 1024, F32)])
 def test_last_row_tiles_in_parts(T, d, w, dtype):
     """One round of tiles and a little more: the last ones' sums are split and joined."""

@@ -83,6 +83,14 @@ def test_forward(T, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,d", [(4201, 1024), (900, 4096), (70, 32768)])
+def test_rows_that_are_asked_for_ahead(T, d, dtype):
+    """More rows than are asked for at a time, in both directions."""
+    test_forward(T, d, dtype)
+    test_gradient(T, d, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("T,d", [(T, d) for d in WIDTHS for T in (1, 6)] + [(4200, 64), (1000, 320), (700, 4096), (200, 16384)])
 def test_gradient(T, d, dtype):
     x, _, gamma, du, dres = (t.cuda() for t in make(T, d, dtype, 2 * T + d))
