@@ -637,10 +637,10 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  *   workspace device, mcft_ffn_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
  * Of desc only d, w and dtype are read. bf16: fp32 sums, h rounded to bf16 once, y once; tcgen05 products with SwiGLU and the
- * checkpoint's rounding in the epilogue, a weight-streaming pair of kernels for few tokens. fp32 layers: operands of the
+ * checkpoint's rounding in the epilogue, a weight-streaming pair of kernels for few tokens (of either type). fp32 layers: operands of the
  * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones; an
  * infinity makes what it goes into NaN), and six products of them on the tensor cores make each fp32 one, in fp32 sums of short
- * runs; few tokens take CUDA-core fp32 arithmetic. The order of a row's sums depends on T and on the row's place. T = 0 is a no-op.
+ * runs. The order of a row's sums depends on T and on the row's place. T = 0 is a no-op.
  * Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (16
  * bytes), y at x's address, a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for T > 2^24 or d or w > 2^20. */
 mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);

@@ -15,11 +15,12 @@ namespace {
 constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
 
 // bf16: up to here the kernels that stream the weights. Graph nodes against the products', 2048 x 1408 and 4096 x 14336: 8 tokens
-// 10.5 and 72 us (20.6 and 71), 16 14.4 and 90 (20.7 and 72), 32 17.7 and 106 (20.6 and 72).
+// 10.5 and 72 us (20.6 and 71), 16 12.4 and 87 (20.7 and 72), 32 16.4 and 106 (20.6 and 72).
 bool few_tokens(int T, size_t weights) {
   return T <= 8 || (T <= 16 && weights <= (size_t(48) << 20)) || (T <= 32 && weights <= (size_t(20) << 20));
 }
-constexpr int kFewTokensF32 = 8;  // fp32: up to here the kernels that read each weight row once for 8 tokens
+// fp32: up to here, 32 at a time. 4096 x 14336: 33 tokens 361 us and 64 453 (products 643); 1024 x 2816: 36 and 43 (52).
+constexpr int kFewTokensF32 = 64;
 
 mcft_status check_T(int T) {
   if (T < 0) return fail(MCFT_ERR_INVALID, "T = %d < 0", T);
@@ -73,9 +74,8 @@ struct Sections {
 size_t elem(int dtype) { return dtype == MCFT_BF16 ? 2 : 4; }
 
 struct ForwardLayout {
-  size_t h, planes;       // h: bf16, or fp32 in parts (few tokens: as it is)
-  size_t gu, x, block;    // fp32: the projections, and operands in parts
-  size_t hdr, off, perm;  // fp32, few tokens: what the expert kernels expect of a permutation
+  size_t h, planes;     // h: bf16, or fp32 in parts
+  size_t gu, x, block;  // fp32: the projections, and operands in parts
   size_t total;
 };
 // Every section grows with T, so a workspace for T_max serves all smaller calls.
@@ -87,9 +87,6 @@ ForwardLayout forward_layout(const mcft_layer_desc* d, int T) {
   L.h = s.add(t * w * (f32 ? 6 : 2));
   size_t planes = dense_plane_bytes(t * D, d->w);
   if (f32) {
-    L.hdr = s.add(sizeof(WsHeader));
-    L.off = s.add(2 * sizeof(int));
-    L.perm = s.add(t * sizeof(int));
     L.gu = s.add(t * 2 * w * 4);
     L.x = s.add(t * D * 6);
     L.block = s.add(3 * w * D * 6);
@@ -124,33 +121,6 @@ GradLayout grad_layout(const mcft_layer_desc* d, int T) {
   L.planes = s.add(planes);
   L.total = s.total;
   return L;
-}
-
-// fp32: y = F(x) by the expert kernels, as one expert that every token takes.
-cudaError_t forward_f32(const mcft_layer_desc* d, const void* x, int T, const void* block, void* y, char* ws,
-                        const ForwardLayout& L, cudaStream_t s) {
-  const DensePlaceArgs p{reinterpret_cast<WsHeader*>(ws + L.hdr), reinterpret_cast<int*>(ws + L.off),
-                         reinterpret_cast<int*>(ws + L.perm), T};
-  const cudaError_t e = launch_dense_place(p, s);
-  if (e != cudaSuccess) return e;
-  FfnArgs a{};
-  a.x = x;
-  a.off = p.off;
-  a.perm = p.perm;
-  a.hdr = p.hdr;
-  a.wblk[0] = block;
-  a.h = ws + L.h;
-  a.o = static_cast<float*>(y);
-  a.o_plane = size_t(T) * d->d;
-  a.ksplit = 1;
-  a.T = T;
-  a.K = 1;
-  a.d = d->d;
-  a.w = d->w;
-  a.nseg = 1;
-  a.E = 1;
-  a.err = device_error_word();
-  return launch_ffn_rowwise(a, MCFT_F32, num_sms(), s, 3);
 }
 
 }  // namespace
@@ -274,8 +244,12 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   char* ws = static_cast<char*>(workspace);
   cudaError_t e;
   if (!ckpt && (desc->dtype == MCFT_F32 ? T <= kFewTokensF32 : few_tokens(T, size_t(3) * desc->w * desc->d))) {
-    e = desc->dtype == MCFT_F32 ? forward_f32(desc, x, T, block, y, ws, L, stream)
-                                : launch_dense_few(DenseFewArgs{x, block, ws + L.h, y, T, desc->d, desc->w}, stream);
+    e = cudaSuccess;
+    if (desc->dtype == MCFT_F32) {
+      e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(x)}, {reinterpret_cast<uint16_t*>(ws + L.x)}, {size_t(T) * desc->d}}, stream);
+      x = ws + L.x;
+    }
+    if (e == cudaSuccess) e = launch_dense_few(DenseFewArgs{x, block, ws + L.h, y, T, desc->d, desc->w}, desc->dtype, stream);
     return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
   }
   const char* w13 = static_cast<const char*>(block);

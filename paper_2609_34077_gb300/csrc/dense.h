@@ -124,20 +124,12 @@ struct DenseActArgs {
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s);
 cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s);
 
-// The whole block for few tokens (at most 32), bf16: h [T, w] is scratch.
+// The whole block for few tokens, 32 at a time: h [T, w] is scratch. fp32 layers: x and h in three bf16 parts.
 struct DenseFewArgs {
   const void *x, *block;
   void *h, *y;
   int T, d, w;
 };
-cudaError_t launch_dense_few(const DenseFewArgs& a, cudaStream_t s);
-
-// What the fp32 expert kernels expect of a permutation, for one expert that all T tokens take in order.
-struct DensePlaceArgs {
-  WsHeader* hdr;
-  int *off, *perm;
-  int T;
-};
-cudaError_t launch_dense_place(const DensePlaceArgs& a, cudaStream_t s);
+cudaError_t launch_dense_few(const DenseFewArgs& a, int dtype, cudaStream_t s);
 
 }  // namespace mcft

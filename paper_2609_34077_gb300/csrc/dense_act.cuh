@@ -1,4 +1,4 @@
-// SwiGLU and its derivative for the dense block's epilogues. Not part of the C ABI.
+// SwiGLU, its derivative and fp32 values in bf16 parts, for the dense block's kernels. Not part of the C ABI.
 #pragma once
 
 #include "common.cuh"
@@ -32,6 +32,18 @@ struct SwigluGrad {
     h = a * u;
     du = dh * a;
     dg = dh * u * (sg.s * fmaf(g, sg.rest, 1.0f));
+  }
+};
+
+// An fp32 value as three bf16 ones, each the rounding of what the ones before leave.
+struct Parts {
+  uint16_t p[3];
+  __device__ __forceinline__ explicit Parts(float v) {
+    // (what would round to an infinity is cut instead; an infinity itself has no rest)
+    p[0] = fabsf(v) >= 3.39e38f && fabsf(v) < INFINITY ? uint16_t(__float_as_uint(v) >> 16) : f2bf(v);
+    const float r = fabsf(v) < INFINITY ? v - __uint_as_float(uint32_t(p[0]) << 16) : 0.f;
+    p[1] = f2bf(r);
+    p[2] = f2bf(r - __uint_as_float(uint32_t(p[1]) << 16));
   }
 };
 

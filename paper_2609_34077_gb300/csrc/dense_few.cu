@@ -1,6 +1,6 @@
-// The dense gated feed-forward block for few tokens (bf16): the weights are what there is to read, once each.
+// The dense gated feed-forward block for few tokens: the weights are what there is to read, once each for 32 tokens.
 //
-//   up    h = silu(x W1^T) (x W3^T), rounded to bf16;      down   y = h W2^T
+//   up    h = silu(x W1^T) (x W3^T), rounded to bf16 (fp32 layers: in three bf16 parts);      down   y = h W2^T
 //
 // A tile is 16 weight rows (up: 8 of W1 and the same 8 of W3, whose sums then stand in one lane) by 8 tokens per column group:
 // mma.sync m16n8k16 with the weights as A, straight from memory. The contraction's order inside 32 elements is chosen so that a
@@ -9,8 +9,13 @@
 // rows. Partial sums are added over warps, then over the cluster's CTAs in the first one's shared memory, in order: the same
 // bits every time. Weights are asked for a batch ahead, and the down kernel's first ones while the up kernel is still running
 // (it starts as soon as that kernel's CTAs all have, and waits before it reads h).
+// fp32 layers: x and h come in three bf16 parts, a lane cuts its weights into three as they arrive, and six products (dense_gemm.cu)
+// make each fp32 one; the accumulators hold one or two steps of 32 and fp32 registers their sums.
 // Bound by HBM; at small sizes by the launches and two dependent passes. 1 token: 2048 x 1408 10.5 us, 4096 x 14336 67 us (5.3 TB/s
-// over both); 16 tokens of 2048 x 1408 14.4 (products: 20.6).
+// over both); 16 tokens of 2048 x 1408 12.4 (products: 20.6). fp32, 4096 x 14336: 8 tokens 150 us, 16 157, 32 227 (4.7, 4.5 and 3.1 TB/s; CUDA-core kernels that
+// read the weights once for 8 tokens took 241 for 8, products of parts 640).
+#include <type_traits>
+
 #include "dense.h"
 #include "dense_act.cuh"
 #include "tc_ptx.cuh"
@@ -19,20 +24,41 @@ namespace mcft {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kBatch = 4;  // steps of 32 elements that a warp asks for at a time
 constexpr int kMaxParts = 8;
+constexpr int kFewTokens = 32;  // that a launch takes
 
 struct FewParams {
-  const uint16_t* x;  // [T, K]
-  const uint16_t* w;  // up: [2 rows, K]; down: [rows, K]
-  uint16_t* out;      // [T, rows]
+  const uint16_t* x;  // [T, K], fp32 layers: in three parts
+  const void* w;      // up: [2 rows, K]; down: [rows, K]
+  void* out;          // [T, rows], fp32 layers: up in three parts
+  int x_part, out_part;  // elements from part to part (of 64 tokens at most: x and h stay far below 2^31)
   int T, K, rows, parts;
 };
 
 __device__ __forceinline__ uint4 ld16(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 
-template <bool UP, int NT>
-__global__ void __launch_bounds__(kWarps * 32) dense_few_kernel(const __grid_constant__ FewParams p) {
+// Eight fp32 values as three bf16 parts that hold all their bits: 8 of the 24 each, cut off (infinities become NaN).
+__device__ __forceinline__ void cut8(const uint4& a, const uint4& b, uint4* part) {
+  float v[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __byte_perm(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]), 0x7632);
+    part[k] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (k < 2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+    }
+  }
+}
+
+template <bool UP, int NT, bool F32>
+__global__ void __launch_bounds__(kWarps * 32, F32 && NT > 1 ? 2 : 0) dense_few_kernel(const __grid_constant__ FewParams p) {
+  using E = std::conditional_t<F32, float, uint16_t>;
+  constexpr int kBatch = !F32 ? 4 : NT < 4 ? 2 : 1;  // steps of 32 elements that a warp asks for at a time
+  constexpr int kVecs = F32 ? 2 : 1, kParts = F32 ? 3 : 1;
   constexpr int kCols = 8 * NT, kSums = 16 * kCols, kOuts = UP ? 8 : 16;
   __shared__ float red[kWarps][kSums];
   __shared__ float peer[kMaxParts][kSums];
@@ -42,40 +68,71 @@ __global__ void __launch_bounds__(kWarps * 32) dense_few_kernel(const __grid_con
   if (UP) pdl_begin();
   const int steps = p.K / 32, stride = p.parts * kWarps, first = part * kWarps + warp;
   // up: a row of W1 and the same of W3; down: rows g and g + 8 of the tile
-  const uint16_t* row0 = p.w + size_t(unit * kOuts + g) * p.K + q * 8;
-  const uint16_t* row1 = row0 + size_t(UP ? p.rows : 8) * p.K;
+  const E* row0 = static_cast<const E*>(p.w) + size_t(unit * kOuts + g) * p.K + q * 8;
+  const E* row1 = row0 + size_t(UP ? p.rows : 8) * p.K;
+  const uint16_t* xq = p.x + g * p.K + q * 8;
   const uint4 none = make_uint4(0, 0, 0, 0);
-  uint4 a[2][kBatch][2];
+  uint4 a[2][kBatch][2][kVecs];
   auto ask = [&](int buf, int s0) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int s = s0 + i * stride;
-      a[buf][i][0] = s < steps ? ld_stream16(row0 + s * 32) : none;
-      a[buf][i][1] = s < steps ? ld_stream16(row1 + s * 32) : none;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+        a[buf][i][0][v] = s < steps ? ld_stream16(row0 + s * 32 + v * 4) : none;
+        a[buf][i][1][v] = s < steps ? ld_stream16(row1 + s * 32 + v * 4) : none;
+      }
     }
   };
   float acc[NT][4] = {};
   ask(0, first);
   if (!UP) pdl_begin();
   auto batch = [&](int buf, int s0) {
-    uint4 b[kBatch][NT];
+    uint4 b[kBatch][kParts][NT];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int s = s0 + i * stride;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int t = 8 * n + g;
-        b[i][n] = s < steps && t < p.T ? ld16(p.x + size_t(t) * p.K + s * 32 + q * 8) : none;
-      }
+      for (int k = 0; k < kParts; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int t = 8 * n + g;
+          b[i][k][n] = s < steps && t < p.T ? ld16(xq + (k * p.x_part + 8 * n * p.K + s * 32)) : none;
+        }
     }
+    if constexpr (!F32) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const uint4 lo = a[buf][i][0], hi = a[buf][i][1];
+      for (int i = 0; i < kBatch; ++i) {
+        const uint4 lo = a[buf][i][0][0], hi = a[buf][i][1][0];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mma16816(acc[n], lo.x, hi.x, lo.y, hi.y, b[i][n].x, b[i][n].y);
-        mma16816(acc[n], lo.z, hi.z, lo.w, hi.w, b[i][n].z, b[i][n].w);
+        for (int n = 0; n < NT; ++n) {
+          mma16816(acc[n], lo.x, hi.x, lo.y, hi.y, b[i][0][n].x, b[i][0][n].y);
+          mma16816(acc[n], lo.z, hi.z, lo.w, hi.w, b[i][0][n].z, b[i][0][n].w);
+        }
       }
+    } else {
+      float run[NT][4] = {};
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        uint4 lo[3], hi[3];
+        cut8(a[buf][i][0][0], a[buf][i][0][1], lo);
+        cut8(a[buf][i][1][0], a[buf][i][1][1], hi);
+        constexpr int kA[6] = {0, 2, 1, 0, 1, 0}, kB[6] = {2, 0, 1, 1, 0, 0};  // the small products first
+#pragma unroll
+        for (int k = 0; k < 6; ++k) {
+          const uint4 l = lo[kA[k]], h = hi[kA[k]];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint4 x = b[i][kB[k]][n];
+            mma16816(run[n], l.x, h.x, l.y, h.y, x.x, x.y);
+            mma16816(run[n], l.z, h.z, l.w, h.w, x.z, x.w);
+          }
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][i] += run[n][i];
     }
   };
   for (int s = first; s < steps; s += 2 * kBatch * stride) {
@@ -121,11 +178,21 @@ __global__ void __launch_bounds__(kWarps * 32) dense_few_kernel(const __grid_con
       const float sum = red[0][(r + i) * kCols + t];
       v[i] = UP ? swiglu(sum, red[0][(r + i + 8) * kCols + t]) : sum;
     }
-    *reinterpret_cast<uint32_t*>(p.out + size_t(t) * p.rows + unit * kOuts + r) = pack2bf(v[0], v[1]);
+    const size_t at = size_t(t) * p.rows + unit * kOuts + r;
+    if constexpr (!F32) {
+      *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack2bf(v[0], v[1]);
+    } else if constexpr (UP) {
+      const Parts lo(v[0]), hi(v[1]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + k * p.out_part + at) = uint32_t(lo.p[k]) | uint32_t(hi.p[k]) << 16;
+    } else {
+      *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at) = make_float2(v[0], v[1]);
+    }
   }
 }
 
-template <bool UP, int NT>
+template <bool UP, int NT, bool F32>
 cudaError_t launch(FewParams p, cudaStream_t s) {
   const int units = p.rows / (UP ? 8 : 16), steps = p.K / 32;
   // a cluster for each unit where the units alone do not give every SM two CTAs, while its warps keep two steps
@@ -145,26 +212,43 @@ cudaError_t launch(FewParams p, cudaStream_t s) {
   cfg.numAttrs = p.parts > 1 ? 2 : 1;
   const int kid = UP ? kProfDenseFewUp : kProfDenseFewDown;
   prof_begin(kid, s);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, dense_few_kernel<UP, NT>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, dense_few_kernel<UP, NT, F32>, p);
   prof_end(kid, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <bool UP>
+template <bool UP, bool F32>
 cudaError_t launch_by_tokens(const FewParams& p, cudaStream_t s) {
-  if (p.T <= 8) return launch<UP, 1>(p, s);
-  if (p.T <= 16) return launch<UP, 2>(p, s);
-  return launch<UP, 4>(p, s);
+  if (p.T <= 8) return launch<UP, 1, F32>(p, s);
+  if (p.T <= 16) return launch<UP, 2, F32>(p, s);
+  return launch<UP, 4, F32>(p, s);
+}
+
+template <bool F32>
+cudaError_t launch_both(const DenseFewArgs& a, cudaStream_t s) {
+  constexpr size_t kElem = F32 ? 4 : 2;
+  const size_t d = size_t(a.d), w = size_t(a.w);
+  cudaError_t e = cudaSuccess;
+  for (int up = 1; up >= 0; --up) {
+    for (int t0 = 0; t0 < a.T && e == cudaSuccess; t0 += kFewTokens) {
+      const size_t t = size_t(t0);
+      const int n = a.T - t0 < kFewTokens ? a.T - t0 : kFewTokens;
+      uint16_t* h = static_cast<uint16_t*>(a.h) + t * w;
+      if (up) {
+        e = launch_by_tokens<true, F32>(FewParams{static_cast<const uint16_t*>(a.x) + t * d, a.block, h, a.T * a.d, a.T * a.w, n, a.d, a.w, 1}, s);
+      } else {
+        const char* w2 = static_cast<const char*>(a.block) + 2 * w * d * kElem;
+        e = launch_by_tokens<false, F32>(FewParams{h, w2, static_cast<char*>(a.y) + t * d * kElem, a.T * a.w, 0, n, a.w, a.d, 1}, s);
+      }
+    }
+  }
+  return e;
 }
 
 }  // namespace
 
-cudaError_t launch_dense_few(const DenseFewArgs& a, cudaStream_t s) {
-  const uint16_t* block = static_cast<const uint16_t*>(a.block);
-  const FewParams up{static_cast<const uint16_t*>(a.x), block, static_cast<uint16_t*>(a.h), a.T, a.d, a.w, 1};
-  const FewParams down{up.out, block + size_t(2) * a.w * a.d, static_cast<uint16_t*>(a.y), a.T, a.w, a.d, 1};
-  const cudaError_t e = launch_by_tokens<true>(up, s);
-  return e != cudaSuccess ? e : launch_by_tokens<false>(down, s);
+cudaError_t launch_dense_few(const DenseFewArgs& a, int dtype, cudaStream_t s) {
+  return dtype == MCFT_BF16 ? launch_both<false>(a, s) : launch_both<true>(a, s);
 }
 
 }  // namespace mcft

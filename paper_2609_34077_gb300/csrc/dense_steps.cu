@@ -9,16 +9,6 @@ namespace mcft {
 
 namespace {
 
-struct Parts {
-  uint16_t p[3];
-  __device__ __forceinline__ explicit Parts(float v) {
-    // (what would round to an infinity is cut instead; an infinity itself has no rest)
-    p[0] = fabsf(v) >= 3.39e38f && fabsf(v) < INFINITY ? uint16_t(__float_as_uint(v) >> 16) : f2bf(v);
-    const float r = fabsf(v) < INFINITY ? v - __uint_as_float(uint32_t(p[0]) << 16) : 0.f;
-    p[1] = f2bf(r);
-    p[2] = f2bf(r - __uint_as_float(uint32_t(p[1]) << 16));
-  }
-};
 // Eight neighbouring values to the three parts.
 __device__ __forceinline__ void put_parts(uint16_t* to, size_t stride, const float* v) {
   uint32_t w[3][4];
@@ -172,17 +162,6 @@ cudaError_t launch_act(const DenseActArgs& a, cudaStream_t s) {
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-__global__ void __launch_bounds__(256) dense_place_kernel(const __grid_constant__ DensePlaceArgs a) {
-  pdl_begin();
-  const int i = int(blockIdx.x) * 256 + int(threadIdx.x);
-  if (i == 0) {
-    *a.hdr = WsHeader{0, 1, a.T, 0};
-    a.off[0] = 0;
-    a.off[1] = a.T;
-  }
-  if (i < a.T) a.perm[i] = i;
-}
-
 }  // namespace
 
 cudaError_t launch_dense_join(const DenseJoinArgs& args, cudaStream_t s) {
@@ -217,12 +196,5 @@ cudaError_t launch_dense_split(const DenseSplitArgs& a, cudaStream_t s) {
 
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s) { return launch_act<false>(a, s); }
 cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s) { return launch_act<true>(a, s); }
-
-cudaError_t launch_dense_place(const DensePlaceArgs& a, cudaStream_t s) {
-  prof_begin(kProfDensePlace, s);
-  const cudaError_t e = launch_pdl(dense_place_kernel, dim3(unsigned((a.T + 255) / 256)), dim3(256), 0, s, a);
-  prof_end(kProfDensePlace, s);
-  return e != cudaSuccess ? e : cudaGetLastError();
-}
 
 }  // namespace mcft
