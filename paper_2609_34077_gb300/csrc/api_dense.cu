@@ -19,8 +19,9 @@ constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
 bool few_tokens(int T, size_t weights) {
   return T <= 8 || (T <= 16 && weights <= (size_t(48) << 20)) || (T <= 32 && weights <= (size_t(20) << 20));
 }
-// fp32: up to here, 32 at a time. 4096 x 14336: 33 tokens 361 us and 64 453 (products 643); 1024 x 2816: 36 and 43 (52).
-constexpr int kFewTokensF32 = 64;
+// fp32: up to here, 32 at a time. 4096 x 14336: 33 tokens 361 us and 64 453 (products 643); 1024 x 2816: 36 and 43 (52). The gradient (with
+// the forward): 16 tokens 643 and 77 us (products: 1007 and 93), 32 837 and 95 (1076 and 99), 33 even at the first.
+constexpr int kFewTokensF32 = 64, kFewTokensF32Grad = 32;
 
 mcft_status check_T(int T) {
   if (T < 0) return fail(MCFT_ERR_INVALID, "T = %d < 0", T);
@@ -249,7 +250,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
       e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(x)}, {reinterpret_cast<uint16_t*>(ws + L.x)}, {size_t(T) * desc->d}}, stream);
       x = ws + L.x;
     }
-    if (e == cudaSuccess) e = launch_dense_few(DenseFewArgs{x, block, ws + L.h, y, T, desc->d, desc->w}, desc->dtype, stream);
+    if (e == cudaSuccess) e = launch_dense_few(DenseFewArgs{x, block, ws + L.h, y, T, desc->d, desc->w, nullptr}, desc->dtype, stream);
     return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
   }
   const char* w13 = static_cast<const char*>(block);
@@ -335,12 +336,14 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   const void *dgu = ws + L.dgu, *h = ws + L.h, *xs = x, *dys = dy, *w13s = w13;
   size_t part_gu = 0, part_h = 0, part_x = 0, part_w = 0;
   auto* products = launch_dense_products;
+  bool few = false;
   if (desc->dtype == MCFT_BF16) {
     if (e == cudaSuccess)
       e = launch_dense_up_grad(DenseUpGradArgs{dy, w2, T, d, w, static_cast<const uint8_t*>(ckpt), x, w13, ws + L.h, ws + L.dgu,
                                                want_x && later ? static_cast<const uint8_t*>(x8) : nullptr, ws + L.x8}, stream);
   } else {
     products = launch_dense_split_products;
+    few = T <= kFewTokensF32Grad;
     uint16_t *x3 = reinterpret_cast<uint16_t*>(ws + L.x), *dy3 = reinterpret_cast<uint16_t*>(ws + L.dy),
              *block3 = reinterpret_cast<uint16_t*>(ws + L.block);
     part_gu = size_t(T) * 2 * w;
@@ -349,12 +352,16 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
     part_w = 3 * wd;
     if (e == cudaSuccess)
       e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(dy), static_cast<const float*>(block), static_cast<const float*>(x)},
-                                            {dy3, block3, x3}, {part_x, part_w, want_x ? part_x : 0}}, stream);
+                                            {dy3, block3, x3}, {part_x, few ? 0 : part_w, want_x ? part_x : 0}}, stream);
     xs = x3;
     dys = dy3;
     w13s = block3;
     float* dh = reinterpret_cast<float*>(ws + L.dh);
-    if (e == cudaSuccess) {
+    if (few) {
+      if (e == cudaSuccess && gu)
+        e = launch_dense_few(DenseFewArgs{x3, block, nullptr, nullptr, T, d, w, gu}, MCFT_F32, stream);
+      if (e == cudaSuccess) e = launch_dense_few_back(dy3, reinterpret_cast<const float*>(w2), dh, T, d, w, stream);
+    } else if (e == cudaSuccess) {
       const DenseProduct back_up[2] = {{dys, block3 + 2 * wd, T, w, d, 0, 0, dh, MCFT_F32, 0, part_x, part_w},
                                        {xs, w13s, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0, part_x, part_w}};
       e = products(back_up, gu ? 2 : 1, planes, stream);
@@ -371,9 +378,12 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
       p[n++] = DenseProduct{dgu, xs, 2 * w, d, T, 1, 0, out, grad_dtype, accumulate, part_gu, part_x};
       p[n++] = DenseProduct{dys, h, d, w, T, 1, 0, out + 2 * wd * elem(grad_dtype), grad_dtype, accumulate, part_x, part_h};
     }
-    if (dx) p[n++] = DenseProduct{dgu, w13s, T, d, 2 * w, 0, 0, dx, desc->dtype, 0, part_gu, part_w};
+    if (dx && few)
+      e = launch_dense_few_back(static_cast<const uint16_t*>(dgu), reinterpret_cast<const float*>(w13), static_cast<float*>(dx), T, 2 * w, d, stream);
+    else if (dx)
+      p[n++] = DenseProduct{dgu, w13s, T, d, 2 * w, 0, 0, dx, desc->dtype, 0, part_gu, part_w};
     for (int i = n - 1; i > 0 && p[i].k > p[i - 1].k; --i) std::swap(p[i], p[i - 1]);  // the longest contraction first
-    e = products(p, n, planes, stream);
+    if (e == cudaSuccess && n) e = products(p, n, planes, stream);
   }
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward gradient launch");
 }

@@ -124,12 +124,16 @@ struct DenseActArgs {
 cudaError_t launch_dense_act(const DenseActArgs& a, cudaStream_t s);
 cudaError_t launch_dense_act_grad(const DenseActArgs& a, cudaStream_t s);
 
-// The whole block for few tokens, 32 at a time: h [T, w] is scratch. fp32 layers: x and h in three bf16 parts.
+// The whole block for few tokens, 32 at a time: h [T, w] is scratch. fp32 layers: x and h in three bf16 parts. x NULL: only the
+// down projection of h; y NULL: only the up projections; gu (fp32 layers): g and u [T, 2w] themselves instead of h.
 struct DenseFewArgs {
   const void *x, *block;
   void *h, *y;
   int T, d, w;
+  float* gu;
 };
 cudaError_t launch_dense_few(const DenseFewArgs& a, int dtype, cudaStream_t s);
+// fp32 layers: out [T, N] = x [T, K] W, W [K, N], x in three bf16 parts (T K below 2^29).
+cudaError_t launch_dense_few_back(const uint16_t* x, const float* w, float* out, int T, int K, int N, cudaStream_t s);
 
 }  // namespace mcft

@@ -11,9 +11,9 @@
 // (it starts as soon as that kernel's CTAs all have, and waits before it reads h).
 // fp32 layers: x and h come in three bf16 parts, a lane cuts its weights into three as they arrive, and six products (dense_gemm.cu)
 // make each fp32 one; the accumulators hold one or two steps of 32 and fp32 registers their sums.
-// Bound by HBM; at small sizes by the launches and two dependent passes. 1 token: 2048 x 1408 10.5 us, 4096 x 14336 67 us (5.3 TB/s
-// over both); 16 tokens of 2048 x 1408 12.4 (products: 20.6). fp32, 4096 x 14336: 8 tokens 150 us, 16 157, 32 227 (4.7, 4.5 and 3.1 TB/s; CUDA-core kernels that
-// read the weights once for 8 tokens took 241 for 8, products of parts 640).
+// Bound by HBM; at small sizes by the launches and two dependent passes. 1 token: 2048 x 1408 10.5 us, 4096 x 14336 67 us (5.3
+// TB/s over both); 16 tokens of 2048 x 1408 12.4 (products: 20.6). fp32, 4096 x 14336: 8 tokens 150 us, 16 157, 32 227 (4.7, 4.5
+// and 3.1 TB/s; CUDA-core kernels that read the weights once for 8 tokens took 241 for 8, products of parts 640).
 #include <type_traits>
 
 #include "dense.h"
@@ -33,6 +33,7 @@ struct FewParams {
   void* out;          // [T, rows], fp32 layers: up in three parts
   int x_part, out_part;  // elements from part to part (of 64 tokens at most: x and h stay far below 2^31)
   int T, K, rows, parts;
+  int raw;  // up, fp32 layers: g and u themselves, fp32 [T, 2 rows]
 };
 
 __device__ __forceinline__ uint4 ld16(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
@@ -182,6 +183,12 @@ __global__ void __launch_bounds__(kWarps * 32, F32 && NT > 1 ? 2 : 0) dense_few_
     if constexpr (!F32) {
       *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack2bf(v[0], v[1]);
     } else if constexpr (UP) {
+      if (p.raw) {
+        float* gu = static_cast<float*>(p.out) + size_t(t) * 2 * p.rows + unit * kOuts + r;
+        *reinterpret_cast<float2*>(gu) = make_float2(red[0][r * kCols + t], red[0][(r + 1) * kCols + t]);
+        *reinterpret_cast<float2*>(gu + p.rows) = make_float2(red[0][(r + 8) * kCols + t], red[0][(r + 9) * kCols + t]);
+        continue;
+      }
       const Parts lo(v[0]), hi(v[1]);
 #pragma unroll
       for (int k = 0; k < 3; ++k)
@@ -192,12 +199,130 @@ __global__ void __launch_bounds__(kWarps * 32, F32 && NT > 1 ? 2 : 0) dense_few_
   }
 }
 
-template <bool UP, int NT, bool F32>
-cudaError_t launch(FewParams p, cudaStream_t s) {
-  const int units = p.rows / (UP ? 8 : 16), steps = p.K / 32;
-  // a cluster for each unit where the units alone do not give every SM two CTAs, while its warps keep two steps
-  p.parts = 1;
-  while (p.parts < kMaxParts && units * p.parts < 2 * num_sms() && steps >= 2 * kWarps * 2 * p.parts) p.parts *= 2;
+// Products with the weights the other way round, fp32 layers: out [T, N] = x [T, K] W, W [K, N], x in three bf16 parts.
+struct BackParams {
+  const uint16_t* x;
+  const float* w;
+  float* out;
+  int x_part, T, K, N, parts;
+};
+
+// The tokens are A (16 by MT), the weights B: a unit is 32 columns, 128 bytes of a row, of which a lane takes 16 bytes of four neighbouring
+// rows: one column each of four groups of eight. A CTA's warps take 16 rows each in turn; sums as above. Bound by HBM: dy W2 and [dg |
+// du] [W1 ; W3] of 4096 x 14336 together 1 token 173 us, 16 212 (6.1 and 5.0 TB/s with two launches), 32 300.
+template <int MT>
+__global__ void __launch_bounds__(kWarps * 32, 2) dense_few_back_kernel(const __grid_constant__ BackParams p) {
+  constexpr int kBatch = MT == 1 ? 2 : 1, kSums = 16 * MT * 32;
+  __shared__ float red[kWarps][kSums];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int part = int(blockIdx.x) % p.parts, unit = int(blockIdx.x) / p.parts;
+  const int steps = p.K / 16, stride = p.parts * kWarps, first = part * kWarps + warp;
+  const float* col = p.w + size_t(4 * q) * p.N + unit * 32 + 4 * g;
+  const uint16_t* xq = p.x + g * p.K + 4 * q;
+  uint4 b[2][kBatch][4];
+  auto ask = [&](int buf, int s0) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int s = s0 + i * stride;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        b[buf][i][r] = s < steps ? ld_stream16(col + (size_t(s) * 16 + r) * p.N) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  float acc[MT][4][4] = {};
+  ask(0, first);
+  pdl_begin();
+  auto batch = [&](int buf, int s0) {
+    uint2 a[kBatch][3][MT][2];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int s = s0 + i * stride;
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int m = 0; m < 2 * MT; ++m)
+          a[i][k][m / 2][m & 1] = s < steps && 8 * m + g < p.T
+                                      ? *reinterpret_cast<const uint2*>(xq + (k * p.x_part + 8 * m * p.K + s * 16))
+                                      : make_uint2(0, 0);
+    }
+    float run[MT][4][4] = {};
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      uint32_t w[3][4][2];  // part, column of a lane, rows' pair
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint4& f = b[buf][i][r];
+          v[r] = __uint_as_float(c == 0 ? f.x : c == 1 ? f.y : c == 2 ? f.z : f.w);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          w[k][c][0] = __byte_perm(__float_as_uint(v[0]), __float_as_uint(v[1]), 0x7632);
+          w[k][c][1] = __byte_perm(__float_as_uint(v[2]), __float_as_uint(v[3]), 0x7632);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] -= __uint_as_float(__float_as_uint(v[r]) & 0xffff0000u);
+        }
+      }
+      constexpr int kA[6] = {0, 2, 1, 0, 1, 0}, kB[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+      for (int k = 0; k < 6; ++k)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint2 lo = a[i][kA[k]][m][0], hi = a[i][kA[k]][m][1];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) mma16816(run[m][c], lo.x, hi.x, lo.y, hi.y, w[kB[k]][c][0], w[kB[k]][c][1]);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m][c][i] += run[m][c][i];
+  };
+  for (int s = first; s < steps; s += 2 * kBatch * stride) {
+    ask(1, s + kBatch * stride);
+    batch(0, s);
+    if (s + kBatch * stride >= steps) break;
+    ask(0, s + 2 * kBatch * stride);
+    batch(1, s + kBatch * stride);
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red[warp][(16 * m + g + (i >> 1) * 8) * 32 + 4 * (2 * q + (i & 1)) + c] = acc[m][c][i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < kSums; e += kWarps * 32) {
+    float s = red[0][e];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) s += red[w][e];
+    red[0][e] = s;
+  }
+  if (p.parts > 1) {
+    cluster_sync();  // the first CTA has read its warps' sums: the others' take their places
+    if (part > 0) {
+      for (int e = threadIdx.x; e < kSums; e += kWarps * 32)
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(&red[part][e], 0)), "f"(red[0][e]) : "memory");
+    }
+    cluster_sync();
+    if (part > 0) return;
+  }
+  // (a thread's own sums: no barrier in between)
+  for (int e = threadIdx.x; e < kSums; e += kWarps * 32) {
+    const int t = e / 32;
+    if (t >= p.T) break;
+    float s = red[0][e];
+    for (int w = 1; w < p.parts; ++w) s += red[w][e];
+    p.out[size_t(t) * p.N + unit * 32 + e % 32] = s;
+  }
+}
+
+template <typename Params>
+cudaError_t launch_clusters(void (*kernel)(const Params), int units, int kid, const Params& p, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(units * p.parts));
   cfg.blockDim = dim3(kWarps * 32);
@@ -210,11 +335,24 @@ cudaError_t launch(FewParams p, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.parts > 1 ? 2 : 1;
-  const int kid = UP ? kProfDenseFewUp : kProfDenseFewDown;
   prof_begin(kid, s);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, dense_few_kernel<UP, NT, F32>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
   prof_end(kid, s);
   return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// A cluster for each unit where the units alone do not give every SM two CTAs, while its warps keep two batches' steps.
+int parts_of(int units, int steps) {
+  int parts = 1;
+  while (parts < kMaxParts && units * parts < 2 * num_sms() && steps >= 2 * kWarps * 2 * parts) parts *= 2;
+  return parts;
+}
+
+template <bool UP, int NT, bool F32>
+cudaError_t launch(FewParams p, cudaStream_t s) {
+  const int units = p.rows / (UP ? 8 : 16);
+  p.parts = parts_of(units, p.K / 32);
+  return launch_clusters(dense_few_kernel<UP, NT, F32>, units, UP ? kProfDenseFewUp : kProfDenseFewDown, p, s);
 }
 
 template <bool UP, bool F32>
@@ -229,16 +367,18 @@ cudaError_t launch_both(const DenseFewArgs& a, cudaStream_t s) {
   constexpr size_t kElem = F32 ? 4 : 2;
   const size_t d = size_t(a.d), w = size_t(a.w);
   cudaError_t e = cudaSuccess;
-  for (int up = 1; up >= 0; --up) {
+  for (int up = a.x ? 1 : 0; up >= (a.y ? 0 : 1); --up) {
     for (int t0 = 0; t0 < a.T && e == cudaSuccess; t0 += kFewTokens) {
       const size_t t = size_t(t0);
       const int n = a.T - t0 < kFewTokens ? a.T - t0 : kFewTokens;
       uint16_t* h = static_cast<uint16_t*>(a.h) + t * w;
       if (up) {
-        e = launch_by_tokens<true, F32>(FewParams{static_cast<const uint16_t*>(a.x) + t * d, a.block, h, a.T * a.d, a.T * a.w, n, a.d, a.w, 1}, s);
+        void* out = a.gu ? static_cast<void*>(a.gu + t * 2 * w) : h;
+        e = launch_by_tokens<true, F32>(FewParams{static_cast<const uint16_t*>(a.x) + t * d, a.block, out, a.T * a.d, a.T * a.w, n, a.d, a.w, 1,
+                                                  a.gu ? 1 : 0}, s);
       } else {
         const char* w2 = static_cast<const char*>(a.block) + 2 * w * d * kElem;
-        e = launch_by_tokens<false, F32>(FewParams{h, w2, static_cast<char*>(a.y) + t * d * kElem, a.T * a.w, 0, n, a.w, a.d, 1}, s);
+        e = launch_by_tokens<false, F32>(FewParams{h, w2, static_cast<char*>(a.y) + t * d * kElem, a.T * a.w, 0, n, a.w, a.d, 1, 0}, s);
       }
     }
   }
@@ -249,6 +389,16 @@ cudaError_t launch_both(const DenseFewArgs& a, cudaStream_t s) {
 
 cudaError_t launch_dense_few(const DenseFewArgs& a, int dtype, cudaStream_t s) {
   return dtype == MCFT_BF16 ? launch_both<false>(a, s) : launch_both<true>(a, s);
+}
+
+cudaError_t launch_dense_few_back(const uint16_t* x, const float* w, float* out, int T, int K, int N, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  for (int t0 = 0; t0 < T && e == cudaSuccess; t0 += kFewTokens) {
+    const int n = T - t0 < kFewTokens ? T - t0 : kFewTokens, units = N / 32;
+    const BackParams p{x + size_t(t0) * K, w, out + size_t(t0) * N, T * K, n, K, N, parts_of(units, K / 16)};
+    e = launch_clusters(n <= 16 ? dense_few_back_kernel<1> : dense_few_back_kernel<2>, units, kProfDenseFewBack, p, s);
+  }
+  return e;
 }
 
 }  // namespace mcft

@@ -476,7 +476,7 @@ enum { kProfRoute, kProfCache, kProfPermute, kProfGather, kProfFfn13, kProfFfn2,
        kProfGemm13Pair, kProfGemm2Pair, kProfMx4Quant, kProfMx4Dequant, kProfMx4Matmul, kProfMx4Prepare,
        kProfMx4Up, kProfMx4Down, kProfMx4Combine, kProfRouteScored, kProfRouteScoredGrad,
        kProfMx8Quant, kProfMx8Dequant, kProfNorm8, kProfNormGrad, kProfDenseUp, kProfDenseUpGrad, kProfDenseOut,
-       kProfDenseJoin, kProfDenseAct, kProfDenseFewUp,
+       kProfDenseJoin, kProfDenseAct, kProfDenseFewUp, kProfDenseFewBack,
        kProfDenseFewDown, kProfDenseSplit, kProfCount };
 void prof_begin(int kid, cudaStream_t s);
 void prof_end(int kid, cudaStream_t s);

@@ -19,7 +19,7 @@ const char* const kNames[kProfCount] = {
     "ffn_decode_fetch", "gemm13_tc_pair", "gemm2_tc_pair", "mx4_quantize", "mx4_dequantize", "mx4_matmul",
     "mx4_prepare", "mx4_up", "mx4_down", "mx4_combine", "route_scored", "route_scored_grad",
     "mx8_quantize", "mx8_dequantize", "rmsnorm_mx8", "rmsnorm_grad", "dense_up", "dense_up_grad", "dense_out", "dense_join",
-    "dense_act", "dense_few_up", "dense_few_down", "dense_split"};
+    "dense_act", "dense_few_up", "dense_few_back", "dense_few_down", "dense_split"};
 
 struct Pending {
   int kid;
