@@ -269,13 +269,19 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
     uint16_t *x3 = reinterpret_cast<uint16_t*>(ws + L.x), *block3 = reinterpret_cast<uint16_t*>(ws + L.block),
              *h3 = reinterpret_cast<uint16_t*>(ws + L.h);
     const size_t nx = size_t(T) * d;
-    e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(x), static_cast<const float*>(block)}, {x3, block3}, {nx, 3 * wd}}, stream);
+    const bool few = T <= kFewTokensF32;  // (beside a checkpoint)
+    e = launch_dense_split(DenseSplitArgs{{static_cast<const float*>(x), static_cast<const float*>(block)}, {x3, block3},
+                                          {nx, few ? 0 : 3 * wd}}, stream);
     const DenseProduct up{x3, block3, T, 2 * w, d, 0, 1, gu, MCFT_F32, 0, nx, 3 * wd};
-    if (e == cudaSuccess) e = launch_dense_split_products(&up, 1, planes, stream);
+    if (e == cudaSuccess)
+      e = few ? launch_dense_few(DenseFewArgs{x3, block, nullptr, nullptr, T, d, w, gu}, MCFT_F32, stream)
+              : launch_dense_split_products(&up, 1, planes, stream);
     if (e == cudaSuccess)
       e = launch_dense_act(DenseActArgs{gu, static_cast<uint8_t*>(ckpt), nullptr, h3, nullptr, T, w}, stream);
     const DenseProduct down{h3, block3 + 2 * wd, T, d, w, 0, 1, y, MCFT_F32, 0, size_t(T) * w, 3 * wd};
-    if (e == cudaSuccess) e = launch_dense_split_products(&down, 1, planes, stream);
+    if (e == cudaSuccess)
+      e = few ? launch_dense_few(DenseFewArgs{nullptr, block, h3, y, T, d, w, nullptr}, MCFT_F32, stream)
+              : launch_dense_split_products(&down, 1, planes, stream);
   }
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "feed-forward launch");
 }
