@@ -303,6 +303,31 @@ def test_offsets_past_32_bits():
     M.mcft_device_error()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [4, 70])
+def test_weights_past_32_bits(T, dtype):
+    """W1, W3 and W2 of 65600 x 32768: 2^31 elements each and more. All are zero but the last 64 units', whose block by itself
+    gives the same values up to the order of sums (both within their bounds of the oracle)."""
+    d, w, n = 32768, 65600, 64
+    c = Case(T, d, n, dtype)
+    D = M.LayerDesc(d, 0, 0, w, 0, 0, M.MCFT_BF16 if dtype == BF16 else M.MCFT_F32)
+    block = torch.zeros(3 * w * d, dtype=dtype, device="cuda")
+    parts = lambda b, w: (b[:w * d].view(w, d), b[w * d: 2 * w * d].view(w, d), b[2 * w * d:].view(d, w))  # noqa: E731
+    for big, small in zip(parts(block, w)[:2], parts(c.block, n)[:2]):
+        big[-n:] = small
+    parts(block, w)[2][:, -n:] = parts(c.block, n)[2]
+    near(M.mcft_ffn_forward(D, c.x, block), *c.forward(), "y")
+    dx, db = M.mcft_ffn_grad(D, c.dy, block, x=c.x)
+    M.mcft_device_error()
+    del block
+    (wx, rx), (wb, rb) = c.gradient(f64(c.x), *c.projections(f64(c.x)))
+    near(dx, wx, rx, "dx")
+    g1, g3, g2 = parts(db, w)
+    last = torch.cat((g1[-n:].flatten(), g3[-n:].flatten(), g2[:, -n:].flatten()))
+    near(last, wb, rb, "dblock")
+    assert not g1[:-n].any() and not g3[:-n].any() and not g2[:, :-n].any()
+
+
 def test_tensors_of_the_host_are_refused():
     c = Case(5, 128, 192, BF16)
     D = desc(c)
