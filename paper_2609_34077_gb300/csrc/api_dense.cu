@@ -20,7 +20,7 @@ bool few_tokens(int T, size_t weights) {
   return T <= 8 || (T <= 16 && weights <= (size_t(48) << 20)) || (T <= 32 && weights <= (size_t(20) << 20));
 }
 // fp32: up to here, 32 at a time. 4096 x 14336: 33 tokens 361 us and 64 453 (products 643); 1024 x 2816: 36 and 43 (52). The gradient (with
-// the forward): 16 tokens 643 and 77 us (products: 1007 and 93), 32 837 and 95 (1076 and 99), 33 even at the first.
+// the forward): 1 token 568 and 63 us (products: 1002 and 87), 16 641 and 77 (1020 and 86), 32 842 and 92 (1093 and 90).
 constexpr int kFewTokensF32 = 64, kFewTokensF32Grad = 32;
 
 mcft_status check_T(int T) {
