@@ -278,10 +278,10 @@ def test_a_block_trained_from_its_checkpoints():
 
 
 def test_offsets_past_32_bits():
-    """70000 tokens by 2 x 30720: the checkpoint, dg and du pass 2^32 elements. The last tokens' rows are those of a call on them
+    """70000 tokens by 2 x 30784: the checkpoint, dg and du pass 2^32 elements. The last tokens' rows are those of a call on them
     alone up to the order of sums (both within their bounds of the oracle); dW sums over all tokens, of which only the last four
     have a gradient."""
-    T, d, w, n = 70_000, 64, 30720, 4
+    T, d, w, n = 70_000, 64, 30784, 4
     c = Case(n, d, w, BF16)
     D = desc(c)
     x = torch.randn(T, d, device="cuda").to(BF16)
