@@ -601,6 +601,8 @@ mcft_status mcft_mx8_dequantize(const void* q, long long rows, long long cols, i
  *   u8, x8 device mx8 [T, d]: u, before its rounding to the layer dtype, and v. u8 is the checkpoint of the block's input that
  *          mcft_ffn_grad takes, x8 that of the stream that mcft_rmsnorm_grad takes
  *   rstd   device [T] fp32: r
+ * Squares and their mean are fp32 numbers: where the mean overflows r is 0, where it vanishes and eps is 0 r is infinite, and
+ * below 2^-126 it has steps of 2^-149.
  * Each output may be NULL, but not all. Of desc only d (at most 32768) and dtype are read. T = 0 is a no-op. Asynchronous; the
  * same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (rstd 4 bytes, the
  * others 16), a bad desc, T < 0, eps outside [0, 1]; MCFT_ERR_UNSUPPORTED for larger d, T > 2^24. */

@@ -81,7 +81,7 @@ struct Sum2 {
 };
 
 // 1 / sqrt(sum / d + eps) as an fp32 number and what is left of it: the rounded root corrected once by its residual.
-// (A sum that overflowed has nothing left to correct.)
+// (A sum that overflowed has nothing left to correct. Squares below 2^-126 are multiples of 2^-149: so is the mean of rows of some 1e-19.)
 __device__ __forceinline__ float2 rstd_of(Sum2 s, int d, float eps) {
   const float n = float(d), lo = fabsf(s.hi) < INFINITY ? s.lo : 0.f;
   const float q = s.hi / n, ql = fabsf(q) < INFINITY ? (fmaf(-q, n, s.hi) + lo) / n : 0.f;
@@ -89,8 +89,8 @@ __device__ __forceinline__ float2 rstd_of(Sum2 s, int d, float eps) {
   m.add(eps, 0.f);
   const float r = 1.0f / sqrtf(m.hi);
   if (!(fabsf(m.hi) < INFINITY) || !(r < INFINITY)) return make_float2(r, 0.f);
-  const float t = r * r, te = fmaf(r, r, -t);
-  const float off = fmaf(m.hi, t, -1.0f) + fmaf(m.hi, te, m.lo * t);
+  const float t = m.hi * r, te = fmaf(m.hi, r, -t);  // (not r * r, which overflows for m below 2^-128)
+  const float off = fmaf(t, r, -1.0f) + fmaf(te, r, m.lo * r * r);
   return make_float2(r, -0.5f * r * off);
 }
 
