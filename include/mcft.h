@@ -642,7 +642,9 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  * checkpoint's rounding in the epilogue, a weight-streaming pair of kernels for few tokens (of either type). fp32 layers: operands of the
  * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones; an
  * infinity makes what it goes into NaN), and six products of them on the tensor cores make each fp32 one, in fp32 sums of short
- * runs. The order of a row's sums depends on T and on the row's place. T = 0 is a no-op.
+ * runs. The order of a row's sums depends on T and on the row's place. On the tensor cores a sum is cut towards zero at every 16
+ * terms, by up to 2^-23 of what it has come to: bf16 sums over d (rounded to bf16 or 8 bits then) lose up to d 2^-27 of themselves,
+ * those over w and, in mcft_ffn_grad, 2w or T are made of runs of at most 8192 terms, added up in fp32. T = 0 is a no-op.
  * Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (16
  * bytes), y at x's address, a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for T > 2^24 or d or w > 2^20. */
 mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
@@ -663,7 +665,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
  *   workspace device, mcft_ffn_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
  * Neither output may overlap an input or the other: both are written while the inputs are read. bf16 layers: dg, du and h are
- * rounded to bf16 as operands, sums are fp32. T = 0 writes zeros to dblock (unless accumulating). Asynchronous; the same bits
+ * rounded to bf16 as operands, sums are fp32 as above (runs of at most 1024 terms where dblock is fp32). T = 0 writes zeros to dblock (unless accumulating). Asynchronous; the same bits
  * whenever the inputs are the same. Errors as above, and for dx and dblock both NULL, another grad_dtype, or an output at an
  * input's address. */
 mcft_status mcft_ffn_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);

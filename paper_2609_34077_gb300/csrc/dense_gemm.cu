@@ -44,8 +44,9 @@ constexpr int kTmemCols = 2 * kTile;
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kTile >> 4) << 24);
 constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
 
-// EPI_BOTH: up and up_grad in one, from x; EPI_PARTS: out, of operands in parts
-enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_BOTH = 2, EPI_OUT = 3, EPI_PARTS = 4 };
+// EPI_BOTH: up and up_grad in one, from x; EPI_RUNS: out, of contractions that take several accumulators; EPI_PARTS: out, of operands in
+// parts
+enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_BOTH = 2, EPI_OUT = 3, EPI_RUNS = 4, EPI_PARTS = 5 };
 
 // Epilogue warps: four lane quarters of TMEM by so many shares of the columns. up_grad: eight warps do not hide the latencies of 45
 // instructions a value, the checkpoint's loads and three outputs; operands in parts: a thread's 64 sums fit its registers.
@@ -68,6 +69,7 @@ struct Problem {
   void* out;
   float* planes;         // splits > 1: fp32 [splits][M][N] instead of out
   int M, N, kblocks, per, splits, mt, nt, group, first;
+  int run;               // steps of the contraction that an accumulator holds
   int a_mn, b_mn, out_f32, accumulate, wide;
 };
 
@@ -127,6 +129,20 @@ __device__ __forceinline__ Item item_at(const Params& q, int item) {
 // contractions).
 constexpr int kPasses = 6;
 constexpr int kRun = 3;
+// Products of bf16 matrices to memory, too: a step of 16 of the contraction costs up to 2^-23 of what the accumulator holds (sums of
+// terms of one sign in one accumulator: 1.5e-5 at 4096 terms, 4.2e-4 at 65536). So one holds this many steps of 64 at most, fewer where the result
+// stays fp32 than where it is rounded to bf16, of whose half step 2^-14 is a 64th; several hold a longer contraction in turn, and the
+// epilogue's threads add them up (128 sums a thread: 168 registers, no room for the next launch's CTAs beside it, 2 us a launch;
+// with runs of 16 for bf16 results a step of 1023 x 960 x 704 took 45.0 us, not 41.1, one of 4096 x 2048 x 1408 169.9, not 164.5). Contractions
+// over d, whose results are rounded to bf16 or 8 bits, have one accumulator.
+constexpr int kRunF32 = 16, kRunBf16 = 128;
+template <int EPI>
+__device__ __forceinline__ int run_of(int most, int steps) {
+  if (EPI == EPI_PARTS) return kRun;
+  if (EPI != EPI_RUNS || steps <= most) return steps;
+  const int runs = (steps + most - 1) / most;
+  return (steps + runs - 1) / runs;
+}
 __device__ __forceinline__ int part_of(bool b, int pass) {
   constexpr uint32_t kA = 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8, kB = 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8;
   return int(((b ? kB : kA) >> (2 * pass)) & 3u);
@@ -567,9 +583,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
         const bool a_mn = EPI >= EPI_OUT && t.p->a_mn;
         const uint64_t ka = a_mn ? (16 * 128) >> 4 : 32 >> 4;
         bool ok = true;
-        // an accumulator's steps: all of the item's, or the products of a run of them
-        for (int k0 = t.k0; k0 < t.k1 && ok; k0 = EPI == EPI_PARTS ? k0 + kRun : t.k1) {
-          const int n = EPI == EPI_PARTS ? kPasses * min(kRun, t.k1 - k0) : t.k1 - k0;
+        const int run = run_of<EPI>(t.p->run, t.k1 - t.k0);
+        // an accumulator's steps: all of the item's, or a run of them
+        for (int k0 = t.k0; k0 < t.k1 && ok; k0 += run) {
+          const int n = (EPI == EPI_PARTS ? kPasses : 1) * min(run, t.k1 - k0);
           const uint32_t b = EPI == EPI_BOTH ? 0u : lt & 1u, turn = EPI == EPI_BOTH ? lt : lt >> 1;
           for (int phase = 0; phase < (EPI == EPI_BOTH ? 2 : 1) && ok; ++phase) {
             // (both: the epilogue before last is done with this dh, or the last one's g and u would not have been begun)
@@ -621,7 +638,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
     uint32_t lt = 0;
     for (int item = cid; item < items; item += ncl) {
       const Item t = item_at(q, item);
-      const int row = t.mt * kTile + int(rank) * 128 + quarter * 32 + lane;
+      const int row = t.mt * kTile + int(rank) * 128 + quarter * 32 + lane, steps = t.k1 - t.k0, run = run_of<EPI>(t.p->run, steps);
       auto begin = [&](uint32_t& taddr) {
         const uint32_t b = EPI == EPI_BOTH ? 0u : lt & 1u, turn = EPI == EPI_BOTH ? lt : lt >> 1;
         int ok = 1;
@@ -638,39 +655,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<EPI>, 1)
         ++lt;
       };
       uint32_t taddr;
-      if constexpr (EPI == EPI_PARTS) {
-        const int share = q.cols / kShares<EPI>, c0 = half * share;  // 64 or 32 columns
-        float sum[2][32];
+      if (EPI == EPI_PARTS || (EPI == EPI_RUNS && run < steps)) {
+        // the runs' sums, in order: 64 columns a thread, or 128; half of them of narrow tiles
+        constexpr int kBlocks = kTile / kShares<EPI> / 32;
+        const int share = q.cols / kShares<EPI>, c0 = half * share;
+        float sum[kBlocks][32] = {};
         bool ok = true;
-        for (int k0 = t.k0; k0 < t.k1 && ok; k0 += kRun) {
+        for (int left = steps; left > 0; left -= run) {
           ok = begin(taddr);
           if (!ok) break;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2 * kBlocks; ++c) {
             if (c * 16 >= share) continue;
             uint32_t v[16];
             tmem_ld16(taddr + c0 + c * 16, v);
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              float& to = sum[c / 2][c % 2 * 16 + i];
-              to = k0 == t.k0 ? __uint_as_float(v[i]) : to + __uint_as_float(v[i]);
+              sum[c / 2][c % 2 * 16 + i] += __uint_as_float(v[i]);
             }
           }
           end();
         }
         if (!ok) break;
+        const Item out = item_at(q, item);  // (again: the sums leave no registers for it meanwhile)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = t.nt * q.cols + c0 + c * 32;
-          if (c * 32 >= share || col >= t.p->N) continue;
-          put_out(t, row, col, reinterpret_cast<uint32_t*>(sum[c]));
+        for (int c = 0; c < kBlocks; ++c) {
+          const int col = out.nt * q.cols + c0 + c * 32;
+          if (c * 32 >= share || col >= out.p->N) continue;
+          put_out(out, out.mt * kTile + int(rank) * 128 + quarter * 32 + lane, col, reinterpret_cast<uint32_t*>(sum[c]));
         }
       } else if constexpr (EPI == EPI_UP_GRAD) {
         const int share = q.cols / kShares<EPI>, c0 = half * share;
         if (!epilogue_up_grad(q, t, item + ncl, row - lane, c0, min(c0 + share, t.p->N - t.nt * q.cols), st, begin)) break;
         end();
-      } else {
+      } else if constexpr (EPI != EPI_PARTS) {
         if (!begin(taddr)) break;
         epilogue<EPI>(q, t, taddr, row, half, int(lt & 1u));
         end();
@@ -935,6 +954,7 @@ cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes,
   q.n = n;
   q.cols = plan.cols;
   size_t used = 0;
+  bool several = false;  // accumulators for an item
   for (int i = 0; i < n; ++i) {
     const int r = in[i].a_t ? 0 : few_rows(in[i].rows);
     q.a_rows = i == 0 ? r : q.a_rows && r ? std::max(q.a_rows, r) : 0;
@@ -957,9 +977,13 @@ cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes,
     if (p.splits > 1) used += size_t(p.splits) * M * N;
     p.out_f32 = d.out_dtype == MCFT_F32;
     p.accumulate = d.accumulate;
+    p.run = p.out_f32 ? kRunF32 : kRunBf16;
+    several = several || p.per > p.run;
     p.wide = p.splits > 1 ? wide(planes) : wide(d.out);
   }
-  cudaError_t e = passes > 1 ? launch<EPI_PARTS>(q, kProfDenseOut, s) : launch<EPI_OUT>(q, kProfDenseOut, s);
+  cudaError_t e = passes > 1 ? launch<EPI_PARTS>(q, kProfDenseOut, s)
+                  : several  ? launch<EPI_RUNS>(q, kProfDenseOut, s)
+                             : launch<EPI_OUT>(q, kProfDenseOut, s);
   DenseJoinArgs join{};
   for (int i = 0; i < n; ++i) {
     if (q.p[i].splits == 1) continue;
