@@ -76,7 +76,7 @@ size_t elem(int dtype) { return dtype == MCFT_BF16 ? 2 : 4; }
 
 struct ForwardLayout {
   size_t h, planes;     // h: bf16, or fp32 in parts
-  size_t gu, x, block;  // fp32: the projections, and operands in parts
+  size_t gu, x, block;  // fp32: the projections, and operands in parts (few tokens: not the block, and no planes)
   size_t total;
 };
 // Every section grows with T, so a workspace for T_max serves all smaller calls.
@@ -86,21 +86,20 @@ ForwardLayout forward_layout(const mcft_layer_desc* d, int T) {
   ForwardLayout L{};
   Sections s;
   L.h = s.add(t * w * (f32 ? 6 : 2));
-  size_t planes = dense_plane_bytes(t * D, d->w);
+  const bool whole = f32 && T > kFewTokensF32;
   if (f32) {
     L.gu = s.add(t * 2 * w * 4);
     L.x = s.add(t * D * 6);
-    L.block = s.add(3 * w * D * 6);
-    planes = std::max(planes, dense_plane_bytes(t * 2 * w, d->d));
   }
-  L.planes = s.add(planes);
+  if (whole) L.block = s.add(3 * w * D * 6);
+  if (!f32 || whole) L.planes = s.add(std::max(dense_plane_bytes(t * D, d->w), whole ? dense_plane_bytes(t * 2 * w, d->d) : 0));
   L.total = s.total;
   return L;
 }
 
 struct GradLayout {
   size_t x8, x, dy, block;  // x8: its values; fp32: operands in parts
-  size_t gu, dh, h, dgu, planes, total;
+  size_t gu, dh, h, dgu, planes, total;  // (block, planes: not for few tokens of fp32 layers)
 };
 GradLayout grad_layout(const mcft_layer_desc* d, int T) {
   const size_t t = size_t(T), w = size_t(d->w), D = size_t(d->d);
@@ -111,15 +110,16 @@ GradLayout grad_layout(const mcft_layer_desc* d, int T) {
   L.h = s.add(t * w * (f32 ? 6 : 2));
   L.dgu = s.add(t * 2 * w * (f32 ? 6 : 2));
   if (f32) L.gu = s.add(t * 2 * w * 4);
-  size_t planes = dense_plane_bytes(t * D + 3 * w * D, std::max(T, 2 * d->w));
+  const bool whole = f32 && T > kFewTokensF32Grad;
   if (f32) {
     L.dh = s.add(t * w * 4);
     L.x = s.add(t * D * 6);
     L.dy = s.add(t * D * 6);
-    L.block = s.add(3 * w * D * 6);
-    planes = std::max(planes, dense_plane_bytes(t * 3 * w, d->d));
   }
-  L.planes = s.add(planes);
+  if (whole) L.block = s.add(3 * w * D * 6);
+  // (few tokens of fp32 layers: what products there are contract over the tokens, one step)
+  if (!f32 || whole)
+    L.planes = s.add(std::max(dense_plane_bytes(t * D + 3 * w * D, std::max(T, 2 * d->w)), whole ? dense_plane_bytes(t * 3 * w, d->d) : 0));
   L.total = s.total;
   return L;
 }
