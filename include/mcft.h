@@ -585,8 +585,9 @@ mcft_status mcft_route_scored_grad(const mcft_scored_desc* desc, const void* x, 
  *   alignment of its type (rows on 32 bytes are read faster); q device, mcft_mx8_size bytes out.
  * mcft_mx8_dequantize: the values that q stands for, exact in either dtype but for subnormal bf16 results, which round;
  *   y device [rows, cols], `ld` elements from row to row.
- * rows = 0 is a no-op. Asynchronous. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer, rows < 0, cols < 1,
- * ld < cols, an unknown dtype; MCFT_ERR_UNSUPPORTED for rows > 2^31 - 1, cols > 536862720 or ld > 2^40. */
+ * The two matrices may not overlap. rows = 0 is a no-op. Asynchronous. Errors: MCFT_ERR_INVALID for a NULL or misaligned
+ * pointer, both matrices at one address, rows < 0, cols < 1, ld < cols, an unknown dtype; MCFT_ERR_UNSUPPORTED for
+ * rows > 2^31 - 1, cols > 536862720 or ld > 2^40. */
 mcft_status mcft_mx8_size(long long rows, long long cols, size_t* bytes);
 mcft_status mcft_mx8_quantize(const void* x, long long rows, long long cols, long long ld, int dtype,
                               void* q, mcft_stream_t stream);
@@ -597,15 +598,16 @@ mcft_status mcft_mx8_dequantize(const void* q, long long rows, long long cols, i
  *   v = x + y (v = x when y is NULL), r = 1 / sqrt(mean_j v[j]^2 + eps), u = gamma * v * r.
  *   x      device [T, d] fp32;  y device [T, d] layer dtype, or NULL;  gamma device [d] layer dtype
  *   out    device [T, d] fp32: v; may be x (then the stream is updated in place)
- *   u      device [T, d] layer dtype
+ *   u      device [T, d] layer dtype; may be y
  *   u8, x8 device mx8 [T, d]: u, before its rounding to the layer dtype, and v. u8 is the checkpoint of the block's input that
  *          mcft_ffn_grad takes, x8 that of the stream that mcft_rmsnorm_grad takes
  *   rstd   device [T] fp32: r
  * Squares and their mean are fp32 numbers: where the mean overflows r is 0, where it vanishes and eps is 0 r is infinite, and
  * below 2^-126 it has steps of 2^-149.
- * Each output may be NULL, but not all. Of desc only d (at most 32768) and dtype are read. T = 0 is a no-op. Asynchronous; the
- * same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (rstd 4 bytes, the
- * others 16), a bad desc, T < 0, eps outside [0, 1]; MCFT_ERR_UNSUPPORTED for larger d, T > 2^24. */
+ * Each output may be NULL, but not all. None may overlap an input (but out = x and u = y) or another. Of desc only d (at most
+ * 32768) and dtype are read. T = 0 is a no-op. Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (rstd 4 bytes, the
+ * others 16), an output at another tensor's address, a bad desc, T < 0, eps outside [0, 1]; MCFT_ERR_UNSUPPORTED for larger d,
+ * T > 2^24. */
 mcft_status mcft_residual_rmsnorm_mx8(const mcft_layer_desc* desc, const float* x, const void* y, int T,
                                       const void* gamma, float eps, float* out, void* u, void* u8,
                                       void* x8, float* rstd, mcft_stream_t stream);
@@ -616,12 +618,12 @@ mcft_status mcft_residual_rmsnorm_mx8(const mcft_layer_desc* desc, const float* 
  *   x, x8     v as fp32 [T, d] or as mx8: one of the two, the other NULL
  *   rstd      as mcft_residual_rmsnorm_mx8 wrote it;  gamma as given to it
  *   du        device [T, d] layer dtype;  dres device [T, d] fp32, or NULL (zero)
- *   dx        device [T, d] fp32 out, may be dres; or NULL
+ *   dx        device [T, d] fp32 out, may be dres or x (or du in fp32 layers); or NULL
  *   dgamma    device [d] fp32 out, added to what it holds if accumulate is non-zero; or NULL
  *   workspace device, mcft_rmsnorm_grad_workspace_size(desc, T) bytes, 256-byte aligned (dgamma NULL: not used), in use until
  *             the call's kernels finish; enough for any smaller T
- * T = 0 writes zeros to dgamma (unless accumulating). Asynchronous; the same bits whenever the inputs are the same. Errors as
- * above, and for dx and dgamma both NULL or a workspace too small. */
+ * Else neither output may overlap an input or the other. T = 0 writes zeros to dgamma (unless accumulating). Asynchronous; the
+ * same bits whenever the inputs are the same. Errors as above, and for dx and dgamma both NULL or a workspace too small. */
 mcft_status mcft_rmsnorm_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
 mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const void* x8, const float* rstd,
                               const void* gamma, const void* du, int T, const float* dres, float* dx,
@@ -633,11 +635,12 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  * layer that DeepSeek-V2-Lite begins with), forward and backward.
  *
  * mcft_ffn_forward: y = W2 (silu(W1 x) * (W3 x)).
- *   x, y      device [T, d] layer dtype (y may not alias x)
+ *   x, y      device [T, d] layer dtype
  *   block     device packed expert block [W1 | W3 | W2]
  *   ckpt      device mx8 [T, 2w] out: g = W1 x and u = W3 x (g first), rounded from fp32, for mcft_ffn_grad; or NULL
  *   workspace device, mcft_ffn_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
+ * Neither output may overlap an input or the other: inputs are read while outputs are written.
  * Of desc only d, w and dtype are read. bf16: fp32 sums, h rounded to bf16 once, y once; tcgen05 products with SwiGLU and the
  * checkpoint's rounding in the epilogue, a weight-streaming pair of kernels for few tokens (of either type). fp32 layers: operands of the
  * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones; an
@@ -646,7 +649,8 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  * terms, by up to 2^-23 of what it has come to: bf16 sums over d (rounded to bf16 or 8 bits then) lose up to d 2^-27 of themselves,
  * those over w and, in mcft_ffn_grad, 2w or T are made of runs of at most 8192 terms, added up in fp32. T = 0 is a no-op.
  * Asynchronous; the same bits whenever the inputs are the same. Errors: MCFT_ERR_INVALID for a NULL or misaligned pointer (16
- * bytes), y at x's address, a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for T > 2^24 or d or w > 2^20. */
+ * bytes), an output at an input's or the other's address, a bad desc, T < 0, a workspace too small; MCFT_ERR_UNSUPPORTED for
+ * T > 2^24 or d or w > 2^20. */
 mcft_status mcft_ffn_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
 mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, const void* block, void* y,
                              void* ckpt, void* workspace, size_t ws_bytes, mcft_stream_t stream);
@@ -665,9 +669,9 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
  *   workspace device, mcft_ffn_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
  * Neither output may overlap an input or the other: both are written while the inputs are read. bf16 layers: dg, du and h are
- * rounded to bf16 as operands, sums are fp32 as above (runs of at most 1024 terms where dblock is fp32). T = 0 writes zeros to dblock (unless accumulating). Asynchronous; the same bits
- * whenever the inputs are the same. Errors as above, and for dx and dblock both NULL, another grad_dtype, or an output at an
- * input's address. */
+ * rounded to bf16 as operands, sums are fp32 as above (runs of at most 1024 terms where dblock is fp32). T = 0 writes zeros to
+ * dblock (unless accumulating). Asynchronous; the same bits whenever the inputs are the same. Errors as above, and for dx and
+ * dblock both NULL, or another grad_dtype. */
 mcft_status mcft_ffn_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);
 mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, const void* block, const void* x,
                           const void* x8, const void* ckpt, void* dx, void* dblock, int grad_dtype,

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "api_check.h"
 #include "dense.h"
@@ -60,6 +61,11 @@ mcft_status check_workspace(const void* p, size_t have, size_t need) {
   if (!aligned(p, 256)) return fail(MCFT_ERR_INVALID, "workspace must be 256-byte aligned");
   if (have < need) return fail(MCFT_ERR_INVALID, "workspace of %zu bytes, %zu needed", have, need);
   return MCFT_OK;
+}
+
+// Whether an output (NULL: none) is at one of these addresses.
+bool at_any(const void* out, std::initializer_list<const void*> others) {
+  return out && std::find(others.begin(), others.end(), out) != others.end();
 }
 
 // Sections of a workspace, on 256 bytes each.
@@ -152,6 +158,7 @@ static mcft_status mx8_call(const void* x, long long rows, long long cols, long 
   if (!x || !q) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
   if (!aligned(x, uintptr_t(elem(dtype)))) return fail(MCFT_ERR_INVALID, "the matrix is not aligned to its type");
   if (!aligned(q, 16)) return fail(MCFT_ERR_INVALID, "an mx8 matrix must be 16-byte aligned");
+  if (x == q) return fail(MCFT_ERR_INVALID, "the matrix and its mx8 matrix are the same");
   const cudaError_t e = launch_mx8_quant(Mx8Args{x, const_cast<void*>(q), rows, cols, ld}, dtype, back, stream);
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "mx8 kernel launch");
 }
@@ -181,6 +188,10 @@ mcft_status mcft_residual_rmsnorm_mx8(const mcft_layer_desc* desc, const float* 
   if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gamma, 16) || !aligned(out, 16) || !aligned(u, 16) ||
       !aligned(u8, 16) || !aligned(x8, 16) || !aligned(rstd, 4))
     return fail(MCFT_ERR_INVALID, "x, y, gamma, out, u, u8 and x8 must be 16-byte aligned, rstd 4-byte");
+  // (a row is in registers before any of it is written, so the stream and the residual may be written in place)
+  if (at_any(out, {y, gamma, u, u8, x8, rstd}) || at_any(u, {x, gamma, u8, x8, rstd}) || at_any(u8, {x, y, gamma, x8, rstd}) ||
+      at_any(x8, {x, y, gamma, rstd}) || at_any(rstd, {x, y, gamma}))
+    return fail(MCFT_ERR_INVALID, "outputs may not be inputs (but out = x and u = y) nor one another");
   const Norm8Args a{x, y, gamma, out, u, static_cast<uint8_t*>(u8), static_cast<uint8_t*>(x8), rstd, T, desc->d, eps};
   const cudaError_t e = launch_norm8(a, desc->dtype, stream);
   return e == cudaSuccess ? MCFT_OK : cuda_fail(e, "RMSNorm kernel launch");
@@ -213,6 +224,8 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
   if (!rstd || !gamma || !du) return fail(MCFT_ERR_INVALID, "NULL pointer argument");
   if (!aligned(x, 16) || !aligned(x8, 16) || !aligned(gamma, 16) || !aligned(du, 16) || !aligned(dres, 16) || !aligned(rstd, 4))
     return fail(MCFT_ERR_INVALID, "x, x8, gamma, du and dres must be 16-byte aligned, rstd 4-byte");
+  if (at_any(dx, {x8, rstd, gamma, dgamma, desc->dtype == MCFT_F32 ? nullptr : du}) || at_any(dgamma, {x, x8, rstd, gamma, du, dres}))
+    return fail(MCFT_ERR_INVALID, "dx and dgamma may not be inputs (but dx = dres, x, or du of fp32 layers) nor one another");
   const size_t need = dgamma ? size_t(norm_grad_planes(T, desc->d)) * desc->d * sizeof(float) : 0;
   st = check_workspace(workspace, ws_bytes, need);
   if (st != MCFT_OK) return st;
@@ -242,6 +255,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
   st = check_workspace(workspace, ws_bytes, L.total);
   if (st != MCFT_OK) return st;
   if (y == x) return fail(MCFT_ERR_INVALID, "y may not be x");
+  if (at_any(y, {block, ckpt}) || at_any(ckpt, {x, block})) return fail(MCFT_ERR_INVALID, "y and ckpt may not be inputs nor one another");
   char* ws = static_cast<char*>(workspace);
   cudaError_t e;
   if (!ckpt && (desc->dtype == MCFT_F32 ? T <= kFewTokensF32 : few_tokens(T, size_t(3) * desc->w * desc->d))) {
@@ -322,9 +336,8 @@ mcft_status mcft_ffn_grad(const mcft_layer_desc* desc, const void* dy, int T, co
   const GradLayout L = grad_layout(desc, T);
   st = check_workspace(workspace, ws_bytes, L.total);
   if (st != MCFT_OK) return st;
-  for (const void* out : {static_cast<const void*>(dx), static_cast<const void*>(dblock)})
-    if (out && (out == dy || out == block || out == x || out == x8 || out == ckpt))
-      return fail(MCFT_ERR_INVALID, "dx and dblock may not be inputs");
+  if (at_any(dx, {dy, block, x, x8, ckpt}) || at_any(dblock, {dy, block, x, x8, ckpt}))
+    return fail(MCFT_ERR_INVALID, "dx and dblock may not be inputs");
   if (dx == dblock) return fail(MCFT_ERR_INVALID, "dx and dblock are the same");
   char* ws = static_cast<char*>(workspace);
   const size_t eb = elem(desc->dtype);
