@@ -734,6 +734,9 @@ bool encode_out(CUtensorMap* m, void* base, size_t cols, size_t rows) {
 
 int wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
 
+// What the plans below reckon with: at least one (no device: the launch then fails, after the division by this).
+int sm_pairs() { return std::max(1, num_sms() / 2); }
+
 constexpr size_t kGroupBytes = size_t(24) << 20;  // of A that the row tiles of a group read
 
 void shape(Problem& p, int M, int N, int K, int tile_cols) {
@@ -877,7 +880,7 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
   q.n = 1;
   Problem& p = q.p[0];
   const Sizes z{a.T, a.w, (a.d + BK - 1) / BK};
-  q.cols = choose(&z, 1, 1, false, 1, num_sms() / 2).cols;
+  q.cols = choose(&z, 1, 1, false, 1, sm_pairs()).cols;
   shape(p, a.T, a.w, a.d, q.cols / 2);
   const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
   q.a_rows = few_rows(a.T);
@@ -906,7 +909,7 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   q.wide_dgu = wide(a.dgu);
   q.n = 1;
   if (a.ckpt) {
-    q.cols = choose(&z, 1, 0, false, 1, num_sms() / 2).cols;
+    q.cols = choose(&z, 1, 0, false, 1, sm_pairs()).cols;
     shape(q.p[0], a.T, a.w, a.d, q.cols);
     if (!encode(&q.p[0].a, a.dy, d, T, box) || !encode(&q.p[0].b, a.w2, w, d, 64)) return cudaErrorInvalidValue;
     if (!encode_out(&q.to_h, a.h, w, T) || !encode_out(&q.to_dgu, a.dgu, 2 * w, T)) return cudaErrorInvalidValue;
@@ -935,10 +938,10 @@ cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes,
   memset(&q, 0, sizeof(q));
   Sizes z[kMaxProducts];
   for (int i = 0; i < n; ++i) z[i] = Sizes{in[i].rows, in[i].cols, (in[i].k + BK - 1) / BK};
-  Plan plan = choose(z, n, 0, true, passes, num_sms() / 2);
+  Plan plan = choose(z, n, 0, true, passes, sm_pairs());
   DenseProduct two[2];
   if (n == 1 && !in[0].a_t) {
-    const Tail tail = tail_of(z[0], plan, passes, num_sms() / 2);
+    const Tail tail = tail_of(z[0], plan, passes, sm_pairs());
     if (tail.rows) {
       two[0] = two[1] = in[0];
       const size_t rows = size_t(in[0].rows - tail.rows), elem = in[0].out_dtype == MCFT_F32 ? 4 : 2;
@@ -1002,7 +1005,7 @@ cudaError_t launch_out(const DenseProduct* in, int n, int passes, float* planes,
 }  // namespace
 
 size_t dense_plane_bytes(size_t outs, int k) {
-  const size_t items = size_t(num_sms()) / 2 * kPlaneTiles * kTile * kTile, parts = size_t(k) / (kLeastPart * BK) + 2;
+  const size_t items = size_t(sm_pairs()) * kPlaneTiles * kTile * kTile, parts = size_t(k) / (kLeastPart * BK) + 2;
   return std::min(items, parts * outs) * sizeof(float);
 }
 
