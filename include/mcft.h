@@ -643,8 +643,8 @@ mcft_status mcft_rmsnorm_grad(const mcft_layer_desc* desc, const float* x, const
  * Neither output may overlap an input or the other: inputs are read while outputs are written.
  * Of desc only d, w and dtype are read. bf16: fp32 sums, h rounded to bf16 once, y once; tcgen05 products with SwiGLU and the
  * checkpoint's rounding in the epilogue, a weight-streaming pair of kernels for few tokens (of either type). fp32 layers: operands of the
- * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones; an
- * infinity makes what it goes into NaN), and six products of them on the tensor cores make each fp32 one, in fp32 sums of short
+ * products are split into three bf16 parts, which hold all 24 bits (values below 2^-100 or so lose their last ones; what an
+ * infinity goes into becomes NaN or infinite), and six products of them on the tensor cores make each fp32 one, in fp32 sums of short
  * runs. The order of a row's sums depends on T and on the row's place. On the tensor cores a sum is cut towards zero at every 16
  * terms, by up to 2^-23 of what it has come to: bf16 sums over d (rounded to bf16 or 8 bits then) lose up to d 2^-27 of themselves,
  * those over w and, in mcft_ffn_grad, 2w or T are made of runs of at most 8192 terms, added up in fp32. T = 0 is a no-op.
