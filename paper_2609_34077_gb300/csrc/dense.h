@@ -96,7 +96,7 @@ cudaError_t launch_dense_join(const DenseJoinArgs& a, cudaStream_t s);
 struct DenseUpArgs {
   const void *x, *w13;
   int T, d, w;
-  void* h;
+  void* h;        // on 32 bytes
   uint8_t* ckpt;  // mx8 [T, 2w] of g and u, or NULL
 };
 cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s);
@@ -107,7 +107,7 @@ struct DenseUpGradArgs {
   int T, d, w;
   const uint8_t* ckpt;
   const void *x, *w13;
-  void *h, *dgu;
+  void *h, *dgu;      // on 32 bytes
   const uint8_t* x8;  // with a checkpoint: mx8 [T, d] to be written out as bf16 besides (on 32 bytes), or NULL
   void* x8_values;
 };
@@ -133,7 +133,7 @@ struct DenseFewArgs {
   float* gu;
 };
 cudaError_t launch_dense_few(const DenseFewArgs& a, int dtype, cudaStream_t s);
-// fp32 layers: out [T, N] = x [T, K] W, W [K, N], x in three bf16 parts (T K below 2^29).
+// fp32 layers: out [T, N] = x [T, K] W, W [K, N], x in three bf16 parts, T at most 32.
 cudaError_t launch_dense_few_back(const uint16_t* x, const float* w, float* out, int T, int K, int N, cudaStream_t s);
 
 }  // namespace mcft

@@ -392,13 +392,10 @@ cudaError_t launch_dense_few(const DenseFewArgs& a, int dtype, cudaStream_t s) {
 }
 
 cudaError_t launch_dense_few_back(const uint16_t* x, const float* w, float* out, int T, int K, int N, cudaStream_t s) {
-  cudaError_t e = cudaSuccess;
-  for (int t0 = 0; t0 < T && e == cudaSuccess; t0 += kFewTokens) {
-    const int n = T - t0 < kFewTokens ? T - t0 : kFewTokens, units = N / 32;
-    const BackParams p{x + size_t(t0) * K, w, out + size_t(t0) * N, T * K, n, K, N, parts_of(units, K / 16)};
-    e = launch_clusters(n <= 16 ? dense_few_back_kernel<1> : dense_few_back_kernel<2>, units, kProfDenseFewBack, p, s);
-  }
-  return e;
+  if (T > kFewTokens) return cudaErrorInvalidValue;
+  const int units = N / 32;
+  const BackParams p{x, w, out, T * K, T, K, N, parts_of(units, K / 16)};
+  return launch_clusters(T <= 16 ? dense_few_back_kernel<1> : dense_few_back_kernel<2>, units, kProfDenseFewBack, p, s);
 }
 
 }  // namespace mcft

@@ -83,8 +83,8 @@ struct Params {
   CUtensorMap to_h, to_dgu;  // up_grad: boxes of 32 rows by 32 bytes
   uint8_t* ckpt;
   const uint8_t* x8;  // up_grad: mx8 [T, d] whose values go to x, for the products after it
-  uint16_t *h, *dgu, *x;
-  int d, w, wide_h, wide_dgu, wide_ckpt;
+  uint16_t *h, *dgu, *x;  // on 32 bytes (the workspace's)
+  int d, w, wide_ckpt;
 };
 static_assert(sizeof(Params) <= 4096, "kernel parameters");
 
@@ -304,10 +304,10 @@ __device__ __forceinline__ void put_grads(const Params& q, bool in, size_t r, in
     dg[i] = pack2bf(lo.dg, hi.dg);
     du[i] = pack2bf(lo.du, hi.du);
   }
-  put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
+  store_rows64(in ? q.h + r * w + col : nullptr, h);
   uint16_t* to = in ? q.dgu + r * 2 * w + col : nullptr;
-  put64(to, dg, q.wide_dgu);
-  put64(to ? to + w : nullptr, du, q.wide_dgu);
+  store_rows64(to, dg);
+  store_rows64(to ? to + w : nullptr, du);
 }
 
 // 32 columns of a row of C, or of its plane.
@@ -376,7 +376,7 @@ __device__ __forceinline__ void epilogue(const Params& q, const Item& t, uint32_
       for (int i = 0; i < 16; ++i)
         h[i] = pack2bf(swiglu(__uint_as_float(g[2 * i]), __uint_as_float(u[2 * i])),
                        swiglu(__uint_as_float(g[2 * i + 1]), __uint_as_float(u[2 * i + 1])));
-      put64(in ? q.h + r * w + col : nullptr, h, q.wide_h);
+      store_rows64(in ? q.h + r * w + col : nullptr, h);
     }
   } else if constexpr (EPI == EPI_BOTH) {
 #pragma unroll 1
@@ -890,7 +890,6 @@ cudaError_t launch_dense_up(const DenseUpArgs& a, cudaStream_t s) {
   q.w = a.w;
   q.h = static_cast<uint16_t*>(a.h);
   q.ckpt = a.ckpt;
-  q.wide_h = wide(a.h);
   q.wide_ckpt = wide(a.ckpt);
   return launch<EPI_UP>(q, kProfDenseUp, s);
 }
@@ -903,10 +902,6 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   const int rows = few_rows(a.T), box = rows ? rows : 128;
   q.a_rows = rows;
   q.w = a.w;
-  q.h = static_cast<uint16_t*>(a.h);
-  q.dgu = static_cast<uint16_t*>(a.dgu);
-  q.wide_h = wide(a.h);
-  q.wide_dgu = wide(a.dgu);
   q.n = 1;
   if (a.ckpt) {
     q.cols = choose(&z, 1, 0, false, 1, sm_pairs()).cols;
@@ -922,6 +917,8 @@ cudaError_t launch_dense_up_grad(const DenseUpGradArgs& a, cudaStream_t s) {
   }
   // g, u and dh of 128 columns in one accumulator each
   q.cols = kTile;
+  q.h = static_cast<uint16_t*>(a.h);
+  q.dgu = static_cast<uint16_t*>(a.dgu);
   const uint16_t* w1 = static_cast<const uint16_t*>(a.w13);
   shape(q.p[0], a.T, a.w, a.d, kTile / 2);
   shape(q.p[1], a.T, a.w, a.d, kTile / 2);
