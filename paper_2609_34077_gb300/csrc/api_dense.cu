@@ -15,8 +15,11 @@ namespace {
 
 constexpr int kMaxT = 1 << 24, kMaxWidth = 1 << 20;
 
-// bf16: up to here the kernels that stream the weights. Graph nodes against the products', 2048 x 1408 and 4096 x 14336: 8 tokens
-// 10.5 and 72 us (20.6 and 71), 16 12.4 and 87 (20.7 and 72), 32 16.4 and 106 (20.6 and 72).
+// bf16: up to here the kernels that stream the weights. A replayed graph with the L2 flushed before it, us (by the products): 8 tokens of
+// 2048 x 1408 15.5 (23.7), 4096 x 4096 33.9 (40.1), 4096 x 14336 76.9 (84.1); 9 and 16 of 2048 x 1408 17.5 (23.7, 25.7), 3584 x 3584 27.8 and
+// 29.8 (36.0), 4096 x 4096 42.1 and 44.2 (40.1, 38.1), 4096 x 14336 89 and 93 (83); 17 and 32 of 2048 x 1408 21.6 and 23.7 (25.7), 2048 x 2816
+// 29.9 and 34.0 (25.8, 27.8), 4096 x 4096 60.6 and 70.8 (40.1). So the two sides meet a little below the borders taken here: near 42 Mi
+// elements up to 16 tokens, near 12 Mi up to 32. (With the weights still in L2 both are some 5 to 8 us shorter and meet at the same sizes.)
 bool few_tokens(int T, size_t weights) {
   return T <= 8 || (T <= 16 && weights <= (size_t(48) << 20)) || (T <= 32 && weights <= (size_t(20) << 20));
 }

@@ -209,7 +209,8 @@ struct BackParams {
 
 // The tokens are A (16 by MT), the weights B: a unit is 32 columns, 128 bytes of a row, of which a lane takes 16 bytes of four neighbouring
 // rows: one column each of four groups of eight. A CTA's warps take 16 rows each in turn; sums as above. Bound by HBM: dy W2 and [dg |
-// du] [W1 ; W3] of 4096 x 14336 together 1 token 173 us, 16 212 (6.1 and 5.0 TB/s with two launches), 32 300.
+// du] [W1 ; W3] of 4096 x 14336 together 1 token 173 us, 16 212 (6.1 and 5.0 TB/s with two launches), 32 300. At 128 registers
+// (two CTAs an SM) a thread spills 8 bytes, for more than 16 tokens 80.
 template <int MT>
 __global__ void __launch_bounds__(kWarps * 32, 2) dense_few_back_kernel(const __grid_constant__ BackParams p) {
   constexpr int kBatch = MT == 1 ? 2 : 1, kSums = 16 * MT * 32;

@@ -19,6 +19,9 @@
 // Bound by the tensor pipe where there are rows enough, by HBM for few. Measured in bursts, TFLOP/s: 4096 tokens, 4096 x 14336 up
 // 1910 and y 1770; 4096 x 8192 up with a checkpoint 1780, up_grad 1450, both 1630, dx and the block's gradient 1730; parts (1024
 // tokens, 2048 x 4096 fp32) 1660 of bf16 products. 16 tokens, 4096 x 14336: 46 + 30 us, 5.1 and 3.9 TB/s with both ends of the launches.
+// h, dg and du are rounded to bf16 where they leave an epilogue: as operands of the products after it they have to be of the weights' type
+// (two types in one MMA are not possible, and fp32 values in three bf16 parts would be three MMAs for each). A bf16 y is 2.35e-3 off 64 bits
+// by that (mean square), of which its own rounding is 1.66e-3; gradients 2.35e-3 to 2.4e-3.
 // Rows and columns past a matrix's end are zeros that TMA fills in, and are not stored.
 // Every wait is bounded: after 2 s the kernel records MCFT_ERR_TIMEOUT, stops issuing, waits (bounded) for its copies and MMAs
 // in flight, frees TMEM and returns.
@@ -49,7 +52,7 @@ constexpr uint32_t kAMn = 1u << 15, kBMn = 1u << 16;
 enum { EPI_UP = 0, EPI_UP_GRAD = 1, EPI_BOTH = 2, EPI_OUT = 3, EPI_RUNS = 4, EPI_PARTS = 5 };
 
 // Epilogue warps: four lane quarters of TMEM by so many shares of the columns. up_grad: eight warps do not hide the latencies of 45
-// instructions a value, the checkpoint's loads and three outputs; operands in parts: a thread's 64 sums fit its registers.
+// instructions a value, the checkpoint's loads and three outputs; operands in parts: a thread's 64 sums fit its 96 registers but for 8 bytes.
 template <int EPI>
 constexpr int kShares = EPI == EPI_UP_GRAD || EPI == EPI_PARTS ? 4 : 2;
 template <int EPI>
@@ -132,7 +135,8 @@ constexpr int kRun = 3;
 // Products of bf16 matrices to memory, too: a step of 16 of the contraction costs up to 2^-23 of what the accumulator holds (sums of
 // terms of one sign in one accumulator: 1.5e-5 at 4096 terms, 4.2e-4 at 65536). So one holds this many steps of 64 at most, fewer where the result
 // stays fp32 than where it is rounded to bf16, of whose half step 2^-14 is a 64th; several hold a longer contraction in turn, and the
-// epilogue's threads add them up (128 sums a thread: 168 registers, no room for the next launch's CTAs beside it, 2 us a launch;
+// epilogue's threads add them up (128 sums a thread: 168 registers, 52 bytes spilled, no room for the next launch's CTAs beside it, 2 us a
+// launch;
 // with runs of 16 for bf16 results a step of 1023 x 960 x 704 took 45.0 us, not 41.1, one of 4096 x 2048 x 1408 169.9, not 164.5). Contractions
 // over d, whose results are rounded to bf16 or 8 bits, have one accumulator.
 constexpr int kRunF32 = 16, kRunBf16 = 128;
