@@ -669,7 +669,7 @@ mcft_status mcft_ffn_forward(const mcft_layer_desc* desc, const void* x, int T, 
  *   workspace device, mcft_ffn_grad_workspace_size(desc, T) bytes, 256-byte aligned, in use until the call's kernels finish;
  *             enough for any smaller T
  * Neither output may overlap an input or the other: both are written while the inputs are read. bf16 layers: dg, du and h are
- * rounded to bf16 as operands, sums are fp32 as above (runs of at most 1024 terms where dblock is fp32). T = 0 writes zeros to
+ * rounded to bf16 as operands, sums are fp32 as above (runs of at most 2048 terms where dblock is fp32). T = 0 writes zeros to
  * dblock (unless accumulating). Asynchronous; the same bits whenever the inputs are the same. Errors as above, and for dx and
  * dblock both NULL, or another grad_dtype. */
 mcft_status mcft_ffn_grad_workspace_size(const mcft_layer_desc* desc, int T_max, size_t* bytes);

@@ -133,13 +133,14 @@ __device__ __forceinline__ Item item_at(const Params& q, int item) {
 constexpr int kPasses = 6;
 constexpr int kRun = 3;
 // Products of bf16 matrices to memory, too: a step of 16 of the contraction costs up to 2^-23 of what the accumulator holds (sums of
-// terms of one sign in one accumulator: 1.5e-5 at 4096 terms, 4.2e-4 at 65536). So one holds this many steps of 64 at most, fewer where the result
-// stays fp32 than where it is rounded to bf16, of whose half step 2^-14 is a 64th; several hold a longer contraction in turn, and the
-// epilogue's threads add them up (128 sums a thread: 168 registers, 52 bytes spilled, no room for the next launch's CTAs beside it, 2 us a
-// launch;
-// with runs of 16 for bf16 results a step of 1023 x 960 x 704 took 45.0 us, not 41.1, one of 4096 x 2048 x 1408 169.9, not 164.5). Contractions
-// over d, whose results are rounded to bf16 or 8 bits, have one accumulator.
-constexpr int kRunF32 = 16, kRunBf16 = 128;
+// terms of one sign in one accumulator: 1.5e-5 at 4096 terms, 4.2e-4 at 65536). So one holds this many steps of 64 at most, fewer where the
+// result stays fp32 than where it is rounded to bf16, of whose half step 2^-14 is a 64th; several hold a longer contraction in turn, and
+// the epilogue's threads add them up (128 sums a thread: 168 registers, 52 bytes spilled, and no room for the next launch's CTAs beside
+// it, 2 us a launch). Shorter runs cost time: with 16 steps for bf16 results a step of 1023 x 960 x 704 took 45.0 us, not 41.1, one of 4096 x
+// 2048 x 1408 169.9, not 164.5; with 16 for fp32 results that are added to 4096 x 4096 x 8192 took 1188, not 1119, the next item's
+// two runs being over before this one's results are read and written. Contractions over d, whose results are rounded to bf16 or 8 bits,
+// have one accumulator.
+constexpr int kRunF32 = 32, kRunBf16 = 128;
 template <int EPI>
 __device__ __forceinline__ int run_of(int most, int steps) {
   if (EPI == EPI_PARTS) return kRun;

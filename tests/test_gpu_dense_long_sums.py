@@ -1,10 +1,11 @@
 """The block's gradient over many tokens: sums of terms of one sign.
 
 The tensor cores cut an accumulator's last bits towards zero at every step of 16 terms, up to 2^-23 of what it holds then. The
-library therefore has an accumulator hold at most 1024 terms where the result stays fp32, 8192 where it is rounded to bf16, and adds
-up the accumulators in fp32. Bounds for the terms below, positive multiples of 2^-15 under 4.7 whose runs of 1024 come to 2500 or so:
-sums are exact up to 2^9, then a step costs up to 2^-14 (13 steps, to 2^10), 2^-13 (27, to 2^11) and 2^-12 (12): 0.007 in all, 2.8e-6
-of a run. The additions of n runs cost up to 2^-24 of half the total each in the mean: 1.9e-6 for the 64 runs here. Together under 2^-17.
+library therefore has an accumulator hold at most 2048 terms where the result stays fp32, 8192 where it is rounded to bf16, and adds
+up the accumulators in fp32. Bounds for the terms below, positive multiples of 2^-15 under 4.7 whose runs of 2048 come to 5000 or so:
+sums are exact up to 2^9, then a step of 38 or so costs up to 2^-14 (14 steps, to 2^10), 2^-13 (27, to 2^11), 2^-12 (54, to 2^12) and 2^-11
+(24): 0.029 in all, 5.8e-6 of a run. The additions of n runs cost up to 2^-24 of half the total each in the mean: 1.0e-6 for the 32 runs
+here. Together under 2^-17.
 A run of 8192 terms costs up to 512 steps of 2^-23 of at most its sum: 2^-14."""
 import numpy as np
 import pytest
@@ -49,6 +50,10 @@ def test_gradient_of_many_tokens(T):
     low, high = (want * (1 - 2.0 ** -14 - 2.0 ** -20)).bfloat16(), (want * (1 + 2.0 ** -20)).bfloat16()
     got = half[2 * w * d:].view(d, w)[rows]
     assert bool(((low <= got) & (got <= high)).all()), (got < low).float().mean().item()
+    _, twice = M.mcft_ffn_grad(D, dy, block, x=x, ckpt=ckpt, dblock=half.clone(), accumulate=True)
+    low, high = ((got.double() + want * (1 + e)).bfloat16() for e in (-2.0 ** -14 - 2.0 ** -20, 2.0 ** -20))
+    got = twice[2 * w * d:].view(d, w)[rows]
+    assert bool(((low <= got) & (got <= high)).all())
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
